@@ -352,6 +352,155 @@ QWM_API qwm_status qwm_dequant_chunk(const qwm_config* cfg, const qwm_cache* cac
 QWM_API qwm_status qwm_top1_keys(const qwm_config* cfg, const void* q, int64_t Nq, const float* keys, int64_t Nk,
                                  int32_t* idx, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * The uncompressed side of the cache: rotary positions over three axes,
+ * Keys and Values appended to paged storage with the rotation applied on the
+ * way, and softmax attention over the pages (block-causal, with a sliding
+ * window and first tokens that stay visible).  Not part of the paper, which
+ * takes post-rotation Keys and compresses finished chunks: these are the
+ * steps next to it in a streaming model (the rotation before
+ * qwm_quantize_append, the recent tokens kept in bf16, single new tokens).
+ *
+ * Conventions of these calls beside those at the top of this file:
+ *   - bf16 or binary16 tensors (qwm_dtype), given as qwm_rows: any order of
+ *     tokens and heads, channels contiguous.
+ *   - Sizes that live on the device (offsets, lengths, page tables) are
+ *     checked on the device: an entry out of its range is not followed, and
+ *     QWM_ERR_INVALID_ARG is recorded in the cache's status word; the results
+ *     of that sequence are then undefined.
+ * --------------------------------------------------------------------------- */
+
+typedef enum qwm_dtype { QWM_BF16 = 0, QWM_F16 = 1 } qwm_dtype;
+
+/* A tensor [tokens][heads][head_dim] in device memory: element (n, h, c) is at
+ * data + n * token_stride + h * head_stride + c (strides in elements, multiples
+ * of 8; data 16-byte aligned). */
+typedef struct qwm_rows {
+  void* data;
+  int64_t token_stride, head_stride;
+  int32_t heads;
+} qwm_rows;
+
+/* Rotary positions over three axes (time, height, width).  P = pairs[0] +
+ * pairs[1] + pairs[2] pairs of channels are rotated, the first pairs[0] of them
+ * by the token's time, the next by its row, the last by its column; the other
+ * head_dim - 2 P channels pass unchanged.  Pair i is channels (2i, 2i+1) when
+ * `interleaved`, else (i, i + P).  head_dim: a multiple of 8, at most 256; P: a
+ * multiple of 8, or of 4 when interleaved, 2 P <= head_dim, at least one pair
+ * (otherwise QWM_ERR_UNSUPPORTED). */
+typedef struct qwm_rope_config {
+  int32_t head_dim, dtype;
+  int32_t pairs[3];
+  int32_t interleaved;
+} qwm_rope_config;
+
+/* Rotate Queries and Keys: for every token n and head, with the angle
+ * t = pos[n][axis of pair i] * inv_freq[i],
+ *   (x0, x1) -> (x0 cos t - x1 sin t, x0 sin t + x1 cos t).
+ * The product and its reduction by turns are exact to fp32 rounding of the
+ * reduced angle at every int32 position, the rotation is in fp32, the result
+ * rounded once.  inv_freq: fp32 [P]; pos: int32 [N][3].  q_out and k_out have
+ * the heads of q and k and may be the same tensors as q and k (same data and
+ * strides: in place); they must not overlap them otherwise.  k and k_out may
+ * both be NULL.  N = 0 is a no-op. */
+QWM_API qwm_status qwm_rope(const qwm_rope_config* cfg, const float* inv_freq, const int32_t* pos, int64_t N,
+                            const qwm_rows* q, const qwm_rows* q_out, const qwm_rows* k, const qwm_rows* k_out,
+                            void* stream);
+
+/* Gradient of qwm_rope: the rotations are orthogonal, so the gradient with
+ * respect to an input is the gradient dq (dk) of its output turned by -t. */
+QWM_API qwm_status qwm_rope_backward(const qwm_rope_config* cfg, const float* inv_freq, const int32_t* pos, int64_t N,
+                                     const qwm_rows* dq, const qwm_rows* dq_out, const qwm_rows* dk,
+                                     const qwm_rows* dk_out, void* stream);
+
+/* Paged storage: num_pages pages of page_tokens tokens (16, 32, 64 or 128) for
+ * kv_heads heads of head_dim 64 or 128 channels.  The caller's device buffer
+ * (256-byte aligned) holds a 256-byte header (device status word), then the
+ * pages [num_pages][Keys, Values][kv_heads][page_tokens][head_dim]; num_pages *
+ * 2 * kv_heads < 2^31. */
+typedef struct qwm_paged_config {
+  int32_t kv_heads, head_dim, page_tokens, dtype;
+  int64_t num_pages;
+} qwm_paged_config;
+typedef struct qwm_paged qwm_paged; /* opaque host descriptor */
+
+#define QWM_PAGED_HEADER_BYTES 256
+
+/* Bytes of the device buffer; 0 for an unsupported configuration. */
+QWM_API size_t qwm_paged_bytes(const qwm_paged_config* cfg);
+/* Descriptor over dev_buf; clears the header on `stream`, leaves the pages as
+ * they are.  Freed with qwm_paged_free; the buffer stays the caller's. */
+QWM_API qwm_status qwm_paged_init(qwm_paged** out, const qwm_paged_config* cfg, void* dev_buf, size_t bytes,
+                                  void* stream);
+QWM_API void qwm_paged_free(qwm_paged* cache);
+/* As qwm_cache_status and qwm_cache_set_wait_limit, for paged storage. */
+QWM_API qwm_status qwm_paged_status(qwm_paged* cache, int32_t* status, void* stream);
+QWM_API qwm_status qwm_paged_set_wait_limit(qwm_paged* cache, uint64_t ns);
+/* Test hook of the timeout path, as qwm_cache_set_idle_role: with role
+ * QWM_ROLE_PAGE_LOADS the attention calls made afterwards load no page, so the
+ * waits for the first tile run out and the call records QWM_ERR_TIMEOUT; 0
+ * restores normal work. */
+#define QWM_ROLE_PAGE_LOADS 2
+QWM_API qwm_status qwm_paged_set_idle_role(qwm_paged* cache, int32_t role);
+
+/* The sequences of one call.  Sequence b has the new tokens (rows of the
+ * call's tensors) q_offsets[b] .. q_offsets[b+1]-1, q_offsets[0] = 0 and
+ * q_offsets[num_seqs] = tokens, and holds kv_len[b] tokens, the new ones at
+ * its end: row q_offsets[b] + i is its token p = kv_len[b] - q_len + i.  Token j
+ * lives in page page_table[b * table_stride + j / page_tokens], slot j %
+ * page_tokens.  A row with p < 0 is not stored and sees nothing.  Entries of
+ * pages that no row of a call touches are not read (pages that a window has
+ * left behind can be given back and their entries set to -1).  max_q and
+ * max_kv bound the new tokens and the length of every sequence (host values
+ * that size the launch; a sequence above them is QWM_ERR_INVALID_ARG in the
+ * status word).  table_stride * page_tokens <= 2^30. */
+typedef struct qwm_paged_batch {
+  int32_t num_seqs, table_stride, max_q, max_kv;
+  int64_t tokens;
+  const int32_t* q_offsets;  /* device, [num_seqs + 1] */
+  const int32_t* kv_len;     /* device, [num_seqs] */
+  const int32_t* page_table; /* device, [num_seqs][table_stride] */
+} qwm_paged_batch;
+
+/* Store the new tokens' Keys and Values in their pages, in one launch.  With
+ * `rope` (then inv_freq and pos as in qwm_rope, its head_dim and dtype the
+ * cache's) the Keys are rotated on the way, and so are the Queries q into
+ * q_out when q is given; without it they are copied as they are.  q and q_out
+ * (both or neither; in place allowed) may have any number of heads. */
+QWM_API qwm_status qwm_paged_append(qwm_paged* cache, const qwm_paged_batch* batch, const qwm_rows* k,
+                                    const qwm_rows* v, const qwm_rope_config* rope, const float* inv_freq,
+                                    const int32_t* pos, const qwm_rows* q, const qwm_rows* q_out, void* stream);
+
+/* Which tokens a Query at token p of its sequence sees: with the end of its
+ * block e = (p / block + 1) * block, token j iff
+ *   j < min(e, kv_len) and (window == 0 or j >= e - window or j < sinks).
+ * block = 1 is token-causal; block = a frame's or chunk's tokens lets the
+ * tokens of a block see each other; block >= max_kv drops the mask.  window and
+ * sinks are in tokens.  1 <= block <= 2^30, window = 0 or >= block (a token sees
+ * its own block), sinks >= 0. */
+typedef struct qwm_mask {
+  int32_t block, window, sinks;
+} qwm_mask;
+
+/* Softmax attention of the batch's rows over the pages of their sequences:
+ * out = softmax(sm_scale q k^T) v over the visible tokens, with q of
+ * q_heads = q->heads heads, a multiple of kv_heads (Query head h reads head
+ * h / (q_heads / kv_heads)).  Logits, softmax statistics and sums are fp32; the
+ * probabilities enter the tensor cores in the cache's type.  lse: fp32
+ * [q_heads][tokens] natural-log sum-exp of the scaled logits, or NULL.  A row
+ * that sees nothing gets 0 and an lse of -inf.  What a row does not see does
+ * not reach it, infinities and NaN included.
+ * workspace: device scratch of at least qwm_paged_attend_workspace_bytes bytes
+ * for the same arguments (256-byte aligned), zeroed once when it is made (each
+ * call leaves its counters at zero); the call then splits long sequences over
+ * the GPU and joins the parts in a fixed order.  NULL or too small: no split.
+ * Calls sharing a workspace must not overlap on the GPU. */
+QWM_API size_t qwm_paged_attend_workspace_bytes(const qwm_paged* cache, const qwm_paged_batch* batch, int32_t q_heads,
+                                                const qwm_mask* mask);
+QWM_API qwm_status qwm_paged_attend(qwm_paged* cache, const qwm_paged_batch* batch, const qwm_rows* q,
+                                    const qwm_mask* mask, float sm_scale, const qwm_rows* out, float* lse,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

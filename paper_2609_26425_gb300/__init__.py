@@ -14,7 +14,9 @@ Functions carry the C names:
 qwm_cache_layout / qwm_cache_chunk_info, ``QueryStats`` wraps a Query
 statistics buffer (qwm_query_stats_bytes / _reset / _update / _read and
 qwm_query_basis), and qwm_dequant_chunk / qwm_top1_keys serve the
-token-selection shift measurement.
+token-selection shift measurement.  ``paged`` binds the uncompressed side:
+rotary positions (``Rope``, qwm_rope*) and paged storage (``PagedCache``,
+``PagedBatch``, qwm_paged_*).
 """
 from __future__ import annotations
 
@@ -26,11 +28,16 @@ import threading
 import numpy as np
 import torch
 
+from . import paged as _paged
+from .paged import (PagedBatch, PagedCache, Rope, paged_attend_workspace, qwm_paged_append, qwm_paged_attend,
+                    qwm_paged_attend_workspace_bytes, qwm_rope, qwm_rope_backward)
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_build", "libqwm.so")
 
 QWM_OK = 0
 QWM_ROLE_V_REBUILD = 1
+QWM_ROLE_PAGE_LOADS = 2
 STATUS_NAMES = {0: "QWM_OK", 1: "QWM_ERR_INVALID_ARG", 2: "QWM_ERR_UNSUPPORTED", 3: "QWM_ERR_CAPACITY",
                 4: "QWM_ERR_CUDA", 5: "QWM_ERR_TIMEOUT", 6: "QWM_ERR_NONFINITE"}
 
@@ -127,6 +134,7 @@ def lib():
             L.qwm_top1_keys.restype = ct.c_int
             L.qwm_quantize_append_full.argtypes = [_CFG, _P, _P, _P, ct.c_int64, _P, _P, _P, _P, _P, _P]
             L.qwm_quantize_append_full.restype = ct.c_int
+            _paged.declare(L)
             L.qwm_cache_set_wait_limit.argtypes = [_P, ct.c_uint64]
             L.qwm_cache_set_wait_limit.restype = ct.c_int
             L.qwm_cache_set_idle_role.argtypes = [_P, ct.c_int32]

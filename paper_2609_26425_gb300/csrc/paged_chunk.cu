@@ -1,0 +1,527 @@
+// paged_chunk.cu -- attention of many rows of a sequence over its pages: chunks
+// and prompts.
+//
+// Mathematics: as in paged_step.cu, with the rows of a sequence ordered (Query
+// token, grouped head), so that the grouped heads of a token share every K and
+// V tile.  The bound is the tensor pipe: 4 D operations per visible (row, key).
+//
+// A CTA takes 256 rows as two tiles of 128 (the M of tcgen05) over a common list
+// of 128-key tiles: S_i = Q_i K^T goes to TMEM, a warpgroup per tile turns it
+// into P (thread = row) written over S as 16-bit pairs, and P V accumulates in
+// TMEM with P read from there.  Two tiles, because the softmax of one then runs
+// beside the MMAs of the other.  TMEM: S0 | S1 | O0 | O1.
+// Warps: 0-3 and 4-7 softmax, 8 MMA issue, 9 TMA producer, 10 the Values' guard.
+// The guard clears the Values of keys that no row of the CTA sees (0 x inf is
+// not 0 in the MMA) in the tiles at the edges of the mask, and waves the others
+// through; infinities and NaN in Values that some rows see and others do not
+// are taken out of the product and added to the rows that see them at the end.
+#include "paged.cuh"
+
+namespace qwm {
+namespace {
+using namespace ptx;
+
+constexpr int TK = 128;
+constexpr int W_MMA = 8, W_TMA = 9;      // warp 10: the guard
+constexpr int NT = 11 * 32;
+constexpr int ST = 2;                     // K tiles and V tiles in flight
+constexpr int BLK = 16384;                // 128 rows x 128 bytes
+constexpr float kTau = 8.0f;              // O is rescaled when a row's maximum grows by more than 2^8
+
+enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VRDY = 6, B_VEMPTY = 8, B_SFULL = 10, B_PFULL = 12, B_QRDY = 14,
+       B_OFIN = 16, N_BAR = 17 };
+
+template <int D>
+struct Smem {
+  static constexpr int NB = D / 64;       // 64-channel blocks of a tile
+  static constexpr int Q = 0;             // tile i, block k at (i * NB + k) * BLK
+  static constexpr int K = 2 * NB * BLK;  // stage s, block k at (s * NB + k) * BLK
+  static constexpr int V = K + ST * NB * BLK;
+  static constexpr int BAR = V + ST * NB * BLK;
+  static constexpr int TOTAL = BAR + 256 + 1024;
+};
+
+__device__ __forceinline__ void umma_ss_e(uint32_t d, uint64_t ad, uint64_t bd, uint32_t id, uint32_t acc, uint32_t e) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(ad), "l"(bd), "r"(id), "r"(acc), "r"(e)
+      : "memory");
+}
+__device__ __forceinline__ void umma_ts_e(uint32_t d, uint32_t at, uint64_t bd, uint32_t id, uint32_t acc, uint32_t e) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(at), "l"(bd), "r"(id), "r"(acc), "r"(e)
+      : "memory");
+}
+__device__ __forceinline__ void commit_e(uint32_t bar, uint32_t e) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(e)
+      : "memory");
+}
+
+// Bits [a, b) of a 32-bit word (any a <= b, also outside 0..32).
+__device__ __forceinline__ uint32_t bits(int a, int b) {
+  const uint32_t hi = b <= 0 ? 0u : (b >= 32 ? 0xFFFFFFFFu : (1u << b) - 1u);
+  const uint32_t lo = a <= 0 ? 0u : (a >= 32 ? 0xFFFFFFFFu : (1u << a) - 1u);
+  return hi & ~lo;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
+  using L = Smem<D>;
+  constexpr int NB = L::NB;
+  extern __shared__ uint8_t raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_err, s_poison, s_last;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int b = blockIdx.z, hk = blockIdx.y;
+  const int rtiles = gridDim.x / a.nsplit;
+  // the row tiles with the most keys first
+  const int rt = rtiles - 1 - (int)(blockIdx.x % rtiles), part = blockIdx.x / rtiles;
+  Seq sq;
+  if (!load_seq(a, b, sq) && blockIdx.x == 0 && hk == 0 && tid == 0) record_status(a.status, QWM_ERR_INVALID_ARG);
+  const int64_t rows = (int64_t)sq.qn * a.G;
+  const int64_t r0 = (int64_t)rt * 256;
+  if (r0 >= rows) return;
+  const int nrow = (int)min((int64_t)256, rows - r0);
+  const int nqt = nrow > 128 ? 2 : 1;
+  const int p0 = sq.kv - sq.qn;                       // token of the sequence's first row
+  const int tokA = (int)(r0 / a.G), tokB = (int)((r0 + nrow - 1) / a.G);
+  const Tiles tl = make_tiles<TK>(p0 + tokA, p0 + tokB, sq.kv, a.block, a.window, a.sinks);
+  const int per = max((tl.n + a.nsplit - 1) / a.nsplit, a.min_tiles);
+  const int parts = max(1, (tl.n + per - 1) / per);
+  if (part >= parts) return;
+  const int t0 = part * per, n = max(0, min(tl.n, t0 + per) - t0);   // this part's tiles: t0 .. t0 + n - 1
+
+  auto bar = [&](int i) { return smem_u32(sm + L::BAR) + 8u * i; };
+  auto wait_all = [&](int i, uint32_t ph) -> bool {
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar(i), ph, a.wait_ns));
+  };
+  if (tid == 0) {
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(bar(B_KFULL + s), 1);
+      mbar_init(bar(B_KEMPTY + s), 1);
+      mbar_init(bar(B_VFULL + s), 1);
+      mbar_init(bar(B_VRDY + s), 1);
+      mbar_init(bar(B_VEMPTY + s), 1);
+      mbar_init(bar(B_SFULL + s), 1);
+      mbar_init(bar(B_PFULL + s), 4);
+      mbar_init(bar(B_QRDY + s), 4);
+    }
+    mbar_init(bar(B_OFIN), 1);
+    s_err = 0;
+    s_poison = 0;
+    fence_mbar_init();
+  }
+  if (warp == W_MMA) {
+    tmem_alloc(smem_u32(&s_tmem), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tbase = s_tmem;
+  const float sl2 = a.scale * 1.4426950408889634f;
+
+  if (warp < 8) {
+    // ------------------------------------------------------------ softmax
+    const int i = warp >> 2, row = tid & 127;
+    if (i < nqt) {
+      // Q_i: each warp its 32 rows, a row's 16-byte chunks over neighbouring lanes
+      uint8_t* sQ = sm + L::Q + i * NB * BLK;
+      constexpr int CH = D / 8;
+#pragma unroll 8
+      for (int it = 0; it < CH; ++it) {
+        const int idx = it * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
+        const int64_t r = r0 + i * 128 + rr;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (r < rows)
+          v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (sq.q0 + r / a.G) * a.q_tok +
+                                              (hk * a.G + r % a.G) * a.q_head + c * 8);
+        *reinterpret_cast<uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v;
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(B_QRDY + i));
+
+      const int64_t r = r0 + i * 128 + row;
+      const bool has = r < rows;
+      const int tok = has ? (int)(r / a.G) : tokB;
+      const int head = hk * a.G + (has ? (int)(r % a.G) : 0);
+      const Span sp = has ? row_span(p0 + tok, sq.kv, a.block, a.window) : Span{0, 0};
+      const uint32_t lrow = (uint32_t)((warp & 3) * 32) << 16;
+      const uint32_t tS = tbase + 128 * i + lrow, tO = tbase + 256 + 128 * i + lrow;
+      float m_run = -INFINITY, l_run = 0.0f;
+      bool ok = true;
+      for (int jt = 0; jt < n; ++jt) {
+        if (!(ok = wait_all(B_SFULL + i, jt & 1))) break;
+        tc_fence_after();
+        const int j0 = tile_at(tl, t0 + jt) * TK;
+        const bool open = __all_sync(0xFFFFFFFFu, !has || (j0 + TK <= sp.hi && (j0 >= sp.lo || j0 + TK <= a.sinks)));
+        uint32_t see[4];
+        float mt = -INFINITY;
+        float va[32], vb[32];
+        if (open) {
+          mt = tmem_max128(tS);
+        } else {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int c = j0 + 32 * w;
+            see[w] = bits(sp.lo - c, sp.hi - c) | bits(-c, min(a.sinks, sp.hi) - c);
+          }
+#pragma unroll
+          for (int cp = 0; cp < 2; ++cp) {
+            tmem_ld32x2(tS + 64 * cp, tS + 64 * cp + 32, va, vb);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              if ((see[2 * cp] >> e) & 1) mt = fmaxf(mt, va[e]);
+              if ((see[2 * cp + 1] >> e) & 1) mt = fmaxf(mt, vb[e]);
+            }
+          }
+        }
+        const float m_new = fmaxf(m_run, mt);
+        // -inf - -inf is NaN and compares false: a row that has seen nothing stays so
+        const bool need = (m_new - m_run) * sl2 > kTau;
+        float alpha = 1.0f;
+        if (need) {
+          alpha = ex2f((m_run - m_new) * sl2);
+          m_run = m_new;
+          l_run *= alpha;
+        }
+        // S_i of this tile being complete, the P_i V before it is too
+        if (__any_sync(0xFFFFFFFFu, need) && jt > 0) {
+#pragma unroll 1
+          for (int cb = 0; cb < D / 16; ++cb) {
+            uint32_t t[16];
+            tmem_ld16(tO + cb * 16, t);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) t[e] = __float_as_uint(__uint_as_float(t[e]) * alpha);
+            tmem_st16(tO + cb * 16, t);
+          }
+        }
+        const float mb = m_run == -INFINITY ? 0.0f : m_run * sl2;
+        const uint64_t SL = f2pack(sl2, sl2), MB = f2pack(-mb, -mb);
+        uint64_t sum = f2pack(0.0f, 0.0f);
+        // P of 32 columns, as 16 words over S columns that have been read
+        auto block32 = [&](const float (&v)[32], uint32_t m, uint32_t dst) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            float x, y;
+            f2unpack(fma2(f2pack(v[e], v[e + 1]), SL, MB), x, y);
+            if (!open) {
+              x = (m >> e) & 1 ? x : -INFINITY;
+              y = (m >> (e + 1)) & 1 ? y : -INFINITY;
+            }
+            x = ex2f(x);
+            y = ex2f(y);
+            sum = add2(sum, f2pack(x, y));
+            pk[e >> 1] = Elem<T>::pack(x, y);
+          }
+          tmem_st16(dst, pk);
+        };
+#pragma unroll 1
+        for (int cp = 0; cp < 2; ++cp) {
+          tmem_ld32x2(tS + 64 * cp, tS + 64 * cp + 32, va, vb);
+          block32(va, cp ? see[2] : see[0], tS + 32 * cp);
+          block32(vb, cp ? see[3] : see[1], tS + 32 * cp + 16);
+        }
+        tmem_wait_st();
+        float sx, sy;
+        f2unpack(sum, sx, sy);
+        l_run += sx + sy;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_PFULL + i));
+      }
+      if (ok && n > 0) ok = wait_all(B_OFIN, 0);
+      if (!ok) s_err = 1;
+      if (ok) {
+        tc_fence_after();
+        const int64_t group = ((int64_t)b * a.Hk + hk) * rtiles + rt;
+        const int64_t pr = (group * a.nsplit + part) * 256 + i * 128 + row;
+        const float inv = l_run > 0.0f || l_run != l_run ? 1.0f / l_run : 0.0f;
+        T* dst = static_cast<T*>(a.out) + (sq.q0 + tok) * a.o_tok + (int64_t)head * a.o_head;
+        const bool poison = *(volatile int*)&s_poison != 0;
+#pragma unroll 1
+        for (int cb = 0; cb < D / 32; ++cb) {
+          float v[32];
+          if (n > 0) {
+            tmem_ld32(tO + cb * 32, v);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = 0.0f;
+          }
+          if (poison && has) {
+            // the Values that the guard took out: this row's share of them
+            for (int jt = 0; jt < n; ++jt) {
+              const int j0 = tile_at(tl, t0 + jt) * TK;
+              if (all_see(tl, j0, j0 + TK, a.sinks)) continue;
+              for (int j = j0; j < j0 + TK; ++j) {
+                if (!sees(j, sp.lo, sp.hi, a.sinks) || all_see(tl, j, j + 1, a.sinks)) continue;
+                const int64_t page = a.table[(int64_t)b * a.table_stride + (j >> a.page_log2)];
+                if (page < 0 || page >= a.num_pages) continue;
+                const T* src = static_cast<const T*>(a.pages) +
+                               ((((page * 2 + 1) * a.Hk + hk) << a.page_log2) + (j & ((1 << a.page_log2) - 1))) * D + cb * 32;
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                  const uint32_t w = *reinterpret_cast<const uint32_t*>(src + e);
+                  const float2 f = Elem<T>::unpack(w);
+                  if ((w & Elem<T>::kExp) == Elem<T>::kExp) v[e] += f.x;
+                  if (((w >> 16) & Elem<T>::kExp) == Elem<T>::kExp) v[e + 1] += f.y;
+                }
+              }
+            }
+          }
+          if (!has) continue;
+          if (parts == 1) {
+            uint4* d4 = reinterpret_cast<uint4*>(dst + cb * 32);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              d4[k] = make_uint4(Elem<T>::pack(v[8 * k] * inv, v[8 * k + 1] * inv),
+                                 Elem<T>::pack(v[8 * k + 2] * inv, v[8 * k + 3] * inv),
+                                 Elem<T>::pack(v[8 * k + 4] * inv, v[8 * k + 5] * inv),
+                                 Elem<T>::pack(v[8 * k + 6] * inv, v[8 * k + 7] * inv));
+          } else {
+            float4* d4 = reinterpret_cast<float4*>(a.part_o + pr * D + cb * 32);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) d4[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+          }
+        }
+        if (has && parts == 1 && a.lse)
+          a.lse[(int64_t)head * a.N + sq.q0 + tok] = m_run == -INFINITY ? -INFINITY : m_run * a.scale + logf(l_run);
+        if (has && parts > 1) a.part_ml[pr] = make_float2(m_run, l_run);
+      }
+    }
+  } else if (warp == W_MMA) {
+    // ------------------------------------------------------------ MMA issue
+    // Order per K/V tile j: P0 V(j), S0(j+1), P1 V(j), S1(j+1); S_i(j+1) may
+    // overwrite P_i(j) because the MMAs of one thread run in issue order.
+    const uint32_t e = elect_one();
+    const uint64_t dQ = desc_sw128(smem_u32(sm + L::Q)), dK = desc_sw128(smem_u32(sm + L::K));
+    const uint64_t dV = desc_sw128_mn(smem_u32(sm + L::V), BLK);
+    auto off = [](int bytes) { return (uint64_t)(bytes >> 4); };
+    constexpr uint32_t idS = idesc_f16(128, TK, false, Elem<T>::bf16);
+    constexpr uint32_t idPV = idesc_f16(128, D, true, Elem<T>::bf16);
+    bool ok = true;
+    auto issue_S = [&](int i, int jt) -> bool {
+      const int s = jt & 1;
+      if (i == 0 && !wait_all(B_KFULL + s, (jt >> 1) & 1)) return false;
+      if (jt == 0 && !wait_all(B_QRDY + i, 0)) return false;
+      tc_fence_after();
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+          umma_ss_e(tbase + 128 * i, dQ + off((i * NB + kb) * BLK + ks * 32), dK + off((s * NB + kb) * BLK + ks * 32),
+                    idS, (kb | ks) != 0, e);
+      commit_e(bar(B_SFULL + i), e);
+      if (i == nqt - 1) commit_e(bar(B_KEMPTY + s), e);
+      return true;
+    };
+    if (n > 0) {
+      for (int i = 0; i < nqt && ok; ++i) ok = issue_S(i, 0);
+      for (int jt = 0; jt < n && ok; ++jt) {
+        const int s = jt & 1;
+        if (!(ok = wait_all(B_VRDY + s, (jt >> 1) & 1))) break;
+        for (int i = 0; i < nqt; ++i) {
+          if (!(ok = wait_all(B_PFULL + i, jt & 1))) break;
+          tc_fence_after();
+#pragma unroll
+          for (int ks = 0; ks < TK / 16; ++ks)
+            umma_ts_e(tbase + 256 + 128 * i, tbase + 128 * i + 8 * ks, dV + off(s * NB * BLK + ks * 2048), idPV,
+                      (jt | ks) != 0, e);
+          if (i == nqt - 1) commit_e(bar(B_VEMPTY + s), e);
+          if (jt + 1 < n && !(ok = issue_S(i, jt + 1))) break;
+        }
+      }
+      commit_e(bar(B_OFIN), e);
+      if (!ok) {
+        // a wait ran out: the MMAs already issued finish before TMEM is freed
+        mbar_wait(bar(B_OFIN), 0, kDrainNs);
+        s_err = 1;
+      }
+    }
+    __syncwarp();
+  } else if (warp == W_TMA) {
+    // ------------------------------------------------------------ producer
+    // lane = box * NB + channel block; a box is the part of a page (at most 64
+    // tokens of it) that lies in the tile.  Boxes no row sees are not read.
+    const int box_log2 = min(a.page_log2, 6);
+    const int boxes = TK >> box_log2;
+    const int box = lane / NB, blk = lane % NB;
+    const bool mine = box < boxes;
+    const int32_t* trow = a.table + (int64_t)b * a.table_stride;
+    auto page_of = [&](int jt, bool& want) -> int {
+      const int j0 = tile_at(tl, t0 + jt) * TK + (box << box_log2);
+      want = mine && any_sees(tl, j0, j0 + (1 << box_log2), a.sinks);
+      return want ? trow[j0 >> a.page_log2] : 0;
+    };
+    bool want = false, ok = true;
+    int page = n > 0 ? page_of(0, want) : 0;
+    int jt = 0;
+    bool k_sent = false;
+    for (; jt < n && !a.idle; ++jt) {
+      const int s = jt & 1;
+      bool want_n = false;
+      int page_n = 0;
+      if (jt + 1 < n) page_n = page_of(jt + 1, want_n);
+      if (want && (page < 0 || page >= a.num_pages)) {   // not followed: the first page in its place
+        record_status(a.status, QWM_ERR_INVALID_ARG);
+        page = 0;
+      }
+      const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, want)) * (128u << box_log2);
+      const int y = (tile_at(tl, t0 + jt) * TK + (box << box_log2)) & ((1 << a.page_log2) - 1);
+      k_sent = false;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        if (jt >= ST && !(ok = wait_all((kv ? B_VEMPTY : B_KEMPTY) + s, ((jt >> 1) - 1) & 1))) break;
+        const uint32_t fb = bar((kv ? B_VFULL : B_KFULL) + s);
+        if (lane == 0) mbar_arrive_expect_tx(fb, bytes);
+        __syncwarp();
+        if (want)
+          tma_load_3d(smem_u32(sm + (kv ? L::V : L::K)) + (s * NB + blk) * BLK + ((box << box_log2) * 128), &map, blk * 64,
+                      y, (page * 2 + kv) * a.Hk + hk, fb);
+        __syncwarp();
+        k_sent = true;
+      }
+      if (!ok) break;
+      page = page_n;
+      want = want_n;
+    }
+    if (!ok) {
+      // a wait ran out: let the copies in flight land before the CTA ends
+      s_err = 1;
+      for (int u = max(0, jt - ST); u < jt; ++u) {
+        mbar_wait(bar(B_KFULL + (u & 1)), (u >> 1) & 1, kDrainNs);
+        mbar_wait(bar(B_VFULL + (u & 1)), (u >> 1) & 1, kDrainNs);
+      }
+      if (k_sent) mbar_wait(bar(B_KFULL + (jt & 1)), (jt >> 1) & 1, kDrainNs);
+    }
+  } else {
+    // ------------------------------------------------------------ guard of the Values
+    bool ok = true;
+    for (int jt = 0; jt < n; ++jt) {
+      const int s = jt & 1;
+      if (!(ok = wait_all(B_VFULL + s, (jt >> 1) & 1))) break;
+      const int j0 = tile_at(tl, t0 + jt) * TK;
+      if (!all_see(tl, j0, j0 + TK, a.sinks)) {
+        bool odd = false;
+        for (int jj = 0; jj < TK; jj += 4) {
+          // four keys a step, eight lanes a key
+          const int key = jj + (lane >> 3), j = j0 + key;
+          if (all_see(tl, j, j + 1, a.sinks)) continue;
+          const bool any = any_sees(tl, j, j + 1, a.sinks);
+#pragma unroll
+          for (int kb = 0; kb < NB; ++kb) {
+            uint4* p = reinterpret_cast<uint4*>(sm + L::V + (s * NB + kb) * BLK + key * 128 + ((lane & 7) << 4));
+            if (!any) {
+              *p = make_uint4(0, 0, 0, 0);
+            } else {
+              uint4 v = *p;
+              uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+              bool hit = false;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                if ((w[k] & Elem<T>::kExp) == Elem<T>::kExp) { w[k] &= 0xFFFF0000u; hit = true; }
+                if (((w[k] >> 16) & Elem<T>::kExp) == Elem<T>::kExp) { w[k] &= 0xFFFFu; hit = true; }
+              }
+              if (hit) *p = v;
+              odd |= hit;
+            }
+          }
+        }
+        if (odd) s_poison = 1;
+        fence_proxy_async_smem();
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(B_VRDY + s));
+    }
+    if (!ok) s_err = 1;
+  }
+
+  tc_fence_before();
+  if (parts > 1) __threadfence();
+  __syncthreads();
+  if (warp == W_MMA) {
+    tc_fence_after();
+    tmem_dealloc(tbase, 512);
+  }
+  if (tid == 0 && s_err) record_status(a.status, QWM_ERR_TIMEOUT);
+  if (parts == 1) return;
+  // the part that arrives last joins all of them, in part order
+  const int64_t group = ((int64_t)b * a.Hk + hk) * rtiles + rt;
+  if (tid == 0) s_last = atomicAdd(a.counter + group, 1) == parts - 1;
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  for (int idx = tid; idx < nrow * (D / 4); idx += NT) {
+    const int r = idx / (D / 4), c = idx % (D / 4);
+    const int64_t pr = group * a.nsplit * 256 + r;
+    float m = -INFINITY;
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, __ldcg(&a.part_ml[pr + p * 256].x));
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+      const float2 ml = __ldcg(&a.part_ml[pr + p * 256]);
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(a.part_o + (pr + p * 256) * D + 4 * c));
+      const float f = ex2f((ml.x - ref) * sl2);
+      l = fmaf(ml.y, f, l);
+      v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
+    }
+    const int64_t rr = r0 + r;
+    const int tok = (int)(rr / a.G), head = hk * a.G + (int)(rr % a.G);
+    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (sq.q0 + tok) * a.o_tok + (int64_t)head * a.o_head + 4 * c) =
+        make_uint2(Elem<T>::pack(v.x * inv, v.y * inv), Elem<T>::pack(v.z * inv, v.w * inv));
+    if (a.lse && c == 0)
+      a.lse[(int64_t)head * a.N + sq.q0 + tok] = m == -INFINITY ? -INFINITY : m * a.scale + logf(l);
+  }
+  if (tid == 0) a.counter[group] = 0;
+}
+
+template <typename T, int D>
+cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
+  cudaError_t e = cudaFuncSetAttribute(paged_chunk<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL);
+  if (e != cudaSuccess) return e;
+  const int64_t rtiles = ((int64_t)a.max_q * a.G + 255) / 256;
+  paged_chunk<T, D><<<dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), NT, Smem<D>::TOTAL, s>>>(map, a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, bool split) {
+  PagedPlan p{};
+  const int64_t rtiles = (rows + 255) / 256;
+  p.groups = (int)(rtiles * B * Hk);
+  p.rows = 256;
+  p.min_tiles = 4;
+  p.nsplit = 1;
+  const int64_t tiles = (max_visible + TK - 1) / TK + 2;
+  if (split && p.groups < 2 * nsm) {
+    // parts so that two waves of CTAs cover the GPU, each of at least 4 tiles
+    const int64_t want = (2 * (int64_t)nsm) / p.groups;
+    const int64_t most = (tiles + p.min_tiles - 1) / p.min_tiles;
+    p.nsplit = (int)(want < most ? want : most);
+    if (p.nsplit < 1) p.nsplit = 1;
+  }
+  return p;
+}
+
+cudaError_t launch_paged_chunk(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s) {
+  if (dtype == QWM_F16) return D == 64 ? go<__half, 64>(a, map, s) : go<__half, 128>(a, map, s);
+  return D == 64 ? go<__nv_bfloat16, 64>(a, map, s) : go<__nv_bfloat16, 128>(a, map, s);
+}
+
+}  // namespace qwm

@@ -6,7 +6,7 @@
 
 #include <cudaTypedefs.h>
 
-#include "qwm_internal.cuh"
+#include "paged.cuh"
 
 namespace qwm {
 namespace {
@@ -45,6 +45,19 @@ bool make_table_map(CUtensorMap* m, const void* tab, int C, int H, int box_rows)
   cuuint32_t es[3] = {1, 1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(tab), dims, strides, box, es,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool make_page_map(CUtensorMap* m, const void* pages, int64_t blocks, int page_tokens, int D, int dtype) {
+  PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
+  if (!fn || blocks < 1) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)page_tokens, (cuuint64_t)blocks};
+  cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)D * 2 * page_tokens};
+  cuuint32_t box[3] = {64, (cuuint32_t)(page_tokens < 64 ? page_tokens : 64), 1};
+  cuuint32_t es[3] = {1, 1, 1};
+  return fn(m, dtype == QWM_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+            const_cast<void*>(pages), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

@@ -1,0 +1,342 @@
+"""GPU: append into paged storage and attention over its pages, against the
+formulas in 64 bits (tests/paged_ref.py).  Every slot that holds no token is
+NaN, so a kernel that let one through would show it."""
+import math
+
+import pytest
+import torch
+
+import paper_2609_26425_gb300 as qwm
+from paged_ref import attend64, inv_freq, make_case, offsets, rope64, rope_bound, visible
+
+pytestmark = pytest.mark.gpu
+BF, HF = torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    qwm.lib()
+
+
+def build(lens, Hk, D, dtype, page, pages, table):
+    cache = qwm.PagedCache(Hk, pages.shape[0], page_tokens=page, head_dim=D, dtype=dtype)
+    cache.pages.copy_(pages)
+    batch = qwm.PagedBatch(offsets(lens).cuda(), torch.tensor([kv for _, kv in lens], dtype=torch.int32).cuda(),
+                           table.cuda(), max(a for a, _ in lens), max(kv for _, kv in lens))
+    return cache, batch
+
+
+def compare(got, lse, want):
+    out, l64, ob, lb = want
+    g = got.double().cpu()
+    assert bool(torch.isfinite(g).all())
+    err = (g - out).abs()
+    assert bool((err <= ob).all()), float((err / ob.clamp(min=1e-300)).max())
+    le = lse.double().cpu()
+    empty = torch.isinf(l64)
+    assert torch.equal(torch.isinf(le) & (le < 0), empty)
+    assert bool(((le - l64).abs()[~empty] <= lb[~empty]).all())
+    assert bool((g[empty.t()] == 0).all())
+
+
+def run_case(seed, lens, Hq, Hk, D, dtype, page, block, window, sinks):
+    q, keys, values, pages, table = make_case(seed, lens, Hq, Hk, D, dtype, page)
+    # pages that no row sees are given back
+    for b, (ql, kv) in enumerate(lens):
+        see = torch.zeros(kv, dtype=torch.bool)
+        for i in range(ql):
+            see |= visible(kv - ql + i, kv, block, window, sinks)
+        for i in range((kv + page - 1) // page):
+            if not bool(see[i * page:(i + 1) * page].any()):
+                table[b, i] = -1
+    cache, batch = build(lens, Hk, D, dtype, page, pages, table)
+    want = attend64(q, keys, values, lens, block, window, sinks)
+    for split in (False, True):
+        ws = qwm.paged_attend_workspace(cache, batch, Hq, window, sinks, block) if split else None
+        if split and ws is None:
+            continue
+        out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), window=window, sinks=sinks, block=block, want_lse=True,
+                                        workspace=ws)
+        compare(out, lse, want)
+        again, _ = qwm.qwm_paged_attend(cache, batch, q.cuda(), window=window, sinks=sinks, block=block, want_lse=True,
+                                        workspace=ws)
+        assert torch.equal(out, again)          # the same bits, whichever part ends last
+    assert cache.status() == 0
+
+
+STEP = [
+    # lens (new, held), Hq, Hk, D, dtype, page, block, window, sinks
+    ([(1, 1)], 1, 1, 128, BF, 16, 1, 0, 0),
+    ([(1, 0), (1, 1), (0, 5), (1, 64), (1, 65)], 4, 4, 128, BF, 16, 1, 0, 0),      # nothing held; no new token
+    ([(1, 127), (1, 128), (1, 129), (1, 1000)], 8, 2, 64, HF, 32, 1, 0, 0),
+    ([(1, 700), (1, 33)], 40, 8, 128, BF, 64, 1, 100, 4),
+    ([(1, 1500), (1, 1499)], 5, 1, 128, HF, 128, 1, 513, 70),
+    ([(4, 300), (3, 3), (2, 1), (1, 90)], 8, 2, 64, BF, 16, 1, 17, 3),              # drafts; rows before the start
+    ([(5, 777)], 6, 1, 128, HF, 32, 4, 64, 20),                                     # 30 rows, blocks of 4
+    ([(7, 1037)], 4, 1, 128, BF, 16, 1, 0, 0),
+    ([(1, 2900)], 32, 1, 64, HF, 64, 1, 0, 0),                                      # 32 heads on one cache head
+    ([(8, 40)], 3, 3, 128, BF, 16, 8, 0, 0),                                        # a whole block at once
+    ([(1, 1200)], 2, 2, 128, BF, 16, 1, 1, 0),                                      # a window of the token itself
+    ([(1, 1200)], 2, 2, 128, BF, 16, 1, 40, 1100),                                  # sinks reach the window
+]
+
+
+@pytest.mark.parametrize("case", range(len(STEP)))
+def test_step(case):
+    run_case(100 + case, *STEP[case])
+
+
+CHUNK = [
+    ([(33, 33)], 1, 1, 128, BF, 16, 1, 0, 0),
+    ([(128, 128)], 1, 1, 128, HF, 64, 1, 0, 0),
+    ([(129, 700), (1, 5), (0, 9), (40, 20)], 2, 2, 64, BF, 32, 1, 0, 0),            # ragged; rows before the start
+    ([(257, 300)], 1, 1, 128, BF, 128, 1, 50, 7),
+    ([(100, 1000)], 3, 1, 64, HF, 16, 1, 130, 200),                                 # 300 rows of three grouped heads
+    ([(90, 360)], 2, 1, 128, BF, 16, 90, 0, 0),                                     # frames of 90
+    ([(90, 810)], 4, 2, 128, HF, 32, 90, 270, 45),                                  # frames, window of 3, half a frame kept
+    ([(50, 500)], 1, 1, 128, BF, 16, 1 << 20, 0, 0),                                # no mask
+    ([(70, 70), (300, 301)], 2, 2, 64, HF, 64, 64, 128, 10),
+    ([(60, 7)], 1, 1, 64, BF, 16, 1, 0, 0),
+    ([(45, 0)], 1, 1, 128, BF, 16, 1, 0, 0),                                        # nothing held: every row empty
+    ([(35, 2100)], 7, 7, 128, BF, 64, 1, 0, 0),                                     # long and few rows: split
+]
+
+
+@pytest.mark.parametrize("case", range(len(CHUNK)))
+def test_chunk(case):
+    run_case(200 + case, *CHUNK[case])
+
+
+@pytest.mark.parametrize("new,heads", [(4, 2), (60, 2)])
+@pytest.mark.parametrize("what", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("dtype,D,page", [(BF, 128, 16), (HF, 64, 64)])
+def test_nonfinite_tokens_reach_the_rows_that_see_them_only(new, heads, what, dtype, D, page):
+    lens = [(new, 300)]
+    q, keys, values, pages, table = make_case(7, lens, heads, 1, D, dtype, page)
+    window, sinks = 200, 5
+    odd_k, odd_v = 298, 300 - new + 1              # the last but one token's Key, the second new token's Value
+    early = 300 - new - window + 2                 # a Value that the first rows see and later ones do not
+    table_of = lambda j: (int(table[0, j // page]), j % page)
+    pk, pv, pe = table_of(odd_k), table_of(odd_v), table_of(early)
+    pages[pk[0], 0, 0, pk[1], 3] = math.nan
+    pages[pv[0], 1, 0, pv[1], 9] = what
+    pages[pe[0], 1, 0, pe[1], 11] = what
+    cache, batch = build(lens, 1, D, dtype, page, pages, table)
+    for ws in (None, qwm.paged_attend_workspace(cache, batch, heads, window, sinks, 1)):
+        out = qwm.qwm_paged_attend(cache, batch, q.cuda(), window=window, sinks=sinks, workspace=ws).cpu()
+        for i in range(new):
+            p = 300 - new + i
+            fine = torch.isfinite(out[i])
+            if p >= odd_k:
+                assert not bool(fine.any())
+                continue
+            want = torch.ones(heads, D, dtype=torch.bool)
+            if p >= odd_v:
+                want[:, 9] = False
+            if early >= p + 1 - window:
+                want[:, 11] = False
+            assert torch.equal(fine, want), (i, p)
+    k2, v2 = [keys[0].clone()], [values[0].clone()]
+    ref = attend64(q, k2, v2, lens, 1, window, sinks)
+    first = out[0].double()                        # the first row sees the early Value only
+    ok = torch.arange(D) != 11
+    assert bool(((first - ref[0][0]).abs() <= ref[2][0])[:, ok].all())
+
+
+def test_strided_and_head_major_tensors():
+    lens, Hq, Hk, D = [(40, 90), (9, 200)], 4, 2, 128
+    q, keys, values, pages, table = make_case(11, lens, Hq, Hk, D, BF, 16)
+    cache, batch = build(lens, Hk, D, BF, 16, pages, table)
+    N = q.shape[0]
+    ref = qwm.qwm_paged_attend(cache, batch, q.cuda())
+    wide = torch.zeros(N, Hq + 3, D + 8, dtype=BF, device="cuda")
+    wide[:, 1:1 + Hq, :D] = q.cuda()
+    out = torch.full((Hq, N, D), 7.0, dtype=BF, device="cuda")
+    got = qwm.qwm_paged_attend(cache, batch, wide[:, 1:1 + Hq, :D], out=out.permute(1, 0, 2))
+    assert torch.equal(got, ref)
+    small = qwm.PagedBatch(offsets([(2, 90), (1, 200)]).cuda(), torch.tensor([90, 200], dtype=torch.int32).cuda(),
+                           table.cuda(), 2, 200)
+    q3 = wide[:3, 1:1 + Hq, :D]
+    a = qwm.qwm_paged_attend(cache, small, q3.contiguous())
+    b = qwm.qwm_paged_attend(cache, small, q3, out=out.permute(1, 0, 2)[:3])
+    assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rope_on,il,dtype,D,page,Hq,Hk", [
+    (True, True, BF, 128, 16, 5, 5), (True, False, HF, 64, 64, 8, 2), (False, True, BF, 64, 128, 3, 1),
+    (True, True, HF, 128, 32, 12, 4)])
+def test_append_stores_each_token_once_and_nothing_else(rope_on, il, dtype, D, page, Hq, Hk):
+    lens = [(1, 1), (37, 100), (0, 12), (130, 130), (5, 3), (1, 65)]
+    g = torch.Generator().manual_seed(D + page)
+    N = sum(a for a, _ in lens)
+    qkv = torch.randn(N, Hq + 2 * Hk, D, generator=g).to(dtype)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hk], qkv[:, Hq + Hk:]
+    pos = torch.randint(0, 300, (N, 3), generator=g, dtype=torch.int32)
+    pairs = (D // 2 - 2 * (D // 6), D // 6, D // 6)
+    freq = inv_freq(pairs)
+    _, _, _, pages, table = make_case(3, lens, 1, Hk, D, dtype, page)
+    marks = torch.randn(pages.shape, generator=g).to(dtype)
+    cache, batch = build(lens, Hk, D, dtype, page, marks, table)
+    rope = qwm.Rope(freq.cuda(), pairs, interleaved=il) if rope_on else None
+    dev = qkv.cuda()
+    q_rot = qwm.qwm_paged_append(cache, batch, dev[:, Hq:Hq + Hk], dev[:, Hq + Hk:], rope=rope,
+                                 pos=pos.cuda() if rope_on else None, q=dev[:, :Hq])
+    k64 = rope64(k, pos, freq, pairs, il) if rope_on else k.double()
+    kb = rope_bound(k, k64, dtype, pairs, il) if rope_on else torch.zeros_like(k64)
+    q64 = rope64(q, pos, freq, pairs, il) if rope_on else q.double()
+    qb = rope_bound(q, q64, dtype, pairs, il) if rope_on else torch.zeros_like(q64)
+    assert bool(((q_rot.double().cpu() - q64).abs() <= qb).all())
+    got, want, bound = cache.pages.double().cpu(), marks.double().clone(), torch.zeros(marks.shape, dtype=torch.float64)
+    row = 0
+    for b, (ql, kv) in enumerate(lens):
+        for i in range(ql):
+            p = kv - ql + i
+            if p >= 0:
+                at = int(table[b, p // page]), p % page
+                want[at[0], 0, :, at[1]], bound[at[0], 0, :, at[1]] = k64[row], kb[row]
+                want[at[0], 1, :, at[1]] = v[row].double()
+            row += 1
+    assert bool(((got - want).abs() <= bound).all())
+    assert cache.status() == 0
+    # without Queries, the same pages
+    cache.pages.copy_(marks)
+    assert qwm.qwm_paged_append(cache, batch, dev[:, Hq:Hq + Hk], dev[:, Hq + Hk:], rope=rope,
+                                pos=pos.cuda() if rope_on else None) is None
+    assert torch.equal(cache.pages.double().cpu(), got)
+
+
+def test_offsets_beyond_32_bits():
+    Hk, page, D = 8, 128, 128
+    num = (1 << 31) // (2 * Hk * page * D) + 9              # the last pages start past 2^31 elements
+    cache = qwm.PagedCache(Hk, num, page_tokens=page, head_dim=D)
+    lens = [(40, 300), (1, 129)]
+    ids = [num - 1, 0, num - 4, num - 2, num - 3]
+    table = torch.tensor([ids[:3], [ids[3], ids[4], -1]], dtype=torch.int32)
+    g = torch.Generator().manual_seed(1)
+    total = [(kv, kv) for _, kv in lens]
+    k = torch.randn(429, Hk, D, generator=g).to(BF)
+    v = torch.randn(429, Hk, D, generator=g).to(BF)
+    load = qwm.PagedBatch(offsets(total).cuda(), torch.tensor([300, 129], dtype=torch.int32).cuda(), table.cuda(), 300, 300)
+    qwm.qwm_paged_append(cache, load, k.cuda(), v.cuda())
+    q = torch.randn(41, Hk, D, generator=g).to(BF)
+    batch = qwm.PagedBatch(offsets(lens).cuda(), torch.tensor([300, 129], dtype=torch.int32).cuda(), table.cuda(), 40, 300)
+    out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True)
+    compare(out, lse, attend64(q, [k[:300], k[300:]], [v[:300], v[300:]], lens, 1, 0, 0))
+    one = qwm.PagedBatch(offsets([(1, 300), (1, 129)]).cuda(), torch.tensor([300, 129], dtype=torch.int32).cuda(),
+                         table.cuda(), 1, 300)
+    out, lse = qwm.qwm_paged_attend(cache, one, q[:2].cuda(), want_lse=True)
+    compare(out, lse, attend64(q[:2], [k[:300], k[300:]], [v[:300], v[300:]], [(1, 300), (1, 129)], 1, 0, 0))
+    assert cache.status() == 0
+
+
+def test_another_stream_and_a_captured_graph():
+    lens, Hq, Hk, D, page = [(1, 500), (1, 30)], 8, 2, 128, 16
+    q, keys, values, pages, table = make_case(21, lens, Hq, Hk, D, BF, page)
+    cache, batch = build(lens, Hk, D, BF, page, pages, table)
+    ws = qwm.paged_attend_workspace(cache, batch, Hq)
+    dq, ref = q.cuda(), qwm.qwm_paged_attend(cache, batch, q.cuda(), workspace=ws).clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(2_000_000)
+        late = dq.clone()
+        got = qwm.qwm_paged_attend(cache, batch, late, workspace=ws)
+    side.synchronize()
+    assert torch.equal(got, ref)
+    graph, out = torch.cuda.CUDAGraph(), torch.empty_like(dq)
+    with torch.cuda.graph(graph):
+        qwm.qwm_paged_attend(cache, batch, dq, out=out, workspace=ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, ref)
+    batch.tensors[1].copy_(torch.tensor([437, 29], dtype=torch.int32))      # shorter sequences, the same graph
+    graph.replay()
+    torch.cuda.synchronize()
+    short = [(1, 437), (1, 29)]
+    want = attend64(q, [keys[0][:437], keys[1][:29]], [values[0][:437], values[1][:29]], short, 1, 0, 0)
+    assert bool(((out.double().cpu() - want[0]).abs() <= want[2]).all())
+
+
+def test_entries_out_of_range_are_recorded_and_not_followed():
+    lens, Hk, D, page = [(1, 100), (40, 100)], 2, 128, 16
+    q, keys, values, pages, table = make_case(31, lens, 2, Hk, D, BF, page)
+    k = torch.zeros(41, Hk, D, dtype=BF, device="cuda")
+    for bad in (pages.shape[0], -7, 1 << 30):
+        broken = table.clone()
+        broken[1, 6] = bad
+        cache, batch = build(lens, Hk, D, BF, page, pages, broken)
+        out = qwm.qwm_paged_attend(cache, batch, q.cuda())
+        assert cache.status() == 1 and cache.status() == 0
+        good = attend64(q[:1], keys[:1], values[:1], lens[:1], 1, 0, 0)     # the other sequence is as it should be
+        assert bool(((out[:1].double().cpu() - good[0]).abs() <= good[2]).all())
+        qwm.qwm_paged_append(cache, batch, k, k)
+        assert cache.status() == 1
+    cache, _ = build(lens, Hk, D, BF, page, pages, table)
+    for off, kvl, mq, mkv in (([0, 1, 42], [100, 100], 41, 100), ([0, 50, 41], [100, 100], 50, 100),
+                              ([0, 1, 41], [100, 101], 40, 100), ([0, 1, 41], [100, -1], 40, 100),
+                              ([0, 1, 41], [100, 1 << 20], 40, 1 << 21), ([0, 1, 41], [100, 100], 39, 100)):
+        batch = qwm.PagedBatch(torch.tensor(off, dtype=torch.int32).cuda(), torch.tensor(kvl, dtype=torch.int32).cuda(),
+                               table.cuda(), mq, mkv)
+        qwm.qwm_paged_attend(cache, batch, q.cuda())
+        assert cache.status() == 1, (off, kvl)
+        qwm.qwm_paged_append(cache, batch, k, k)
+        assert cache.status() == 1, (off, kvl)
+
+
+def test_refusals():
+    lens, Hk, D, page = [(3, 40)], 2, 128, 16
+    q, _, _, pages, table = make_case(41, lens, 4, Hk, D, BF, page)
+    cache, batch = build(lens, Hk, D, BF, page, pages, table)
+    dq = q.cuda()
+
+    def status(fn):
+        with pytest.raises(qwm.QwmError) as e:
+            fn()
+        return e.value.status
+
+    assert status(lambda: qwm.qwm_paged_attend(cache, batch, dq[:, :3])) == 1                    # heads not grouped
+    assert status(lambda: qwm.qwm_paged_attend(cache, batch, dq, block=0)) == 1
+    assert status(lambda: qwm.qwm_paged_attend(cache, batch, dq, window=-1)) == 1
+    assert status(lambda: qwm.qwm_paged_attend(cache, batch, dq, window=7, block=8)) == 1        # less than a block
+    assert status(lambda: qwm.qwm_paged_attend(cache, batch, dq, sinks=-1)) == 1
+    assert status(lambda: qwm.qwm_paged_attend(cache, batch, dq, sm_scale=0.0)) == 1
+    assert status(lambda: qwm.qwm_paged_attend(cache, batch, dq, sm_scale=math.nan)) == 1
+    assert status(lambda: qwm.qwm_paged_attend(cache, batch, dq, out=dq[:1].expand(3, 4, D).clone()[:1].expand(3, 4, D))) == 1
+    assert status(lambda: qwm.PagedCache(2, 4, page_tokens=24)) == 2
+    assert status(lambda: qwm.PagedCache(2, 4, head_dim=96)) == 2
+    assert status(lambda: qwm.PagedCache(0, 4)) == 2
+    for bad in (dq.half(), dq[..., :64], dq.cpu(), dq[0]):
+        with pytest.raises(ValueError):
+            qwm.qwm_paged_attend(cache, batch, bad)
+    k = torch.zeros(3, Hk, D, dtype=BF, device="cuda")
+    rope = qwm.Rope(inv_freq((22, 21, 21)).cuda(), (22, 21, 21))
+    with pytest.raises(ValueError):
+        qwm.qwm_paged_append(cache, batch, k, k, rope=rope)                                      # no positions
+    with pytest.raises(ValueError):
+        qwm.qwm_paged_append(cache, batch, k, k[:2])
+    assert status(lambda: qwm.qwm_paged_append(cache, batch, k[:, :1], k)) == 1
+    with pytest.raises(ValueError):
+        qwm.PagedBatch(batch.tensors[0].long(), batch.tensors[1], batch.tensors[2], 3, 40)
+    none = torch.empty(0, 4, D, dtype=BF, device="cuda")
+    assert qwm.qwm_paged_attend(cache, batch, none).shape == none.shape                          # no rows: nothing to do
+    assert cache.status() == 0
+
+
+@pytest.mark.parametrize("new", [1, 60])
+def test_a_wait_that_runs_out_is_recorded_and_the_next_call_is_exact(new):
+    lens, Hk, D, page = [(new, 900)], 2, 128, 16
+    q, keys, values, pages, table = make_case(51, lens, 2, Hk, D, BF, page)
+    cache, batch = build(lens, Hk, D, BF, page, pages, table)
+    ws = qwm.paged_attend_workspace(cache, batch, 2)
+    cache.set_wait_limit(1_000_000)                # 1 ms
+    cache.set_idle_role(qwm.QWM_ROLE_PAGE_LOADS)
+    qwm.qwm_paged_attend(cache, batch, q.cuda(), workspace=ws)
+    torch.cuda.synchronize()
+    assert cache.status() == 5
+    cache.set_idle_role(0)
+    cache.set_wait_limit(2_000_000_000)
+    out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True, workspace=ws)
+    compare(out, lse, attend64(q, keys, values, lens, 1, 0, 0))
+    assert cache.status() == 0

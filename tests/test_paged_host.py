@@ -1,0 +1,60 @@
+"""Host-only checks of the rotary and paged entry points: sizes and refusals that
+need no GPU (every call here returns before anything is launched)."""
+import ctypes as ct
+
+import pytest
+
+from paper_2609_26425_gb300 import paged
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2609_26425_gb300 import build
+    build.build()
+    import paper_2609_26425_gb300 as qwm
+    return qwm.lib()
+
+
+def rows(heads=2, data=4096, token=256, head=128):
+    return paged.QwmRows(data, token, head, heads)
+
+
+def test_buffer_holds_a_header_and_the_pages(L):
+    for hk, d, t, n in ((8, 128, 64, 5), (1, 64, 16, 1), (40, 128, 128, 1000)):
+        assert L.qwm_paged_bytes(paged.QwmPagedConfig(hk, d, t, 0, n)) == 256 + n * 2 * hk * t * d * 2
+    for hk, d, t, dt, n in ((0, 128, 64, 0, 5), (8, 96, 64, 0, 5), (8, 128, 24, 0, 5), (8, 128, 256, 0, 5),
+                            (8, 128, 64, 2, 5), (8, 128, 64, 0, 0), (4096, 128, 16, 0, 1 << 19)):
+        assert L.qwm_paged_bytes(paged.QwmPagedConfig(hk, d, t, dt, n)) == 0
+
+
+def test_rope_refusals(L):
+    def call(pairs=(22, 21, 21), d=128, dt=0, il=1, n=4, q=None, qo=None, k=None, ko=None, freq=4096, pos=4096):
+        cfg = paged.QwmRopeConfig(d, dt, (ct.c_int32 * 3)(*pairs), il)
+        return L.qwm_rope(cfg, freq, pos, n, q or rows(), qo or rows(), k, ko, None)
+
+    assert call(n=0) == 0                                   # nothing to do
+    assert call(n=0, freq=None, pos=None) == 0
+    assert call(freq=None) == 1 and call(pos=None) == 1 and call(n=-1) == 1
+    assert call(pairs=(22, 21, 22)) == 2                    # more channels than there are
+    assert call(pairs=(0, 0, 0)) == 2 and call(pairs=(1, 1, 1)) == 2
+    assert call(pairs=(4, 4, 4), il=0) == 2                 # halves come in eights
+    assert call(pairs=(-4, 4, 4)) == 1
+    assert call(d=264) == 2 and call(d=100) == 2 and call(dt=2) == 2
+    assert call(q=rows(3)) == 1                             # heads differ
+    assert call(q=rows(data=4098)) == 1 and call(q=rows(token=252)) == 1 and call(q=rows(head=-128)) == 1
+    assert call(qo=rows(token=0)) == 1                      # written rows that share memory
+    assert call(k=rows()) == 1                              # Keys in, none out
+
+
+def test_calls_without_a_cache_or_a_batch_are_refused(L):
+    b = paged.QwmPagedBatch(1, 1, 1, 1, 1, 4096, 4096, 4096)
+    m = paged.QwmMask(1, 0, 0)
+    assert L.qwm_paged_append(None, b, rows(), rows(), None, None, None, None, None, None) == 1
+    assert L.qwm_paged_attend(None, b, rows(), m, 1.0, rows(), None, None, 0, None) == 1
+    assert L.qwm_paged_attend_workspace_bytes(None, b, 2, m) == 0
+    assert L.qwm_paged_set_wait_limit(None, 2000) == 1 and L.qwm_paged_set_idle_role(None, 0) == 1
+    h = ct.c_void_p()
+    assert L.qwm_paged_init(ct.byref(h), paged.QwmPagedConfig(8, 128, 64, 0, 5), None, 1 << 30, None) == 1
+    assert L.qwm_paged_init(ct.byref(h), paged.QwmPagedConfig(8, 80, 64, 0, 5), 4096, 1 << 30, None) == 2
+    assert L.qwm_paged_init(ct.byref(h), paged.QwmPagedConfig(8, 128, 64, 0, 5), 4097, 1 << 30, None) == 1
+    assert L.qwm_paged_init(ct.byref(h), paged.QwmPagedConfig(8, 128, 64, 0, 5), 4096, 256, None) == 3
