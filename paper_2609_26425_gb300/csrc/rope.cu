@@ -14,7 +14,6 @@ namespace {
 using namespace ptx;
 
 constexpr int NT = 256;
-constexpr int kMaxPairs = 128;
 
 // (cos, sin) of pos * f.  The product is carried as hi + lo (exact for |pos| <
 // 2^24; the rest of a larger position adds its own product), then reduced by
@@ -50,12 +49,48 @@ __device__ __forceinline__ float2 turn(int pos, float f, float sign) {
   return make_float2(cs, sign * sn);
 }
 
-// Up to kLoads 16-byte vectors are in flight per thread.
+// Vectors (pairs of vectors) in flight per thread: with 3 or 4 CTAs an SM holds
+// 48 to 64 KB of loads in flight, what 6.8 TB/s at about 1 us wants.
 constexpr int kLoads = 4;
+constexpr int kMaxTokens = 16;                     // tokens of a CTA
+
+// Where a token's Keys and Values go: the first [heads] block of its page and
+// its slot, block < 0: nowhere.
+struct Place {
+  int64_t block;
+  int slot;
+};
+__device__ __forceinline__ Place place_of(const RopeArgs& a, int64_t n) {
+  int lo = 0, hi = a.B;                            // last b with q_off[b] <= n
+  while (hi - lo > 1) {
+    const int m = (lo + hi) >> 1;
+    if (a.q_off[m] <= n) lo = m; else hi = m;
+  }
+  const int64_t q0 = a.q_off[lo], q1 = a.q_off[lo + 1], kv = a.kv_len[lo];
+  int64_t cap = (int64_t)a.table_stride << a.page_log2;
+  if (cap > a.max_kv) cap = a.max_kv;
+  Place r{-1, 0};
+  if (!(n >= q0 && n < q1 && q1 <= a.N && q1 - q0 <= a.max_q && kv >= 0 && kv <= cap)) {
+    record_status(a.status, QWM_ERR_INVALID_ARG);
+    return r;
+  }
+  const int64_t p = kv - q1 + n;
+  if (p < 0) return r;
+  const int64_t page = a.table[(int64_t)lo * a.table_stride + (p >> a.page_log2)];
+  if (page < 0 || page >= a.num_pages) {
+    record_status(a.status, QWM_ERR_INVALID_ARG);
+    return r;
+  }
+  r.block = page * 2 * a.kv_heads;
+  r.slot = (int)(p & ((1 << a.page_log2) - 1));
+  return r;
+}
 
 template <typename T, bool INTERLEAVED, bool PAGED>
 __global__ void __launch_bounds__(NT) rope_kernel(const RopeArgs a, int tokens_per_cta) {
-  extern __shared__ float2 table[];  // [tokens_per_cta][P]
+  extern __shared__ float4 table4[];               // (cos, sin) [tokens_per_cta][P]
+  float2* table = reinterpret_cast<float2*>(table4);
+  __shared__ Place places[kMaxTokens];
   const int tid = threadIdx.x;
   const int64_t n0 = (int64_t)blockIdx.x * tokens_per_cta;
   const int nt = (int)min((int64_t)tokens_per_cta, a.N - n0);
@@ -64,117 +99,104 @@ __global__ void __launch_bounds__(NT) rope_kernel(const RopeArgs a, int tokens_p
   // of vectors (u, u + P / 8) and the vectors that pass
   const int pv = INTERLEAVED ? P / 4 : P / 8;      // rotated units
   const int U = INTERLEAVED ? nvec : nvec - pv;
-  const int hpar = NT / U;                         // heads side by side
+  const int hpar = NT / U;                         // rows (token, head) side by side
   const int u = tid % U, hl = tid / U;
+  if (PAGED && tid < nt) places[tid] = place_of(a, n0 + tid);
   if (a.inv_freq) {
     for (int i = tid; i < nt * P; i += NT) {
       const int t = i / P, j = i - t * P;
       const int axis = j < a.pairs[0] ? 0 : (j < a.pairs[0] + a.pairs[1] ? 1 : 2);
       table[i] = turn(a.pos[(n0 + t) * 3 + axis], a.inv_freq[j], a.sign);
     }
-    __syncthreads();
   }
+  __syncthreads();
   if (hl >= hpar) return;
   const bool turned = a.inv_freq != nullptr && u < pv;
   const bool two = !INTERLEAVED && u < pv;         // two vectors a unit
   const int c0 = 8 * (INTERLEAVED || two ? u : u + pv);
   const int c1 = c0 + P;
-  for (int t = 0; t < nt; ++t) {
-    const int64_t n = n0 + t;
-    // the page and slot of the token
-    int64_t block0 = -1;
-    int slot = 0;
-    if (PAGED) {
-      int lo = 0, hi = a.B;                        // last b with q_off[b] <= n
-      while (hi - lo > 1) {
-        const int m = (lo + hi) >> 1;
-        if (a.q_off[m] <= n) lo = m; else hi = m;
-      }
-      const int64_t q0 = a.q_off[lo], q1 = a.q_off[lo + 1], kv = a.kv_len[lo];
-      int64_t cap = (int64_t)a.table_stride << a.page_log2;
-      if (cap > a.max_kv) cap = a.max_kv;
-      const bool ok = n >= q0 && n < q1 && q1 <= a.N && q1 - q0 <= a.max_q && kv >= 0 && kv <= cap;
-      if (!ok) {
-        if (tid == 0) record_status(a.status, QWM_ERR_INVALID_ARG);
-      } else {
-        const int64_t p = kv - q1 + n;
-        if (p >= 0) {
-          const int64_t page = a.table[(int64_t)lo * a.table_stride + (p >> a.page_log2)];
-          if (page >= 0 && page < a.num_pages) {
-            block0 = page * 2 * a.kv_heads;
-            slot = (int)(p & ((1 << a.page_log2) - 1));
-          } else if (tid == 0) {
-            record_status(a.status, QWM_ERR_INVALID_ARG);
-          }
-        }
-      }
-    }
-    float2 cs[8];
-    if (turned) {
-      constexpr int K = INTERLEAVED ? 4 : 8;
+  // rows hl, hl + hpar, ... of the CTA's tokens x heads
+  const int H = a.total_heads;
+  const int step_t = hpar / H, step_h = hpar % H;
+  int t = hl / H, h = hl % H;
+  while (t < nt) {
+    uint4 x[kLoads], y[kLoads];
+    T* dst[kLoads];
+    int cs_at[kLoads];                             // token's row of the table, -1: not turned
 #pragma unroll
-      for (int k = 0; k < K; ++k) cs[k] = table[t * P + u * K + k];
-    }
-    for (int h0 = hl; h0 < a.total_heads; h0 += kLoads * hpar) {
-      uint4 x[kLoads], y[kLoads];
-      T* dst[kLoads];
-      bool rot[kLoads];
-#pragma unroll
-      for (int k = 0; k < kLoads; ++k) {
-        int h = h0 + k * hpar;
-        dst[k] = nullptr;
-        rot[k] = false;
-        if (h < a.total_heads) {
-          int s = 0;
-          if (a.nseg > 1 && h >= a.seg[0].heads) { h -= a.seg[0].heads; s = 1; }
-          if (a.nseg > 2 && s == 1 && h >= a.seg[1].heads) { h -= a.seg[1].heads; s = 2; }
-          const RopeSegment& g = a.seg[s];
-          const T* src = static_cast<const T*>(g.src) + n * g.s_tok + h * g.s_head;
-          if (!PAGED || g.page < 0) dst[k] = static_cast<T*>(g.dst) + n * g.d_tok + h * g.d_head;
-          else if (block0 >= 0)
+    for (int k = 0; k < kLoads; ++k) {
+      dst[k] = nullptr;
+      if (t < nt) {
+        int hs = h, s = 0;
+        if (a.nseg > 1 && hs >= a.seg[0].heads) { hs -= a.seg[0].heads; s = 1; }
+        if (a.nseg > 2 && s == 1 && hs >= a.seg[1].heads) { hs -= a.seg[1].heads; s = 2; }
+        const RopeSegment& g = a.seg[s];
+        const int64_t n = n0 + t;
+        const T* src = static_cast<const T*>(g.src) + n * g.s_tok + hs * g.s_head;
+        if (!PAGED || g.page < 0) {
+          dst[k] = static_cast<T*>(g.dst) + n * g.d_tok + hs * g.d_head;
+        } else {
+          const Place pl = places[t];
+          if (pl.block >= 0)
             dst[k] = static_cast<T*>(a.pages) +
-                     (((block0 + (int64_t)g.page * a.kv_heads + h) << a.page_log2) + slot) * a.D;
-          rot[k] = g.rotate != 0;
-          if (dst[k]) {
-            x[k] = *reinterpret_cast<const uint4*>(src + c0);
-            if (two) y[k] = *reinterpret_cast<const uint4*>(src + c1);
-          }
+                     (((pl.block + (int64_t)g.page * a.kv_heads + hs) << a.page_log2) + pl.slot) * a.D;
         }
+        cs_at[k] = turned && g.rotate ? t * P : -1;
+        if (dst[k]) {
+          x[k] = __ldcs(reinterpret_cast<const uint4*>(src + c0));
+          if (two) y[k] = __ldcs(reinterpret_cast<const uint4*>(src + c1));
+        }
+        t += step_t;
+        h += step_h;
+        if (h >= H) { h -= H; ++t; }
       }
+    }
 #pragma unroll
-      for (int k = 0; k < kLoads; ++k) {
-        if (!dst[k]) continue;
-        if (turned && rot[k]) {
-          uint32_t* xw = reinterpret_cast<uint32_t*>(&x[k]);
-          uint32_t* yw = reinterpret_cast<uint32_t*>(&y[k]);
+    for (int k = 0; k < kLoads; ++k) {
+      if (!dst[k]) continue;
+      if (cs_at[k] >= 0) {
+        uint32_t* xw = reinterpret_cast<uint32_t*>(&x[k]);
+        uint32_t* yw = reinterpret_cast<uint32_t*>(&y[k]);
+        const float4* cs = reinterpret_cast<const float4*>(table + cs_at[k]) + u * (INTERLEAVED ? 2 : 4);
+        if (INTERLEAVED) {
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const float4 c = cs[w];
+            const float2 v = Elem<T>::unpack(xw[2 * w]), z = Elem<T>::unpack(xw[2 * w + 1]);
+            xw[2 * w] = Elem<T>::pack(v.x * c.x - v.y * c.y, v.x * c.y + v.y * c.x);
+            xw[2 * w + 1] = Elem<T>::pack(z.x * c.z - z.y * c.w, z.x * c.w + z.y * c.z);
+          }
+        } else {
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
-            if (INTERLEAVED) {
-              const float2 v = Elem<T>::unpack(xw[w]);
-              xw[w] = Elem<T>::pack(v.x * cs[w].x - v.y * cs[w].y, v.x * cs[w].y + v.y * cs[w].x);
-            } else {
-              const float2 v = Elem<T>::unpack(xw[w]), z = Elem<T>::unpack(yw[w]);
-              const float2 ca = cs[2 * w], cb = cs[2 * w + 1];
-              xw[w] = Elem<T>::pack(v.x * ca.x - z.x * ca.y, v.y * cb.x - z.y * cb.y);
-              yw[w] = Elem<T>::pack(v.x * ca.y + z.x * ca.x, v.y * cb.y + z.y * cb.x);
-            }
+            const float4 c = cs[w];
+            const float2 v = Elem<T>::unpack(xw[w]), z = Elem<T>::unpack(yw[w]);
+            xw[w] = Elem<T>::pack(v.x * c.x - z.x * c.y, v.y * c.z - z.y * c.w);
+            yw[w] = Elem<T>::pack(v.x * c.y + z.x * c.x, v.y * c.w + z.y * c.z);
           }
         }
-        *reinterpret_cast<uint4*>(dst[k] + c0) = x[k];
-        if (two) *reinterpret_cast<uint4*>(dst[k] + c1) = y[k];
       }
+      *reinterpret_cast<uint4*>(dst[k] + c0) = x[k];
+      if (two) *reinterpret_cast<uint4*>(dst[k] + c1) = y[k];
     }
   }
 }
 
 template <typename T, bool IL>
 cudaError_t go(const RopeArgs& a, cudaStream_t s) {
-  // one token a CTA until the grid fills the SMs several times over, then four
-  const int tpc = a.N >= 4096 ? 4 : 1;
+  // tokens of a CTA: enough that each thread has two rounds of kLoads rows, as
+  // long as the grid still covers the SMs about four times
+  const int U = IL ? a.D / 8 : a.D / 8 - a.P / 8;
+  const int hpar = NT / U;
+  int64_t tpc = (2 * kLoads * hpar + a.total_heads - 1) / a.total_heads;
+  const int64_t most = a.N / (4 * 152);
+  if (tpc > most) tpc = most;
+  if (tpc > kMaxTokens) tpc = kMaxTokens;
+  if (tpc < 1) tpc = 1;
   const unsigned grid = (unsigned)((a.N + tpc - 1) / tpc);
   const size_t smem = (size_t)tpc * a.P * sizeof(float2);
-  if (a.pages) rope_kernel<T, IL, true><<<grid, NT, smem, s>>>(a, tpc);
-  else rope_kernel<T, IL, false><<<grid, NT, smem, s>>>(a, tpc);
+  if (a.pages) rope_kernel<T, IL, true><<<grid, NT, smem, s>>>(a, (int)tpc);
+  else rope_kernel<T, IL, false><<<grid, NT, smem, s>>>(a, (int)tpc);
   return cudaGetLastError();
 }
 

@@ -48,8 +48,12 @@ _BATCH = ct.POINTER(QwmPagedBatch)
 _MASK = ct.POINTER(QwmMask)
 
 
+_C = None  # the loaded library, argument types declared
+
+
 def declare(L):
     """Argument types of the entry points in the loaded library."""
+    global _C
     rope = [_ROPE, _P, _P, ct.c_int64, _ROWS, _ROWS, _ROWS, _ROWS, _P]
     for name, args, res in (
             ("qwm_rope", rope, ct.c_int), ("qwm_rope_backward", rope, ct.c_int),
@@ -65,11 +69,14 @@ def declare(L):
              ct.c_int)):
         fn = getattr(L, name)
         fn.argtypes, fn.restype = args, res
+    _C = L
 
 
 def _lib():
-    from . import lib
-    return lib()
+    if _C is None:
+        from . import lib
+        lib()
+    return _C
 
 
 def _check(fn, st):
@@ -78,21 +85,23 @@ def _check(fn, st):
         raise QwmError(fn, st)
 
 
-def _stream():
-    return torch.cuda.current_stream().cuda_stream
+def _stream(t):
+    """The current stream of a tensor's device."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _rows(t, dtype, name, tokens=None, head_dim=None):
     """A [tokens][heads][head_dim] tensor as qwm_rows (any strides of tokens and heads)."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype):
         raise ValueError(f"{name} must be a {dtype} CUDA tensor")
-    if t.dim() != 3 or (tokens is not None and t.shape[0] != tokens) or (
-            head_dim is not None and t.shape[2] != head_dim):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({tokens}, heads, {head_dim})")
+    shape = t.shape
+    if len(shape) != 3 or (tokens is not None and shape[0] != tokens) or (
+            head_dim is not None and shape[2] != head_dim):
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected ({tokens}, heads, {head_dim})")
     st, sh, sc = t.stride()
     if sc != 1:
         raise ValueError(f"{name} must have contiguous channels")
-    n, h, _ = t.shape  # the stride of a dimension of one is never used
+    n, h, _ = shape  # the stride of a dimension of one is never used
     return QwmRows(t.data_ptr(), st if n > 1 else 0, sh if h > 1 else 0, h)
 
 
@@ -150,7 +159,7 @@ def _turn(name, rope, q, pos, k, q_out, k_out):
             raise ValueError(f"k_out has shape {tuple(k_out.shape)}, expected {tuple(k.shape)}")
         ko = _rows(k_out, q.dtype, "k_out")
     _check(name, getattr(_lib(), name)(cfg, rope.inv_freq.data_ptr(), pos.data_ptr(), n, qr,
-                                       _rows(q_out, q.dtype, "q_out"), kr, ko, _stream()))
+                                       _rows(q_out, q.dtype, "q_out"), kr, ko, _stream(q)))
     return q_out if k is None else (q_out, k_out)
 
 
@@ -185,15 +194,14 @@ class PagedCache:
         self.buffer = raw[off:off + n]
         self.pages = self.buffer[256:].view(dtype).view(num_pages, 2, kv_heads, page_tokens, head_dim)
         h = _P()
-        _check("qwm_paged_init", _lib().qwm_paged_init(ct.byref(h), self.cfg, self.buffer.data_ptr(), n, _stream()))
+        _check("qwm_paged_init", _lib().qwm_paged_init(ct.byref(h), self.cfg, self.buffer.data_ptr(), n,
+                                                      _stream(self.buffer)))
         self.handle = h
 
     def __del__(self):
         h = getattr(self, "handle", None)
-        if h:
-            from . import _lib as loaded
-            if loaded is not None:
-                loaded.qwm_paged_free(h)
+        if h and _C is not None:
+            _C.qwm_paged_free(h)
             self.handle = None
 
     def set_wait_limit(self, ns: int):
@@ -206,7 +214,7 @@ class PagedCache:
     def status(self) -> int:
         """Read and clear the device status word (synchronises the stream)."""
         v = ct.c_int32()
-        _check("qwm_paged_status", _lib().qwm_paged_status(self.handle, ct.byref(v), _stream()))
+        _check("qwm_paged_status", _lib().qwm_paged_status(self.handle, ct.byref(v), _stream(self.buffer)))
         return v.value
 
 
@@ -261,7 +269,7 @@ def qwm_paged_append(cache: PagedCache, batch: PagedBatch, k, v, rope: Rope = No
             raise ValueError(f"q_out has shape {tuple(q_out.shape)}, expected {tuple(q.shape)}")
         qo = _rows(q_out, t, "q_out")
     _check("qwm_paged_append", _lib().qwm_paged_append(cache.handle, batch.struct(n), kr, vr, cfg, freq, at, qr, qo,
-                                                       _stream()))
+                                                       _stream(k)))
     return q_out if q is not None else None
 
 
@@ -303,5 +311,5 @@ def qwm_paged_attend(cache: PagedCache, batch: PagedBatch, q, window=0, sinks=0,
     _check("qwm_paged_attend", _lib().qwm_paged_attend(
         cache.handle, batch.struct(n), qr, QwmMask(block, window, sinks), scale, _rows(out, t, "out"),
         None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
-        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(q)))
     return (out, lse) if lse is not None else out
