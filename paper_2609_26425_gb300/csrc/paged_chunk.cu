@@ -94,7 +94,10 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   const int nrow = (int)min((int64_t)256, rows - r0);
   const int nqt = nrow > 128 ? 2 : 1;
   const int p0 = sq.kv - sq.qn;                       // token of the sequence's first row
-  const int tokA = (int)(r0 / a.G), tokB = (int)((r0 + nrow - 1) / a.G);
+  // row r0 + i is new token tokA + (remA + i) / G, grouped head (remA + i) % G
+  const int tokA = (int)(r0 / a.G);
+  const uint32_t G = (uint32_t)a.G, remA = (uint32_t)(r0 - (int64_t)tokA * a.G);
+  const int tokB = tokA + (int)((remA + (uint32_t)nrow - 1) / G);
   const Tiles tl = make_tiles<TK>(p0 + tokA, p0 + tokB, sq.kv, a.block, a.window, a.sinks);
   const int per = max((tl.n + a.nsplit - 1) / a.nsplit, a.min_tiles);
   const int parts = max(1, (tl.n + per - 1) / per);
@@ -141,21 +144,20 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
 #pragma unroll 8
       for (int it = 0; it < CH; ++it) {
         const int idx = it * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
-        const int64_t r = r0 + i * 128 + rr;
+        const uint32_t r = remA + i * 128 + rr;
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (r < rows)
-          v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (sq.q0 + r / a.G) * a.q_tok +
-                                              (hk * a.G + r % a.G) * a.q_head + c * 8);
+        if (i * 128 + rr < nrow)
+          v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (sq.q0 + tokA + r / G) * a.q_tok +
+                                              (hk * a.G + (int)(r % G)) * a.q_head + c * 8);
         *reinterpret_cast<uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v;
       }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(B_QRDY + i));
 
-      const int64_t r = r0 + i * 128 + row;
-      const bool has = r < rows;
-      const int tok = has ? (int)(r / a.G) : tokB;
-      const int head = hk * a.G + (has ? (int)(r % a.G) : 0);
+      const bool has = i * 128 + row < nrow;
+      const int tok = has ? tokA + (int)((remA + i * 128 + row) / G) : tokB;
+      const int head = hk * a.G + (has ? (int)((remA + i * 128 + row) % G) : 0);
       const Span sp = has ? row_span(p0 + tok, sq.kv, a.block, a.window) : Span{0, 0};
       const uint32_t lrow = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t tS = tbase + 128 * i + lrow, tO = tbase + 256 + 128 * i + lrow;
@@ -414,31 +416,48 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       if (!(ok = wait_all(B_VFULL + s, (jt >> 1) & 1))) break;
       const int j0 = tile_at(tl, t0 + jt) * TK;
       if (!all_see(tl, j0, j0 + TK, a.sinks)) {
+        uint8_t* vt = sm + L::V + s * NB * BLK;
+        // The tile's keys fall into runs: [0, s_any) are first tokens that some
+        // row sees, of which [0, s_all) are seen by all; then a gap up to the
+        // windows, [w_lo, w_all) seen by some, [w_all, w_hi) by all, [w_hi,
+        // w_end) by some, and nothing after.  Runs seen by none are cleared,
+        // runs seen by some are searched for infinities and NaN.
+        auto in = [&](int j) { return max(0, min(TK, j - j0)); };
+        const int s_any = in(min(a.sinks, tl.hi_max)), s_all = in(min(a.sinks, tl.hi_min));
+        const int w_lo = max(s_any, in(tl.lo_min)), w_end = max(w_lo, in(tl.hi_max));
+        const int w_all = max(w_lo, min(w_end, in(tl.lo_max))), w_hi = max(w_all, min(w_end, in(tl.hi_min)));
+        // a run of keys: four keys a step, eight lanes a key
+        auto clear = [&](int k0, int k1) {
+          for (int key = k0 + (lane >> 3); key < k1; key += 4)
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+              *reinterpret_cast<uint4*>(vt + kb * BLK + key * 128 + ((lane & 7) << 4)) = make_uint4(0, 0, 0, 0);
+        };
         bool odd = false;
-        for (int jj = 0; jj < TK; jj += 4) {
-          // four keys a step, eight lanes a key
-          const int key = jj + (lane >> 3), j = j0 + key;
-          if (all_see(tl, j, j + 1, a.sinks)) continue;
-          const bool any = any_sees(tl, j, j + 1, a.sinks);
+        auto search = [&](int k0, int k1) {
+#pragma unroll 4
+          for (int key = k0 + (lane >> 3); key < k1; key += 4)
 #pragma unroll
-          for (int kb = 0; kb < NB; ++kb) {
-            uint4* p = reinterpret_cast<uint4*>(sm + L::V + (s * NB + kb) * BLK + key * 128 + ((lane & 7) << 4));
-            if (!any) {
-              *p = make_uint4(0, 0, 0, 0);
-            } else {
+            for (int kb = 0; kb < NB; ++kb) {
+              uint4* p = reinterpret_cast<uint4*>(vt + kb * BLK + key * 128 + ((lane & 7) << 4));
               uint4 v = *p;
-              uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-              bool hit = false;
+              if (nonfinite2<T>(v.x) || nonfinite2<T>(v.y) || nonfinite2<T>(v.z) || nonfinite2<T>(v.w)) {
+                uint32_t* w = reinterpret_cast<uint32_t*>(&v);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                if ((w[k] & Elem<T>::kExp) == Elem<T>::kExp) { w[k] &= 0xFFFF0000u; hit = true; }
-                if (((w[k] >> 16) & Elem<T>::kExp) == Elem<T>::kExp) { w[k] &= 0xFFFFu; hit = true; }
+                for (int k = 0; k < 4; ++k) {
+                  if ((w[k] & Elem<T>::kExp) == Elem<T>::kExp) w[k] &= 0xFFFF0000u;
+                  if (((w[k] >> 16) & Elem<T>::kExp) == Elem<T>::kExp) w[k] &= 0xFFFFu;
+                }
+                *p = v;
+                odd = true;
               }
-              if (hit) *p = v;
-              odd |= hit;
             }
-          }
-        }
+        };
+        search(s_all, s_any);
+        clear(s_any, w_lo);
+        search(w_lo, w_all);
+        search(w_hi, w_end);
+        clear(w_end, TK);
         if (odd) s_poison = 1;
         fence_proxy_async_smem();
       }
@@ -509,12 +528,17 @@ PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, 
   p.min_tiles = 4;
   p.nsplit = 1;
   const int64_t tiles = (max_visible + TK - 1) / TK + 2;
-  if (split && p.groups < 2 * nsm) {
-    // parts so that two waves of CTAs cover the GPU, each of at least 4 tiles
-    const int64_t want = (2 * (int64_t)nsm) / p.groups;
-    const int64_t most = (tiles + p.min_tiles - 1) / p.min_tiles;
-    p.nsplit = (int)(want < most ? want : most);
-    if (p.nsplit < 1) p.nsplit = 1;
+  if (split) {
+    // the split with the least waves x (tiles of a part + a CTA's fixed cost,
+    // about 6 tiles' time with the join); parts of at least 4 tiles
+    int64_t best = 0;
+    for (int64_t n = 1; n <= 64 && n * p.min_tiles <= tiles + p.min_tiles - 1; ++n) {
+      const int64_t waves = (p.groups * n + nsm - 1) / nsm, cost = waves * ((tiles + n - 1) / n + 6);
+      if (n == 1 || cost < best) {
+        best = cost;
+        p.nsplit = (int)n;
+      }
+    }
   }
   return p;
 }
