@@ -10,6 +10,12 @@
 // into P (thread = row) written over S as 16-bit pairs, and P V accumulates in
 // TMEM with P read from there.  Two tiles, because the softmax of one then runs
 // beside the MMAs of the other.  TMEM: S0 | S1 | O0 | O1.
+// The chain S, softmax, P V, next S sets the pace, so the row maximum is kept off
+// it: P is taken against the maximum known before the tile, one pass over S with
+// the exponentials (32 a cycle and SM) as its only bound, and the tile's own
+// maximum is formed beside it.  Where it is above the known one by more than
+// 2^kTau the pass is repeated against the new one; P, l and O are floating-point
+// multiples of the same power, so nothing is lost below that.
 // Warps: 0-3 and 4-7 softmax, 8 MMA issue, 9 TMA producer, 10 the Values' guard.
 // The guard clears the Values of keys that no row of the CTA sees (0 x inf is
 // not 0 in the MMA) in the tiles at the edges of the mask, and waves the others
@@ -26,7 +32,7 @@ constexpr int W_MMA = 8, W_TMA = 9;      // warp 10: the guard
 constexpr int NT = 11 * 32;
 constexpr int ST = 2;                     // K tiles and V tiles in flight
 constexpr int BLK = 16384;                // 128 rows x 128 bytes
-constexpr float kTau = 8.0f;              // O is rescaled when a row's maximum grows by more than 2^8
+constexpr float kTau = 8.0f;              // binary16 P stays below 2^8, far from 65504
 
 enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VRDY = 6, B_VEMPTY = 8, B_SFULL = 10, B_PFULL = 12, B_QRDY = 14,
        B_OFIN = 16, N_BAR = 17 };
@@ -134,22 +140,29 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   const uint32_t tbase = s_tmem;
   const float sl2 = a.scale * 1.4426950408889634f;
 
-  if (warp < 8) {
+  if (warp < W_MMA) {
     // ------------------------------------------------------------ softmax
     const int i = warp >> 2, row = tid & 127;
     if (i < nqt) {
       // Q_i: each warp its 32 rows, a row's 16-byte chunks over neighbouring lanes
       uint8_t* sQ = sm + L::Q + i * NB * BLK;
       constexpr int CH = D / 8;
-#pragma unroll 8
-      for (int it = 0; it < CH; ++it) {
-        const int idx = it * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
-        const uint32_t r = remA + i * 128 + rr;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (i * 128 + rr < nrow)
-          v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (sq.q0 + tokA + r / G) * a.q_tok +
-                                              (hk * a.G + (int)(r % G)) * a.q_head + c * 8);
-        *reinterpret_cast<uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v;
+#pragma unroll 1
+      for (int i0 = 0; i0 < CH; i0 += 8) {
+        uint4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int idx = (i0 + k) * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
+          const uint32_t r = remA + min(i * 128 + rr, nrow - 1);
+          v[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (sq.q0 + tokA + r / G) * a.q_tok +
+                                                 (hk * a.G + (int)(r % G)) * a.q_head + c * 8);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int idx = (i0 + k) * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
+          if (i * 128 + rr >= nrow) v[k] = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[k];
+        }
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -162,44 +175,19 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       const uint32_t lrow = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t tS = tbase + 128 * i + lrow, tO = tbase + 256 + 128 * i + lrow;
       float m_run = -INFINITY, l_run = 0.0f;
-      bool ok = true;
-      for (int jt = 0; jt < n; ++jt) {
-        if (!(ok = wait_all(B_SFULL + i, jt & 1))) break;
-        tc_fence_after();
-        const int j0 = tile_at(tl, t0 + jt) * TK;
-        const bool open = __all_sync(0xFFFFFFFFu, !has || (j0 + TK <= sp.hi && (j0 >= sp.lo || j0 + TK <= a.sinks)));
-        uint32_t see[4];
-        float mt = -INFINITY;
-        float va[32], vb[32];
-        if (open) {
-          mt = tmem_max128(tS);
-        } else {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const int c = j0 + 32 * w;
-            see[w] = bits(sp.lo - c, sp.hi - c) | bits(-c, min(a.sinks, sp.hi) - c);
-          }
-#pragma unroll
-          for (int cp = 0; cp < 2; ++cp) {
-            tmem_ld32x2(tS + 64 * cp, tS + 64 * cp + 32, va, vb);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              if ((see[2 * cp] >> e) & 1) mt = fmaxf(mt, va[e]);
-              if ((see[2 * cp + 1] >> e) & 1) mt = fmaxf(mt, vb[e]);
-            }
-          }
-        }
-        const float m_new = fmaxf(m_run, mt);
+      const uint64_t SL = f2pack(sl2, sl2);
+      // raises the known maximum to m_new where it has grown by more than 2^tau,
+      // and O with it (S of this tile being complete, the P V before it is too)
+      auto raise = [&](float m_new, float tau, bool rescale) {
         // -inf - -inf is NaN and compares false: a row that has seen nothing stays so
-        const bool need = (m_new - m_run) * sl2 > kTau;
+        const bool need = (m_new - m_run) * sl2 > tau;
         float alpha = 1.0f;
         if (need) {
           alpha = ex2f((m_run - m_new) * sl2);
           m_run = m_new;
           l_run *= alpha;
         }
-        // S_i of this tile being complete, the P_i V before it is too
-        if (__any_sync(0xFFFFFFFFu, need) && jt > 0) {
+        if (__any_sync(0xFFFFFFFFu, need) && rescale) {
 #pragma unroll 1
           for (int cb = 0; cb < D / 16; ++cb) {
             uint32_t t[16];
@@ -209,37 +197,82 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
             tmem_st16(tO + cb * 16, t);
           }
         }
-        const float mb = m_run == -INFINITY ? 0.0f : m_run * sl2;
-        const uint64_t SL = f2pack(sl2, sl2), MB = f2pack(-mb, -mb);
-        uint64_t sum = f2pack(0.0f, 0.0f);
-        // P of 32 columns, as 16 words over S columns that have been read
-        auto block32 = [&](const float (&v)[32], uint32_t m, uint32_t dst) {
-          uint32_t pk[16];
+      };
+      bool ok = true;
+      for (int jt = 0; jt < n; ++jt) {
+        if (!(ok = wait_all(B_SFULL + i, jt & 1))) break;
+        tc_fence_after();
+        const int j0 = tile_at(tl, t0 + jt) * TK;
+        const bool open = __all_sync(0xFFFFFFFFu, !has || (j0 + TK <= sp.hi && (j0 >= sp.lo || j0 + TK <= a.sinks)));
+        uint32_t pk[64];
+        if (open) {
+          if (jt == 0) raise(tmem_max128(tS), 0.0f, false);
+          while (true) {
+            const float mb = m_run == -INFINITY ? 0.0f : m_run * sl2;
+            const uint64_t MB = f2pack(-mb, -mb);
+            uint64_t sum = f2pack(0.0f, 0.0f);
+            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            uint32_t v[2][32];
+            tmem_ld32_start(tS, v[0]);
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            float x, y;
-            f2unpack(fma2(f2pack(v[e], v[e + 1]), SL, MB), x, y);
-            if (!open) {
-              x = (m >> e) & 1 ? x : -INFINITY;
-              y = (m >> (e + 1)) & 1 ? y : -INFINITY;
+            for (int blk = 0; blk < 4; ++blk) {
+              tmem_ld32_wait(v[blk & 1]);
+              if (blk < 3) tmem_ld32_start(tS + 32 * (blk + 1), v[(blk + 1) & 1]);
+#pragma unroll
+              for (int e = 0; e < 32; e += 2) {
+                const float s0 = __uint_as_float(v[blk & 1][e]), s1 = __uint_as_float(v[blk & 1][e + 1]);
+                m4[(e >> 1) & 3] = fmax3f(m4[(e >> 1) & 3], s0, s1);
+                float x, y;
+                f2unpack(fma2(f2pack(s0, s1), SL, MB), x, y);
+                x = ex2f(x);
+                y = ex2f(y);
+                sum = add2(sum, f2pack(x, y));
+                pk[16 * blk + (e >> 1)] = Elem<T>::pack(x, y);
+              }
             }
-            x = ex2f(x);
-            y = ex2f(y);
-            sum = add2(sum, f2pack(x, y));
-            pk[e >> 1] = Elem<T>::pack(x, y);
+            const float mt = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            // (an infinite maximum stays what it is: inf - inf is NaN)
+            if (!__any_sync(0xFFFFFFFFu, (mt - m_run) * sl2 > kTau)) {
+              float sx, sy;
+              f2unpack(sum, sx, sy);
+              l_run += sx + sy;
+              break;
+            }
+            raise(mt, kTau, jt > 0);
           }
-          tmem_st16(dst, pk);
-        };
-#pragma unroll 1
-        for (int cp = 0; cp < 2; ++cp) {
-          tmem_ld32x2(tS + 64 * cp, tS + 64 * cp + 32, va, vb);
-          block32(va, cp ? see[2] : see[0], tS + 32 * cp);
-          block32(vb, cp ? see[3] : see[1], tS + 32 * cp + 16);
+        } else {
+          // a tile at the mask's edge: the maximum of what each row sees first
+          uint32_t see[4];
+          float mt = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int c = j0 + 32 * w;
+            see[w] = bits(sp.lo - c, sp.hi - c) | bits(-c, min(a.sinks, sp.hi) - c);
+            float v[32];
+            tmem_ld32(tS + 32 * w, v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) mt = fmaxf(mt, (see[w] >> e) & 1 ? v[e] : -INFINITY);
+          }
+          raise(mt, kTau, jt > 0);
+          const float mb = m_run == -INFINITY ? 0.0f : m_run * sl2;
+          float sum = 0.0f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            float v[32];
+            tmem_ld32(tS + 32 * w, v);
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const float x = (see[w] >> e) & 1 ? ex2f(fmaf(v[e], sl2, -mb)) : 0.0f;
+              const float y = (see[w] >> (e + 1)) & 1 ? ex2f(fmaf(v[e + 1], sl2, -mb)) : 0.0f;
+              sum += x + y;
+              pk[16 * w + (e >> 1)] = Elem<T>::pack(x, y);
+            }
+          }
+          l_run += sum;
         }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) tmem_st16(tS + 16 * w, *reinterpret_cast<uint32_t(*)[16]>(pk + 16 * w));
         tmem_wait_st();
-        float sx, sy;
-        f2unpack(sum, sx, sy);
-        l_run += sx + sy;
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_PFULL + i));
@@ -255,6 +288,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
         const bool poison = *(volatile int*)&s_poison != 0;
 #pragma unroll 1
         for (int cb = 0; cb < D / 32; ++cb) {
+          const int c0 = cb * 32;
           float v[32];
           if (n > 0) {
             tmem_ld32(tO + cb * 32, v);
@@ -272,7 +306,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
                 const int64_t page = a.table[(int64_t)b * a.table_stride + (j >> a.page_log2)];
                 if (page < 0 || page >= a.num_pages) continue;
                 const T* src = static_cast<const T*>(a.pages) +
-                               ((((page * 2 + 1) * a.Hk + hk) << a.page_log2) + (j & ((1 << a.page_log2) - 1))) * D + cb * 32;
+                               ((((page * 2 + 1) * a.Hk + hk) << a.page_log2) + (j & ((1 << a.page_log2) - 1))) * D + c0;
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
                   const uint32_t w = *reinterpret_cast<const uint32_t*>(src + e);
@@ -285,7 +319,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
           }
           if (!has) continue;
           if (parts == 1) {
-            uint4* d4 = reinterpret_cast<uint4*>(dst + cb * 32);
+            uint4* d4 = reinterpret_cast<uint4*>(dst + c0);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
               d4[k] = make_uint4(Elem<T>::pack(v[8 * k] * inv, v[8 * k + 1] * inv),
@@ -293,7 +327,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
                                  Elem<T>::pack(v[8 * k + 4] * inv, v[8 * k + 5] * inv),
                                  Elem<T>::pack(v[8 * k + 6] * inv, v[8 * k + 7] * inv));
           } else {
-            float4* d4 = reinterpret_cast<float4*>(a.part_o + pr * D + cb * 32);
+            float4* d4 = reinterpret_cast<float4*>(a.part_o + pr * D + c0);
 #pragma unroll
             for (int k = 0; k < 8; ++k) d4[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
           }
@@ -482,29 +516,57 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   __syncthreads();
   if (!s_last) return;
   __threadfence();
-  for (int idx = tid; idx < nrow * (D / 4); idx += NT) {
-    const int r = idx / (D / 4), c = idx % (D / 4);
-    const int64_t pr = group * a.nsplit * 256 + r;
-    float m = -INFINITY;
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, __ldcg(&a.part_ml[pr + p * 256].x));
+  // a part's weight in each row, 2^((m_p - m) c) / l, in the ring's place
+  float* wgt = reinterpret_cast<float*>(sm);           // [part][256]
+  const float2* ml = a.part_ml + group * a.nsplit * 256;
+  for (int r = tid; r < nrow; r += NT) {
+    float m = -INFINITY, l = 0.0f;
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, __ldcg(&ml[p * 256 + r].x));
     const float ref = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
     for (int p = 0; p < parts; ++p) {
-      const float2 ml = __ldcg(&a.part_ml[pr + p * 256]);
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(a.part_o + (pr + p * 256) * D + 4 * c));
-      const float f = ex2f((ml.x - ref) * sl2);
-      l = fmaf(ml.y, f, l);
-      v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
+      const float2 x = __ldcg(&ml[p * 256 + r]);
+      const float f = ex2f((x.x - ref) * sl2);
+      wgt[p * 256 + r] = f;
+      l = fmaf(x.y, f, l);
     }
-    const int64_t rr = r0 + r;
-    const int tok = (int)(rr / a.G), head = hk * a.G + (int)(rr % a.G);
     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (sq.q0 + tok) * a.o_tok + (int64_t)head * a.o_head + 4 * c) =
-        make_uint2(Elem<T>::pack(v.x * inv, v.y * inv), Elem<T>::pack(v.z * inv, v.w * inv));
-    if (a.lse && c == 0)
+    for (int p = 0; p < parts; ++p) wgt[p * 256 + r] *= inv;
+    if (a.lse) {
+      const int tok = tokA + (int)((remA + r) / G), head = hk * a.G + (int)((remA + r) % G);
       a.lse[(int64_t)head * a.N + sq.q0 + tok] = m == -INFINITY ? -INFINITY : m * a.scale + logf(l);
+    }
+  }
+  __syncthreads();
+  constexpr int IT = 4;                                // float4 columns of a thread side by side
+  const float4* po = reinterpret_cast<const float4*>(a.part_o + group * a.nsplit * 256 * D);
+  const int items = nrow * (D / 4);
+  for (int i0 = tid; i0 < items; i0 += IT * NT) {
+    float4 v[IT];
+#pragma unroll
+    for (int k = 0; k < IT; ++k) v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p = 0; p < parts; ++p) {
+      float4 x[IT];
+#pragma unroll
+      for (int k = 0; k < IT; ++k)
+        if (i0 + k * NT < items) x[k] = __ldcg(po + (int64_t)p * 256 * (D / 4) + i0 + k * NT);
+#pragma unroll
+      for (int k = 0; k < IT; ++k) {
+        if (i0 + k * NT >= items) continue;
+        const float f = wgt[p * 256 + (i0 + k * NT) / (D / 4)];
+        v[k].x = fmaf(x[k].x, f, v[k].x); v[k].y = fmaf(x[k].y, f, v[k].y);
+        v[k].z = fmaf(x[k].z, f, v[k].z); v[k].w = fmaf(x[k].w, f, v[k].w);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < IT; ++k) {
+      const int idx = i0 + k * NT;
+      if (idx >= items) continue;
+      const uint32_t r = remA + idx / (D / 4);
+      const int c = idx % (D / 4);
+      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (sq.q0 + tokA + r / G) * a.o_tok +
+                                (int64_t)(hk * a.G + (int)(r % G)) * a.o_head + 4 * c) =
+          make_uint2(Elem<T>::pack(v[k].x, v[k].y), Elem<T>::pack(v[k].z, v[k].w));
+    }
   }
   if (tid == 0) a.counter[group] = 0;
 }
