@@ -54,7 +54,7 @@ struct PagedArgs {
   int32_t idle;                          // nonzero: the producers load nothing (test hook)
   // split along the keys: at most nsplit parts of at least min_tiles tiles
   int32_t nsplit, min_tiles;
-  float* part_o;                         // [group][nsplit][rows][D]
+  float* part_o;                         // [group][nsplit], a part's rows x D floats
   float2* part_ml;                       // [group][nsplit][rows] running (max, sum)
   int32_t* counter;                      // [group], zero between calls
 };
@@ -122,11 +122,13 @@ __device__ __forceinline__ Span row_span(int p, int kv, int block, int window) {
 }
 
 // What the rows of tokens p0 <= p <= p1 of a sequence see together, as a list
-// of tiles of TK keys: tiles that hold first tokens, then the window's.  lo and
-// hi of a row grow with its token, so the first and the last row bound all.
+// of tiles of TK keys: the window's, then tiles that hold first tokens before
+// it (few keys: taken first they would give the running maxima a poor start).
+// lo and hi of a row grow with its token, so the first and the last row bound
+// all.
 struct Tiles {
   int32_t lo_min, lo_max, hi_min, hi_max;  // over the rows; a row with p < 0 has hi = 0
-  int32_t n_first, w_start, n;
+  int32_t n_win, w_start, n;
 };
 template <int TK>
 __device__ __forceinline__ Tiles make_tiles(int p0, int p1, int kv, int block, int window, int sinks) {
@@ -137,14 +139,14 @@ __device__ __forceinline__ Tiles make_tiles(int p0, int p1, int kv, int block, i
   t.lo_max = b.lo;
   t.hi_max = b.hi;
   const int s_end = min(min(sinks, t.lo_min), t.hi_max);
-  t.n_first = (s_end + TK - 1) / TK;
-  t.w_start = max(t.lo_min / TK, t.n_first);
-  t.n = t.n_first + max(0, (t.hi_max + TK - 1) / TK - t.w_start);
-  if (t.hi_max == 0) t.n = 0;
+  const int n_first = (s_end + TK - 1) / TK;
+  t.w_start = max(t.lo_min / TK, n_first);
+  t.n_win = max(0, (t.hi_max + TK - 1) / TK - t.w_start);
+  t.n = t.hi_max == 0 ? 0 : t.n_win + n_first;
   return t;
 }
 __device__ __forceinline__ int tile_at(const Tiles& t, int i) {
-  return i < t.n_first ? i : t.w_start + (i - t.n_first);
+  return i < t.n_win ? t.w_start + i : i - t.n_win;
 }
 __device__ __forceinline__ bool sees(int j, int lo, int hi, int sinks) { return j < hi && (j >= lo || j < sinks); }
 // Whether some row of the tiles sees a token of [j0, j1).
@@ -169,6 +171,11 @@ template <>
 struct Elem<__nv_bfloat16> {
   static constexpr bool bf16 = true;
   static constexpr uint32_t kExp = 0x7F80u;  // exponent field: all ones in infinities and NaN
+  // growth of a row's maximum (as a power of two) up to which P is still taken
+  // against the old one: P, l and O are floating-point multiples of the same
+  // power, so only the type's range bounds it (fp32's for bf16: 2^40 times any
+  // number of keys; 65504 for binary16)
+  static constexpr float kTau = 40.0f;
   __device__ static __forceinline__ uint32_t pack(float a, float b) { return ptx::pack_bf16(a, b); }
   __device__ static __forceinline__ float2 unpack(uint32_t w) {
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
@@ -184,6 +191,7 @@ template <>
 struct Elem<__half> {
   static constexpr bool bf16 = false;
   static constexpr uint32_t kExp = 0x7C00u;
+  static constexpr float kTau = 14.0f;
   __device__ static __forceinline__ uint32_t pack(float a, float b) { return ptx::pack_f16(a, b); }
   __device__ static __forceinline__ float2 unpack(uint32_t w) {
     return __half22float2(*reinterpret_cast<const __half2*>(&w));

@@ -16,11 +16,15 @@
 // maximum is formed beside it.  Where it is above the known one by more than
 // 2^kTau the pass is repeated against the new one; P, l and O are floating-point
 // multiples of the same power, so nothing is lost below that.
-// Warps: 0-3 and 4-7 softmax, 8 MMA issue, 9 TMA producer, 10 the Values' guard.
+// Warps: four per row tile softmax, then MMA issue, a TMA producer each for K and
+// V (a 16-token page is a copy of 2 KB: one warp's issue rate would bound the
+// tile), and the Values' guard.
 // The guard clears the Values of keys that no row of the CTA sees (0 x inf is
 // not 0 in the MMA) in the tiles at the edges of the mask, and waves the others
 // through; infinities and NaN in Values that some rows see and others do not
 // are taken out of the product and added to the rows that see them at the end.
+#include <type_traits>
+
 #include "paged.cuh"
 
 namespace qwm {
@@ -28,20 +32,21 @@ namespace {
 using namespace ptx;
 
 constexpr int TK = 128;
-constexpr int W_MMA = 8, W_TMA = 9;      // warp 10: the guard
-constexpr int NT = 11 * 32;
 constexpr int ST = 2;                     // K tiles and V tiles in flight
 constexpr int BLK = 16384;                // 128 rows x 128 bytes
-constexpr float kTau = 8.0f;              // binary16 P stays below 2^8, far from 65504
 
 enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VRDY = 6, B_VEMPTY = 8, B_SFULL = 10, B_PFULL = 12, B_QRDY = 14,
        B_OFIN = 16, N_BAR = 17 };
 
+constexpr int NQ = 2, ROWS = 128 * NQ;               // row tiles and rows of a CTA
+constexpr int W_MMA = 4 * NQ, W_K = W_MMA + 1, W_V = W_MMA + 2;  // W_MMA + 3: the guard
+constexpr int NT = (4 * NQ + 4) * 32;
+
 template <int D>
 struct Smem {
-  static constexpr int NB = D / 64;       // 64-channel blocks of a tile
-  static constexpr int Q = 0;             // tile i, block k at (i * NB + k) * BLK
-  static constexpr int K = 2 * NB * BLK;  // stage s, block k at (s * NB + k) * BLK
+  static constexpr int NB = D / 64;                  // 64-channel blocks of a tile
+  static constexpr int Q = 0;                        // tile i, block k at (i * NB + k) * BLK
+  static constexpr int K = NQ * NB * BLK;            // stage s, block k at (s * NB + k) * BLK
   static constexpr int V = K + ST * NB * BLK;
   static constexpr int BAR = V + ST * NB * BLK;
   static constexpr int TOTAL = BAR + 256 + 1024;
@@ -95,9 +100,9 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   Seq sq;
   if (!load_seq(a, b, sq) && blockIdx.x == 0 && hk == 0 && tid == 0) record_status(a.status, QWM_ERR_INVALID_ARG);
   const int64_t rows = (int64_t)sq.qn * a.G;
-  const int64_t r0 = (int64_t)rt * 256;
+  const int64_t r0 = (int64_t)rt * ROWS;
   if (r0 >= rows) return;
-  const int nrow = (int)min((int64_t)256, rows - r0);
+  const int nrow = (int)min((int64_t)ROWS, rows - r0);
   const int nqt = nrow > 128 ? 2 : 1;
   const int p0 = sq.kv - sq.qn;                       // token of the sequence's first row
   // row r0 + i is new token tokA + (remA + i) / G, grouped head (remA + i) % G
@@ -173,21 +178,19 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       const int head = hk * a.G + (has ? (int)((remA + i * 128 + row) % G) : 0);
       const Span sp = has ? row_span(p0 + tok, sq.kv, a.block, a.window) : Span{0, 0};
       const uint32_t lrow = (uint32_t)((warp & 3) * 32) << 16;
-      const uint32_t tS = tbase + 128 * i + lrow, tO = tbase + 256 + 128 * i + lrow;
-      float m_run = -INFINITY, l_run = 0.0f;
+      const uint32_t tS = tbase + 128 * i + lrow, tO = tbase + 128 * NQ + D * i + lrow;
+      float m_run = has ? -INFINITY : 0.0f, l_run = 0.0f;
       const uint64_t SL = f2pack(sl2, sl2);
-      // raises the known maximum to m_new where it has grown by more than 2^tau,
-      // and O with it (S of this tile being complete, the P V before it is too)
-      auto raise = [&](float m_new, float tau, bool rescale) {
-        // -inf - -inf is NaN and compares false: a row that has seen nothing stays so
-        const bool need = (m_new - m_run) * sl2 > tau;
-        float alpha = 1.0f;
-        if (need) {
-          alpha = ex2f((m_run - m_new) * sl2);
-          m_run = m_new;
-          l_run *= alpha;
-        }
-        if (__any_sync(0xFFFFFFFFu, need) && rescale) {
+      // Where some row's maximum has grown by more than 2^kTau: raises every row of
+      // the warp to its own, and O with it (S of this tile being complete, the
+      // P V before it is too).  -inf - -inf and inf - inf are NaN and compare
+      // false: a row that has seen nothing, or an infinity, stays as it is.
+      auto raise = [&](float mt, bool rescale) -> bool {
+        if (!__any_sync(0xFFFFFFFFu, (mt - m_run) * sl2 > Elem<T>::kTau)) return false;
+        const float alpha = mt > m_run ? ex2f((m_run - mt) * sl2) : 1.0f;
+        m_run = fmaxf(m_run, mt);
+        l_run *= alpha;
+        if (rescale) {
 #pragma unroll 1
           for (int cb = 0; cb < D / 16; ++cb) {
             uint32_t t[16];
@@ -197,6 +200,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
             tmem_st16(tO + cb * 16, t);
           }
         }
+        return true;
       };
       bool ok = true;
       for (int jt = 0; jt < n; ++jt) {
@@ -205,71 +209,83 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
         const int j0 = tile_at(tl, t0 + jt) * TK;
         const bool open = __all_sync(0xFFFFFFFFu, !has || (j0 + TK <= sp.hi && (j0 >= sp.lo || j0 + TK <= a.sinks)));
         uint32_t pk[64];
-        if (open) {
-          if (jt == 0) raise(tmem_max128(tS), 0.0f, false);
-          while (true) {
-            const float mb = m_run == -INFINITY ? 0.0f : m_run * sl2;
-            const uint64_t MB = f2pack(-mb, -mb);
-            uint64_t sum = f2pack(0.0f, 0.0f);
-            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            uint32_t v[2][32];
-            tmem_ld32_start(tS, v[0]);
+        // Which keys of each 32-key block this row sees; a warp whose rows all
+        // see a whole block, or none of it, takes it without the selection.
+        enum { kNone, kSome, kAll };
+        auto seen = [&](int blk, uint32_t& see) -> int {
+          see = 0xFFFFFFFFu;
+          const int c = j0 + 32 * blk;
+          if (has) see = bits(sp.lo - c, sp.hi - c) | bits(-c, min(a.sinks, sp.hi) - c);
+          return __all_sync(0xFFFFFFFFu, see == 0xFFFFFFFFu) ? kAll : (__any_sync(0xFFFFFFFFu, has && see != 0) ? kSome : kNone);
+        };
+        auto select = [&](uint32_t (&w)[32], uint32_t see) {
 #pragma unroll
-            for (int blk = 0; blk < 4; ++blk) {
-              tmem_ld32_wait(v[blk & 1]);
-              if (blk < 3) tmem_ld32_start(tS + 32 * (blk + 1), v[(blk + 1) & 1]);
-#pragma unroll
-              for (int e = 0; e < 32; e += 2) {
-                const float s0 = __uint_as_float(v[blk & 1][e]), s1 = __uint_as_float(v[blk & 1][e + 1]);
-                m4[(e >> 1) & 3] = fmax3f(m4[(e >> 1) & 3], s0, s1);
-                float x, y;
-                f2unpack(fma2(f2pack(s0, s1), SL, MB), x, y);
-                x = ex2f(x);
-                y = ex2f(y);
-                sum = add2(sum, f2pack(x, y));
-                pk[16 * blk + (e >> 1)] = Elem<T>::pack(x, y);
-              }
-            }
-            const float mt = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-            // (an infinite maximum stays what it is: inf - inf is NaN)
-            if (!__any_sync(0xFFFFFFFFu, (mt - m_run) * sl2 > kTau)) {
-              float sx, sy;
-              f2unpack(sum, sx, sy);
-              l_run += sx + sy;
-              break;
-            }
-            raise(mt, kTau, jt > 0);
-          }
-        } else {
-          // a tile at the mask's edge: the maximum of what each row sees first
-          uint32_t see[4];
-          float mt = -INFINITY;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const int c = j0 + 32 * w;
-            see[w] = bits(sp.lo - c, sp.hi - c) | bits(-c, min(a.sinks, sp.hi) - c);
-            float v[32];
-            tmem_ld32(tS + 32 * w, v);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) mt = fmaxf(mt, (see[w] >> e) & 1 ? v[e] : -INFINITY);
-          }
-          raise(mt, kTau, jt > 0);
+          for (int e = 0; e < 32; ++e) w[e] = (see >> e) & 1 ? w[e] : 0xFF800000u;
+        };
+        // one pass over S: P and its sum against m_run; returns the tile's maximum
+        auto pass = [&](auto masked, float& total) -> float {
           const float mb = m_run == -INFINITY ? 0.0f : m_run * sl2;
-          float sum = 0.0f;
+          const uint64_t MB = f2pack(-mb, -mb);
+          uint64_t sum = f2pack(0.0f, 0.0f);
+          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          uint32_t v[2][32];
+          tmem_ld32_start(tS, v[0]);
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            float v[32];
-            tmem_ld32(tS + 32 * w, v);
+          for (int blk = 0; blk < 4; ++blk) {
+            uint32_t (&w)[32] = v[blk & 1];
+            tmem_ld32_wait(w);
+            if (blk < 3) tmem_ld32_start(tS + 32 * (blk + 1), v[(blk + 1) & 1]);
+            if (masked) {
+              uint32_t see;
+              const int kind = seen(blk, see);
+              if (kind == kNone) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) pk[16 * blk + e] = 0u;
+                continue;
+              }
+              if (kind == kSome) select(w, see);
+            }
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              const float x = (see[w] >> e) & 1 ? ex2f(fmaf(v[e], sl2, -mb)) : 0.0f;
-              const float y = (see[w] >> (e + 1)) & 1 ? ex2f(fmaf(v[e + 1], sl2, -mb)) : 0.0f;
-              sum += x + y;
-              pk[16 * w + (e >> 1)] = Elem<T>::pack(x, y);
+              const float s0 = __uint_as_float(w[e]), s1 = __uint_as_float(w[e + 1]);
+              m4[(e >> 1) & 3] = fmax3f(m4[(e >> 1) & 3], s0, s1);
+              float x, y;
+              f2unpack(fma2(f2pack(s0, s1), SL, MB), x, y);
+              x = ex2f(x);
+              y = ex2f(y);
+              sum = add2(sum, f2pack(x, y));
+              pk[16 * blk + (e >> 1)] = Elem<T>::pack(x, y);
             }
           }
-          l_run += sum;
+          float sx, sy;
+          f2unpack(sum, sx, sy);
+          total = sx + sy;
+          return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+        };
+        // where a row has no maximum yet, the tile's comes first
+        if (__any_sync(0xFFFFFFFFu, m_run == -INFINITY)) {
+          float mt = -INFINITY;
+          if (open) {
+            mt = tmem_max128(tS);
+          } else {
+#pragma unroll
+            for (int blk = 0; blk < 4; ++blk) {
+              uint32_t see, w[32];
+              const int kind = seen(blk, see);
+              if (kind == kNone) continue;
+              tmem_ld32_start(tS + 32 * blk, w);
+              tmem_ld32_wait(w);
+              if (kind == kSome) select(w, see);
+#pragma unroll
+              for (int e = 0; e < 32; e += 2) mt = fmax3f(mt, __uint_as_float(w[e]), __uint_as_float(w[e + 1]));
+            }
+          }
+          raise(mt, jt > 0);
         }
+        float total;
+        while (raise(open ? pass(std::false_type{}, total) : pass(std::true_type{}, total), jt > 0)) {
+        }
+        l_run += total;
 #pragma unroll
         for (int w = 0; w < 4; ++w) tmem_st16(tS + 16 * w, *reinterpret_cast<uint32_t(*)[16]>(pk + 16 * w));
         tmem_wait_st();
@@ -282,9 +298,8 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       if (ok) {
         tc_fence_after();
         const int64_t group = ((int64_t)b * a.Hk + hk) * rtiles + rt;
-        const int64_t pr = (group * a.nsplit + part) * 256 + i * 128 + row;
+        const int64_t pr = (group * a.nsplit + part) * ROWS + i * 128 + row;
         const float inv = l_run > 0.0f || l_run != l_run ? 1.0f / l_run : 0.0f;
-        T* dst = static_cast<T*>(a.out) + (sq.q0 + tok) * a.o_tok + (int64_t)head * a.o_head;
         const bool poison = *(volatile int*)&s_poison != 0;
 #pragma unroll 1
         for (int cb = 0; cb < D / 32; ++cb) {
@@ -317,19 +332,36 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
               }
             }
           }
-          if (!has) continue;
           if (parts == 1) {
-            uint4* d4 = reinterpret_cast<uint4*>(dst + c0);
+            // through Q_i's rows of this warp (every MMA is done), so that the
+            // rows leave as whole lines
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              d4[k] = make_uint4(Elem<T>::pack(v[8 * k] * inv, v[8 * k + 1] * inv),
-                                 Elem<T>::pack(v[8 * k + 2] * inv, v[8 * k + 3] * inv),
-                                 Elem<T>::pack(v[8 * k + 4] * inv, v[8 * k + 5] * inv),
-                                 Elem<T>::pack(v[8 * k + 6] * inv, v[8 * k + 7] * inv));
-          } else {
-            float4* d4 = reinterpret_cast<float4*>(a.part_o + pr * D + c0);
+            for (int k = 0; k < 4; ++k) {
+              const int c = cb * 4 + k;
+              *reinterpret_cast<uint4*>(sQ + (c >> 3) * BLK + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+                  make_uint4(Elem<T>::pack(v[8 * k] * inv, v[8 * k + 1] * inv),
+                             Elem<T>::pack(v[8 * k + 2] * inv, v[8 * k + 3] * inv),
+                             Elem<T>::pack(v[8 * k + 4] * inv, v[8 * k + 5] * inv),
+                             Elem<T>::pack(v[8 * k + 6] * inv, v[8 * k + 7] * inv));
+            }
+          } else if (has) {
+            // a part: [channels / 4][row], so that a warp writes whole lines
+            float4* d4 = reinterpret_cast<float4*>(a.part_o) + (group * a.nsplit + part) * ROWS * (D / 4) +
+                         (int64_t)(c0 / 4) * ROWS + i * 128 + row;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) d4[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+            for (int k = 0; k < 8; ++k) d4[k * ROWS] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+          }
+        }
+        if (parts == 1) {
+          __syncwarp();
+#pragma unroll 4
+          for (int it = 0; it < CH; ++it) {
+            const int idx = it * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
+            if (i * 128 + rr >= nrow) continue;
+            const uint32_t r = remA + i * 128 + rr;
+            *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + (sq.q0 + tokA + r / G) * a.o_tok +
+                                      (int64_t)(hk * a.G + (int)(r % G)) * a.o_head + c * 8) =
+                *reinterpret_cast<const uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4));
           }
         }
         if (has && parts == 1 && a.lse)
@@ -373,7 +405,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
           tc_fence_after();
 #pragma unroll
           for (int ks = 0; ks < TK / 16; ++ks)
-            umma_ts_e(tbase + 256 + 128 * i, tbase + 128 * i + 8 * ks, dV + off(s * NB * BLK + ks * 2048), idPV,
+            umma_ts_e(tbase + 128 * NQ + D * i, tbase + 128 * i + 8 * ks, dV + off(s * NB * BLK + ks * 2048), idPV,
                       (jt | ks) != 0, e);
           if (i == nqt - 1) commit_e(bar(B_VEMPTY + s), e);
           if (jt + 1 < n && !(ok = issue_S(i, jt + 1))) break;
@@ -387,15 +419,18 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       }
     }
     __syncwarp();
-  } else if (warp == W_TMA) {
-    // ------------------------------------------------------------ producer
+  } else if (warp == W_K || warp == W_V) {
+    // ------------------------------------------------------------ producers of K and V
     // lane = box * NB + channel block; a box is the part of a page (at most 64
     // tokens of it) that lies in the tile.  Boxes no row sees are not read.
+    const int kv = warp == W_V;
+    const int full = kv ? B_VFULL : B_KFULL, empty = kv ? B_VEMPTY : B_KEMPTY;
     const int box_log2 = min(a.page_log2, 6);
     const int boxes = TK >> box_log2;
     const int box = lane / NB, blk = lane % NB;
     const bool mine = box < boxes;
     const int32_t* trow = a.table + (int64_t)b * a.table_stride;
+    const uint32_t ring = smem_u32(sm + (kv ? L::V : L::K)) + blk * BLK + ((box << box_log2) * 128);
     auto page_of = [&](int jt, bool& want) -> int {
       const int j0 = tile_at(tl, t0 + jt) * TK + (box << box_log2);
       want = mine && any_sees(tl, j0, j0 + (1 << box_log2), a.sinks);
@@ -404,43 +439,29 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
     bool want = false, ok = true;
     int page = n > 0 ? page_of(0, want) : 0;
     int jt = 0;
-    bool k_sent = false;
     for (; jt < n && !a.idle; ++jt) {
       const int s = jt & 1;
       bool want_n = false;
       int page_n = 0;
-      if (jt + 1 < n) page_n = page_of(jt + 1, want_n);
-      if (want && (page < 0 || page >= a.num_pages)) {   // not followed: the first page in its place
+      if (jt + 1 < n) page_n = page_of(jt + 1, want_n);   // its latency runs beside the copies
+      if (want && (page < 0 || page >= a.num_pages)) {    // not followed: the first page in its place
         record_status(a.status, QWM_ERR_INVALID_ARG);
         page = 0;
       }
       const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, want)) * (128u << box_log2);
       const int y = (tile_at(tl, t0 + jt) * TK + (box << box_log2)) & ((1 << a.page_log2) - 1);
-      k_sent = false;
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        if (jt >= ST && !(ok = wait_all((kv ? B_VEMPTY : B_KEMPTY) + s, ((jt >> 1) - 1) & 1))) break;
-        const uint32_t fb = bar((kv ? B_VFULL : B_KFULL) + s);
-        if (lane == 0) mbar_arrive_expect_tx(fb, bytes);
-        __syncwarp();
-        if (want)
-          tma_load_3d(smem_u32(sm + (kv ? L::V : L::K)) + (s * NB + blk) * BLK + ((box << box_log2) * 128), &map, blk * 64,
-                      y, (page * 2 + kv) * a.Hk + hk, fb);
-        __syncwarp();
-        k_sent = true;
-      }
-      if (!ok) break;
+      if (jt >= ST && !(ok = wait_all(empty + s, ((jt >> 1) - 1) & 1))) break;
+      if (lane == 0) mbar_arrive_expect_tx(bar(full + s), bytes);
+      __syncwarp();
+      if (want) tma_load_3d(ring + s * NB * BLK, &map, blk * 64, y, (page * 2 + kv) * a.Hk + hk, bar(full + s));
+      __syncwarp();
       page = page_n;
       want = want_n;
     }
     if (!ok) {
       // a wait ran out: let the copies in flight land before the CTA ends
       s_err = 1;
-      for (int u = max(0, jt - ST); u < jt; ++u) {
-        mbar_wait(bar(B_KFULL + (u & 1)), (u >> 1) & 1, kDrainNs);
-        mbar_wait(bar(B_VFULL + (u & 1)), (u >> 1) & 1, kDrainNs);
-      }
-      if (k_sent) mbar_wait(bar(B_KFULL + (jt & 1)), (jt >> 1) & 1, kDrainNs);
+      for (int u = max(0, jt - ST); u < jt; ++u) mbar_wait(bar(full + (u & 1)), (u >> 1) & 1, kDrainNs);
     }
   } else {
     // ------------------------------------------------------------ guard of the Values
@@ -517,55 +538,73 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   if (!s_last) return;
   __threadfence();
   // a part's weight in each row, 2^((m_p - m) c) / l, in the ring's place
-  float* wgt = reinterpret_cast<float*>(sm);           // [part][256]
-  const float2* ml = a.part_ml + group * a.nsplit * 256;
+  float* wgt = reinterpret_cast<float*>(sm);           // [part][ROWS]
+  const float2* ml = a.part_ml + group * a.nsplit * ROWS;
   for (int r = tid; r < nrow; r += NT) {
     float m = -INFINITY, l = 0.0f;
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, __ldcg(&ml[p * 256 + r].x));
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, __ldcg(&ml[p * ROWS + r].x));
     const float ref = m == -INFINITY ? 0.0f : m;
     for (int p = 0; p < parts; ++p) {
-      const float2 x = __ldcg(&ml[p * 256 + r]);
+      const float2 x = __ldcg(&ml[p * ROWS + r]);
       const float f = ex2f((x.x - ref) * sl2);
-      wgt[p * 256 + r] = f;
+      wgt[p * ROWS + r] = f;
       l = fmaf(x.y, f, l);
     }
     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    for (int p = 0; p < parts; ++p) wgt[p * 256 + r] *= inv;
+    for (int p = 0; p < parts; ++p) wgt[p * ROWS + r] *= inv;
     if (a.lse) {
       const int tok = tokA + (int)((remA + r) / G), head = hk * a.G + (int)((remA + r) % G);
       a.lse[(int64_t)head * a.N + sq.q0 + tok] = m == -INFINITY ? -INFINITY : m * a.scale + logf(l);
     }
   }
   __syncthreads();
-  constexpr int IT = 4;                                // float4 columns of a thread side by side
-  const float4* po = reinterpret_cast<const float4*>(a.part_o + group * a.nsplit * 256 * D);
-  const int items = nrow * (D / 4);
+  // eight channels of a row per item; two items and four parts of them in
+  // flight per thread (48 to 96 KB an SM: one SM reads a group's parts)
+  constexpr int IT = 2, PU = 4, items = ROWS * (D / 8);
+  const float4* po = reinterpret_cast<const float4*>(a.part_o) + group * a.nsplit * ROWS * (D / 4);
   for (int i0 = tid; i0 < items; i0 += IT * NT) {
-    float4 v[IT];
+    float4 v[IT][2];
 #pragma unroll
-    for (int k = 0; k < IT; ++k) v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p = 0; p < parts; ++p) {
-      float4 x[IT];
+    for (int k = 0; k < IT; ++k) v[k][0] = v[k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int pb = 0; pb < parts; pb += PU) {
+      float4 x[PU][IT][2];
+      float f[PU][IT];
 #pragma unroll
-      for (int k = 0; k < IT; ++k)
-        if (i0 + k * NT < items) x[k] = __ldcg(po + (int64_t)p * 256 * (D / 4) + i0 + k * NT);
+      for (int u = 0; u < PU; ++u)
 #pragma unroll
-      for (int k = 0; k < IT; ++k) {
-        if (i0 + k * NT >= items) continue;
-        const float f = wgt[p * 256 + (i0 + k * NT) / (D / 4)];
-        v[k].x = fmaf(x[k].x, f, v[k].x); v[k].y = fmaf(x[k].y, f, v[k].y);
-        v[k].z = fmaf(x[k].z, f, v[k].z); v[k].w = fmaf(x[k].w, f, v[k].w);
-      }
+        for (int k = 0; k < IT; ++k) {
+          const int idx = i0 + k * NT, r = idx % ROWS, c8 = idx / ROWS, p = pb + u;
+          if (p < parts && idx < items && r < nrow) {
+            const float4* src = po + ((int64_t)p * (D / 4) + 2 * c8) * ROWS + r;
+            x[u][k][0] = __ldcg(src);
+            x[u][k][1] = __ldcg(src + ROWS);
+            f[u][k] = wgt[p * ROWS + r];
+          } else {
+            x[u][k][0] = x[u][k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+            f[u][k] = 0.0f;
+          }
+        }
+#pragma unroll
+      for (int u = 0; u < PU; ++u)
+#pragma unroll
+        for (int k = 0; k < IT; ++k)
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            v[k][w].x = fmaf(x[u][k][w].x, f[u][k], v[k][w].x);
+            v[k][w].y = fmaf(x[u][k][w].y, f[u][k], v[k][w].y);
+            v[k][w].z = fmaf(x[u][k][w].z, f[u][k], v[k][w].z);
+            v[k][w].w = fmaf(x[u][k][w].w, f[u][k], v[k][w].w);
+          }
     }
 #pragma unroll
     for (int k = 0; k < IT; ++k) {
-      const int idx = i0 + k * NT;
-      if (idx >= items) continue;
-      const uint32_t r = remA + idx / (D / 4);
-      const int c = idx % (D / 4);
-      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (sq.q0 + tokA + r / G) * a.o_tok +
-                                (int64_t)(hk * a.G + (int)(r % G)) * a.o_head + 4 * c) =
-          make_uint2(Elem<T>::pack(v[k].x, v[k].y), Elem<T>::pack(v[k].z, v[k].w));
+      const int idx = i0 + k * NT, row = idx % ROWS, c8 = idx / ROWS;
+      if (idx >= items || row >= nrow) continue;
+      const uint32_t r = remA + row;
+      *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + (sq.q0 + tokA + r / G) * a.o_tok +
+                                (int64_t)(hk * a.G + (int)(r % G)) * a.o_head + 8 * c8) =
+          make_uint4(Elem<T>::pack(v[k][0].x, v[k][0].y), Elem<T>::pack(v[k][0].z, v[k][0].w),
+                     Elem<T>::pack(v[k][1].x, v[k][1].y), Elem<T>::pack(v[k][1].z, v[k][1].w));
     }
   }
   if (tid == 0) a.counter[group] = 0;
@@ -575,7 +614,7 @@ template <typename T, int D>
 cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   cudaError_t e = cudaFuncSetAttribute(paged_chunk<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL);
   if (e != cudaSuccess) return e;
-  const int64_t rtiles = ((int64_t)a.max_q * a.G + 255) / 256;
+  const int64_t rtiles = ((int64_t)a.max_q * a.G + ROWS - 1) / ROWS;
   paged_chunk<T, D><<<dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), NT, Smem<D>::TOTAL, s>>>(map, a);
   return cudaGetLastError();
 }
@@ -584,9 +623,9 @@ cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
 
 PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, bool split) {
   PagedPlan p{};
-  const int64_t rtiles = (rows + 255) / 256;
+  p.rows = ROWS;
+  const int64_t rtiles = (rows + p.rows - 1) / p.rows;
   p.groups = (int)(rtiles * B * Hk);
-  p.rows = 256;
   p.min_tiles = 4;
   p.nsplit = 1;
   const int64_t tiles = (max_visible + TK - 1) / TK + 2;
