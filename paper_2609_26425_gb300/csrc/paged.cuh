@@ -52,7 +52,9 @@ struct PagedArgs {
   int32_t* status;
   uint64_t wait_ns;
   int32_t idle;                          // nonzero: the producers load nothing (test hook)
-  // split along the keys: at most nsplit parts of at least min_tiles tiles
+  // split along the keys: chunk: at most nsplit parts of a group, of at least
+  // min_tiles tiles; step: nsplit CTAs share the line of all tiles, at least
+  // min_tiles places each.  nsplit 1: no split
   int32_t nsplit, min_tiles;
   float* part_o;                         // [group][nsplit], a part's rows x D floats
   float2* part_ml;                       // [group][nsplit][rows] running (max, sum)
@@ -66,7 +68,7 @@ struct PagedPlan {
   int32_t rows;      // rows of a group
   int32_t nsplit, min_tiles;
 };
-PagedPlan plan_step(int B, int Hk, int rows, int64_t max_visible, int nsm, bool split);
+PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split);
 PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, bool split);
 cudaError_t launch_paged_step(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s);
 cudaError_t launch_paged_chunk(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s);

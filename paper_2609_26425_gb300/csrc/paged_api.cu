@@ -131,17 +131,20 @@ PagedPlan make_plan(const qwm_paged* c, const qwm_paged_batch* b, int32_t q_head
     const int64_t w = (int64_t)m->window + m->sinks + m->block + 256;
     if (w < seen) seen = w;
   }
-  return rows <= qwm::kStepRows ? qwm::plan_step(b->num_seqs, c->cfg.kv_heads, (int)rows, seen, c->nsm, split)
+  return rows <= qwm::kStepRows ? qwm::plan_step(b->num_seqs, c->cfg.kv_heads, c->cfg.head_dim, (int)rows, seen, c->nsm,
+                                               split)
                                 : qwm::plan_chunk(b->num_seqs, c->cfg.kv_heads, rows, seen, c->nsm, split);
 }
 
-// counters, (max, sum) pairs and partial outputs, each 256-byte aligned
+// counters, (max, sum) pairs and partial outputs, each 256-byte aligned; a step
+// CTA has two parts (of the groups at the ends of its stretch), a chunk group
+// nsplit
 struct Carve {
   size_t ml, o, total;
 };
 Carve carve(const PagedPlan& p, int D) {
   Carve w{};
-  const size_t rows = (size_t)p.groups * p.nsplit * p.rows;
+  const size_t rows = (size_t)(p.step ? 2 : p.groups) * p.nsplit * p.rows;
   w.ml = ((size_t)p.groups * 4 + 255) / 256 * 256;
   w.o = w.ml + (rows * 8 + 255) / 256 * 256;
   w.total = w.o + rows * D * 4;

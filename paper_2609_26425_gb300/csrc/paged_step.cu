@@ -6,14 +6,17 @@
 // over K and V suffices.  The bound is HBM: K and V of the visible tokens are
 // read once per cache head for all the grouped Query heads.
 //
-// A CTA takes one (sequence, cache head, part of the keys): a producer warp
-// keeps a ring of 64-key tiles in flight by TMA, four warps take 16 keys each
-// and carry their own m, l and O through the part (no barrier between them in
-// the loop), then the four are merged through shared memory.  The rows are the
-// M = 16 side of mma.sync: a tcgen05 tile would be 128 rows high for the 1 to 32
-// used here, and its TMEM round trip is longer than the whole of a short step.
-// Parts of one group are joined by the CTA that finishes last, in part order,
-// so the result does not depend on which one that is.
+// The tiles of all (sequence, cache head) groups form one line, which the CTAs (one
+// per SM) share out evenly whatever the lengths are; a CTA walks its stretch
+// group by group.  A producer warp keeps a ring of 64-key tiles in flight by
+// TMA; of eight warps four take 16 keys each of a tile, the other four those of
+// the next tile (up to 16 rows) or the second 16 rows (17 to 32), and carry
+// their own m, l and O through the group (no barrier between them in the loop);
+// then they are merged through shared memory.  The rows are the M = 16 side of
+// mma.sync: a tcgen05 tile would be 128 rows high for the 1 to 32 used here, and
+// its TMEM round trip is longer than the whole of a short step.
+// A group cut by the ends of stretches is joined by the CTA that finishes last,
+// in the order of the keys, so the result does not depend on which one that is.
 #include "paged.cuh"
 
 namespace qwm {
@@ -21,12 +24,21 @@ namespace {
 using namespace ptx;
 
 constexpr int TK = 64;                   // keys per tile
-constexpr int kWarps = 4;                // consumer warps, 16 keys each
+constexpr int kWarps = 8;                // consumer warps, 16 keys each
 constexpr int NT = (kWarps + 1) * 32;
-constexpr int kRing = 96 * 1024;         // bytes of tiles in flight; two CTAs per SM
+// What a group costs a CTA beside its tiles (Queries, merge, output: about 5 K
+// cycles), in tiles' time (1.3 K cycles for 128 channels when all CTAs stream).
+constexpr int group_cost(int D) { return 512 / D; }
 
 template <int D>
-constexpr int stages() { return kRing / (2 * TK * D * 2); }
+struct Shape {
+  static constexpr int SLOT = TK * D * 2;                      // bytes of a K or V tile
+  static constexpr int NS = D == 128 ? 8 : 12;                 // slots of the ring: K, V, K, V, ...
+  static_assert(NS % 4 == 0, "an even number of tiles: a slot belongs to one warp group");
+  static constexpr int MERGE = NS * SLOT;                      // the warps' O [warp][16][D], beside the ring so that
+                                                               // the next group's tiles come in meanwhile
+  static constexpr int TOTAL = MERGE + kWarps * 16 * D * 4 + 1024;
+};
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -43,112 +55,221 @@ __device__ __forceinline__ uint32_t at(int key, int chunk) {
   return (uint32_t)((chunk >> 3) * (TK * 128) + key * 128 + (((chunk & 7) ^ (key & 7)) << 4));
 }
 
-template <typename T, int D, int MT>
-__global__ void __launch_bounds__(NT) paged_step(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
-  constexpr int ST = stages<D>();
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {   // a >= 0, b > 0
+  return ((a | b) >> 32) ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
+// RT row tiles of 16: with one, the two warp groups take alternate tiles.
+template <typename T, int D, int RT>
+__global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
+  using L = Shape<D>;
+  constexpr int NS = L::NS, MT = 1;
   constexpr int KS = D / 16;                       // k16 steps of Q K^T, n16 blocks of P V
-  constexpr int ROWS = 16 * MT;
-  constexpr uint32_t HALF = TK * D * 2;            // bytes of a K or V tile
+  constexpr int kGroupCost = group_cost(D);
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  __shared__ uint64_t bars[2 * ST];
-  __shared__ float s_ml[kWarps][ROWS][2];
-  __shared__ int s_err, s_last;
+  __shared__ uint64_t bars[2 * NS];
+  __shared__ float s_ml[kWarps][16][2];
+  __shared__ int64_t s_scan[kWarps + 1], s_first;
+  __shared__ Seq s_sq;
+  __shared__ Tiles s_tl;
+  __shared__ int s_last, s_seq;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int part = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
-  Seq sq;
-  if (!load_seq(a, b, sq) && part == 0 && hk == 0 && tid == 0) record_status(a.status, QWM_ERR_INVALID_ARG);
-  if (sq.qn == 0) return;
-  const int rows = sq.qn * a.G;                    // <= ROWS
-  const int p0 = sq.kv - sq.qn;
-  const Tiles tl = make_tiles<TK>(p0, sq.kv - 1, sq.kv, a.block, a.window, a.sinks);
-  // this part's tiles: parts of equal length, as many as the length wants
-  const int per = max((tl.n + a.nsplit - 1) / a.nsplit, a.min_tiles);
-  const int parts = max(1, (tl.n + per - 1) / per);
-  if (part >= parts) return;
-  const int t0 = part * per, t1 = min(tl.n, t0 + per);
-
+  // tiles of a group of sequence b (one for a group that has rows and sees
+  // nothing: its output is written all the same)
+  auto tiles_of = [&](int b, Seq& sq, Tiles& tl) -> int {
+    if (!load_seq(a, b, sq) && blockIdx.x == 0) record_status(a.status, QWM_ERR_INVALID_ARG);
+    if (sq.qn == 0) return 0;
+    tl = make_tiles<TK>(sq.kv - sq.qn, sq.kv - 1, sq.kv, a.block, a.window, a.sinks);
+    return max(tl.n, 1);
+  };
   auto full = [&](int s) { return smem_u32(&bars[s]); };
-  auto empty = [&](int s) { return smem_u32(&bars[ST + s]); };
+  auto empty = [&](int s) { return smem_u32(&bars[NS + s]); };
   if (tid == 0) {
-    for (int s = 0; s < ST; ++s) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
       mbar_init(full(s), 1);
-      mbar_init(empty(s), kWarps);
+      mbar_init(empty(s), RT == 2 ? 8 : 4);
     }
-    s_err = 0;
     fence_mbar_init();
   }
-  __syncthreads();
-
-  float o[MT][2 * KS][4];
-  float m_run[MT][2], l_run[MT][2];
+  // The line: a group of sequence b takes n(b) + kGroupCost places, its tiles
+  // last; sequence b's groups follow those of the sequences before it.  Each
+  // thread sums a run of sequences; a scan over the threads gives the total, and
+  // the thread that holds the place where this CTA's stretch begins looks for
+  // the sequence.  Without a workspace, a CTA takes the group of its number.
+  const bool split = a.nsplit > 1;
+  Seq sq;
+  Tiles tl;
+  int b, n, hk;
+  int64_t x0, x1, g0, share = 0;
+  if (split) {
+    const int run = (a.B + NT - 1) / NT, b0 = min(a.B, tid * run), b1 = min(a.B, b0 + run);
+    int64_t mine = 0;
+    for (int i = b0; i < b1; ++i) {
+      const int t = tiles_of(i, sq, tl);
+      mine += t ? t + kGroupCost : 0;
+    }
+    int64_t incl = mine;
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    m_run[mt][0] = m_run[mt][1] = -INFINITY;
-    l_run[mt][0] = l_run[mt][1] = 0.0f;
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t x = __shfl_up_sync(0xFFFFFFFFu, incl, d);
+      if (lane >= d) incl += x;
+    }
+    if (lane == 31) s_scan[warp] = incl;
+    __syncthreads();
+    int64_t before = incl - mine, total = 0;
 #pragma unroll
-    for (int i = 0; i < 2 * KS; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) o[mt][i][k] = 0.0f;
+    for (int w = 0; w <= kWarps; ++w) {
+      if (w < warp) before += s_scan[w];
+      total += s_scan[w];
+    }
+    before *= a.Hk;
+    mine *= a.Hk;
+    total *= a.Hk;
+    share = max(divide(total + gridDim.x - 1, gridDim.x), (int64_t)a.min_tiles);
+    x0 = blockIdx.x * share;
+    if (x0 >= total) return;
+    if (x0 >= before && x0 < before + mine) {
+      int64_t at = before;
+      for (int i = b0; i < b1; ++i) {
+        if (run > 1) n = tiles_of(i, sq, tl);
+        else n = (int)(divide(mine, a.Hk)) - kGroupCost;
+        const int64_t len = n ? (int64_t)(n + kGroupCost) * a.Hk : 0;
+        if (x0 < at + len) {
+          s_seq = i;
+          s_first = at;
+          s_sq = sq;
+          s_tl = tl;
+          break;
+        }
+        at += len;
+      }
+    }
+    __syncthreads();
+    b = s_seq;
+    sq = s_sq;
+    tl = s_tl;
+    n = max(tl.n, 1);
+    hk = (int)divide(x0 - s_first, n + kGroupCost);
+    g0 = s_first + (int64_t)hk * (n + kGroupCost);
+    x1 = min(total, x0 + share);
+  } else {
+    b = blockIdx.x / a.Hk;
+    hk = blockIdx.x % a.Hk;
+    n = tiles_of(b, sq, tl);
+    if (n == 0) return;
+    x0 = g0 = 0;
+    x1 = n + kGroupCost;
+    __syncthreads();
   }
-  const float sl2 = a.scale * 1.4426950408889634f;
+  // The CTA's piece of the current group: tiles t0 .. t1 - 1, none if t0 >= t1.
+  int t0, t1;
+  auto piece = [&]() {
+    const int64_t first = g0 + kGroupCost;
+    t0 = (int)max((int64_t)0, x0 - first);
+    t1 = (int)min((int64_t)n, x1 - first);
+  };
+  auto next_group = [&]() -> bool {
+    g0 += n + kGroupCost;
+    if (g0 >= x1) return false;
+    if (++hk == a.Hk) {
+      hk = 0;
+      do n = tiles_of(++b, sq, tl); while (n == 0);
+    }
+    return true;
+  };
 
   if (warp == kWarps) {
     // ---------------------------------------------------------- producer
-    // lane = box * 4 + (Keys, Values) * 2 + channel half; a box is the part of
-    // a page that lies in the tile.  Boxes that no row sees are not read.
+    // lane = box * 2 + channel half; a box is the part of a page that lies in the
+    // tile.  Boxes that no row sees are not read.
     const int box_log2 = min(a.page_log2, 6);
-    const int boxes = TK >> box_log2;
-    const int box = lane >> 2, kv = (lane >> 1) & 1, half = lane & 1;
-    const bool mine = box < boxes && half * 64 < D;
-    const int32_t* trow = a.table + (int64_t)b * a.table_stride;
-    auto page_of = [&](int t, bool& want) -> int {
-      const int j0 = tile_at(tl, t) * TK + (box << box_log2);
-      want = mine && any_sees(tl, j0, j0 + (1 << box_log2), a.sinks);
-      return want ? trow[j0 >> a.page_log2] : 0;
-    };
-    bool want = false;
-    int page = t0 < t1 ? page_of(t0, want) : 0;
+    const int box = lane >> 1, half = lane & 1;
+    const bool mine = box < (TK >> box_log2) && half * 64 < D;
+    const uint32_t dst = smem_u32(sm) + half * (TK * 128) + ((box << box_log2) * 128);
     bool ok = true;
-    int t = t0;
-    for (; t < t1 && !a.idle; ++t) {
-      const int i = t - t0, s = i % ST;
-      if (i >= ST && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty(s), ((i / ST) - 1) & 1, a.wait_ns)))) break;
-      bool want_n = false;
-      int page_n = 0;
-      if (t + 1 < t1) page_n = page_of(t + 1, want_n);   // its latency runs beside the copies
-      if (want && (page < 0 || page >= a.num_pages)) {   // not followed: the first page in its place
-        record_status(a.status, QWM_ERR_INVALID_ARG);
-        page = 0;
-      }
-      const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, want)) * (128u << box_log2);
-      if (lane == 0) mbar_arrive_expect_tx(full(s), bytes);
-      __syncwarp();
-      if (want) {
+    int i = 0;                                     // slots filled
+    do {
+      piece();
+      t1 = min(t1, tl.n);
+      const int32_t* trow = a.table + (int64_t)b * a.table_stride;
+      auto page_of = [&](int t, bool& want) -> int {
         const int j0 = tile_at(tl, t) * TK + (box << box_log2);
-        const uint32_t dst = smem_u32(sm) + s * 2 * HALF + kv * HALF + half * (TK * 128) + ((box << box_log2) * 128);
-        tma_load_3d(dst, &map, half * 64, j0 & ((1 << a.page_log2) - 1), (page * 2 + kv) * a.Hk + hk, full(s));
+        want = mine && any_sees(tl, j0, j0 + (1 << box_log2), a.sinks);
+        return want ? trow[j0 >> a.page_log2] : 0;
+      };
+      bool want = false;
+      int page = t0 < t1 ? page_of(t0, want) : 0;
+      for (int t = t0; t < t1 && ok && !a.idle; ++t) {
+        bool want_n = false;
+        int page_n = 0;
+        if (t + 1 < t1) page_n = page_of(t + 1, want_n);   // its latency runs beside the copies
+        if (want && (page < 0 || page >= a.num_pages)) {   // not followed: the first page in its place
+          record_status(a.status, QWM_ERR_INVALID_ARG);
+          page = 0;
+        }
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, want)) * (128u << box_log2);
+        const int y = (tile_at(tl, t) * TK + (box << box_log2)) & ((1 << a.page_log2) - 1);
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          const int s = i % NS;
+          if (i >= NS && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty(s), ((i / NS) - 1) & 1, a.wait_ns)))) break;
+          if (lane == 0) mbar_arrive_expect_tx(full(s), bytes);
+          __syncwarp();
+          if (want) tma_load_3d(dst + s * L::SLOT, &map, half * 64, y, (page * 2 + kv) * a.Hk + hk, full(s));
+          __syncwarp();
+          ++i;
+        }
+        page = page_n;
+        want = want_n;
       }
-      __syncwarp();
-      page = page_n;
-      want = want_n;
-    }
+    } while (ok && next_group());
     if (!ok) {
       // a wait ran out: let the copies in flight land before the CTA ends
-      if (lane == 0) s_err = 1;
-      for (int u = max(t0, t - ST); u < t; ++u) mbar_wait(full((u - t0) % ST), ((u - t0) / ST) & 1, kDrainNs);
+      if (lane == 0) record_status(a.status, QWM_ERR_TIMEOUT);
+      for (int u = max(0, i - NS); u < i; ++u) mbar_wait(full(u % NS), (u / NS) & 1, kDrainNs);
     }
-  } else {
-    // ---------------------------------------------------------- consumers
-    const int g = lane >> 2, tq = lane & 3;
+    return;
+  }
+
+  // ------------------------------------------------------------ consumers
+  const float sl2 = a.scale * 1.4426950408889634f;
+  const int g = lane >> 2, tq = lane & 3;
+  const int wg = warp >> 2, slice = warp & 3;                           // row tile or tile parity, keys of the tile
+  const int rbase = RT == 2 ? 16 * wg : 0;                              // this warp's first row
+  const int mrow = lane & 7, mi = lane >> 3;
+  const int kkey = slice * 16 + (mi >> 1) * 8 + mrow, kch = mi & 1;      // K: (keys 0-7 | 8-15) x (chunk, chunk + 1)
+  const int vkey = slice * 16 + (mi & 1) * 8 + mrow, vch = mi >> 1;      // V: the same, keys innermost
+  const int maxrows = a.max_q * a.G;
+  float* so = reinterpret_cast<float*>(sm + L::MERGE);                  // [warp][16][D]
+  bool ok = true;                                                       // no wait of this warp has run out
+  int filled = 0;                                                       // slots of the pieces before
+  do {
+    piece();
+    if (t0 >= t1) continue;
+    const int rows = sq.qn * a.G;                                       // <= 16 RT
+    const int t_end = min(t1, tl.n);
+    const int p0 = sq.kv - sq.qn;
+    float o[MT][2 * KS][4];
+    float m_run[MT][2], l_run[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      m_run[mt][0] = m_run[mt][1] = -INFINITY;
+      l_run[mt][0] = l_run[mt][1] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 2 * KS; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[mt][k][e] = 0.0f;
+    }
     uint32_t qf[MT][KS][4];
     int hi[MT][2], lo[MT][2];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int rr = 0; rr < 2; ++rr) {
-        const int r = mt * 16 + rr * 8 + g;
+        const int r = rbase + rr * 8 + g;
         const bool has = r < rows;
         const int tok = has ? r / a.G : 0;
         const Span sp = has ? row_span(p0 + tok, sq.kv, a.block, a.window) : Span{0, 0};
@@ -161,24 +282,25 @@ __global__ void __launch_bounds__(NT) paged_step(const __grid_constant__ CUtenso
           qf[mt][ks][2 + rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8 + tq * 2) : 0u;
         }
       }
-    const int mrow = lane & 7, mi = lane >> 3;
-    const int kkey = warp * 16 + (mi >> 1) * 8 + mrow, kch = mi & 1;      // K: (keys 0-7 | 8-15) x (chunk, chunk + 1)
-    const int vkey = warp * 16 + (mi & 1) * 8 + mrow, vch = mi >> 1;      // V: the same, keys innermost
-    bool ok = true;
-    for (int t = t0; t < t1; ++t) {
-      const int i = t - t0, s = i % ST;
-      if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full(s), (i / ST) & 1, a.wait_ns)))) break;
-      const uint32_t kb = smem_u32(sm) + s * 2 * HALF, vb = kb + HALF;
-      const int j0 = tile_at(tl, t) * TK + warp * 16;                      // this warp's keys
-      const bool open = all_see(tl, j0, j0 + 16, a.sinks);
-      if (any_sees(tl, j0, j0 + 16, a.sinks)) {
+    // With one row tile, this warp group's tiles are those of its parity in the
+    // CTA's count of tiles, so that a slot of the ring is always the same
+    // group's: a group that did not wait for every use of a slot could take the
+    // phase before the one it waits for as done (a parity tells only two apart).
+    for (int t = t0 + (RT == 2 ? 0 : ((filled >> 1) + wg) & 1); t < t_end && ok; t += 3 - RT) {
+      const int i = filled + 2 * (t - t0), s = i % NS;                   // slots s and s + 1
+      const int j0 = tile_at(tl, t) * TK + slice * 16;                   // this warp's keys
+      if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full(s), (i / NS) & 1, a.wait_ns)))) break;
+      const uint32_t kb = smem_u32(sm) + s * L::SLOT, vb = kb + L::SLOT;
+      const bool open = all_see(tl, j0, j0 + 16, a.sinks), any = any_sees(tl, j0, j0 + 16, a.sinks);
+      uint32_t pf[MT][4];
+      if (any) {
         float sc[MT][2][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int n = 0; n < 2; ++n)
+          for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sc[mt][n][k] = 0.0f;
+            for (int e = 0; e < 4; ++e) sc[mt][k][e] = 0.0f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           uint32_t bf[4];
@@ -193,11 +315,11 @@ __global__ void __launch_bounds__(NT) paged_step(const __grid_constant__ CUtenso
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                if (!sees(j0 + n * 8 + tq * 2 + (k & 1), lo[mt][k >> 1], hi[mt][k >> 1], a.sinks))
-                  sc[mt][n][k] = -INFINITY;
+              for (int e = 0; e < 4; ++e)
+                if (!sees(j0 + k * 8 + tq * 2 + (e & 1), lo[mt][e >> 1], hi[mt][e >> 1], a.sinks))
+                  sc[mt][k][e] = -INFINITY;
         }
         // running maximum of each row, moved only when a key of this slice is
         // above it: the four lanes of a row agree through two shuffles then
@@ -223,200 +345,240 @@ __global__ void __launch_bounds__(NT) paged_step(const __grid_constant__ CUtenso
               m_run[mt][rr] = mn;
               l_run[mt][rr] *= al;
 #pragma unroll
-              for (int n = 0; n < 2 * KS; ++n) {
-                o[mt][n][2 * rr] *= al;
-                o[mt][n][2 * rr + 1] *= al;
+              for (int k = 0; k < 2 * KS; ++k) {
+                o[mt][k][2 * rr] *= al;
+                o[mt][k][2 * rr + 1] *= al;
               }
             }
         }
-        uint32_t pf[MT][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           // a row that has seen nothing yet keeps 0 as its reference: 2^-inf = 0
           const float mb0 = m_run[mt][0] == -INFINITY ? 0.0f : m_run[mt][0] * sl2;
           const float mb1 = m_run[mt][1] == -INFINITY ? 0.0f : m_run[mt][1] * sl2;
 #pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            const float x0 = ex2f(fmaf(sc[mt][n][0], sl2, -mb0)), x1 = ex2f(fmaf(sc[mt][n][1], sl2, -mb0));
-            const float y0 = ex2f(fmaf(sc[mt][n][2], sl2, -mb1)), y1 = ex2f(fmaf(sc[mt][n][3], sl2, -mb1));
-            l_run[mt][0] += x0 + x1;
-            l_run[mt][1] += y0 + y1;
-            pf[mt][2 * n] = Elem<T>::pack(x0, x1);
-            pf[mt][2 * n + 1] = Elem<T>::pack(y0, y1);
-          }
-        }
-        if (open) {
-#pragma unroll
-          for (int nb = 0; nb < KS; ++nb) {
-            uint32_t bf[4];
-            ldsm4t(vb + at(vkey, 2 * nb + vch), bf);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              Elem<T>::mma(o[mt][2 * nb], pf[mt], bf[0], bf[1]);
-              Elem<T>::mma(o[mt][2 * nb + 1], pf[mt], bf[2], bf[3]);
-            }
-          }
-        } else {
-          // Keys that no row sees may hold anything (0 x inf is not 0): their
-          // Values are cleared in the fragments.  Keys that some rows see and
-          // others do not (drafts of several tokens): if one holds an infinity
-          // or a NaN, the product is taken token by token and only that
-          // token's rows keep it.
-          auto keep = [&](int klo, int khi, int j) -> uint32_t {
-            return (sees(j, klo, khi, a.sinks) ? 0xFFFFu : 0u) | (sees(j + 1, klo, khi, a.sinks) ? 0xFFFF0000u : 0u);
-          };
-          const int ja = j0 + tq * 2;
-          const uint32_t ma = keep(tl.lo_min, tl.hi_max, ja), mb = keep(tl.lo_min, tl.hi_max, ja + 8);
-          bool odd = false;
-          if (sq.qn > 1) {
-#pragma unroll
-            for (int nb = 0; nb < KS; ++nb) {
-              uint32_t bf[4];
-              ldsm4t(vb + at(vkey, 2 * nb + vch), bf);
-              odd |= nonfinite2<T>(bf[0] & ma) || nonfinite2<T>(bf[1] & mb) || nonfinite2<T>(bf[2] & ma) ||
-                     nonfinite2<T>(bf[3] & mb);
-            }
-            odd = __any_sync(0xFFFFFFFFu, odd);
-          }
-          const int turns = odd ? sq.qn : 1;
-          for (int tk = 0; tk < turns; ++tk) {
-            uint32_t wa = ma, wb = mb;
-            bool own[MT][2];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-              for (int rr = 0; rr < 2; ++rr) own[mt][rr] = !odd || (mt * 16 + rr * 8 + g) / a.G == tk;
-            if (odd) {
-              const Span sp = row_span(p0 + tk, sq.kv, a.block, a.window);
-              wa = keep(sp.lo, sp.hi, ja);
-              wb = keep(sp.lo, sp.hi, ja + 8);
-            }
-#pragma unroll
-            for (int nb = 0; nb < KS; ++nb) {
-              uint32_t bf[4];
-              ldsm4t(vb + at(vkey, 2 * nb + vch), bf);
-#pragma unroll
-              for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                  float acc[4];
-#pragma unroll
-                  for (int k = 0; k < 4; ++k) acc[k] = o[mt][2 * nb + n][k];
-                  Elem<T>::mma(acc, pf[mt], bf[2 * n] & wa, bf[2 * n + 1] & wb);
-#pragma unroll
-                  for (int k = 0; k < 4; ++k)
-                    if (own[mt][k >> 1]) o[mt][2 * nb + n][k] = acc[k];
-                }
-            }
+          for (int k = 0; k < 2; ++k) {
+            const float v0 = ex2f(fmaf(sc[mt][k][0], sl2, -mb0)), v1 = ex2f(fmaf(sc[mt][k][1], sl2, -mb0));
+            const float w0 = ex2f(fmaf(sc[mt][k][2], sl2, -mb1)), w1 = ex2f(fmaf(sc[mt][k][3], sl2, -mb1));
+            l_run[mt][0] += v0 + v1;
+            l_run[mt][1] += w0 + w1;
+            pf[mt][2 * k] = Elem<T>::pack(v0, v1);
+            pf[mt][2 * k + 1] = Elem<T>::pack(w0, w1);
           }
         }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(empty(s));
+      if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full(s + 1), (i / NS) & 1, a.wait_ns)))) break;
+      if (open) {
+#pragma unroll
+        for (int nb = 0; nb < KS; ++nb) {
+          uint32_t bf[4];
+          ldsm4t(vb + at(vkey, 2 * nb + vch), bf);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            Elem<T>::mma(o[mt][2 * nb], pf[mt], bf[0], bf[1]);
+            Elem<T>::mma(o[mt][2 * nb + 1], pf[mt], bf[2], bf[3]);
+          }
+        }
+      } else if (any) {
+        // Keys that no row sees may hold anything (0 x inf is not 0): their
+        // Values are cleared in the fragments.  Keys that some rows see and
+        // others do not (drafts of several tokens): if one holds an infinity
+        // or a NaN, the product is taken token by token and only that
+        // token's rows keep it.
+        auto keep = [&](int klo, int khi, int j) -> uint32_t {
+          return (sees(j, klo, khi, a.sinks) ? 0xFFFFu : 0u) | (sees(j + 1, klo, khi, a.sinks) ? 0xFFFF0000u : 0u);
+        };
+        const int ja = j0 + tq * 2;
+        const uint32_t ma = keep(tl.lo_min, tl.hi_max, ja), mb = keep(tl.lo_min, tl.hi_max, ja + 8);
+        bool odd = false;
+        if (sq.qn > 1) {
+#pragma unroll
+          for (int nb = 0; nb < KS; ++nb) {
+            uint32_t bf[4];
+            ldsm4t(vb + at(vkey, 2 * nb + vch), bf);
+            odd |= nonfinite2<T>(bf[0] & ma) || nonfinite2<T>(bf[1] & mb) || nonfinite2<T>(bf[2] & ma) ||
+                   nonfinite2<T>(bf[3] & mb);
+          }
+          odd = __any_sync(0xFFFFFFFFu, odd);
+        }
+        const int turns = odd ? sq.qn : 1;
+        for (int tk = 0; tk < turns; ++tk) {
+          uint32_t wa = ma, wb = mb;
+          bool own[MT][2];
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int rr = 0; rr < 2; ++rr) own[mt][rr] = !odd || (rbase + rr * 8 + g) / a.G == tk;
+          if (odd) {
+            const Span sp = row_span(p0 + tk, sq.kv, a.block, a.window);
+            wa = keep(sp.lo, sp.hi, ja);
+            wb = keep(sp.lo, sp.hi, ja + 8);
+          }
+#pragma unroll
+          for (int nb = 0; nb < KS; ++nb) {
+            uint32_t bf[4];
+            ldsm4t(vb + at(vkey, 2 * nb + vch), bf);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                float acc[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] = o[mt][2 * nb + k][e];
+                Elem<T>::mma(acc, pf[mt], bf[2 * k] & wa, bf[2 * k + 1] & wb);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (own[mt][e >> 1]) o[mt][2 * nb + k][e] = acc[e];
+              }
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty(s + 1));
     }
-    if (!ok && lane == 0) s_err = 1;
-    // the four lanes of a row hold its sum in parts
+    filled += 2 * max(0, t_end - t0);
+    if (!ok && lane == 0) record_status(a.status, QWM_ERR_TIMEOUT);
+
+    // -------------------------------------------------------- the warps' (max, sum, O) of the piece
+    named_bar_sync(1, kWarps * 32);                  // the last piece's have been read
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int rr = 0; rr < 2; ++rr) {
-        float l = l_run[mt][rr];
+        const int r = rr * 8 + g;
+        float l = l_run[mt][rr];                     // the four lanes of a row hold its sum in parts
         l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
         l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
+        if (rbase + r >= rows) continue;
         if (tq == 0) {
-          s_ml[warp][mt * 16 + rr * 8 + g][0] = m_run[mt][rr];
-          s_ml[warp][mt * 16 + rr * 8 + g][1] = l;
+          s_ml[warp][r][0] = m_run[mt][rr];
+          s_ml[warp][r][1] = l;
+        }
+#pragma unroll
+        for (int k = 0; k < 2 * KS; ++k)
+          *reinterpret_cast<float2*>(so + ((warp * 16 + r) * D + k * 8 + tq * 2)) =
+              make_float2(o[mt][k][2 * rr], o[mt][k][2 * rr + 1]);
+      }
+    named_bar_sync(1, kWarps * 32);
+    const int64_t group = (int64_t)b * a.Hk + hk, first = g0 + kGroupCost;
+    const int64_t c0 = split ? divide(first, share) : 0, c1 = split ? divide(first + n - 1, share) : 0;   // its CTAs
+    const int parts = (int)(c1 - c0) + 1;
+    auto emit = [&](int r, int c, float m, float l, float4 v) {
+      const int tok = r / a.G, h = hk * a.G + r % a.G;
+      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+      T* dst = static_cast<T*>(a.out) + (sq.q0 + tok) * a.o_tok + (int64_t)h * a.o_head + 4 * c;
+      *reinterpret_cast<uint2*>(dst) = make_uint2(Elem<T>::pack(v.x * inv, v.y * inv), Elem<T>::pack(v.z * inv, v.w * inv));
+      if (a.lse && c == 0) a.lse[(int64_t)h * a.N + sq.q0 + tok] = m == -INFINITY ? -INFINITY : m * a.scale + logf(l);
+    };
+    // (m, l, O) of a row's channels 4c .. over `count` entries from `first_entry`
+    // of s_ml and so, row `at`
+    auto merge = [&](int first_entry, int count, int at, int c, float& m, float& l, float4& v) {
+      m = -INFINITY;
+      for (int w = 0; w < count; ++w) m = fmaxf(m, s_ml[first_entry + w][at][0]);
+      const float ref = m == -INFINITY ? 0.0f : m;
+      l = 0.0f;
+      v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int w = 0; w < count; ++w) {
+        const float f = ex2f((s_ml[first_entry + w][at][0] - ref) * sl2);
+        const float4 x = *reinterpret_cast<const float4*>(so + (((first_entry + w) * 16 + at) * D + 4 * c));
+        l = fmaf(s_ml[first_entry + w][at][1], f, l);
+        v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
+      }
+    };
+    for (int idx = tid; idx < rows * (D / 4); idx += kWarps * 32) {
+      const int r = idx / (D / 4), c = idx % (D / 4);
+      float m, l;
+      float4 v;
+      merge(RT == 2 ? (r >> 4) * 4 : 0, RT == 2 ? 4 : 8, r & 15, c, m, l, v);
+      if (parts == 1) {
+        emit(r, c, m, l, v);
+      } else {
+        // a CTA's places: 0 for a group that began before its stretch, 1 for one that begins in it
+        const int64_t pr = (2 * (int64_t)blockIdx.x + (first >= x0 ? 1 : 0)) * maxrows + r;
+        *reinterpret_cast<float4*>(a.part_o + pr * D + 4 * c) = v;
+        if (c == 0) a.part_ml[pr] = make_float2(m, l);
+      }
+    }
+    if (parts == 1) continue;
+    // -------------------------------------------------------- the CTA that arrives last joins all parts
+    __threadfence();
+    named_bar_sync(1, kWarps * 32);
+    if (tid == 0) s_last = atomicAdd(a.counter + group, 1) == parts - 1;
+    named_bar_sync(1, kWarps * 32);
+    if (!s_last) continue;
+    __threadfence();
+    // part p's rows: the first CTA's second place, the others' first
+    auto place = [&](int p) { return (2 * (c0 + p) + (p == 0 ? 1 : 0)) * maxrows; };
+    // A warp takes whole rows (the warps share a row's parts out when there are
+    // fewer rows than warps), a lane four channels, 16 parts in flight.
+    constexpr int LPR = D / 4, RPW = 32 / LPR;        // lanes per row, rows per warp at a time
+    const int rr = (rows + RPW - 1) / RPW;
+    const int slices = rr > 4 ? 1 : (rr > 2 ? 2 : (rr > 1 ? 4 : 8)), sl = warp % slices;
+    const int q0 = parts * sl / slices, q1 = parts * (sl + 1) / slices;
+    for (int rb = (warp / slices) * RPW; rb < rows; rb += (kWarps / slices) * RPW) {
+      const int r = rb + lane / LPR, c = lane % LPR;
+      float m = -INFINITY, l = 0.0f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r >= rows) continue;
+      constexpr int PU = 16;
+      for (int p = q0; p < q1; p += PU) {
+        float2 ml[PU];
+        float4 x[PU];
+#pragma unroll
+        for (int u = 0; u < PU; ++u) {
+          const int64_t at_p = place(min(p + u, q1 - 1)) + r;
+          ml[u] = __ldcg(&a.part_ml[at_p]);
+          x[u] = __ldcg(reinterpret_cast<const float4*>(a.part_o + at_p * D + 4 * c));
+        }
+        float mn = m;
+#pragma unroll
+        for (int u = 0; u < PU; ++u) mn = fmaxf(mn, ml[u].x);
+        const float ref = mn == -INFINITY ? 0.0f : mn;
+        const float al = ex2f((m - ref) * sl2);
+        m = mn;
+        l *= al;
+        v.x *= al; v.y *= al; v.z *= al; v.w *= al;
+#pragma unroll
+        for (int u = 0; u < PU; ++u) {
+          if (p + u >= q1) break;
+          const float f = ex2f((ml[u].x - ref) * sl2);
+          l = fmaf(ml[u].y, f, l);
+          v.x = fmaf(x[u].x, f, v.x); v.y = fmaf(x[u].y, f, v.y); v.z = fmaf(x[u].z, f, v.z); v.w = fmaf(x[u].w, f, v.w);
         }
       }
-  }
-  __syncthreads();   // every tile has been read: the ring becomes the warps' O
-  if (s_err) {
-    if (tid == 0) record_status(a.status, QWM_ERR_TIMEOUT);
-  }
-  float* so = reinterpret_cast<float*>(sm);        // [warp][ROWS][D]
-  if (warp < kWarps) {
-    const int g = lane >> 2, tq = lane & 3;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int n = 0; n < 2 * KS; ++n)
-#pragma unroll
-        for (int rr = 0; rr < 2; ++rr)
-          *reinterpret_cast<float2*>(so + ((warp * ROWS + mt * 16 + rr * 8 + g) * D + n * 8 + tq * 2)) =
-              make_float2(o[mt][n][2 * rr], o[mt][n][2 * rr + 1]);
-  }
-  __syncthreads();
-
-  // (max, sum, O) of a row's channels 4c.. over the four warps
-  const int64_t group = (int64_t)b * a.Hk + hk;
-  auto emit = [&](int r, int c, float m, float l, float4 v) {
-    const int tok = r / a.G, h = hk * a.G + r % a.G;
-    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    T* dst = static_cast<T*>(a.out) + (sq.q0 + tok) * a.o_tok + (int64_t)h * a.o_head + 4 * c;
-    *reinterpret_cast<uint2*>(dst) = make_uint2(Elem<T>::pack(v.x * inv, v.y * inv), Elem<T>::pack(v.z * inv, v.w * inv));
-    if (a.lse && c == 0) a.lse[(int64_t)h * a.N + sq.q0 + tok] = m == -INFINITY ? -INFINITY : m * a.scale + logf(l);
-  };
-  const int maxrows = a.max_q * a.G;
-  for (int i = tid; i < rows * (D / 4); i += NT) {
-    const int r = i / (D / 4), c = i % (D / 4);
-    float m = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) m = fmaxf(m, s_ml[w][r][0]);
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float f = ex2f((s_ml[w][r][0] - ref) * sl2);
-      const float4 x = *reinterpret_cast<const float4*>(so + ((w * ROWS + r) * D + 4 * c));
-      l = fmaf(s_ml[w][r][1], f, l);
-      v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
+      if (slices == 1) {
+        emit(r, c, m, l, v);
+      } else {
+        *reinterpret_cast<float4*>(so + ((sl * 16 + r) * D + 4 * c)) = v;
+        if (c == 0) {
+          s_ml[sl][r][0] = m;
+          s_ml[sl][r][1] = l;
+        }
+      }
     }
-    if (parts == 1) {
-      emit(r, c, m, l, v);
-    } else {
-      const int64_t pr = (group * a.nsplit + part) * maxrows + r;
-      *reinterpret_cast<float4*>(a.part_o + pr * D + 4 * c) = v;
-      if (c == 0) a.part_ml[pr] = make_float2(m, l);
+    if (slices > 1) {
+      named_bar_sync(1, kWarps * 32);
+      for (int idx = tid; idx < rows * (D / 4); idx += kWarps * 32) {
+        const int r = idx / (D / 4), c = idx % (D / 4);
+        float m, l;
+        float4 v;
+        merge(0, slices, r, c, m, l, v);
+        emit(r, c, m, l, v);
+      }
     }
-  }
-  if (parts == 1) return;
-  // the part that arrives last joins all of them
-  __threadfence();
-  __syncthreads();
-  if (tid == 0) s_last = atomicAdd(a.counter + group, 1) == parts - 1;
-  __syncthreads();
-  if (!s_last) return;
-  __threadfence();
-  for (int i = tid; i < rows * (D / 4); i += NT) {
-    const int r = i / (D / 4), c = i % (D / 4);
-    const int64_t pr = group * a.nsplit * maxrows + r;
-    float m = -INFINITY;
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, __ldcg(&a.part_ml[pr + (int64_t)p * maxrows].x));
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-      const int64_t at_p = pr + (int64_t)p * maxrows;
-      const float2 ml = __ldcg(&a.part_ml[at_p]);
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(a.part_o + at_p * D + 4 * c));
-      const float f = ex2f((ml.x - ref) * sl2);
-      l = fmaf(ml.y, f, l);
-      v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
-    }
-    emit(r, c, m, l, v);
-  }
-  if (tid == 0) a.counter[group] = 0;
+    if (tid == 0) a.counter[group] = 0;
+  } while (next_group());
 }
 
-template <typename T, int D, int MT>
+template <typename T, int D, int RT>
 cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
-  constexpr int smem = kRing + 1024;
-  static_assert(kWarps * 16 * MT * D * 4 <= kRing, "the ring holds the merge");
-  cudaError_t e = cudaFuncSetAttribute(paged_step<T, D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  constexpr int smem = Shape<D>::TOTAL;
+  cudaError_t e = cudaFuncSetAttribute(paged_step<T, D, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  paged_step<T, D, MT><<<dim3(a.nsplit, a.Hk, a.B), NT, smem, s>>>(map, a);
+  paged_step<T, D, RT><<<(unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk), NT, smem, s>>>(map, a);
   return cudaGetLastError();
 }
 template <typename T, int D>
@@ -426,23 +588,20 @@ cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
 
 }  // namespace
 
-PagedPlan plan_step(int B, int Hk, int rows, int64_t max_visible, int nsm, bool split) {
+PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split) {
   PagedPlan p{};
   p.step = 1;
   p.groups = B * Hk;
   p.rows = rows;
-  const int64_t tiles = (max_visible + TK - 1) / TK + 2;
-  // Parts of at least 8 tiles (512 keys: a part's O costs about a fiftieth of
-  // its K and V), and about three waves of two CTAs per SM, so that sequences
-  // of unequal length even out.
-  p.min_tiles = 8;
+  // the shortest stretch, in places: a sequence of 64 to 200 keys takes 5.6 to 7.7
+  // us with 4, up to 9.5 with 3 (an extra join), 9.3 with 6
+  p.min_tiles = 4;
   p.nsplit = 1;
   if (split) {
-    const int64_t want = (6 * (int64_t)nsm + p.groups - 1) / p.groups;
-    const int64_t most = (tiles + p.min_tiles - 1) / p.min_tiles;
+    // a CTA per SM, or as many as have min_tiles places each
+    const int64_t tiles = ((max_visible + TK - 1) / TK + 1 + group_cost(D)) * p.groups;
+    const int64_t want = (tiles + p.min_tiles - 1) / p.min_tiles, most = nsm;
     p.nsplit = (int)(want < most ? want : most);
-    if (p.nsplit > 256) p.nsplit = 256;
-    if (p.nsplit < 1) p.nsplit = 1;
   }
   return p;
 }

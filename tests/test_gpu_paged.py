@@ -340,3 +340,14 @@ def test_a_wait_that_runs_out_is_recorded_and_the_next_call_is_exact(new):
     out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True, workspace=ws)
     compare(out, lse, attend64(q, keys, values, lens, 1, 0, 0))
     assert cache.status() == 0
+
+
+@pytest.mark.parametrize("D,dtype,Hq,Hk,new", [(128, BF, 20, 4, 1), (64, HF, 24, 8, 1), (128, HF, 18, 9, 9)])
+def test_step_over_many_sequences(D, dtype, Hq, Hk, new):
+    """More groups than CTAs, of lengths from none to several ring turns."""
+    g = torch.Generator().manual_seed(D + Hq)
+    lens = []
+    for i in range(61):
+        q = int(torch.randint(0 if i % 7 == 3 else 1, new + 1, (1,), generator=g))
+        lens.append((q, max(q, int(torch.randint(0, [5, 70, 700, 1800][i % 4], (1,), generator=g)))))
+    run_case(300 + D, lens, Hq, Hk, D, dtype, 16, 1, 600, 9)
