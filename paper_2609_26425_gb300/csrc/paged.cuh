@@ -75,6 +75,18 @@ cudaError_t launch_paged_chunk(const PagedArgs& a, const CUtensorMap& map, int D
 // Limit of the waits that let copies and MMAs in flight finish after another
 // wait has run out, before a CTA gives up its shared memory and TMEM.
 constexpr uint64_t kDrainNs = 1000000000ull;
+// cudaFuncSetAttribute once per device for a kernel with dynamic shared memory
+// (`done`: the caller's static).
+template <class K>
+inline cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64]) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
+  return e;
+}
 // Rows (Query tokens x Query heads per cache head) up to which a sequence goes
 // to the step kernel.
 constexpr int kStepRows = 32;

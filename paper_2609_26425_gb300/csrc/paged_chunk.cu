@@ -612,7 +612,8 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
 
 template <typename T, int D>
 cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
-  cudaError_t e = cudaFuncSetAttribute(paged_chunk<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL);
+  static bool done[64];
+  cudaError_t e = allow_smem(paged_chunk<T, D>, Smem<D>::TOTAL, done);
   if (e != cudaSuccess) return e;
   const int64_t rtiles = ((int64_t)a.max_q * a.G + ROWS - 1) / ROWS;
   paged_chunk<T, D><<<dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), NT, Smem<D>::TOTAL, s>>>(map, a);

@@ -576,7 +576,8 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
 template <typename T, int D, int RT>
 cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   constexpr int smem = Shape<D>::TOTAL;
-  cudaError_t e = cudaFuncSetAttribute(paged_step<T, D, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static bool done[64];
+  cudaError_t e = allow_smem(paged_step<T, D, RT>, smem, done);
   if (e != cudaSuccess) return e;
   paged_step<T, D, RT><<<(unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk), NT, smem, s>>>(map, a);
   return cudaGetLastError();

@@ -85,9 +85,7 @@ def _check(fn, st):
         raise QwmError(fn, st)
 
 
-def _stream(t):
-    """The current stream of a tensor's device."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
+_raw_stream = torch._C._cuda_getCurrentRawStream  # current stream of a device, without a Stream object
 
 
 def _rows(t, dtype, name, tokens=None, head_dim=None):
@@ -105,12 +103,28 @@ def _rows(t, dtype, name, tokens=None, head_dim=None):
     return QwmRows(t.data_ptr(), st if n > 1 else 0, sh if h > 1 else 0, h)
 
 
+def _out(like, out, name):
+    """An output with the shape and dtype of `like`: the caller's, or a new contiguous tensor."""
+    if out is None:
+        out = torch.empty_like(like) if like.is_contiguous() else torch.empty(like.shape, dtype=like.dtype,
+                                                                              device=like.device)
+        _, h, d = like.shape
+        return out, QwmRows(out.data_ptr(), h * d, d, h)
+    if out.shape != like.shape:
+        raise ValueError(f"{name} has shape {tuple(out.shape)}, expected {tuple(like.shape)}")
+    return out, _rows(out, like.dtype, name)
+
+
 def _ints(t, shape, name):
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.int32 and t.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous int32 CUDA tensor")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
     return t
+
+
+def _stream(t):
+    return _raw_stream(t.get_device())
 
 
 # ------------------------------------------------------------------ rope
@@ -127,6 +141,7 @@ class Rope:
                 and inv_freq.is_contiguous() and tuple(inv_freq.shape) == (sum(pairs),)):
             raise ValueError(f"inv_freq must be a contiguous fp32 CUDA tensor [{sum(pairs)}]")
         self.inv_freq, self.pairs, self.interleaved = inv_freq, pairs, bool(interleaved)
+        self.freq_ptr = inv_freq.data_ptr()
         self._cfg = {}
 
     def config(self, head_dim, dtype):
@@ -144,22 +159,16 @@ def _turn(name, rope, q, pos, k, q_out, k_out):
         raise ValueError("q must be a [tokens][heads][head_dim] tensor")
     n, _, d = q.shape
     cfg = rope.config(d, q.dtype)
-    _ints(pos, (n, 3), "pos")
     qr = _rows(q, q.dtype, "q")
-    if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    elif q_out.shape != q.shape:
-        raise ValueError(f"q_out has shape {tuple(q_out.shape)}, expected {tuple(q.shape)}")
+    q_out, qo = _out(q, q_out, "q_out")
     kr = ko = None
     if k is not None:
         kr = _rows(k, q.dtype, "k", n, d)
-        if k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        elif k_out.shape != k.shape:
-            raise ValueError(f"k_out has shape {tuple(k_out.shape)}, expected {tuple(k.shape)}")
-        ko = _rows(k_out, q.dtype, "k_out")
-    _check(name, getattr(_lib(), name)(cfg, rope.inv_freq.data_ptr(), pos.data_ptr(), n, qr,
-                                       _rows(q_out, q.dtype, "q_out"), kr, ko, _stream(q)))
+        k_out, ko = _out(k, k_out, "k_out")
+    st = getattr(_C or _lib(), name)(cfg, rope.freq_ptr, _ints(pos, (n, 3), "pos").data_ptr(), n, qr, qo, kr, ko,
+                                     _raw_stream(q.get_device()))
+    if st:
+        _check(name, st)
     return q_out if k is None else (q_out, k_out)
 
 
@@ -184,7 +193,7 @@ class PagedCache:
             raise ValueError("pages hold bf16 or fp16")
         self.cfg = QwmPagedConfig(kv_heads, head_dim, page_tokens, _DTYPES[dtype], num_pages)
         self.dtype, self.head_dim, self.kv_heads, self.page_tokens = dtype, head_dim, kv_heads, page_tokens
-        self.num_pages = num_pages
+        self.num_pages, self.scale = num_pages, 1.0 / math.sqrt(head_dim) if head_dim > 0 else 1.0
         n = int(_lib().qwm_paged_bytes(self.cfg))
         if n == 0:
             _check("qwm_paged_bytes", 2)
@@ -260,16 +269,14 @@ def qwm_paged_append(cache: PagedCache, batch: PagedBatch, k, v, rope: Rope = No
     kr, vr = _rows(k, t, "k", n, d), _rows(v, t, "v", n, d)
     cfg = freq = at = qr = qo = None
     if rope is not None:
-        cfg, freq, at = rope.config(d, t), rope.inv_freq.data_ptr(), _ints(pos, (n, 3), "pos").data_ptr()
+        cfg, freq, at = rope.config(d, t), rope.freq_ptr, _ints(pos, (n, 3), "pos").data_ptr()
     if q is not None:
         qr = _rows(q, t, "q", n, d)
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=t, device=q.device)
-        elif q_out.shape != q.shape:
-            raise ValueError(f"q_out has shape {tuple(q_out.shape)}, expected {tuple(q.shape)}")
-        qo = _rows(q_out, t, "q_out")
-    _check("qwm_paged_append", _lib().qwm_paged_append(cache.handle, batch.struct(n), kr, vr, cfg, freq, at, qr, qo,
-                                                       _stream(k)))
+        q_out, qo = _out(q, q_out, "q_out")
+    st = (_C or _lib()).qwm_paged_append(cache.handle, batch.struct(n), kr, vr, cfg, freq, at, qr, qo,
+                                         _raw_stream(k.get_device()))
+    if st:
+        _check("qwm_paged_append", st)
     return q_out if q is not None else None
 
 
@@ -295,21 +302,18 @@ def qwm_paged_attend(cache: PagedCache, batch: PagedBatch, q, window=0, sinks=0,
     """Attention of the batch's rows over the pages of their sequences: block-causal
     (``block`` tokens a block, 1 = token-causal), the last ``window`` tokens up to
     the end of the row's block (0: all) and the first ``sinks`` tokens."""
-    d, t = cache.head_dim, cache.dtype
-    qr = _rows(q, t, "q", None, d)
-    n = q.shape[0]
-    if out is None:
-        out = torch.empty(q.shape, dtype=t, device=q.device)
-    elif out.shape != q.shape:
-        raise ValueError(f"out has shape {tuple(out.shape)}, expected {tuple(q.shape)}")
-    if want_lse and lse is None:
-        lse = torch.empty(q.shape[1], n, dtype=torch.float32, device=q.device)
-    if lse is not None and not (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous()
-                                and tuple(lse.shape) == (q.shape[1], n)):
-        raise ValueError("lse must be a contiguous fp32 CUDA tensor [heads][tokens]")
-    scale = 1.0 / math.sqrt(d) if sm_scale is None else float(sm_scale)
-    _check("qwm_paged_attend", _lib().qwm_paged_attend(
-        cache.handle, batch.struct(n), qr, QwmMask(block, window, sinks), scale, _rows(out, t, "out"),
-        None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
-        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(q)))
-    return (out, lse) if lse is not None else out
+    qr = _rows(q, cache.dtype, "q", None, cache.head_dim)
+    n, h, _ = q.shape
+    out, orows = _out(q, out, "out")
+    if lse is not None:
+        if not (lse.is_cuda and lse.dtype is torch.float32 and lse.is_contiguous() and lse.shape == (h, n)):
+            raise ValueError("lse must be a contiguous fp32 CUDA tensor [heads][tokens]")
+    elif want_lse:
+        lse = torch.empty((h, n), dtype=torch.float32, device=q.device)
+    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    st = (_C or _lib()).qwm_paged_attend(
+        cache.handle, batch.struct(n), qr, QwmMask(block, window, sinks), cache.scale if sm_scale is None else sm_scale,
+        orows, None if lse is None else lse.data_ptr(), ws, size, _raw_stream(q.get_device()))
+    if st:
+        _check("qwm_paged_attend", st)
+    return out if lse is None else (out, lse)
