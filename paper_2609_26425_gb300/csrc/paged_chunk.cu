@@ -35,8 +35,8 @@ constexpr int TK = 128;
 constexpr int ST = 2;                     // K tiles and V tiles in flight
 constexpr int BLK = 16384;                // 128 rows x 128 bytes
 
-enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VRDY = 6, B_VEMPTY = 8, B_SFULL = 10, B_PFULL = 12, B_QRDY = 14,
-       B_OFIN = 16, N_BAR = 17 };
+enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VRDY = 6, B_VEMPTY = 8, B_SFULL = 10, B_QRDY = 12, B_PV = 14,
+       B_PFULL = 16 /* tile, half */, B_OFIN = 20 };
 
 constexpr int NQ = 2, ROWS = 128 * NQ;               // row tiles and rows of a CTA
 constexpr int W_MMA = 4 * NQ, W_K = W_MMA + 1, W_V = W_MMA + 2;  // W_MMA + 3: the guard
@@ -127,7 +127,9 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       mbar_init(bar(B_VRDY + s), 1);
       mbar_init(bar(B_VEMPTY + s), 1);
       mbar_init(bar(B_SFULL + s), 1);
-      mbar_init(bar(B_PFULL + s), 4);
+      mbar_init(bar(B_PV + s), 1);
+      mbar_init(bar(B_PFULL + 2 * s), 4);
+      mbar_init(bar(B_PFULL + 2 * s + 1), 4);
       mbar_init(bar(B_QRDY + s), 4);
     }
     mbar_init(bar(B_OFIN), 1);
@@ -181,12 +183,13 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       const uint32_t tS = tbase + 128 * i + lrow, tO = tbase + 128 * NQ + D * i + lrow;
       float m_run = has ? -INFINITY : 0.0f, l_run = 0.0f;
       const uint64_t SL = f2pack(sl2, sl2);
-      // Where some row's maximum has grown by more than 2^kTau: raises every row of
-      // the warp to its own, and O with it (S of this tile being complete, the
-      // P V before it is too).  -inf - -inf and inf - inf are NaN and compare
-      // false: a row that has seen nothing, or an infinity, stays as it is.
-      auto raise = [&](float mt, bool rescale) -> bool {
-        if (!__any_sync(0xFFFFFFFFu, (mt - m_run) * sl2 > Elem<T>::kTau)) return false;
+      // Whether some row's maximum has grown by more than 2^kTau (-inf - -inf and
+      // inf - inf are NaN and compare false: a row that has seen nothing, or an
+      // infinity, stays as it is)
+      auto grown = [&](float mt) -> bool { return __any_sync(0xFFFFFFFFu, (mt - m_run) * sl2 > Elem<T>::kTau); };
+      // Raises every row of the warp to its own maximum, and O with it (the P V
+      // before it are complete)
+      auto raise = [&](float mt, bool rescale) {
         const float alpha = mt > m_run ? ex2f((m_run - mt) * sl2) : 1.0f;
         m_run = fmaxf(m_run, mt);
         l_run *= alpha;
@@ -200,7 +203,6 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
             tmem_st16(tO + cb * 16, t);
           }
         }
-        return true;
       };
       bool ok = true;
       for (int jt = 0; jt < n; ++jt) {
@@ -208,7 +210,6 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
         tc_fence_after();
         const int j0 = tile_at(tl, t0 + jt) * TK;
         const bool open = __all_sync(0xFFFFFFFFu, !has || (j0 + TK <= sp.hi && (j0 >= sp.lo || j0 + TK <= a.sinks)));
-        uint32_t pk[64];
         // Which keys of each 32-key block this row sees; a warp whose rows all
         // see a whole block, or none of it, takes it without the selection.
         enum { kNone, kSome, kAll };
@@ -221,46 +222,6 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
         auto select = [&](uint32_t (&w)[32], uint32_t see) {
 #pragma unroll
           for (int e = 0; e < 32; ++e) w[e] = (see >> e) & 1 ? w[e] : 0xFF800000u;
-        };
-        // one pass over S: P and its sum against m_run; returns the tile's maximum
-        auto pass = [&](auto masked, float& total) -> float {
-          const float mb = m_run == -INFINITY ? 0.0f : m_run * sl2;
-          const uint64_t MB = f2pack(-mb, -mb);
-          uint64_t sum = f2pack(0.0f, 0.0f);
-          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          uint32_t v[2][32];
-          tmem_ld32_start(tS, v[0]);
-#pragma unroll
-          for (int blk = 0; blk < 4; ++blk) {
-            uint32_t (&w)[32] = v[blk & 1];
-            tmem_ld32_wait(w);
-            if (blk < 3) tmem_ld32_start(tS + 32 * (blk + 1), v[(blk + 1) & 1]);
-            if (masked) {
-              uint32_t see;
-              const int kind = seen(blk, see);
-              if (kind == kNone) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) pk[16 * blk + e] = 0u;
-                continue;
-              }
-              if (kind == kSome) select(w, see);
-            }
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const float s0 = __uint_as_float(w[e]), s1 = __uint_as_float(w[e + 1]);
-              m4[(e >> 1) & 3] = fmax3f(m4[(e >> 1) & 3], s0, s1);
-              float x, y;
-              f2unpack(fma2(f2pack(s0, s1), SL, MB), x, y);
-              x = ex2f(x);
-              y = ex2f(y);
-              sum = add2(sum, f2pack(x, y));
-              pk[16 * blk + (e >> 1)] = Elem<T>::pack(x, y);
-            }
-          }
-          float sx, sy;
-          f2unpack(sum, sx, sy);
-          total = sx + sy;
-          return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
         };
         // where a row has no maximum yet, the tile's comes first
         if (__any_sync(0xFFFFFFFFu, m_run == -INFINITY)) {
@@ -280,18 +241,86 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
               for (int e = 0; e < 32; e += 2) mt = fmax3f(mt, __uint_as_float(w[e]), __uint_as_float(w[e + 1]));
             }
           }
-          raise(mt, jt > 0);
+          if (grown(mt)) raise(mt, jt > 0);
         }
-        float total;
-        while (raise(open ? pass(std::false_type{}, total) : pass(std::true_type{}, total), jt > 0)) {
-        }
-        l_run += total;
+        // One pass over S in two halves of 64 keys, each handed on as soon as it is
+        // done: P against m_run, its sum, and the half's own maximum beside it.
+        uint32_t pk[32];
+        float m4[4];
+        uint64_t sum, MB;
+        auto begin_half = [&]() {
+          const float mb = m_run == -INFINITY ? 0.0f : m_run * sl2;
+          MB = f2pack(-mb, -mb);
+          sum = f2pack(0.0f, 0.0f);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) tmem_st16(tS + 16 * w, *reinterpret_cast<uint32_t(*)[16]>(pk + 16 * w));
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_PFULL + i));
+          for (int e = 0; e < 4; ++e) m4[e] = -INFINITY;
+        };
+        auto block = [&](auto masked, int blk, uint32_t (&w)[32]) {
+          if (masked) {
+            uint32_t see;
+            const int kind = seen(blk, see);
+            if (kind == kNone) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) pk[16 * (blk & 1) + e] = 0u;
+              return;
+            }
+            if (kind == kSome) select(w, see);
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float s0 = __uint_as_float(w[e]), s1 = __uint_as_float(w[e + 1]);
+            m4[(e >> 1) & 3] = fmax3f(m4[(e >> 1) & 3], s0, s1);
+            float x, y;
+            f2unpack(fma2(f2pack(s0, s1), SL, MB), x, y);
+            x = ex2f(x);
+            y = ex2f(y);
+            sum = add2(sum, f2pack(x, y));
+            pk[16 * (blk & 1) + (e >> 1)] = Elem<T>::pack(x, y);
+          }
+        };
+        auto pass = [&](auto masked) {
+          uint32_t v[2][32];
+          tmem_ld32_start(tS, v[0]);
+#pragma unroll
+          for (int blk = 0; blk < 4; ++blk) {
+            tmem_ld32_wait(v[blk & 1]);
+            if (blk < 3) tmem_ld32_start(tS + 32 * (blk + 1), v[(blk + 1) & 1]);
+            if ((blk & 1) == 0) begin_half();
+            block(masked, blk, v[blk & 1]);
+            if ((blk & 1) == 0) continue;
+            const int half = blk >> 1;
+            const float mt = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            if (grown(mt)) {
+              // again against the new maximum; the first half's P V has to be in O
+              // before O is scaled for the second's
+              if (half == 1) {
+                if (!(ok = wait_all(B_PV + i, jt & 1))) return;
+                tc_fence_after();
+              }
+              raise(mt, half == 1 || jt > 0);
+              begin_half();
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                uint32_t u[32];
+                tmem_ld32_start(tS + 64 * half + 32 * k, u);
+                tmem_ld32_wait(u);
+                block(std::true_type{}, 2 * half + k, u);
+              }
+            }
+            float sx, sy;
+            f2unpack(sum, sx, sy);
+            l_run += sx + sy;
+            tmem_st16(tS + 32 * half, *reinterpret_cast<uint32_t(*)[16]>(pk));
+            tmem_st16(tS + 32 * half + 16, *reinterpret_cast<uint32_t(*)[16]>(pk + 16));
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(B_PFULL + 2 * i + half));
+          }
+        };
+        if (open) pass(std::false_type{});
+        else pass(std::true_type{});
+        if (!ok) break;
       }
       if (ok && n > 0) ok = wait_all(B_OFIN, 0);
       if (!ok) s_err = 1;
@@ -371,7 +400,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
     }
   } else if (warp == W_MMA) {
     // ------------------------------------------------------------ MMA issue
-    // Order per K/V tile j: P0 V(j), S0(j+1), P1 V(j), S1(j+1); S_i(j+1) may
+    // Order per K/V tile j: P0 V(j) in two halves, S0(j+1), P1 V(j), S1(j+1); S_i(j+1) may
     // overwrite P_i(j) because the MMAs of one thread run in issue order.
     const uint32_t e = elect_one();
     const uint64_t dQ = desc_sw128(smem_u32(sm + L::Q)), dK = desc_sw128(smem_u32(sm + L::K));
@@ -401,12 +430,17 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
         const int s = jt & 1;
         if (!(ok = wait_all(B_VRDY + s, (jt >> 1) & 1))) break;
         for (int i = 0; i < nqt; ++i) {
-          if (!(ok = wait_all(B_PFULL + i, jt & 1))) break;
-          tc_fence_after();
 #pragma unroll
-          for (int ks = 0; ks < TK / 16; ++ks)
-            umma_ts_e(tbase + 128 * NQ + D * i, tbase + 128 * i + 8 * ks, dV + off(s * NB * BLK + ks * 2048), idPV,
-                      (jt | ks) != 0, e);
+          for (int half = 0; half < 2 && ok; ++half) {
+            if (!(ok = wait_all(B_PFULL + 2 * i + half, jt & 1))) break;
+            tc_fence_after();
+#pragma unroll
+            for (int ks = 4 * half; ks < 4 * half + 4; ++ks)
+              umma_ts_e(tbase + 128 * NQ + D * i, tbase + 128 * i + 8 * ks, dV + off(s * NB * BLK + ks * 2048), idPV,
+                        (jt | ks) != 0, e);
+            if (half == 0) commit_e(bar(B_PV + i), e);
+          }
+          if (!ok) break;
           if (i == nqt - 1) commit_e(bar(B_VEMPTY + s), e);
           if (jt + 1 < n && !(ok = issue_S(i, jt + 1))) break;
         }

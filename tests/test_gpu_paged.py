@@ -351,3 +351,32 @@ def test_step_over_many_sequences(D, dtype, Hq, Hk, new):
         q = int(torch.randint(0 if i % 7 == 3 else 1, new + 1, (1,), generator=g))
         lens.append((q, max(q, int(torch.randint(0, [5, 70, 700, 1800][i % 4], (1,), generator=g)))))
     run_case(300 + D, lens, Hq, Hk, D, dtype, 16, 1, 600, 9)
+
+
+@pytest.mark.parametrize("new", [3, 150])
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 64)])
+@pytest.mark.parametrize("order", ["rising", "falling", "peak late", "waves"])
+def test_running_maxima_that_move(new, dtype, D, order):
+    """Logits along one direction whose maximum moves by far more than a tile's
+    probabilities span, up, down and in the middle of a tile, for some rows only."""
+    kv, page = 700, 16
+    lens = [(new, kv)]
+    q, keys, values, pages, table = make_case(61, lens, 2, 1, D, dtype, page)
+    j = torch.arange(kv, dtype=torch.float32)
+    a = {"rising": j / 4, "falling": (kv - j) / 4, "peak late": 100 * ((j % 256) == 200) + 80 * (j == 610) + 0 * j,
+         "waves": 60 * torch.sin(j / 37) + j / 20}[order]
+    keys[0] = 0.05 * keys[0].float()
+    keys[0][:, 0, 5] = a                                       # the direction is one channel
+    keys[0] = keys[0].to(dtype)
+    q = 0.2 * q.float()
+    q[:, 0, 5] = torch.linspace(-1, 1, q.shape[0])             # some rows climb, some descend
+    q[:, 1, 5] = 1.0
+    q = q.to(dtype)
+    for i in range((kv + page - 1) // page):
+        n = min(page, kv - i * page)
+        pages[int(table[0, i]), 0, :, :n] = keys[0][i * page:i * page + n].permute(1, 0, 2)
+    cache, batch = build(lens, 1, D, dtype, page, pages, table)
+    want = attend64(q, keys, values, lens, 1, 0, 0, scale=1.0)
+    for ws in (None, qwm.paged_attend_workspace(cache, batch, 2)):
+        out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), sm_scale=1.0, want_lse=True, workspace=ws)
+        compare(out, lse, want)
