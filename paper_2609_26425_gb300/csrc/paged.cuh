@@ -52,13 +52,13 @@ struct PagedArgs {
   int32_t* status;
   uint64_t wait_ns;
   int32_t idle;                          // nonzero: the producers load nothing (test hook)
-  // split along the keys: chunk: at most nsplit parts of a group, of at least
+  // split along the keys.  chunk: at most nsplit parts of a group, of at least
   // min_tiles tiles; step: nsplit CTAs share the line of all tiles, at least
   // min_tiles places each.  nsplit 1: no split
   int32_t nsplit, min_tiles;
-  float* part_o;                         // [group][nsplit], a part's rows x D floats
-  float2* part_ml;                       // [group][nsplit][rows] running (max, sum)
-  int32_t* counter;                      // [group], zero between calls
+  float* part_o;                         // chunk [group][nsplit][D / 4][row][4]; step [CTA][2][row][D]
+  float2* part_ml;                       // running (max, sum): chunk [group][nsplit][row]; step [CTA][2][row]
+  int32_t* counter;                      // step: [group], zero between calls
 };
 
 // Launch shape of an attention call: which kernel, and its split.

@@ -16,6 +16,11 @@
 // maximum is formed beside it.  Where it is above the known one by more than
 // 2^kTau the pass is repeated against the new one; P, l and O are floating-point
 // multiples of the same power, so nothing is lost below that.
+// Few rows over many keys are split along the keys; the parts' O, m and l go
+// through global memory to a second kernel over all SMs, launched ahead so that
+// it stands ready.  (A join by a group's last CTA took 11 us of 69 at 880 Queries
+// x 12 heads: one SM reads 384 KB at 42 bytes a cycle.  Parts as clusters joined
+// through shared memory: 46 clusters of 3 fit where 48 were wanted, 97 us.)
 // Warps: four per row tile softmax, then MMA issue, a TMA producer each for K and
 // V (a 16-token page is a copy of 2 KB: one warp's issue rate would bound the
 // tile), and the Values' guard.
@@ -90,7 +95,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   __shared__ uint32_t s_tmem;
-  __shared__ int s_err, s_poison, s_last;
+  __shared__ int s_err, s_poison;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int b = blockIdx.z, hk = blockIdx.y;
@@ -112,6 +117,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   const Tiles tl = make_tiles<TK>(p0 + tokA, p0 + tokB, sq.kv, a.block, a.window, a.sinks);
   const int per = max((tl.n + a.nsplit - 1) / a.nsplit, a.min_tiles);
   const int parts = max(1, (tl.n + per - 1) / per);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (part >= parts) return;
   const int t0 = part * per, n = max(0, min(tl.n, t0 + per) - t0);   // this part's tiles: t0 .. t0 + n - 1
 
@@ -557,91 +563,98 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   }
 
   tc_fence_before();
-  if (parts > 1) __threadfence();
   __syncthreads();
   if (warp == W_MMA) {
     tc_fence_after();
     tmem_dealloc(tbase, 512);
   }
   if (tid == 0 && s_err) record_status(a.status, QWM_ERR_TIMEOUT);
-  if (parts == 1) return;
-  // the part that arrives last joins all of them, in part order
+}
+
+// The parts of the groups that were cut, in part order: m = max m_p, l = sum l_p
+// 2^((m_p - m) c), O = sum O_p 2^((m_p - m) c) / l.  A CTA takes 64 rows, a warp 8
+// of them; lanes 8 rows x 4 groups of 8 channels, so that reads (a part lies
+// [channels / 4][row]) and writes are whole sectors.
+constexpr int JR = 64;
+template <typename T, int D>
+__global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int b = blockIdx.z, hk = blockIdx.y, rt = blockIdx.x / (ROWS / JR);
+  const int rtiles = gridDim.x / (ROWS / JR);
+  Seq sq;
+  load_seq(a, b, sq);
+  const int64_t rows = (int64_t)sq.qn * a.G, r0 = (int64_t)rt * ROWS;
+  if (r0 >= rows) return;
+  const int nrow = (int)min((int64_t)ROWS, rows - r0);
+  const int tokA = (int)(r0 / a.G), p0 = sq.kv - sq.qn;
+  const uint32_t G = (uint32_t)a.G, remA = (uint32_t)(r0 - (int64_t)tokA * a.G);
+  const int tokB = tokA + (int)((remA + (uint32_t)nrow - 1) / G);
+  const Tiles tl = make_tiles<TK>(p0 + tokA, p0 + tokB, sq.kv, a.block, a.window, a.sinks);
+  const int per = max((tl.n + a.nsplit - 1) / a.nsplit, a.min_tiles);
+  const int parts = max(1, (tl.n + per - 1) / per);
+  const int lane = threadIdx.x & 31;
+  const int r = (blockIdx.x % (ROWS / JR)) * JR + (threadIdx.x >> 5) * 8 + (lane & 7);
+  if (parts == 1 || r >= nrow) return;
   const int64_t group = ((int64_t)b * a.Hk + hk) * rtiles + rt;
-  if (tid == 0) s_last = atomicAdd(a.counter + group, 1) == parts - 1;
-  __syncthreads();
-  if (!s_last) return;
-  __threadfence();
-  // a part's weight in each row, 2^((m_p - m) c) / l, in the ring's place
-  float* wgt = reinterpret_cast<float*>(sm);           // [part][ROWS]
-  const float2* ml = a.part_ml + group * a.nsplit * ROWS;
-  for (int r = tid; r < nrow; r += NT) {
-    float m = -INFINITY, l = 0.0f;
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, __ldcg(&ml[p * ROWS + r].x));
-    const float ref = m == -INFINITY ? 0.0f : m;
-    for (int p = 0; p < parts; ++p) {
-      const float2 x = __ldcg(&ml[p * ROWS + r]);
-      const float f = ex2f((x.x - ref) * sl2);
-      wgt[p * ROWS + r] = f;
-      l = fmaf(x.y, f, l);
+  const float2* ml = a.part_ml + group * a.nsplit * ROWS + r;
+  const float4* po = reinterpret_cast<const float4*>(a.part_o) + group * a.nsplit * ROWS * (D / 4) + r;
+  const float sl2 = a.scale * 1.4426950408889634f;
+  constexpr int CB = D / 32, PU = 4;                  // channel blocks of a lane, parts in flight
+  float m = -INFINITY, l = 0.0f;
+  float4 v[CB][2];
+#pragma unroll
+  for (int k = 0; k < CB; ++k) v[k][0] = v[k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int pb = 0; pb < parts; pb += PU) {
+    float2 w[PU];
+    float4 x[PU][CB][2];
+#pragma unroll
+    for (int u = 0; u < PU; ++u) {
+      const int p = min(pb + u, parts - 1);
+      w[u] = __ldcg(ml + p * ROWS);
+      if (pb + u >= parts) w[u] = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+      for (int k = 0; k < CB; ++k) {
+        const float4* src = po + ((int64_t)p * (D / 4) + 2 * (4 * k + (lane >> 3))) * ROWS;
+        x[u][k][0] = __ldcg(src);
+        x[u][k][1] = __ldcg(src + ROWS);
+      }
     }
-    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    for (int p = 0; p < parts; ++p) wgt[p * ROWS + r] *= inv;
-    if (a.lse) {
-      const int tok = tokA + (int)((remA + r) / G), head = hk * a.G + (int)((remA + r) % G);
-      a.lse[(int64_t)head * a.N + sq.q0 + tok] = m == -INFINITY ? -INFINITY : m * a.scale + logf(l);
-    }
-  }
-  __syncthreads();
-  // eight channels of a row per item; two items and four parts of them in
-  // flight per thread (48 to 96 KB an SM: one SM reads a group's parts)
-  constexpr int IT = 2, PU = 4, items = ROWS * (D / 8);
-  const float4* po = reinterpret_cast<const float4*>(a.part_o) + group * a.nsplit * ROWS * (D / 4);
-  for (int i0 = tid; i0 < items; i0 += IT * NT) {
-    float4 v[IT][2];
+    float mn = m;
 #pragma unroll
-    for (int k = 0; k < IT; ++k) v[k][0] = v[k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int pb = 0; pb < parts; pb += PU) {
-      float4 x[PU][IT][2];
-      float f[PU][IT];
+    for (int u = 0; u < PU; ++u) mn = fmaxf(mn, w[u].x);
+    const float ref = mn == -INFINITY ? 0.0f : mn;
+    const float al = ex2f((m - ref) * sl2);
+    m = mn;
+    l *= al;
 #pragma unroll
-      for (int u = 0; u < PU; ++u)
+    for (int k = 0; k < CB; ++k)
 #pragma unroll
-        for (int k = 0; k < IT; ++k) {
-          const int idx = i0 + k * NT, r = idx % ROWS, c8 = idx / ROWS, p = pb + u;
-          if (p < parts && idx < items && r < nrow) {
-            const float4* src = po + ((int64_t)p * (D / 4) + 2 * c8) * ROWS + r;
-            x[u][k][0] = __ldcg(src);
-            x[u][k][1] = __ldcg(src + ROWS);
-            f[u][k] = wgt[p * ROWS + r];
-          } else {
-            x[u][k][0] = x[u][k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-            f[u][k] = 0.0f;
-          }
+      for (int h = 0; h < 2; ++h) {
+        v[k][h].x *= al; v[k][h].y *= al; v[k][h].z *= al; v[k][h].w *= al;
+      }
+#pragma unroll
+    for (int u = 0; u < PU; ++u) {
+      if (pb + u >= parts) break;
+      const float f = ex2f((w[u].x - ref) * sl2);
+      l = fmaf(w[u].y, f, l);
+#pragma unroll
+      for (int k = 0; k < CB; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          v[k][h].x = fmaf(x[u][k][h].x, f, v[k][h].x); v[k][h].y = fmaf(x[u][k][h].y, f, v[k][h].y);
+          v[k][h].z = fmaf(x[u][k][h].z, f, v[k][h].z); v[k][h].w = fmaf(x[u][k][h].w, f, v[k][h].w);
         }
-#pragma unroll
-      for (int u = 0; u < PU; ++u)
-#pragma unroll
-        for (int k = 0; k < IT; ++k)
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            v[k][w].x = fmaf(x[u][k][w].x, f[u][k], v[k][w].x);
-            v[k][w].y = fmaf(x[u][k][w].y, f[u][k], v[k][w].y);
-            v[k][w].z = fmaf(x[u][k][w].z, f[u][k], v[k][w].z);
-            v[k][w].w = fmaf(x[u][k][w].w, f[u][k], v[k][w].w);
-          }
-    }
-#pragma unroll
-    for (int k = 0; k < IT; ++k) {
-      const int idx = i0 + k * NT, row = idx % ROWS, c8 = idx / ROWS;
-      if (idx >= items || row >= nrow) continue;
-      const uint32_t r = remA + row;
-      *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + (sq.q0 + tokA + r / G) * a.o_tok +
-                                (int64_t)(hk * a.G + (int)(r % G)) * a.o_head + 8 * c8) =
-          make_uint4(Elem<T>::pack(v[k][0].x, v[k][0].y), Elem<T>::pack(v[k][0].z, v[k][0].w),
-                     Elem<T>::pack(v[k][1].x, v[k][1].y), Elem<T>::pack(v[k][1].z, v[k][1].w));
     }
   }
-  if (tid == 0) a.counter[group] = 0;
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+  const int tok = tokA + (int)((remA + r) / G), head = hk * a.G + (int)((remA + r) % G);
+  T* dst = static_cast<T*>(a.out) + (sq.q0 + tok) * a.o_tok + (int64_t)head * a.o_head + 8 * (lane >> 3);
+#pragma unroll
+  for (int k = 0; k < CB; ++k)
+    *reinterpret_cast<uint4*>(dst + 32 * k) =
+        make_uint4(Elem<T>::pack(v[k][0].x * inv, v[k][0].y * inv), Elem<T>::pack(v[k][0].z * inv, v[k][0].w * inv),
+                   Elem<T>::pack(v[k][1].x * inv, v[k][1].y * inv), Elem<T>::pack(v[k][1].z * inv, v[k][1].w * inv));
+  if (a.lse && lane < 8) a.lse[(int64_t)head * a.N + sq.q0 + tok] = m == -INFINITY ? -INFINITY : m * a.scale + logf(l);
 }
 
 template <typename T, int D>
@@ -651,7 +664,20 @@ cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   const int64_t rtiles = ((int64_t)a.max_q * a.G + ROWS - 1) / ROWS;
   paged_chunk<T, D><<<dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), NT, Smem<D>::TOTAL, s>>>(map, a);
-  return cudaGetLastError();
+  e = cudaGetLastError();
+  if (e != cudaSuccess || a.nsplit == 1) return e;
+  // the join may be set up while the parts run; it waits for all of them
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(rtiles * (ROWS / JR)), a.Hk, a.B);
+  cfg.blockDim = dim3(256);
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, paged_join<T, D>, a);
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
@@ -666,10 +692,10 @@ PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, 
   const int64_t tiles = (max_visible + TK - 1) / TK + 2;
   if (split) {
     // the split with the least waves x (tiles of a part + a CTA's fixed cost,
-    // about 6 tiles' time with the join); parts of at least 4 tiles
+    // about 6 tiles' time), 4 more for the join; parts of at least 4 tiles
     int64_t best = 0;
     for (int64_t n = 1; n <= 64 && n * p.min_tiles <= tiles + p.min_tiles - 1; ++n) {
-      const int64_t waves = (p.groups * n + nsm - 1) / nsm, cost = waves * ((tiles + n - 1) / n + 6);
+      const int64_t waves = (p.groups * n + nsm - 1) / nsm, cost = waves * ((tiles + n - 1) / n + 6) + (n > 1 ? 4 : 0);
       if (n == 1 || cost < best) {
         best = cost;
         p.nsplit = (int)n;
