@@ -136,9 +136,10 @@ __device__ __forceinline__ Span row_span(int p, int kv, int block, int window) {
 }
 
 // What the rows of tokens p0 <= p <= p1 of a sequence see together, as a list
-// of tiles of TK keys: the window's, then tiles that hold first tokens before
-// it (few keys: taken first they would give the running maxima a poor start).
-// lo and hi of a row grow with its token, so the first and the last row bound
+// of tiles of TK keys: the window's from its second tile on, its first tile (cut
+// by the rows' windows), then tiles that hold first tokens before it (few keys).
+// The first tile taken gives the running maxima their start, so it is one that
+// the rows see whole where there is such a tile.  lo and hi of a row grow with its token, so the first and the last row bound
 // all.
 struct Tiles {
   int32_t lo_min, lo_max, hi_min, hi_max;  // over the rows; a row with p < 0 has hi = 0
@@ -160,7 +161,7 @@ __device__ __forceinline__ Tiles make_tiles(int p0, int p1, int kv, int block, i
   return t;
 }
 __device__ __forceinline__ int tile_at(const Tiles& t, int i) {
-  return i < t.n_win ? t.w_start + i : i - t.n_win;
+  return i < t.n_win ? t.w_start + (i + 1 < t.n_win ? i + 1 : 0) : i - t.n_win;
 }
 __device__ __forceinline__ bool sees(int j, int lo, int hi, int sinks) { return j < hi && (j >= lo || j < sinks); }
 // Whether some row of the tiles sees a token of [j0, j1).

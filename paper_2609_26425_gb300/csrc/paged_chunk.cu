@@ -98,6 +98,25 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   __shared__ int s_err, s_poison;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  auto bar = [&](int i) { return smem_u32(sm + L::BAR) + 8u * i; };
+  if (tid == 0) {
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(bar(B_KFULL + s), 1);
+      mbar_init(bar(B_KEMPTY + s), 1);
+      mbar_init(bar(B_VFULL + s), 1);
+      mbar_init(bar(B_VRDY + s), 1);
+      mbar_init(bar(B_VEMPTY + s), 1);
+      mbar_init(bar(B_SFULL + s), 1);
+      mbar_init(bar(B_PV + s), 1);
+      mbar_init(bar(B_PFULL + 2 * s), 4);
+      mbar_init(bar(B_PFULL + 2 * s + 1), 4);
+      mbar_init(bar(B_QRDY + s), 4);
+    }
+    mbar_init(bar(B_OFIN), 1);
+    s_err = 0;
+    s_poison = 0;
+    fence_mbar_init();
+  }
   const int b = blockIdx.z, hk = blockIdx.y;
   const int rtiles = gridDim.x / a.nsplit;
   // the row tiles with the most keys first
@@ -121,28 +140,9 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   if (part >= parts) return;
   const int t0 = part * per, n = max(0, min(tl.n, t0 + per) - t0);   // this part's tiles: t0 .. t0 + n - 1
 
-  auto bar = [&](int i) { return smem_u32(sm + L::BAR) + 8u * i; };
   auto wait_all = [&](int i, uint32_t ph) -> bool {
     return __all_sync(0xFFFFFFFFu, mbar_wait(bar(i), ph, a.wait_ns));
   };
-  if (tid == 0) {
-    for (int s = 0; s < 2; ++s) {
-      mbar_init(bar(B_KFULL + s), 1);
-      mbar_init(bar(B_KEMPTY + s), 1);
-      mbar_init(bar(B_VFULL + s), 1);
-      mbar_init(bar(B_VRDY + s), 1);
-      mbar_init(bar(B_VEMPTY + s), 1);
-      mbar_init(bar(B_SFULL + s), 1);
-      mbar_init(bar(B_PV + s), 1);
-      mbar_init(bar(B_PFULL + 2 * s), 4);
-      mbar_init(bar(B_PFULL + 2 * s + 1), 4);
-      mbar_init(bar(B_QRDY + s), 4);
-    }
-    mbar_init(bar(B_OFIN), 1);
-    s_err = 0;
-    s_poison = 0;
-    fence_mbar_init();
-  }
   if (warp == W_MMA) {
     tmem_alloc(smem_u32(&s_tmem), 512);
     tmem_relinquish();
@@ -160,19 +160,18 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       // Q_i: each warp its 32 rows, a row's 16-byte chunks over neighbouring lanes
       uint8_t* sQ = sm + L::Q + i * NB * BLK;
       constexpr int CH = D / 8;
-#pragma unroll 1
-      for (int i0 = 0; i0 < CH; i0 += 8) {
-        uint4 v[8];
+      {
+        uint4 v[CH];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int idx = (i0 + k) * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
+        for (int k = 0; k < CH; ++k) {
+          const int idx = k * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
           const uint32_t r = remA + min(i * 128 + rr, nrow - 1);
           v[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (sq.q0 + tokA + r / G) * a.q_tok +
                                                  (hk * a.G + (int)(r % G)) * a.q_head + c * 8);
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int idx = (i0 + k) * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
+        for (int k = 0; k < CH; ++k) {
+          const int idx = k * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
           if (i * 128 + rr >= nrow) v[k] = make_uint4(0, 0, 0, 0);
           *reinterpret_cast<uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[k];
         }
