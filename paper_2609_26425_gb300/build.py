@@ -10,12 +10,14 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT, "libqwm.so")
+BINDING = os.path.join(OUT, "qwm_binding.so")  # csrc/binding.cpp, against PyTorch's headers
 SOURCES = ["qwm_api.cu", "append.cu", "append_fused.cu", "append_fused_r8.cu", "append_fused_r16.cu",
            "append_fused_r32.cu", "append_generic.cu", "append_full.cu", "attend.cu", "fit.cu", "qstats.cu",
            "metrics.cu", "rope.cu", "paged_api.cu", "paged_step.cu", "paged_chunk.cu"]
@@ -41,9 +43,9 @@ def _deps():
 
 
 def up_to_date() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(BINDING):
         return False
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
     return all(os.path.getmtime(f) <= t for f in _deps())
 
 
@@ -64,14 +66,36 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
             sys.stderr.write(r.stderr)
         return obj
 
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    def compile_binding():
+        import torch  # headers and library paths only
+        inc = [os.path.join(os.path.dirname(torch.__file__), "include"), sysconfig.get_paths()["include"],
+               os.path.join(os.path.dirname(os.path.realpath(cc)), "..", "include")]
+        obj = os.path.join(OUT, "binding.o")
+        cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden",
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *("-I" + i for i in inc), "-c",
+               os.path.join(CSRC, "binding.cpp"), "-o", obj]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"g++ failed for binding.cpp:\n{r.stderr}")
+        return obj, os.path.join(os.path.dirname(torch.__file__), "lib")
+
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        bound = ex.submit(compile_binding)
         objs = list(ex.map(compile_one, SOURCES))
+        bobj, torch_lib = bound.result()
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [cc, *ARCH, "-shared", "--cudart", "static", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, LIB)
+    tmp = BINDING + f".tmp{os.getpid()}"
+    cmd = ["g++", "-shared", "-o", tmp, bobj, "-L" + OUT, "-lqwm", "-Wl,-rpath,$ORIGIN", "-L" + torch_lib,
+           "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath," + torch_lib]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link failed:\n{r.stderr}")
+    os.replace(tmp, BINDING)
     return LIB
 
 

@@ -1,16 +1,19 @@
 """Rotary positions over three axes and the uncompressed, paged side of the
 cache (binding of the qwm_rope* and qwm_paged* entry points of include/qwm.h).
 
-Like the rest of the binding this only marshals arguments: it checks dtypes,
-shapes, strides and devices, passes device pointers and the current stream, and
-uses PyTorch for device memory.  ``Rope`` holds a rotation's frequencies,
-``PagedCache`` the pages, ``PagedBatch`` the sequences of a step; the calls are
-qwm_rope, qwm_rope_backward, qwm_paged_append and qwm_paged_attend.
+``Rope`` holds a rotation's frequencies, ``PagedCache`` the pages, ``PagedBatch``
+the sequences of a step; the calls are qwm_rope, qwm_rope_backward,
+qwm_paged_append and qwm_paged_attend.  Like the rest of the binding these only
+marshal arguments (dtypes, shapes, strides and devices are checked, PyTorch is
+used for device memory); they go through the compiled csrc/binding.cpp, because
+a call for a single token is as long as its binding.
 """
 from __future__ import annotations
 
 import ctypes as ct
+import importlib.util
 import math
+import os
 
 import torch
 
@@ -79,40 +82,34 @@ def _lib():
     return _C
 
 
+_B = None  # csrc/binding.cpp
+
+
+def binding():
+    """Load the compiled binding (raises if it has not been built)."""
+    global _B
+    if _B is None:
+        from . import LIB_PATH, QwmError
+        _lib()
+        path = os.path.join(os.path.dirname(LIB_PATH), "qwm_binding.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'`")
+        spec = importlib.util.spec_from_file_location("qwm_binding", path)
+        mod = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(mod)
+        mod.set_error(QwmError)
+        _B = mod
+    return _B
+
+
 def _check(fn, st):
     if st:
         from . import QwmError
         raise QwmError(fn, st)
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream  # current stream of a device, without a Stream object
-
-
-def _rows(t, dtype, name, tokens=None, head_dim=None):
-    """A [tokens][heads][head_dim] tensor as qwm_rows (any strides of tokens and heads)."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype):
-        raise ValueError(f"{name} must be a {dtype} CUDA tensor")
-    shape = t.shape
-    if len(shape) != 3 or (tokens is not None and shape[0] != tokens) or (
-            head_dim is not None and shape[2] != head_dim):
-        raise ValueError(f"{name} has shape {tuple(shape)}, expected ({tokens}, heads, {head_dim})")
-    st, sh, sc = t.stride()
-    if sc != 1:
-        raise ValueError(f"{name} must have contiguous channels")
-    n, h, _ = shape  # the stride of a dimension of one is never used
-    return QwmRows(t.data_ptr(), st if n > 1 else 0, sh if h > 1 else 0, h)
-
-
-def _out(like, out, name):
-    """An output with the shape and dtype of `like`: the caller's, or a new contiguous tensor."""
-    if out is None:
-        out = torch.empty_like(like) if like.is_contiguous() else torch.empty(like.shape, dtype=like.dtype,
-                                                                              device=like.device)
-        _, h, d = like.shape
-        return out, QwmRows(out.data_ptr(), h * d, d, h)
-    if out.shape != like.shape:
-        raise ValueError(f"{name} has shape {tuple(out.shape)}, expected {tuple(like.shape)}")
-    return out, _rows(out, like.dtype, name)
+def _stream(t):
+    return torch.cuda.current_stream(t.device).cuda_stream
 
 
 def _ints(t, shape, name):
@@ -121,10 +118,6 @@ def _ints(t, shape, name):
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
     return t
-
-
-def _stream(t):
-    return _raw_stream(t.get_device())
 
 
 # ------------------------------------------------------------------ rope
@@ -141,46 +134,18 @@ class Rope:
                 and inv_freq.is_contiguous() and tuple(inv_freq.shape) == (sum(pairs),)):
             raise ValueError(f"inv_freq must be a contiguous fp32 CUDA tensor [{sum(pairs)}]")
         self.inv_freq, self.pairs, self.interleaved = inv_freq, pairs, bool(interleaved)
-        self.freq_ptr = inv_freq.data_ptr()
-        self._cfg = {}
-
-    def config(self, head_dim, dtype):
-        cfg = self._cfg.get((head_dim, dtype))
-        if cfg is None:
-            if dtype not in _DTYPES:
-                raise ValueError("the rotation takes bf16 or fp16 tensors")
-            cfg = QwmRopeConfig(head_dim, _DTYPES[dtype], (ct.c_int32 * 3)(*self.pairs), int(self.interleaved))
-            self._cfg[(head_dim, dtype)] = cfg
-        return cfg
-
-
-def _turn(name, rope, q, pos, k, q_out, k_out):
-    if not isinstance(q, torch.Tensor) or q.dim() != 3:
-        raise ValueError("q must be a [tokens][heads][head_dim] tensor")
-    n, _, d = q.shape
-    cfg = rope.config(d, q.dtype)
-    qr = _rows(q, q.dtype, "q")
-    q_out, qo = _out(q, q_out, "q_out")
-    kr = ko = None
-    if k is not None:
-        kr = _rows(k, q.dtype, "k", n, d)
-        k_out, ko = _out(k, k_out, "k_out")
-    st = getattr(_C or _lib(), name)(cfg, rope.freq_ptr, _ints(pos, (n, 3), "pos").data_ptr(), n, qr, qo, kr, ko,
-                                     _raw_stream(q.get_device()))
-    if st:
-        _check(name, st)
-    return q_out if k is None else (q_out, k_out)
+        self._key = (inv_freq.data_ptr(), *pairs, int(self.interleaved))
 
 
 def qwm_rope(rope: Rope, q, pos, k=None, q_out=None, k_out=None):
     """Queries (and Keys) turned to their positions ``pos`` (int32 [tokens][3]);
     ``q_out=q`` works in place.  Returns q_out, or (q_out, k_out) with Keys."""
-    return _turn("qwm_rope", rope, q, pos, k, q_out, k_out)
+    return (_B or binding()).turn(False, rope._key, q, pos, k, q_out, k_out)
 
 
 def qwm_rope_backward(rope: Rope, dq, pos, dk=None, dq_out=None, dk_out=None):
     """Gradient of qwm_rope: the outputs' gradients turned back."""
-    return _turn("qwm_rope_backward", rope, dq, pos, dk, dq_out, dk_out)
+    return (_B or binding()).turn(True, rope._key, dq, pos, dk, dq_out, dk_out)
 
 
 # ------------------------------------------------------------------ pages
@@ -206,6 +171,7 @@ class PagedCache:
         _check("qwm_paged_init", _lib().qwm_paged_init(ct.byref(h), self.cfg, self.buffer.data_ptr(), n,
                                                       _stream(self.buffer)))
         self.handle = h
+        self._key = (h.value, head_dim, _DTYPES[dtype])
 
     def __del__(self):
         h = getattr(self, "handle", None)
@@ -246,38 +212,22 @@ class PagedBatch:
         self.tensors = (q_offsets, kv_len, page_table)
         self.num_seqs, self.max_q, self.max_kv = B, int(max_q), int(max_kv)
         self.tokens = tokens
-        self._c = {}
+        self._c = QwmPagedBatch(B, page_table.shape[1], self.max_q, self.max_kv, -1 if tokens is None else tokens,
+                                q_offsets.data_ptr(), kv_len.data_ptr(), page_table.data_ptr())
+        self._key = (ct.addressof(self._c), self._c.tokens)
 
     def struct(self, tokens):
-        if self.tokens is not None and tokens != self.tokens:
-            raise ValueError(f"the batch has {self.tokens} rows, the tensor {tokens}")
-        s = self._c.get(tokens)
-        if s is None:
-            q_offsets, kv_len, table = self.tensors
-            s = self._c[tokens] = QwmPagedBatch(self.num_seqs, table.shape[1], self.max_q, self.max_kv, tokens,
-                                                q_offsets.data_ptr(), kv_len.data_ptr(), table.data_ptr())
-        return s
+        """The C descriptor for a call of `tokens` rows."""
+        c = QwmPagedBatch.from_buffer_copy(self._c)
+        c.tokens = tokens
+        return c
 
 
 def qwm_paged_append(cache: PagedCache, batch: PagedBatch, k, v, rope: Rope = None, pos=None, q=None, q_out=None):
     """Store the new tokens' Keys and Values in their pages; with ``rope`` the Keys
     are turned to ``pos`` on the way, and ``q`` is turned beside them.  Returns
     the Queries (a new tensor, or q_out), or None without q."""
-    if not isinstance(k, torch.Tensor) or k.dim() != 3:
-        raise ValueError("k must be a [tokens][heads][head_dim] tensor")
-    n, d, t = k.shape[0], cache.head_dim, cache.dtype
-    kr, vr = _rows(k, t, "k", n, d), _rows(v, t, "v", n, d)
-    cfg = freq = at = qr = qo = None
-    if rope is not None:
-        cfg, freq, at = rope.config(d, t), rope.freq_ptr, _ints(pos, (n, 3), "pos").data_ptr()
-    if q is not None:
-        qr = _rows(q, t, "q", n, d)
-        q_out, qo = _out(q, q_out, "q_out")
-    st = (_C or _lib()).qwm_paged_append(cache.handle, batch.struct(n), kr, vr, cfg, freq, at, qr, qo,
-                                         _raw_stream(k.get_device()))
-    if st:
-        _check("qwm_paged_append", st)
-    return q_out if q is not None else None
+    return (_B or binding()).append(cache._key, batch._key, k, v, None if rope is None else rope._key, pos, q, q_out)
 
 
 def qwm_paged_attend_workspace_bytes(cache: PagedCache, batch: PagedBatch, q_heads, tokens, window=0, sinks=0,
@@ -302,18 +252,5 @@ def qwm_paged_attend(cache: PagedCache, batch: PagedBatch, q, window=0, sinks=0,
     """Attention of the batch's rows over the pages of their sequences: block-causal
     (``block`` tokens a block, 1 = token-causal), the last ``window`` tokens up to
     the end of the row's block (0: all) and the first ``sinks`` tokens."""
-    qr = _rows(q, cache.dtype, "q", None, cache.head_dim)
-    n, h, _ = q.shape
-    out, orows = _out(q, out, "out")
-    if lse is not None:
-        if not (lse.is_cuda and lse.dtype is torch.float32 and lse.is_contiguous() and lse.shape == (h, n)):
-            raise ValueError("lse must be a contiguous fp32 CUDA tensor [heads][tokens]")
-    elif want_lse:
-        lse = torch.empty((h, n), dtype=torch.float32, device=q.device)
-    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
-    st = (_C or _lib()).qwm_paged_attend(
-        cache.handle, batch.struct(n), qr, QwmMask(block, window, sinks), cache.scale if sm_scale is None else sm_scale,
-        orows, None if lse is None else lse.data_ptr(), ws, size, _raw_stream(q.get_device()))
-    if st:
-        _check("qwm_paged_attend", st)
-    return out if lse is None else (out, lse)
+    return (_B or binding()).attend(cache._key, batch._key, q, block, window, sinks,
+                                    cache.scale if sm_scale is None else sm_scale, out, lse, want_lse, workspace)
