@@ -87,6 +87,26 @@ inline cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64]) {
   if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
   return e;
 }
+// A launch that may be set up while the kernel before it on the stream still
+// runs (programmatic dependent launch).  Every thread of the kernel calls
+// grid_begin() before its first access to global memory: it waits for that
+// kernel's end, then lets the next one be set up.  Back to back this hides the
+// launch and the start of a CTA, 1 to 2 us of a short step's 5 to 12.
+template <class... P, class... A>
+inline cudaError_t launch_ahead(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A&&... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
 // Rows (Query tokens x Query heads per cache head) up to which a sequence goes
 // to the step kernel.
 constexpr int kStepRows = 32;
@@ -97,6 +117,11 @@ bool make_page_map(CUtensorMap* m, const void* pages, int64_t blocks, int page_t
 
 // ------------------------------------------------------------ device helpers
 #ifdef __CUDACC__
+
+// See launch_ahead.
+__device__ __forceinline__ void grid_begin() {
+  asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory");
+}
 
 __device__ __forceinline__ void record_status(int32_t* status, int code) {
   if (status) atomicCAS(status, 0, code);

@@ -117,6 +117,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
     s_poison = 0;
     fence_mbar_init();
   }
+  grid_begin();
   const int b = blockIdx.z, hk = blockIdx.y;
   const int rtiles = gridDim.x / a.nsplit;
   // the row tiles with the most keys first
@@ -136,7 +137,6 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   const Tiles tl = make_tiles<TK>(p0 + tokA, p0 + tokB, sq.kv, a.block, a.window, a.sinks);
   const int per = max((tl.n + a.nsplit - 1) / a.nsplit, a.min_tiles);
   const int parts = max(1, (tl.n + per - 1) / per);
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (part >= parts) return;
   const int t0 = part * per, n = max(0, min(tl.n, t0 + per) - t0);   // this part's tiles: t0 .. t0 + n - 1
 
@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
 constexpr int JR = 64;
 template <typename T, int D>
 __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  grid_begin();
   const int b = blockIdx.z, hk = blockIdx.y, rt = blockIdx.x / (ROWS / JR);
   const int rtiles = gridDim.x / (ROWS / JR);
   Seq sq;
@@ -662,21 +662,9 @@ cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   cudaError_t e = allow_smem(paged_chunk<T, D>, Smem<D>::TOTAL, done);
   if (e != cudaSuccess) return e;
   const int64_t rtiles = ((int64_t)a.max_q * a.G + ROWS - 1) / ROWS;
-  paged_chunk<T, D><<<dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), NT, Smem<D>::TOTAL, s>>>(map, a);
-  e = cudaGetLastError();
+  e = launch_ahead(paged_chunk<T, D>, dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), NT, Smem<D>::TOTAL, s, map, a);
   if (e != cudaSuccess || a.nsplit == 1) return e;
-  // the join may be set up while the parts run; it waits for all of them
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(rtiles * (ROWS / JR)), a.Hk, a.B);
-  cfg.blockDim = dim3(256);
-  cfg.stream = s;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, paged_join<T, D>, a);
-  return e != cudaSuccess ? e : cudaGetLastError();
+  return launch_ahead(paged_join<T, D>, dim3((unsigned)(rtiles * (ROWS / JR)), a.Hk, a.B), 256, 0, s, a);
 }
 
 }  // namespace

@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     }
     fence_mbar_init();
   }
+  grid_begin();
   // The line: a group of sequence b takes n(b) + kGroupCost places, its tiles
   // last; sequence b's groups follow those of the sequences before it.  Each
   // thread sums a run of sequences; a scan over the threads gives the total, and
@@ -579,8 +580,7 @@ cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   static bool done[64];
   cudaError_t e = allow_smem(paged_step<T, D, RT>, smem, done);
   if (e != cudaSuccess) return e;
-  paged_step<T, D, RT><<<(unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk), NT, smem, s>>>(map, a);
-  return cudaGetLastError();
+  return launch_ahead(paged_step<T, D, RT>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, map, a);
 }
 template <typename T, int D>
 cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {

@@ -101,6 +101,7 @@ __global__ void __launch_bounds__(NT) rope_kernel(const RopeArgs a, int tokens_p
   const int U = INTERLEAVED ? nvec : nvec - pv;
   const int hpar = NT / U;                         // rows (token, head) side by side
   const int u = tid % U, hl = tid / U;
+  grid_begin();
   if (PAGED && tid < nt) places[tid] = place_of(a, n0 + tid);
   if (a.inv_freq) {
     for (int i = tid; i < nt * P; i += NT) {
@@ -195,9 +196,7 @@ cudaError_t go(const RopeArgs& a, cudaStream_t s) {
   if (tpc < 1) tpc = 1;
   const unsigned grid = (unsigned)((a.N + tpc - 1) / tpc);
   const size_t smem = (size_t)tpc * a.P * sizeof(float2);
-  if (a.pages) rope_kernel<T, IL, true><<<grid, NT, smem, s>>>(a, (int)tpc);
-  else rope_kernel<T, IL, false><<<grid, NT, smem, s>>>(a, (int)tpc);
-  return cudaGetLastError();
+  return launch_ahead(a.pages ? rope_kernel<T, IL, true> : rope_kernel<T, IL, false>, dim3(grid), NT, smem, s, a, (int)tpc);
 }
 
 }  // namespace
