@@ -96,21 +96,24 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   }
   grid_begin();
   // The line: a group of sequence b takes n(b) + kGroupCost places, its tiles
-  // last; sequence b's groups follow those of the sequences before it.  Each
-  // thread sums a run of sequences; a scan over the threads gives the total, and
-  // the thread that holds the place where this CTA's stretch begins looks for
-  // the sequence.  Without a workspace, a CTA takes the group of its number.
+  // last; sequence b's groups follow those of the sequences before it.  A scan
+  // over the sequences gives the total and the sequence in which this CTA's
+  // stretch begins: up to 32 sequences by each warp for itself, more by the CTA,
+  // each thread with a run of sequences.  Without a workspace, a CTA takes the
+  // group of its number.
   const bool split = a.nsplit > 1;
   Seq sq;
   Tiles tl;
   int b, n, hk;
   int64_t x0, x1, g0, share = 0;
   if (split) {
-    const int run = (a.B + NT - 1) / NT, b0 = min(a.B, tid * run), b1 = min(a.B, b0 + run);
+    const bool alone = a.B <= 32;
+    const int who = alone ? lane : tid, run = alone ? 1 : (a.B + NT - 1) / NT;
+    const int b0 = min(a.B, who * run), b1 = min(a.B, b0 + run);
     int64_t mine = 0;
     for (int i = b0; i < b1; ++i) {
-      const int t = tiles_of(i, sq, tl);
-      mine += t ? t + kGroupCost : 0;
+      n = tiles_of(i, sq, tl);
+      mine += n ? n + kGroupCost : 0;
     }
     int64_t incl = mine;
 #pragma unroll
@@ -118,13 +121,16 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       const int64_t x = __shfl_up_sync(0xFFFFFFFFu, incl, d);
       if (lane >= d) incl += x;
     }
-    if (lane == 31) s_scan[warp] = incl;
-    __syncthreads();
-    int64_t before = incl - mine, total = 0;
+    int64_t before = incl - mine, total = __shfl_sync(0xFFFFFFFFu, incl, 31);
+    if (!alone) {
+      if (lane == 31) s_scan[warp] = incl;
+      __syncthreads();
+      total = 0;
 #pragma unroll
-    for (int w = 0; w <= kWarps; ++w) {
-      if (w < warp) before += s_scan[w];
-      total += s_scan[w];
+      for (int w = 0; w <= kWarps; ++w) {
+        if (w < warp) before += s_scan[w];
+        total += s_scan[w];
+      }
     }
     before *= a.Hk;
     mine *= a.Hk;
@@ -132,30 +138,50 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     share = max(divide(total + gridDim.x - 1, gridDim.x), (int64_t)a.min_tiles);
     x0 = blockIdx.x * share;
     if (x0 >= total) return;
-    if (x0 >= before && x0 < before + mine) {
-      int64_t at = before;
-      for (int i = b0; i < b1; ++i) {
-        if (run > 1) n = tiles_of(i, sq, tl);
-        else n = (int)(divide(mine, a.Hk)) - kGroupCost;
-        const int64_t len = n ? (int64_t)(n + kGroupCost) * a.Hk : 0;
-        if (x0 < at + len) {
-          s_seq = i;
-          s_first = at;
-          s_sq = sq;
-          s_tl = tl;
-          break;
-        }
-        at += len;
-      }
-    }
-    __syncthreads();
-    b = s_seq;
-    sq = s_sq;
-    tl = s_tl;
-    n = max(tl.n, 1);
-    hk = (int)divide(x0 - s_first, n + kGroupCost);
-    g0 = s_first + (int64_t)hk * (n + kGroupCost);
     x1 = min(total, x0 + share);
+    const bool here = x0 >= before && x0 < before + mine;
+    if (alone) {
+      // lane `src` has the sequence
+      const int src = __ffs(__ballot_sync(0xFFFFFFFFu, here)) - 1;
+      auto from = [&](auto v) { return __shfl_sync(0xFFFFFFFFu, v, src); };
+      b = src;
+      sq.q0 = from(sq.q0);
+      sq.qn = from(sq.qn);
+      sq.kv = from(sq.kv);
+      tl.lo_min = from(tl.lo_min);
+      tl.lo_max = from(tl.lo_max);
+      tl.hi_min = from(tl.hi_min);
+      tl.hi_max = from(tl.hi_max);
+      tl.n_win = from(tl.n_win);
+      tl.w_start = from(tl.w_start);
+      tl.n = from(tl.n);
+      g0 = from(before);
+      __syncthreads();                              // the barriers are set up
+    } else {
+      if (here) {
+        int64_t at = before;
+        for (int i = b0; i < b1; ++i) {
+          n = tiles_of(i, sq, tl);
+          const int64_t len = n ? (int64_t)(n + kGroupCost) * a.Hk : 0;
+          if (x0 < at + len) {
+            s_seq = i;
+            s_first = at;
+            s_sq = sq;
+            s_tl = tl;
+            break;
+          }
+          at += len;
+        }
+      }
+      __syncthreads();
+      b = s_seq;
+      sq = s_sq;
+      tl = s_tl;
+      g0 = s_first;
+    }
+    n = max(tl.n, 1);
+    hk = (int)divide(x0 - g0, n + kGroupCost);
+    g0 += (int64_t)hk * (n + kGroupCost);
   } else {
     b = blockIdx.x / a.Hk;
     hk = blockIdx.x % a.Hk;
@@ -252,6 +278,10 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     if (t0 >= t1) continue;
     const int rows = sq.qn * a.G;                                       // <= 16 RT
     const int t_end = min(t1, tl.n);
+    const int64_t group = (int64_t)b * a.Hk + hk, first = g0 + kGroupCost;
+    const bool whole = first >= x0 && first + n <= x1;                  // the group is this CTA's alone
+    const int64_t c0 = whole ? 0 : divide(first, share), c1 = whole ? 0 : divide(first + n - 1, share);   // its CTAs
+    const int parts = (int)(c1 - c0) + 1;
     const int p0 = sq.kv - sq.qn;
     float o[MT][2 * KS][4];
     float m_run[MT][2], l_run[MT][2];
@@ -463,9 +493,6 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
               make_float2(o[mt][k][2 * rr], o[mt][k][2 * rr + 1]);
       }
     named_bar_sync(1, kWarps * 32);
-    const int64_t group = (int64_t)b * a.Hk + hk, first = g0 + kGroupCost;
-    const int64_t c0 = split ? divide(first, share) : 0, c1 = split ? divide(first + n - 1, share) : 0;   // its CTAs
-    const int parts = (int)(c1 - c0) + 1;
     auto emit = [&](int r, int c, float m, float l, float4 v) {
       const int tok = r / a.G, h = hk * a.G + r % a.G;
       const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
@@ -513,18 +540,19 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     __threadfence();
     // part p's rows: the first CTA's second place, the others' first
     auto place = [&](int p) { return (2 * (c0 + p) + (p == 0 ? 1 : 0)) * maxrows; };
-    // A warp takes whole rows (the warps share a row's parts out when there are
-    // fewer rows than warps), a lane four channels, 16 parts in flight.
+    // A warp takes whole rows (where there are fewer rows than warps and more
+    // parts than a warp has in flight, the warps share a row's parts out), a lane
+    // four channels.
     constexpr int LPR = D / 4, RPW = 32 / LPR;        // lanes per row, rows per warp at a time
+    constexpr int PU = 20;                            // parts in flight
     const int rr = (rows + RPW - 1) / RPW;
-    const int slices = rr > 4 ? 1 : (rr > 2 ? 2 : (rr > 1 ? 4 : 8)), sl = warp % slices;
+    const int slices = rr > 4 || parts <= PU ? 1 : (rr > 2 ? 2 : (rr > 1 ? 4 : 8)), sl = warp % slices;
     const int q0 = parts * sl / slices, q1 = parts * (sl + 1) / slices;
     for (int rb = (warp / slices) * RPW; rb < rows; rb += (kWarps / slices) * RPW) {
       const int r = rb + lane / LPR, c = lane % LPR;
       float m = -INFINITY, l = 0.0f;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (r >= rows) continue;
-      constexpr int PU = 16;
       for (int p = q0; p < q1; p += PU) {
         float2 ml[PU];
         float4 x[PU];
