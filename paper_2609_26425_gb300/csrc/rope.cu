@@ -4,9 +4,9 @@
 // Mathematics: pair i of a token's channels turns by t = pos[axis(i)] *
 // inv_freq[i].  One pass over the data: every element is read once and written
 // once, so the bound is HBM (4 bytes an element; the angles cost 12 bytes a
-// token).  A CTA takes a few tokens: its threads first fill a table of (cos t,
-// sin t) of those tokens, shared by all heads of Queries and Keys, then move
-// 16-byte vectors, several in flight per thread.
+// token).  A CTA takes a few tokens: its threads fill a table of (cos t, sin t) of
+// those tokens, shared by all heads of Queries and Keys, then turn 16-byte
+// vectors, a row of 64 to 256 channels in neighbouring threads.
 #include "paged.cuh"
 
 namespace qwm {
@@ -49,9 +49,6 @@ __device__ __forceinline__ float2 turn(int pos, float f, float sign) {
   return make_float2(cs, sign * sn);
 }
 
-// Vectors (pairs of vectors) in flight per thread: with 3 or 4 CTAs an SM holds
-// 48 to 64 KB of loads in flight, what 6.8 TB/s at about 1 us wants.
-constexpr int kLoads = 4;
 constexpr int kMaxTokens = 16;                     // tokens of a CTA
 
 // Where a token's Keys and Values go: the first [heads] block of its page and
@@ -102,94 +99,93 @@ __global__ void __launch_bounds__(NT) rope_kernel(const RopeArgs a, int tokens_p
   const int hpar = NT / U;                         // rows (token, head) side by side
   const int u = tid % U, hl = tid / U;
   grid_begin();
-  if (PAGED && tid < nt) places[tid] = place_of(a, n0 + tid);
-  if (a.inv_freq) {
-    for (int i = tid; i < nt * P; i += NT) {
-      const int t = i / P, j = i - t * P;
-      const int axis = j < a.pairs[0] ? 0 : (j < a.pairs[0] + a.pairs[1] ? 1 : 2);
-      table[i] = turn(a.pos[(n0 + t) * 3 + axis], a.inv_freq[j], a.sign);
-    }
-  }
-  __syncthreads();
-  if (hl >= hpar) return;
+  const bool active = hl < hpar;
   const bool turned = a.inv_freq != nullptr && u < pv;
   const bool two = !INTERLEAVED && u < pv;         // two vectors a unit
   const int c0 = 8 * (INTERLEAVED || two ? u : u + pv);
   const int c1 = c0 + P;
-  // rows hl, hl + hpar, ... of the CTA's tokens x heads
+  // This thread's rows are hl, hl + hpar, ... of the CTA's tokens x heads, one in
+  // flight (the first on its way while the table is made): 1300 to 2000 threads
+  // an SM keep 32 to 64 KB in flight, and more rows per thread were slower (two:
+  // append of 4680 x 120 heads 51 -> 56 us, four: 63; the writes of a page's
+  // heads then come further apart).
   const int H = a.total_heads;
   const int step_t = hpar / H, step_h = hpar % H;
-  int t = hl / H, h = hl % H;
-  while (t < nt) {
-    uint4 x[kLoads], y[kLoads];
-    T* dst[kLoads];
-    int cs_at[kLoads];                             // token's row of the table, -1: not turned
+  int t = active ? hl / H : nt, h = hl % H;
+  uint4 x, y;
+  int rt, rh, rs;                                  // token (-1: none), head and tensor of the row in flight
+  auto fetch = [&]() {
+    rt = -1;
+    if (t < nt) {
+      int hs = h, s = 0;
+      if (a.nseg > 1 && hs >= a.seg[0].heads) { hs -= a.seg[0].heads; s = 1; }
+      if (a.nseg > 2 && s == 1 && hs >= a.seg[1].heads) { hs -= a.seg[1].heads; s = 2; }
+      const RopeSegment& g = a.seg[s];
+      const T* src = static_cast<const T*>(g.src) + (n0 + t) * g.s_tok + hs * g.s_head;
+      x = __ldcs(reinterpret_cast<const uint4*>(src + c0));
+      if (two) y = __ldcs(reinterpret_cast<const uint4*>(src + c1));
+      rt = t;
+      rh = hs;
+      rs = s;
+      t += step_t;
+      h += step_h;
+      if (h >= H) { h -= H; ++t; }
+    }
+  };
+  fetch();
+  if (PAGED && tid < nt) places[tid] = place_of(a, n0 + tid);
+  if (a.inv_freq) {
+    for (int i = tid; i < nt * P; i += NT) {
+      const int tt = i / P, j = i - tt * P;
+      const int axis = j < a.pairs[0] ? 0 : (j < a.pairs[0] + a.pairs[1] ? 1 : 2);
+      table[i] = turn(a.pos[(n0 + tt) * 3 + axis], a.inv_freq[j], a.sign);
+    }
+  }
+  __syncthreads();
+  for (; rt >= 0; fetch()) {
+    const RopeSegment& g = a.seg[rs];
+    T* dst;
+    if (!PAGED || g.page < 0) {
+      dst = static_cast<T*>(g.dst) + (n0 + rt) * g.d_tok + rh * g.d_head;
+    } else {
+      const Place pl = places[rt];
+      if (pl.block < 0) continue;
+      dst = static_cast<T*>(a.pages) + (((pl.block + (int64_t)g.page * a.kv_heads + rh) << a.page_log2) + pl.slot) * a.D;
+    }
+    if (turned && g.rotate) {
+      uint32_t* xw = reinterpret_cast<uint32_t*>(&x);
+      uint32_t* yw = reinterpret_cast<uint32_t*>(&y);
+      const float4* cs = reinterpret_cast<const float4*>(table + rt * P) + u * (INTERLEAVED ? 2 : 4);
+      if (INTERLEAVED) {
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      dst[k] = nullptr;
-      if (t < nt) {
-        int hs = h, s = 0;
-        if (a.nseg > 1 && hs >= a.seg[0].heads) { hs -= a.seg[0].heads; s = 1; }
-        if (a.nseg > 2 && s == 1 && hs >= a.seg[1].heads) { hs -= a.seg[1].heads; s = 2; }
-        const RopeSegment& g = a.seg[s];
-        const int64_t n = n0 + t;
-        const T* src = static_cast<const T*>(g.src) + n * g.s_tok + hs * g.s_head;
-        if (!PAGED || g.page < 0) {
-          dst[k] = static_cast<T*>(g.dst) + n * g.d_tok + hs * g.d_head;
-        } else {
-          const Place pl = places[t];
-          if (pl.block >= 0)
-            dst[k] = static_cast<T*>(a.pages) +
-                     (((pl.block + (int64_t)g.page * a.kv_heads + hs) << a.page_log2) + pl.slot) * a.D;
+        for (int w = 0; w < 2; ++w) {
+          const float4 c = cs[w];
+          const float2 v = Elem<T>::unpack(xw[2 * w]), z = Elem<T>::unpack(xw[2 * w + 1]);
+          xw[2 * w] = Elem<T>::pack(v.x * c.x - v.y * c.y, v.x * c.y + v.y * c.x);
+          xw[2 * w + 1] = Elem<T>::pack(z.x * c.z - z.y * c.w, z.x * c.w + z.y * c.z);
         }
-        cs_at[k] = turned && g.rotate ? t * P : -1;
-        if (dst[k]) {
-          x[k] = __ldcs(reinterpret_cast<const uint4*>(src + c0));
-          if (two) y[k] = __ldcs(reinterpret_cast<const uint4*>(src + c1));
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float4 c = cs[w];
+          const float2 v = Elem<T>::unpack(xw[w]), z = Elem<T>::unpack(yw[w]);
+          xw[w] = Elem<T>::pack(v.x * c.x - z.x * c.y, v.y * c.z - z.y * c.w);
+          yw[w] = Elem<T>::pack(v.x * c.y + z.x * c.x, v.y * c.w + z.y * c.z);
         }
-        t += step_t;
-        h += step_h;
-        if (h >= H) { h -= H; ++t; }
       }
     }
-#pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      if (!dst[k]) continue;
-      if (cs_at[k] >= 0) {
-        uint32_t* xw = reinterpret_cast<uint32_t*>(&x[k]);
-        uint32_t* yw = reinterpret_cast<uint32_t*>(&y[k]);
-        const float4* cs = reinterpret_cast<const float4*>(table + cs_at[k]) + u * (INTERLEAVED ? 2 : 4);
-        if (INTERLEAVED) {
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            const float4 c = cs[w];
-            const float2 v = Elem<T>::unpack(xw[2 * w]), z = Elem<T>::unpack(xw[2 * w + 1]);
-            xw[2 * w] = Elem<T>::pack(v.x * c.x - v.y * c.y, v.x * c.y + v.y * c.x);
-            xw[2 * w + 1] = Elem<T>::pack(z.x * c.z - z.y * c.w, z.x * c.w + z.y * c.z);
-          }
-        } else {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const float4 c = cs[w];
-            const float2 v = Elem<T>::unpack(xw[w]), z = Elem<T>::unpack(yw[w]);
-            xw[w] = Elem<T>::pack(v.x * c.x - z.x * c.y, v.y * c.z - z.y * c.w);
-            yw[w] = Elem<T>::pack(v.x * c.y + z.x * c.x, v.y * c.w + z.y * c.z);
-          }
-        }
-      }
-      *reinterpret_cast<uint4*>(dst[k] + c0) = x[k];
-      if (two) *reinterpret_cast<uint4*>(dst[k] + c1) = y[k];
-    }
+    *reinterpret_cast<uint4*>(dst + c0) = x;
+    if (two) *reinterpret_cast<uint4*>(dst + c1) = y;
   }
 }
 
 template <typename T, bool IL>
 cudaError_t go(const RopeArgs& a, cudaStream_t s) {
-  // tokens of a CTA: enough that each thread has two rounds of kLoads rows, as
-  // long as the grid still covers the SMs about four times
+  // tokens of a CTA: two rows for each thread, as long as the grid still covers
+  // the SMs about four times
   const int U = IL ? a.D / 8 : a.D / 8 - a.P / 8;
   const int hpar = NT / U;
-  int64_t tpc = (2 * kLoads * hpar + a.total_heads - 1) / a.total_heads;
+  int64_t tpc = (2 * hpar + a.total_heads - 1) / a.total_heads;
   const int64_t most = a.N / (4 * 152);
   if (tpc > most) tpc = most;
   if (tpc > kMaxTokens) tpc = kMaxTokens;
