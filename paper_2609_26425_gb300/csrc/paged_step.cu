@@ -1,5 +1,5 @@
 // paged_step.cu -- attention of a few rows of a sequence over its pages: single
-// new tokens and short drafts (Query tokens x grouped heads <= 32 rows).
+// new tokens and short drafts (Query tokens x grouped heads <= 16 rows).
 //
 // Mathematics: softmax over the visible keys with a running maximum m and sum l
 // per row (O and l scaled by 2^((m_old - m_new) c) when m grows), so one pass
@@ -8,13 +8,13 @@
 //
 // The tiles of all (sequence, cache head) groups form one line, which the CTAs (one
 // per SM) share out evenly whatever the lengths are; a CTA walks its stretch
-// group by group.  A producer warp keeps a ring of 64-key tiles in flight by
-// TMA; of eight warps four take 16 keys each of a tile, the other four those of
-// the next tile (up to 16 rows) or the second 16 rows (17 to 32), and carry
-// their own m, l and O through the group (no barrier between them in the loop);
-// then they are merged through shared memory.  The rows are the M = 16 side of
-// mma.sync: a tcgen05 tile would be 128 rows high for the 1 to 32 used here, and
-// its TMEM round trip is longer than the whole of a short step.
+// group by group.  A producer warp keeps a ring of tiles (64 keys of 128
+// channels, 128 of 64) in flight by TMA; of eight warps four take a quarter of a
+// tile's keys each, the other four those of the next tile, and carry their own
+// m, l and O through the group (no barrier between them in the loop); then they
+// are merged through shared memory.  The rows are the M = 16 side of mma.sync: a
+// tcgen05 tile would be 128 rows high for the 1 to 16 used here, and its TMEM
+// round trip is longer than the whole of a short step.
 // A group cut by the ends of stretches is joined by the CTA that finishes last,
 // in the order of the keys, so the result does not depend on which one that is.
 #include "paged.cuh"
@@ -23,17 +23,20 @@ namespace qwm {
 namespace {
 using namespace ptx;
 
-constexpr int TK = 64;                   // keys per tile
-constexpr int kWarps = 8;                // consumer warps, 16 keys each
+constexpr int kWarps = 8;                // consumer warps
 constexpr int NT = (kWarps + 1) * 32;
 // What a group costs a CTA beside its tiles (Queries, merge, output: about 5 K
-// cycles), in tiles' time (1.3 K cycles for 128 channels when all CTAs stream).
-constexpr int group_cost(int D) { return 512 / D; }
+// cycles), in tiles' time (1.3 K cycles when all CTAs stream).
+constexpr int kGroupCost = 4;
 
 template <int D>
 struct Shape {
+  static constexpr int KP = 128 / D;                           // 16-key groups of a warp: a tile's chain of products,
+                                                               // exponentials and products is as long for one as for
+                                                               // two, and 64 channels need twice the keys per time
+  static constexpr int TK = 64 * KP;                           // keys per tile
   static constexpr int SLOT = TK * D * 2;                      // bytes of a K or V tile
-  static constexpr int NS = D == 128 ? 8 : 12;                 // slots of the ring: K, V, K, V, ...
+  static constexpr int NS = 8;                                 // slots of the ring: K, V, K, V, ...
   static_assert(NS % 4 == 0, "an even number of tiles: a slot belongs to one warp group");
   static constexpr int MERGE = NS * SLOT;                      // the warps' O [warp][16][D], beside the ring so that
                                                                // the next group's tiles come in meanwhile
@@ -49,8 +52,9 @@ __device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 
-// Byte of 16-byte chunk `chunk` (8 channels) of key `key` in a tile [D / 64][64
+// Byte of 16-byte chunk `chunk` (8 channels) of key `key` in a tile [D / 64][TK
 // keys][128 bytes], 128-byte swizzled.
+template <int TK>
 __device__ __forceinline__ uint32_t at(int key, int chunk) {
   return (uint32_t)((chunk >> 3) * (TK * 128) + key * 128 + (((chunk & 7) ^ (key & 7)) << 4));
 }
@@ -59,13 +63,11 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {   // a >= 0, b
   return ((a | b) >> 32) ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
 }
 
-// RT row tiles of 16: with one, the two warp groups take alternate tiles.
-template <typename T, int D, int RT>
+template <typename T, int D>
 __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
   using L = Shape<D>;
-  constexpr int NS = L::NS, MT = 1;
+  constexpr int NS = L::NS, KP = L::KP, TK = L::TK;
   constexpr int KS = D / 16;                       // k16 steps of Q K^T, n16 blocks of P V
-  constexpr int kGroupCost = group_cost(D);
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   __shared__ uint64_t bars[2 * NS];
@@ -90,7 +92,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       mbar_init(full(s), 1);
-      mbar_init(empty(s), RT == 2 ? 8 : 4);
+      mbar_init(empty(s), kWarps / 2);
     }
     fence_mbar_init();
   }
@@ -264,11 +266,10 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   // ------------------------------------------------------------ consumers
   const float sl2 = a.scale * 1.4426950408889634f;
   const int g = lane >> 2, tq = lane & 3;
-  const int wg = warp >> 2, slice = warp & 3;                           // row tile or tile parity, keys of the tile
-  const int rbase = RT == 2 ? 16 * wg : 0;                              // this warp's first row
+  const int wg = warp >> 2, key0 = (warp & 3) * 16 * KP;                // tile parity, first key of the tile
   const int mrow = lane & 7, mi = lane >> 3;
-  const int kkey = slice * 16 + (mi >> 1) * 8 + mrow, kch = mi & 1;      // K: (keys 0-7 | 8-15) x (chunk, chunk + 1)
-  const int vkey = slice * 16 + (mi & 1) * 8 + mrow, vch = mi >> 1;      // V: the same, keys innermost
+  const int kkey = key0 + (mi >> 1) * 8 + mrow, kch = mi & 1;           // K: (keys 0-7 | 8-15) x (chunk, chunk + 1)
+  const int vkey = key0 + (mi & 1) * 8 + mrow, vch = mi >> 1;           // V: the same, keys innermost
   const int maxrows = a.max_q * a.G;
   float* so = reinterpret_cast<float*>(sm + L::MERGE);                  // [warp][16][D]
   bool ok = true;                                                       // no wait of this warp has run out
@@ -276,142 +277,134 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   do {
     piece();
     if (t0 >= t1) continue;
-    const int rows = sq.qn * a.G;                                       // <= 16 RT
+    const int rows = sq.qn * a.G;                                       // <= 16
     const int t_end = min(t1, tl.n);
     const int64_t group = (int64_t)b * a.Hk + hk, first = g0 + kGroupCost;
     const bool whole = first >= x0 && first + n <= x1;                  // the group is this CTA's alone
     const int64_t c0 = whole ? 0 : divide(first, share), c1 = whole ? 0 : divide(first + n - 1, share);   // its CTAs
     const int parts = (int)(c1 - c0) + 1;
     const int p0 = sq.kv - sq.qn;
-    float o[MT][2 * KS][4];
-    float m_run[MT][2], l_run[MT][2];
+    // the fragments of mma.sync: this lane has rows g and g + 8 (index rr)
+    float o[2 * KS][4];
+    float m_run[2], l_run[2];
+    uint32_t qf[KS][4];
+    int hi[2], lo[2];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      m_run[mt][0] = m_run[mt][1] = -INFINITY;
-      l_run[mt][0] = l_run[mt][1] = 0.0f;
+    for (int k = 0; k < 2 * KS; ++k)
 #pragma unroll
-      for (int k = 0; k < 2 * KS; ++k)
+      for (int e = 0; e < 4; ++e) o[k][e] = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[mt][k][e] = 0.0f;
-    }
-    uint32_t qf[MT][KS][4];
-    int hi[MT][2], lo[MT][2];
+    for (int rr = 0; rr < 2; ++rr) {
+      m_run[rr] = -INFINITY;
+      l_run[rr] = 0.0f;
+      const int r = rr * 8 + g;
+      const bool has = r < rows;
+      const int tok = has ? r / a.G : 0;
+      const Span sp = has ? row_span(p0 + tok, sq.kv, a.block, a.window) : Span{0, 0};
+      hi[rr] = sp.hi;
+      lo[rr] = sp.lo;
+      const T* src = static_cast<const T*>(a.q) + (sq.q0 + tok) * a.q_tok + (int64_t)(hk * a.G + (has ? r % a.G : 0)) * a.q_head;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int rr = 0; rr < 2; ++rr) {
-        const int r = rbase + rr * 8 + g;
-        const bool has = r < rows;
-        const int tok = has ? r / a.G : 0;
-        const Span sp = has ? row_span(p0 + tok, sq.kv, a.block, a.window) : Span{0, 0};
-        hi[mt][rr] = sp.hi;
-        lo[mt][rr] = sp.lo;
-        const T* src = static_cast<const T*>(a.q) + (sq.q0 + tok) * a.q_tok + (int64_t)(hk * a.G + (has ? r % a.G : 0)) * a.q_head;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          qf[mt][ks][rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + tq * 2) : 0u;
-          qf[mt][ks][2 + rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8 + tq * 2) : 0u;
-        }
+      for (int ks = 0; ks < KS; ++ks) {
+        qf[ks][rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + tq * 2) : 0u;
+        qf[ks][2 + rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8 + tq * 2) : 0u;
       }
-    // With one row tile, this warp group's tiles are those of its parity in the
-    // CTA's count of tiles, so that a slot of the ring is always the same
-    // group's: a group that did not wait for every use of a slot could take the
-    // phase before the one it waits for as done (a parity tells only two apart).
-    for (int t = t0 + (RT == 2 ? 0 : ((filled >> 1) + wg) & 1); t < t_end && ok; t += 3 - RT) {
+    }
+    // This warp group's tiles are those of its parity in the CTA's count of tiles,
+    // so that a slot of the ring is always the same group's: a group that did not
+    // wait for every use of a slot could take the phase before the one it waits
+    // for as done (a parity tells only two apart).
+    for (int t = t0 + (((filled >> 1) + wg) & 1); t < t_end && ok; t += 2) {
       const int i = filled + 2 * (t - t0), s = i % NS;                   // slots s and s + 1
-      const int j0 = tile_at(tl, t) * TK + slice * 16;                   // this warp's keys
+      const int j0 = tile_at(tl, t) * TK + key0;                         // this warp's keys: j0 .. j0 + 16 KP - 1
       if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full(s), (i / NS) & 1, a.wait_ns)))) break;
       const uint32_t kb = smem_u32(sm) + s * L::SLOT, vb = kb + L::SLOT;
-      const bool open = all_see(tl, j0, j0 + 16, a.sinks), any = any_sees(tl, j0, j0 + 16, a.sinks);
-      uint32_t pf[MT][4];
+      const bool open = all_see(tl, j0, j0 + 16 * KP, a.sinks), any = any_sees(tl, j0, j0 + 16 * KP, a.sinks);
+      uint32_t pf[KP][4];
       if (any) {
-        float sc[MT][2][4];
+        float sc[KP][2][4];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
           for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[mt][k][e] = 0.0f;
+            for (int e = 0; e < 4; ++e) sc[kp][k][e] = 0.0f;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          uint32_t bf[4];
-          ldsm4(kb + at(kkey, 2 * ks + kch), bf);
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            Elem<T>::mma(sc[mt][0], qf[mt][ks], bf[0], bf[1]);
-            Elem<T>::mma(sc[mt][1], qf[mt][ks], bf[2], bf[3]);
+          for (int kp = 0; kp < KP; ++kp) {
+            uint32_t bf[4];
+            ldsm4(kb + at<TK>(kkey + 16 * kp, 2 * ks + kch), bf);
+            Elem<T>::mma(sc[kp][0], qf[ks], bf[0], bf[1]);
+            Elem<T>::mma(sc[kp][1], qf[ks], bf[2], bf[3]);
           }
-        }
         if (!open) {
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
+          for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (!sees(j0 + k * 8 + tq * 2 + (e & 1), lo[mt][e >> 1], hi[mt][e >> 1], a.sinks))
-                  sc[mt][k][e] = -INFINITY;
+                if (!sees(j0 + kp * 16 + k * 8 + tq * 2 + (e & 1), lo[e >> 1], hi[e >> 1], a.sinks)) sc[kp][k][e] = -INFINITY;
         }
         // running maximum of each row, moved only when a key of this slice is
         // above it: the four lanes of a row agree through two shuffles then
         bool grow = false;
-        float top[MT][2];
+        float top[2];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int rr = 0; rr < 2; ++rr) {
+          top[rr] = -INFINITY;
 #pragma unroll
-          for (int rr = 0; rr < 2; ++rr) {
-            top[mt][rr] = fmaxf(fmaxf(sc[mt][0][2 * rr], sc[mt][0][2 * rr + 1]), fmaxf(sc[mt][1][2 * rr], sc[mt][1][2 * rr + 1]));
-            grow |= top[mt][rr] > m_run[mt][rr];
-          }
+          for (int kp = 0; kp < KP; ++kp)
+            top[rr] = fmaxf(top[rr], fmaxf(fmaxf(sc[kp][0][2 * rr], sc[kp][0][2 * rr + 1]),
+                                           fmaxf(sc[kp][1][2 * rr], sc[kp][1][2 * rr + 1])));
+          grow |= top[rr] > m_run[rr];
+        }
         if (__any_sync(0xFFFFFFFFu, grow)) {
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
+          for (int rr = 0; rr < 2; ++rr) {
+            float v = top[rr];
+            v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
+            v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
+            const float mn = fmaxf(m_run[rr], v);
+            const float al = mn == m_run[rr] ? 1.0f : ex2f((m_run[rr] - mn) * sl2);
+            m_run[rr] = mn;
+            l_run[rr] *= al;
 #pragma unroll
-            for (int rr = 0; rr < 2; ++rr) {
-              float v = top[mt][rr];
-              v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
-              v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
-              const float mn = fmaxf(m_run[mt][rr], v);
-              const float al = mn == m_run[mt][rr] ? 1.0f : ex2f((m_run[mt][rr] - mn) * sl2);
-              m_run[mt][rr] = mn;
-              l_run[mt][rr] *= al;
-#pragma unroll
-              for (int k = 0; k < 2 * KS; ++k) {
-                o[mt][k][2 * rr] *= al;
-                o[mt][k][2 * rr + 1] *= al;
-              }
+            for (int k = 0; k < 2 * KS; ++k) {
+              o[k][2 * rr] *= al;
+              o[k][2 * rr + 1] *= al;
             }
-        }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          // a row that has seen nothing yet keeps 0 as its reference: 2^-inf = 0
-          const float mb0 = m_run[mt][0] == -INFINITY ? 0.0f : m_run[mt][0] * sl2;
-          const float mb1 = m_run[mt][1] == -INFINITY ? 0.0f : m_run[mt][1] * sl2;
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float v0 = ex2f(fmaf(sc[mt][k][0], sl2, -mb0)), v1 = ex2f(fmaf(sc[mt][k][1], sl2, -mb0));
-            const float w0 = ex2f(fmaf(sc[mt][k][2], sl2, -mb1)), w1 = ex2f(fmaf(sc[mt][k][3], sl2, -mb1));
-            l_run[mt][0] += v0 + v1;
-            l_run[mt][1] += w0 + w1;
-            pf[mt][2 * k] = Elem<T>::pack(v0, v1);
-            pf[mt][2 * k + 1] = Elem<T>::pack(w0, w1);
           }
         }
+        // a row that has seen nothing yet keeps 0 as its reference: 2^-inf = 0
+        const float mb0 = m_run[0] == -INFINITY ? 0.0f : m_run[0] * sl2;
+        const float mb1 = m_run[1] == -INFINITY ? 0.0f : m_run[1] * sl2;
+#pragma unroll
+        for (int kp = 0; kp < KP; ++kp)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float v0 = ex2f(fmaf(sc[kp][k][0], sl2, -mb0)), v1 = ex2f(fmaf(sc[kp][k][1], sl2, -mb0));
+            const float w0 = ex2f(fmaf(sc[kp][k][2], sl2, -mb1)), w1 = ex2f(fmaf(sc[kp][k][3], sl2, -mb1));
+            l_run[0] += v0 + v1;
+            l_run[1] += w0 + w1;
+            pf[kp][2 * k] = Elem<T>::pack(v0, v1);
+            pf[kp][2 * k + 1] = Elem<T>::pack(w0, w1);
+          }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(empty(s));
       if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full(s + 1), (i / NS) & 1, a.wait_ns)))) break;
       if (open) {
 #pragma unroll
-        for (int nb = 0; nb < KS; ++nb) {
-          uint32_t bf[4];
-          ldsm4t(vb + at(vkey, 2 * nb + vch), bf);
+        for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            Elem<T>::mma(o[mt][2 * nb], pf[mt], bf[0], bf[1]);
-            Elem<T>::mma(o[mt][2 * nb + 1], pf[mt], bf[2], bf[3]);
+          for (int nb = 0; nb < KS; ++nb) {
+            uint32_t bf[4];
+            ldsm4t(vb + at<TK>(vkey + 16 * kp, 2 * nb + vch), bf);
+            Elem<T>::mma(o[2 * nb], pf[kp], bf[0], bf[1]);
+            Elem<T>::mma(o[2 * nb + 1], pf[kp], bf[2], bf[3]);
           }
-        }
       } else if (any) {
         // Keys that no row sees may hold anything (0 x inf is not 0): their
         // Values are cleared in the fragments.  Keys that some rows see and
@@ -421,48 +414,47 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         auto keep = [&](int klo, int khi, int j) -> uint32_t {
           return (sees(j, klo, khi, a.sinks) ? 0xFFFFu : 0u) | (sees(j + 1, klo, khi, a.sinks) ? 0xFFFF0000u : 0u);
         };
-        const int ja = j0 + tq * 2;
-        const uint32_t ma = keep(tl.lo_min, tl.hi_max, ja), mb = keep(tl.lo_min, tl.hi_max, ja + 8);
-        bool odd = false;
-        if (sq.qn > 1) {
 #pragma unroll
-          for (int nb = 0; nb < KS; ++nb) {
-            uint32_t bf[4];
-            ldsm4t(vb + at(vkey, 2 * nb + vch), bf);
-            odd |= nonfinite2<T>(bf[0] & ma) || nonfinite2<T>(bf[1] & mb) || nonfinite2<T>(bf[2] & ma) ||
-                   nonfinite2<T>(bf[3] & mb);
+        for (int kp = 0; kp < KP; ++kp) {
+          const int ja = j0 + kp * 16 + tq * 2;
+          const uint32_t ma = keep(tl.lo_min, tl.hi_max, ja), mb = keep(tl.lo_min, tl.hi_max, ja + 8);
+          bool odd = false;
+          if (sq.qn > 1) {
+#pragma unroll
+            for (int nb = 0; nb < KS; ++nb) {
+              uint32_t bf[4];
+              ldsm4t(vb + at<TK>(vkey + 16 * kp, 2 * nb + vch), bf);
+              odd |= nonfinite2<T>(bf[0] & ma) || nonfinite2<T>(bf[1] & mb) || nonfinite2<T>(bf[2] & ma) ||
+                     nonfinite2<T>(bf[3] & mb);
+            }
+            odd = __any_sync(0xFFFFFFFFu, odd);
           }
-          odd = __any_sync(0xFFFFFFFFu, odd);
-        }
-        const int turns = odd ? sq.qn : 1;
-        for (int tk = 0; tk < turns; ++tk) {
-          uint32_t wa = ma, wb = mb;
-          bool own[MT][2];
+          const int turns = odd ? sq.qn : 1;
+          for (int tk = 0; tk < turns; ++tk) {
+            uint32_t wa = ma, wb = mb;
+            bool own[2];
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
+            for (int rr = 0; rr < 2; ++rr) own[rr] = !odd || (rr * 8 + g) / a.G == tk;
+            if (odd) {
+              const Span sp = row_span(p0 + tk, sq.kv, a.block, a.window);
+              wa = keep(sp.lo, sp.hi, ja);
+              wb = keep(sp.lo, sp.hi, ja + 8);
+            }
 #pragma unroll
-            for (int rr = 0; rr < 2; ++rr) own[mt][rr] = !odd || (rbase + rr * 8 + g) / a.G == tk;
-          if (odd) {
-            const Span sp = row_span(p0 + tk, sq.kv, a.block, a.window);
-            wa = keep(sp.lo, sp.hi, ja);
-            wb = keep(sp.lo, sp.hi, ja + 8);
-          }
-#pragma unroll
-          for (int nb = 0; nb < KS; ++nb) {
-            uint32_t bf[4];
-            ldsm4t(vb + at(vkey, 2 * nb + vch), bf);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int nb = 0; nb < KS; ++nb) {
+              uint32_t bf[4];
+              ldsm4t(vb + at<TK>(vkey + 16 * kp, 2 * nb + vch), bf);
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
                 float acc[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = o[mt][2 * nb + k][e];
-                Elem<T>::mma(acc, pf[mt], bf[2 * k] & wa, bf[2 * k + 1] & wb);
+                for (int e = 0; e < 4; ++e) acc[e] = o[2 * nb + k][e];
+                Elem<T>::mma(acc, pf[kp], bf[2 * k] & wa, bf[2 * k + 1] & wb);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                  if (own[mt][e >> 1]) o[mt][2 * nb + k][e] = acc[e];
+                  if (own[e >> 1]) o[2 * nb + k][e] = acc[e];
               }
+            }
           }
         }
       }
@@ -475,23 +467,20 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     // -------------------------------------------------------- the warps' (max, sum, O) of the piece
     named_bar_sync(1, kWarps * 32);                  // the last piece's have been read
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int rr = 0; rr < 2; ++rr) {
-        const int r = rr * 8 + g;
-        float l = l_run[mt][rr];                     // the four lanes of a row hold its sum in parts
-        l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
-        l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
-        if (rbase + r >= rows) continue;
-        if (tq == 0) {
-          s_ml[warp][r][0] = m_run[mt][rr];
-          s_ml[warp][r][1] = l;
-        }
-#pragma unroll
-        for (int k = 0; k < 2 * KS; ++k)
-          *reinterpret_cast<float2*>(so + ((warp * 16 + r) * D + k * 8 + tq * 2)) =
-              make_float2(o[mt][k][2 * rr], o[mt][k][2 * rr + 1]);
+    for (int rr = 0; rr < 2; ++rr) {
+      const int r = rr * 8 + g;
+      float l = l_run[rr];                           // the four lanes of a row hold its sum in parts
+      l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
+      l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
+      if (r >= rows) continue;
+      if (tq == 0) {
+        s_ml[warp][r][0] = m_run[rr];
+        s_ml[warp][r][1] = l;
       }
+#pragma unroll
+      for (int k = 0; k < 2 * KS; ++k)
+        *reinterpret_cast<float2*>(so + ((warp * 16 + r) * D + k * 8 + tq * 2)) = make_float2(o[k][2 * rr], o[k][2 * rr + 1]);
+    }
     named_bar_sync(1, kWarps * 32);
     auto emit = [&](int r, int c, float m, float l, float4 v) {
       const int tok = r / a.G, h = hk * a.G + r % a.G;
@@ -500,19 +489,18 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       *reinterpret_cast<uint2*>(dst) = make_uint2(Elem<T>::pack(v.x * inv, v.y * inv), Elem<T>::pack(v.z * inv, v.w * inv));
       if (a.lse && c == 0) a.lse[(int64_t)h * a.N + sq.q0 + tok] = m == -INFINITY ? -INFINITY : m * a.scale + logf(l);
     };
-    // (m, l, O) of a row's channels 4c .. over `count` entries from `first_entry`
-    // of s_ml and so, row `at`
-    auto merge = [&](int first_entry, int count, int at, int c, float& m, float& l, float4& v) {
+    // (m, l, O) of row r's channels 4c .. over the first `count` entries of s_ml and so
+    auto merge = [&](int count, int r, int c, float& m, float& l, float4& v) {
       m = -INFINITY;
-      for (int w = 0; w < count; ++w) m = fmaxf(m, s_ml[first_entry + w][at][0]);
+      for (int w = 0; w < count; ++w) m = fmaxf(m, s_ml[w][r][0]);
       const float ref = m == -INFINITY ? 0.0f : m;
       l = 0.0f;
       v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
       for (int w = 0; w < count; ++w) {
-        const float f = ex2f((s_ml[first_entry + w][at][0] - ref) * sl2);
-        const float4 x = *reinterpret_cast<const float4*>(so + (((first_entry + w) * 16 + at) * D + 4 * c));
-        l = fmaf(s_ml[first_entry + w][at][1], f, l);
+        const float f = ex2f((s_ml[w][r][0] - ref) * sl2);
+        const float4 x = *reinterpret_cast<const float4*>(so + ((w * 16 + r) * D + 4 * c));
+        l = fmaf(s_ml[w][r][1], f, l);
         v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
       }
     };
@@ -520,7 +508,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       const int r = idx / (D / 4), c = idx % (D / 4);
       float m, l;
       float4 v;
-      merge(RT == 2 ? (r >> 4) * 4 : 0, RT == 2 ? 4 : 8, r & 15, c, m, l, v);
+      merge(kWarps, r, c, m, l, v);
       if (parts == 1) {
         emit(r, c, m, l, v);
       } else {
@@ -594,7 +582,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         const int r = idx / (D / 4), c = idx % (D / 4);
         float m, l;
         float4 v;
-        merge(0, slices, r, c, m, l, v);
+        merge(slices, r, c, m, l, v);
         emit(r, c, m, l, v);
       }
     }
@@ -602,17 +590,13 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   } while (next_group());
 }
 
-template <typename T, int D, int RT>
+template <typename T, int D>
 cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   constexpr int smem = Shape<D>::TOTAL;
   static bool done[64];
-  cudaError_t e = allow_smem(paged_step<T, D, RT>, smem, done);
+  cudaError_t e = allow_smem(paged_step<T, D>, smem, done);
   if (e != cudaSuccess) return e;
-  return launch_ahead(paged_step<T, D, RT>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, map, a);
-}
-template <typename T, int D>
-cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
-  return a.max_q * a.G <= 16 ? go<T, D, 1>(a, map, s) : go<T, D, 2>(a, map, s);
+  return launch_ahead(paged_step<T, D>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, map, a);
 }
 
 }  // namespace
@@ -628,7 +612,8 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
   p.nsplit = 1;
   if (split) {
     // a CTA per SM, or as many as have min_tiles places each
-    const int64_t tiles = ((max_visible + TK - 1) / TK + 1 + group_cost(D)) * p.groups;
+    const int TK = D == 128 ? Shape<128>::TK : Shape<64>::TK;
+    const int64_t tiles = ((max_visible + TK - 1) / TK + 1 + kGroupCost) * p.groups;
     const int64_t want = (tiles + p.min_tiles - 1) / p.min_tiles, most = nsm;
     p.nsplit = (int)(want < most ? want : most);
   }
@@ -636,8 +621,8 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
 }
 
 cudaError_t launch_paged_step(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s) {
-  if (dtype == QWM_F16) return D == 64 ? pick<__half, 64>(a, map, s) : pick<__half, 128>(a, map, s);
-  return D == 64 ? pick<__nv_bfloat16, 64>(a, map, s) : pick<__nv_bfloat16, 128>(a, map, s);
+  if (dtype == QWM_F16) return D == 64 ? go<__half, 64>(a, map, s) : go<__half, 128>(a, map, s);
+  return D == 64 ? go<__nv_bfloat16, 64>(a, map, s) : go<__nv_bfloat16, 128>(a, map, s);
 }
 
 }  // namespace qwm
