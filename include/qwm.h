@@ -487,14 +487,17 @@ typedef struct qwm_mask {
  * q_heads = q->heads heads, a multiple of kv_heads (Query head h reads head
  * h / (q_heads / kv_heads)).  Logits, softmax statistics and sums are fp32; the
  * probabilities enter the tensor cores in the cache's type.  lse: fp32
- * [q_heads][tokens] natural-log sum-exp of the scaled logits, or NULL.  A row
- * that sees nothing gets 0 and an lse of -inf.  What a row does not see does
+ * [q_heads][tokens] natural-log sum-exp of the scaled logits, or NULL.  out must
+ * not overlap q.  0 < sm_scale <= 1e38.  A row that sees nothing gets 0 and an
+ * lse of -inf.  What a row does not see does
  * not reach it, infinities and NaN included.
  * workspace: device scratch of at least qwm_paged_attend_workspace_bytes bytes
- * for the same arguments (256-byte aligned), zeroed once when it is made (each
- * call leaves its counters at zero); the call then splits long sequences over
- * the GPU and joins the parts in a fixed order.  NULL or too small: no split.
- * Calls sharing a workspace must not overlap on the GPU. */
+ * for the same arguments (256-byte aligned), its first QWM_PAGED_COUNTER_BYTES
+ * zeroed once when it is made (each call leaves them at zero); the call then
+ * splits long sequences over the GPU and joins the parts in a fixed order.  NULL
+ * or too small: no split.  Calls of any arguments may take turns on one workspace,
+ * but must not overlap on the GPU. */
+#define QWM_PAGED_COUNTER_BYTES 65536
 QWM_API size_t qwm_paged_attend_workspace_bytes(const qwm_paged* cache, const qwm_paged_batch* batch, int32_t q_heads,
                                                 const qwm_mask* mask);
 QWM_API qwm_status qwm_paged_attend(qwm_paged* cache, const qwm_paged_batch* batch, const qwm_rows* q,

@@ -136,16 +136,17 @@ PagedPlan make_plan(const qwm_paged* c, const qwm_paged_batch* b, int32_t q_head
                                 : qwm::plan_chunk(b->num_seqs, c->cfg.kv_heads, rows, seen, c->nsm, split);
 }
 
-// counters, (max, sum) pairs and partial outputs, each 256-byte aligned; a step
-// CTA has two parts (of the groups at the ends of its stretch), a chunk group
-// nsplit
+// A workspace: counters, at the same place for every call (they stay zero between
+// calls of whatever sizes), then (max, sum) pairs and partial outputs, each
+// 256-byte aligned.  A step CTA has two parts (of the groups at the ends of its
+// stretch), a chunk group nsplit.
 struct Carve {
   size_t ml, o, total;
 };
 Carve carve(const PagedPlan& p, int D) {
   Carve w{};
   const size_t rows = (size_t)(p.step ? 2 : p.groups) * p.nsplit * p.rows;
-  w.ml = ((size_t)p.groups * 4 + 255) / 256 * 256;
+  w.ml = QWM_PAGED_COUNTER_BYTES;
   w.o = w.ml + (rows * 8 + 255) / 256 * 256;
   w.total = w.o + rows * D * 4;
   return w;
@@ -279,7 +280,7 @@ qwm_status qwm_paged_attend(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   if (!c || !b || !q || !mask || !out) return QWM_ERR_INVALID_ARG;
   qwm_status st = check_batch(c, b);
   if (st != QWM_OK) return st;
-  if (!mask_ok(mask) || !(sm_scale > 0.0f) || sm_scale > 3.0e38f) return QWM_ERR_INVALID_ARG;
+  if (!mask_ok(mask) || !(sm_scale > 0.0f) || sm_scale > 1.0e38f) return QWM_ERR_INVALID_ARG;  // x log2(e) fits
   if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return QWM_ERR_INVALID_ARG;
   if (b->tokens == 0) return QWM_OK;
   const int D = c->cfg.head_dim;

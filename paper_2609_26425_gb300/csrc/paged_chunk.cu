@@ -673,7 +673,8 @@ PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, 
   PagedPlan p{};
   p.rows = ROWS;
   const int64_t rtiles = (rows + p.rows - 1) / p.rows;
-  p.groups = (int)(rtiles * B * Hk);
+  const int64_t groups = rtiles * B * Hk;
+  p.groups = (int)(groups < 1 << 30 ? groups : 1 << 30);   // (as many are not split)
   p.min_tiles = 4;
   p.nsplit = 1;
   const int64_t tiles = (max_visible + TK - 1) / TK + 2;
@@ -682,7 +683,7 @@ PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, 
     // about 6 tiles' time), 4 more for the join; parts of at least 4 tiles
     int64_t best = 0;
     for (int64_t n = 1; n <= 64 && n * p.min_tiles <= tiles + p.min_tiles - 1; ++n) {
-      const int64_t waves = (p.groups * n + nsm - 1) / nsm, cost = waves * ((tiles + n - 1) / n + 6) + (n > 1 ? 4 : 0);
+      const int64_t waves = ((int64_t)p.groups * n + nsm - 1) / nsm, cost = waves * ((tiles + n - 1) / n + 6) + (n > 1 ? 4 : 0);
       if (n == 1 || cost < best) {
         best = cost;
         p.nsplit = (int)n;

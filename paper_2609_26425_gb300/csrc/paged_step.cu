@@ -610,7 +610,8 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
   // us with 4, up to 9.5 with 3 (an extra join), 9.3 with 6
   p.min_tiles = 4;
   p.nsplit = 1;
-  if (split) {
+  // (more groups than counters fill the SMs without being cut)
+  if (split && p.groups <= QWM_PAGED_COUNTER_BYTES / 4) {
     // a CTA per SM, or as many as have min_tiles places each
     const int TK = D == 128 ? Shape<128>::TK : Shape<64>::TK;
     const int64_t tiles = ((max_visible + TK - 1) / TK + 1 + kGroupCost) * p.groups;

@@ -380,3 +380,44 @@ def test_running_maxima_that_move(new, dtype, D, order):
     for ws in (None, qwm.paged_attend_workspace(cache, batch, 2)):
         out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), sm_scale=1.0, want_lse=True, workspace=ws)
         compare(out, lse, want)
+
+
+def test_more_sequences_than_threads():
+    g = torch.Generator().manual_seed(77)
+    lens = []
+    for i in range(700):
+        q = int(torch.randint(0, 2, (1,), generator=g))
+        lens.append((q, max(q, int(torch.randint(0, 40, (1,), generator=g)))))
+    run_case(401, lens, 2, 2, 64, BF, 16, 1, 20, 3)
+    N = sum(a for a, _ in lens)
+    k = torch.randn(N, 2, 64, generator=g).to(BF)
+    _, _, _, pages, table = make_case(402, lens, 1, 2, 64, BF, 16)
+    marks = torch.randn(pages.shape, generator=g).to(BF)
+    cache, batch = build(lens, 2, 64, BF, 16, marks, table)
+    qwm.qwm_paged_append(cache, batch, k.cuda(), (2 * k).cuda())
+    want, row = marks.clone(), 0
+    for b, (ql, kv) in enumerate(lens):
+        for i in range(ql):
+            p = kv - ql + i
+            want[int(table[b, p // 16]), 0, :, p % 16] = k[row]
+            want[int(table[b, p // 16]), 1, :, p % 16] = 2 * k[row]
+            row += 1
+    assert torch.equal(cache.pages.cpu(), want) and cache.status() == 0
+
+
+def test_calls_of_any_sizes_take_turns_on_one_workspace():
+    shapes = [([(1, 2000)], 40, 8, 128, BF), ([(1, 700)] * 37, 8, 8, 128, BF), ([(60, 1500)], 4, 2, 128, BF),
+              ([(1, 900)] * 200, 12, 12, 128, BF), ([(300, 2500)], 1, 1, 128, BF)]
+    made = []
+    for i, (lens, Hq, Hk, D, dtype) in enumerate(shapes):
+        q, keys, values, pages, table = make_case(500 + i, lens, Hq, Hk, D, dtype, 32)
+        cache, batch = build(lens, Hk, D, dtype, 32, pages, table)
+        own = qwm.paged_attend_workspace(cache, batch, Hq)
+        assert own is not None
+        made.append((cache, batch, q.cuda(), own))
+    shared = torch.zeros(max(m[3].numel() for m in made), dtype=torch.uint8, device="cuda")
+    want = [qwm.qwm_paged_attend(c, b, q, workspace=own).clone() for c, b, q, own in made]
+    for _ in range(2):
+        for (c, b, q, _), w in list(zip(made, want)) + list(zip(made, want))[::-1]:
+            assert torch.equal(qwm.qwm_paged_attend(c, b, q, workspace=shared), w)
+    assert bool((shared[:65536] == 0).all())
