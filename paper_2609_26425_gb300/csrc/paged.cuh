@@ -214,10 +214,10 @@ template <>
 struct Elem<__nv_bfloat16> {
   static constexpr bool bf16 = true;
   static constexpr uint32_t kExp = 0x7F80u;  // exponent field: all ones in infinities and NaN
-  // growth of a row's maximum (as a power of two) up to which P is still taken
-  // against the old one: P, l and O are floating-point multiples of the same
-  // power, so only the type's range bounds it (fp32's for bf16: 2^40 times any
-  // number of keys; 65504 for binary16)
+  // how far (as a power of two) P may grow above 1 before it is taken against a
+  // new maximum: P, l and O are floating-point multiples of the same power, so
+  // only the type's range bounds it (fp32's for bf16: 2^40 times any number of
+  // keys; 65504 for binary16)
   static constexpr float kTau = 40.0f;
   __device__ static __forceinline__ uint32_t pack(float a, float b) { return ptx::pack_bf16(a, b); }
   __device__ static __forceinline__ float2 unpack(uint32_t w) {

@@ -12,10 +12,11 @@
 // beside the MMAs of the other.  TMEM: S0 | S1 | O0 | O1.
 // The chain S, softmax, P V, next S sets the pace, so the row maximum is kept off
 // it: P is taken against the maximum known before the tile, one pass over S with
-// the exponentials (32 a cycle and SM) as its only bound, and the tile's own
-// maximum is formed beside it.  Where it is above the known one by more than
-// 2^kTau the pass is repeated against the new one; P, l and O are floating-point
-// multiples of the same power, so nothing is lost below that.
+// the exponentials (32 a cycle and SM) as its only bound.  P, l and O are
+// floating-point multiples of the same power of two, so a maximum that has grown
+// costs nothing until P could leave its type's range; a half tile whose sum is
+// above 2^kTau (no P above it can hide in a smaller sum) is taken again against
+// its rows' new maxima.
 // Few rows over many keys are split along the keys; the parts' O, m and l go
 // through global memory to a second kernel over all SMs, launched ahead so that
 // it stands ready.  (A join by a group's last CTA took 11 us of 69 at 880 Queries
@@ -188,10 +189,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       const uint32_t tS = tbase + 128 * i + lrow, tO = tbase + 128 * NQ + D * i + lrow;
       float m_run = has ? -INFINITY : 0.0f, l_run = 0.0f;
       const uint64_t SL = f2pack(sl2, sl2);
-      // Whether some row's maximum has grown by more than 2^kTau (-inf - -inf and
-      // inf - inf are NaN and compare false: a row that has seen nothing, or an
-      // infinity, stays as it is)
-      auto grown = [&](float mt) -> bool { return __any_sync(0xFFFFFFFFu, (mt - m_run) * sl2 > Elem<T>::kTau); };
+      const float kMost = exp2f(Elem<T>::kTau);
       // Raises every row of the warp to its own maximum, and O with it (the P V
       // before it are complete)
       auto raise = [&](float mt, bool rescale) {
@@ -246,19 +244,16 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
               for (int e = 0; e < 32; e += 2) mt = fmax3f(mt, __uint_as_float(w[e]), __uint_as_float(w[e + 1]));
             }
           }
-          if (grown(mt)) raise(mt, jt > 0);
+          if (__any_sync(0xFFFFFFFFu, mt > m_run)) raise(mt, jt > 0);
         }
         // One pass over S in two halves of 64 keys, each handed on as soon as it is
-        // done: P against m_run, its sum, and the half's own maximum beside it.
+        // done: P against m_run, and its sum.
         uint32_t pk[32];
-        float m4[4];
         uint64_t sum, MB;
         auto begin_half = [&]() {
           const float mb = m_run == -INFINITY ? 0.0f : m_run * sl2;
           MB = f2pack(-mb, -mb);
           sum = f2pack(0.0f, 0.0f);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) m4[e] = -INFINITY;
         };
         auto block = [&](auto masked, int blk, uint32_t (&w)[32]) {
           if (masked) {
@@ -274,7 +269,6 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
             const float s0 = __uint_as_float(w[e]), s1 = __uint_as_float(w[e + 1]);
-            m4[(e >> 1) & 3] = fmax3f(m4[(e >> 1) & 3], s0, s1);
             float x, y;
             f2unpack(fma2(f2pack(s0, s1), SL, MB), x, y);
             x = ex2f(x);
@@ -294,26 +288,38 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
             block(masked, blk, v[blk & 1]);
             if ((blk & 1) == 0) continue;
             const int half = blk >> 1;
-            const float mt = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-            if (grown(mt)) {
+            float sx, sy;
+            f2unpack(sum, sx, sy);
+            if (__any_sync(0xFFFFFFFFu, sx + sy > kMost)) {
               // again against the new maximum; the first half's P V has to be in O
               // before O is scaled for the second's
               if (half == 1) {
                 if (!(ok = wait_all(B_PV + i, jt & 1))) return;
                 tc_fence_after();
               }
+              uint32_t u[32];
+              float mt = -INFINITY;
+#pragma unroll 1
+              for (int k = 0; k < 2; ++k) {
+                uint32_t see;
+                const int kind = seen(2 * half + k, see);
+                tmem_ld32_start(tS + 64 * half + 32 * k, u);
+                tmem_ld32_wait(u);
+                if (kind == kNone) continue;
+                if (kind == kSome) select(u, see);
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) mt = fmax3f(mt, __uint_as_float(u[e]), __uint_as_float(u[e + 1]));
+              }
               raise(mt, half == 1 || jt > 0);
               begin_half();
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
-                uint32_t u[32];
                 tmem_ld32_start(tS + 64 * half + 32 * k, u);
                 tmem_ld32_wait(u);
                 block(std::true_type{}, 2 * half + k, u);
               }
+              f2unpack(sum, sx, sy);
             }
-            float sx, sy;
-            f2unpack(sum, sx, sy);
             l_run += sx + sy;
             tmem_st16(tS + 32 * half, *reinterpret_cast<uint32_t(*)[16]>(pk));
             tmem_st16(tS + 32 * half + 16, *reinterpret_cast<uint32_t(*)[16]>(pk + 16));
