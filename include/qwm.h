@@ -374,7 +374,7 @@ typedef enum qwm_dtype { QWM_BF16 = 0, QWM_F16 = 1 } qwm_dtype;
 
 /* A tensor [tokens][heads][head_dim] in device memory: element (n, h, c) is at
  * data + n * token_stride + h * head_stride + c (strides in elements, multiples
- * of 8; data 16-byte aligned). */
+ * of 8 below 2^31; data 16-byte aligned). */
 typedef struct qwm_rows {
   void* data;
   int64_t token_stride, head_stride;

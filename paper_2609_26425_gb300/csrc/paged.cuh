@@ -11,8 +11,8 @@ namespace qwm {
 struct RopeSegment {            // a tensor [N][heads][D] and where its rows go
   const void* src;
   void* dst;
-  int64_t s_tok, s_head;        // strides in elements
-  int64_t d_tok, d_head;
+  int32_t s_tok, s_head;        // strides in elements
+  int32_t d_tok, d_head;
   int32_t heads;
   int32_t rotate;               // 0: copied
   int32_t page;                 // -1: to dst; 0 / 1: to the Keys / Values of the token's page

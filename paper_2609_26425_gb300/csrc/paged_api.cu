@@ -38,7 +38,8 @@ bool paged_supported(const qwm_paged_config* c) {
 // A tensor that the kernels can read in 16-byte vectors.
 bool rows_ok(const qwm_rows* r) {
   return r->data && (reinterpret_cast<uintptr_t>(r->data) & 15u) == 0 && (r->token_stride & 7) == 0 &&
-         (r->head_stride & 7) == 0 && r->token_stride >= 0 && r->head_stride >= 0 && r->heads >= 1;
+         (r->head_stride & 7) == 0 && r->token_stride >= 0 && r->head_stride >= 0 && r->heads >= 1 &&
+         r->token_stride < (int64_t)1 << 31 && r->head_stride < (int64_t)1 << 31;
 }
 // A tensor that is written: no two (token, head) may share a row.
 bool out_ok(const qwm_rows* r, int64_t N, int D) {
@@ -72,12 +73,12 @@ void set_rope(qwm::RopeArgs& a, const qwm_rope_config* c, const float* inv_freq,
 void add_segment(qwm::RopeArgs& a, const qwm_rows* src, const qwm_rows* dst, bool rotate, int page) {
   qwm::RopeSegment& g = a.seg[a.nseg++];
   g.src = src->data;
-  g.s_tok = src->token_stride;
-  g.s_head = src->head_stride;
+  g.s_tok = (int32_t)src->token_stride;
+  g.s_head = (int32_t)src->head_stride;
   g.heads = src->heads;
   g.dst = dst ? dst->data : nullptr;
-  g.d_tok = dst ? dst->token_stride : 0;
-  g.d_head = dst ? dst->head_stride : 0;
+  g.d_tok = dst ? (int32_t)dst->token_stride : 0;
+  g.d_head = dst ? (int32_t)dst->head_stride : 0;
   g.rotate = rotate;
   g.page = page;
   a.total_heads += src->heads;

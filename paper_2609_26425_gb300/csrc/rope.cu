@@ -51,11 +51,11 @@ __device__ __forceinline__ float2 turn(int pos, float f, float sign) {
 
 constexpr int kMaxTokens = 16;                     // tokens of a CTA
 
-// Where a token's Keys and Values go: the first [heads] block of its page and
-// its slot, block < 0: nowhere.
+__device__ __forceinline__ int64_t wide(int a, int b) { return (int64_t)a * b; }
+
+// Where a token's first Key goes in the pages (elements), < 0: nowhere.
 struct Place {
-  int64_t block;
-  int slot;
+  int64_t at;
 };
 __device__ __forceinline__ Place place_of(const RopeArgs& a, int64_t n) {
   int lo = 0, hi = a.B;                            // last b with q_off[b] <= n
@@ -66,7 +66,7 @@ __device__ __forceinline__ Place place_of(const RopeArgs& a, int64_t n) {
   const int64_t q0 = a.q_off[lo], q1 = a.q_off[lo + 1], kv = a.kv_len[lo];
   int64_t cap = (int64_t)a.table_stride << a.page_log2;
   if (cap > a.max_kv) cap = a.max_kv;
-  Place r{-1, 0};
+  Place r{-1};
   if (!(n >= q0 && n < q1 && q1 <= a.N && q1 - q0 <= a.max_q && kv >= 0 && kv <= cap)) {
     record_status(a.status, QWM_ERR_INVALID_ARG);
     return r;
@@ -78,8 +78,7 @@ __device__ __forceinline__ Place place_of(const RopeArgs& a, int64_t n) {
     record_status(a.status, QWM_ERR_INVALID_ARG);
     return r;
   }
-  r.block = page * 2 * a.kv_heads;
-  r.slot = (int)(p & ((1 << a.page_log2) - 1));
+  r.at = (((page * 2 * a.kv_heads) << a.page_log2) + (p & ((1 << a.page_log2) - 1))) * a.D;
   return r;
 }
 
@@ -89,7 +88,7 @@ __global__ void __launch_bounds__(NT) rope_kernel(const RopeArgs a, int tokens_p
   float2* table = reinterpret_cast<float2*>(table4);
   __shared__ Place places[kMaxTokens];
   const int tid = threadIdx.x;
-  const int64_t n0 = (int64_t)blockIdx.x * tokens_per_cta;
+  const int n0 = blockIdx.x * tokens_per_cta;      // (N <= 2^30)
   const int nt = (int)min((int64_t)tokens_per_cta, a.N - n0);
   const int P = a.P, nvec = a.D / 8;
   // units of a head's row: interleaved, its nvec vectors; halves, P / 8 pairs
@@ -121,7 +120,7 @@ __global__ void __launch_bounds__(NT) rope_kernel(const RopeArgs a, int tokens_p
       if (a.nseg > 1 && hs >= a.seg[0].heads) { hs -= a.seg[0].heads; s = 1; }
       if (a.nseg > 2 && s == 1 && hs >= a.seg[1].heads) { hs -= a.seg[1].heads; s = 2; }
       const RopeSegment& g = a.seg[s];
-      const T* src = static_cast<const T*>(g.src) + (n0 + t) * g.s_tok + hs * g.s_head;
+      const T* src = static_cast<const T*>(g.src) + wide(n0 + t, g.s_tok) + wide(hs, g.s_head);
       x = __ldcs(reinterpret_cast<const uint4*>(src + c0));
       if (two) y = __ldcs(reinterpret_cast<const uint4*>(src + c1));
       rt = t;
@@ -138,7 +137,7 @@ __global__ void __launch_bounds__(NT) rope_kernel(const RopeArgs a, int tokens_p
     for (int i = tid; i < nt * P; i += NT) {
       const int tt = i / P, j = i - tt * P;
       const int axis = j < a.pairs[0] ? 0 : (j < a.pairs[0] + a.pairs[1] ? 1 : 2);
-      table[i] = turn(a.pos[(n0 + tt) * 3 + axis], a.inv_freq[j], a.sign);
+      table[i] = turn(a.pos[wide(n0 + tt, 3) + axis], a.inv_freq[j], a.sign);
     }
   }
   __syncthreads();
@@ -146,11 +145,11 @@ __global__ void __launch_bounds__(NT) rope_kernel(const RopeArgs a, int tokens_p
     const RopeSegment& g = a.seg[rs];
     T* dst;
     if (!PAGED || g.page < 0) {
-      dst = static_cast<T*>(g.dst) + (n0 + rt) * g.d_tok + rh * g.d_head;
+      dst = static_cast<T*>(g.dst) + wide(n0 + rt, g.d_tok) + wide(rh, g.d_head);
     } else {
       const Place pl = places[rt];
-      if (pl.block < 0) continue;
-      dst = static_cast<T*>(a.pages) + (((pl.block + (int64_t)g.page * a.kv_heads + rh) << a.page_log2) + pl.slot) * a.D;
+      if (pl.at < 0) continue;
+      dst = static_cast<T*>(a.pages) + pl.at + wide(g.page * a.kv_heads + rh, a.D << a.page_log2);
     }
     if (turned && g.rotate) {
       uint32_t* xw = reinterpret_cast<uint32_t*>(&x);
