@@ -610,13 +610,19 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
   // us with 4, up to 9.5 with 3 (an extra join), 9.3 with 6
   p.min_tiles = 4;
   p.nsplit = 1;
-  // (more groups than counters fill the SMs without being cut)
-  if (split && p.groups <= QWM_PAGED_COUNTER_BYTES / 4) {
+  const int TK = D == 128 ? Shape<128>::TK : Shape<64>::TK;
+  const int64_t tiles = (max_visible + TK - 1) / TK + 1;              // of a group, at most
+  // Whole groups, a CTA each, take their waves x (tiles + 6 for a CTA's start and
+  // end); the line takes an even share of all places and 15 for start, parts and
+  // join (in tiles of 0.6 us: 12 groups of 517 keys 8.9 us whole and 9.3 shared, of
+  // 800 keys 11.4 and 9.3; 96 groups of 1000 keys 13.7 and 15.3).  More groups than
+  // counters fill the SMs without being cut.
+  const int64_t whole = (p.groups + nsm - 1) / nsm * (tiles + 6);
+  const int64_t shared = p.groups * (tiles + kGroupCost) / nsm + 15;
+  if (split && whole > shared && p.groups <= QWM_PAGED_COUNTER_BYTES / 4) {
     // a CTA per SM, or as many as have min_tiles places each
-    const int TK = D == 128 ? Shape<128>::TK : Shape<64>::TK;
-    const int64_t tiles = ((max_visible + TK - 1) / TK + 1 + kGroupCost) * p.groups;
-    const int64_t want = (tiles + p.min_tiles - 1) / p.min_tiles, most = nsm;
-    p.nsplit = (int)(want < most ? want : most);
+    const int64_t all = (tiles + kGroupCost) * p.groups, want = (all + p.min_tiles - 1) / p.min_tiles;
+    p.nsplit = (int)(want < nsm ? want : nsm);
   }
   return p;
 }
