@@ -29,14 +29,17 @@ constexpr int NT = (kWarps + 1) * 32;
 // cycles), in tiles' time (1.3 K cycles when all CTAs stream).
 constexpr int kGroupCost = 4;
 
-template <int D>
+// KP 16-key groups of a warp.  A tile's chain of products, exponentials and
+// products takes as long for two groups as for one, so two where the chain bounds
+// (64 channels; whole groups), one where HBM does and finer slots keep it busier
+// (128 channels on the line: 131071 keys 86 us with one, 91 with two; 517 keys x 12
+// whole groups 8.9 and 7.5).
+template <int D, int KP_>
 struct Shape {
-  static constexpr int KP = 128 / D;                           // 16-key groups of a warp: a tile's chain of products,
-                                                               // exponentials and products is as long for one as for
-                                                               // two, and 64 channels need twice the keys per time
+  static constexpr int KP = KP_;
   static constexpr int TK = 64 * KP;                           // keys per tile
   static constexpr int SLOT = TK * D * 2;                      // bytes of a K or V tile
-  static constexpr int NS = 8;                                 // slots of the ring: K, V, K, V, ...
+  static constexpr int NS = SLOT == 32768 ? 4 : 8;             // slots of the ring: K, V, K, V, ...
   static_assert(NS % 4 == 0, "an even number of tiles: a slot belongs to one warp group");
   static constexpr int MERGE = NS * SLOT;                      // the warps' O [warp][16][D], beside the ring so that
                                                                // the next group's tiles come in meanwhile
@@ -63,10 +66,10 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {   // a >= 0, b
   return ((a | b) >> 32) ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
 }
 
-template <typename T, int D>
+template <typename T, int D, int KP>
 __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
-  using L = Shape<D>;
-  constexpr int NS = L::NS, KP = L::KP, TK = L::TK;
+  using L = Shape<D, KP>;
+  constexpr int NS = L::NS, TK = L::TK;
   constexpr int KS = D / 16;                       // k16 steps of Q K^T, n16 blocks of P V
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -590,13 +593,18 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   } while (next_group());
 }
 
-template <typename T, int D>
+template <typename T, int D, int KP>
 cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
-  constexpr int smem = Shape<D>::TOTAL;
+  constexpr int smem = Shape<D, KP>::TOTAL;
   static bool done[64];
-  cudaError_t e = allow_smem(paged_step<T, D>, smem, done);
+  cudaError_t e = allow_smem(paged_step<T, D, KP>, smem, done);
   if (e != cudaSuccess) return e;
-  return launch_ahead(paged_step<T, D>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, map, a);
+  return launch_ahead(paged_step<T, D, KP>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, map, a);
+}
+template <typename T>
+cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, int D, cudaStream_t s) {
+  if (D == 64) return go<T, 64, 2>(a, map, s);
+  return a.nsplit > 1 ? go<T, 128, 1>(a, map, s) : go<T, 128, 2>(a, map, s);
 }
 
 }  // namespace
@@ -606,30 +614,34 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
   p.step = 1;
   p.groups = B * Hk;
   p.rows = rows;
-  // the shortest stretch, in places: a sequence of 64 to 200 keys takes 5.6 to 7.7
-  // us with 4, up to 9.5 with 3 (an extra join), 9.3 with 6
+  // the shortest stretch, in places (3 and 6 were no better from 300 to 4000 keys)
   p.min_tiles = 4;
   p.nsplit = 1;
-  const int TK = D == 128 ? Shape<128>::TK : Shape<64>::TK;
-  const int64_t tiles = (max_visible + TK - 1) / TK + 1;              // of a group, at most
-  // Whole groups, a CTA each, take their waves x (tiles + 6 for a CTA's start and
-  // end); the line takes an even share of all places and 15 for start, parts and
-  // join (in tiles of 0.6 us: 12 groups of 517 keys 8.9 us whole and 9.3 shared, of
-  // 800 keys 11.4 and 9.3; 96 groups of 1000 keys 13.7 and 15.3).  More groups than
-  // counters fill the SMs without being cut.
-  const int64_t whole = (p.groups + nsm - 1) / nsm * (tiles + 6);
-  const int64_t shared = p.groups * (tiles + kGroupCost) / nsm + 15;
-  if (split && whole > shared && p.groups <= QWM_PAGED_COUNTER_BYTES / 4) {
+  const int64_t tiles = (max_visible + 63) / 64 + 1;                  // of 64 keys, of a group at most
+  // Whole groups, a CTA each, take their waves x (a CTA's start and end and its
+  // tiles), the line an even share of all places after its start, parts and join;
+  // in 0.4 us, the time of 64 keys of 128 channels by themselves (0.3 us for 64
+  // channels, 0.7 when all SMs stream): 9 and 20 for start and end.  12 groups of
+  // 517 keys take 7.6 us whole and 9.2 shared, of 1000 keys 10.0 and 9.3; 96 groups
+  // of 1500 keys 14.4 and 18.6, 48 of 2000 keys 16.5 and 14.4.  Long groups are
+  // shared: they seldom have one length.  More groups than counters fill the SMs
+  // uncut.
+  const double tile = D == 128 ? 1.0 : 0.73, stream = 1.73 * tile * p.groups / nsm;
+  const double each = p.groups >= nsm ? 1.73 * tile : (stream > tile ? stream : tile);
+  const double whole = (double)((p.groups + nsm - 1) / nsm) * (9 + tiles * each);
+  const double shared = 20 + 1.3 * tile * (double)(tiles + kGroupCost) * p.groups / nsm;
+  if (split && (tiles > 40 || whole > shared) && p.groups <= QWM_PAGED_COUNTER_BYTES / 4) {
     // a CTA per SM, or as many as have min_tiles places each
-    const int64_t all = (tiles + kGroupCost) * p.groups, want = (all + p.min_tiles - 1) / p.min_tiles;
+    const int64_t places = ((max_visible + (D == 128 ? 63 : 127)) / (D == 128 ? 64 : 128) + 1 + kGroupCost) * p.groups;
+    const int64_t want = (places + p.min_tiles - 1) / p.min_tiles;
     p.nsplit = (int)(want < nsm ? want : nsm);
   }
   return p;
 }
 
 cudaError_t launch_paged_step(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s) {
-  if (dtype == QWM_F16) return D == 64 ? go<__half, 64>(a, map, s) : go<__half, 128>(a, map, s);
-  return D == 64 ? go<__nv_bfloat16, 64>(a, map, s) : go<__nv_bfloat16, 128>(a, map, s);
+  if (dtype == QWM_F16) return pick<__half>(a, map, D, s);
+  return pick<__nv_bfloat16>(a, map, D, s);
 }
 
 }  // namespace qwm
