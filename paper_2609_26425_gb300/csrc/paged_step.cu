@@ -8,8 +8,11 @@
 //
 // The tiles of all (sequence, cache head) groups form one line, which the CTAs (one
 // per SM) share out evenly whatever the lengths are; a CTA walks its stretch
-// group by group.  A producer warp keeps a ring of tiles (64 keys of 128
-// channels, 128 of 64) in flight by TMA; of eight warps four take a quarter of a
+// group by group.  Two producer warps, one of K and one of V, keep a ring of tiles
+// (64 or 128 keys) in flight by TMA.  One warp for both sent them one after the
+// other: 32 sequences of 100 to 30000 keys x 8 heads, window 8192, took 84.3 us and
+// take 80.8 with two; one token over 517 keys x 12 heads in pages of 16, where a
+// tile is many copies, 9.9 and 8.1.  Of eight more warps four take a quarter of a
 // tile's keys each, the other four those of the next tile, and carry their own
 // m, l and O through the group (no barrier between them in the loop); then they
 // are merged through shared memory.  The rows are the M = 16 side of mma.sync: a
@@ -24,7 +27,7 @@ namespace {
 using namespace ptx;
 
 constexpr int kWarps = 8;                // consumer warps
-constexpr int NT = (kWarps + 1) * 32;
+constexpr int NT = (kWarps + 2) * 32;    // and two producers, of K and of V
 // What a group costs a CTA beside its tiles (Queries, merge, output: about 5 K
 // cycles), in tiles' time (1.3 K cycles when all CTAs stream).
 constexpr int kGroupCost = 4;
@@ -75,7 +78,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   __shared__ uint64_t bars[2 * NS];
   __shared__ float s_ml[kWarps][16][2];
-  __shared__ int64_t s_scan[kWarps + 1], s_first;
+  __shared__ int64_t s_scan[kWarps + 2], s_first;
   __shared__ Seq s_sq;
   __shared__ Tiles s_tl;
   __shared__ int s_last, s_seq;
@@ -132,7 +135,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       __syncthreads();
       total = 0;
 #pragma unroll
-      for (int w = 0; w <= kWarps; ++w) {
+      for (int w = 0; w < kWarps + 2; ++w) {
         if (w < warp) before += s_scan[w];
         total += s_scan[w];
       }
@@ -213,16 +216,17 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     return true;
   };
 
-  if (warp == kWarps) {
-    // ---------------------------------------------------------- producer
-    // lane = box * 2 + channel half; a box is the part of a page that lies in the
-    // tile.  Boxes that no row sees are not read.
+  if (warp >= kWarps) {
+    // ---------------------------------------------------------- producers of K and V
+    // lane = box * 2 + channel half; a box is the part of a page (at most 64 tokens
+    // of it) that lies in the tile.  Boxes that no row sees are not read.
+    const int kv = warp - kWarps;
     const int box_log2 = min(a.page_log2, 6);
     const int box = lane >> 1, half = lane & 1;
     const bool mine = box < (TK >> box_log2) && half * 64 < D;
     const uint32_t dst = smem_u32(sm) + half * (TK * 128) + ((box << box_log2) * 128);
     bool ok = true;
-    int i = 0;                                     // slots filled
+    int i = 0;                                     // tiles sent
     do {
       piece();
       t1 = min(t1, tl.n);
@@ -234,7 +238,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       };
       bool want = false;
       int page = t0 < t1 ? page_of(t0, want) : 0;
-      for (int t = t0; t < t1 && ok && !a.idle; ++t) {
+      for (int t = t0; t < t1 && !a.idle; ++t) {
         bool want_n = false;
         int page_n = 0;
         if (t + 1 < t1) page_n = page_of(t + 1, want_n);   // its latency runs beside the copies
@@ -244,16 +248,13 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         }
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, want)) * (128u << box_log2);
         const int y = (tile_at(tl, t) * TK + (box << box_log2)) & ((1 << a.page_log2) - 1);
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const int s = i % NS;
-          if (i >= NS && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty(s), ((i / NS) - 1) & 1, a.wait_ns)))) break;
-          if (lane == 0) mbar_arrive_expect_tx(full(s), bytes);
-          __syncwarp();
-          if (want) tma_load_3d(dst + s * L::SLOT, &map, half * 64, y, (page * 2 + kv) * a.Hk + hk, full(s));
-          __syncwarp();
-          ++i;
-        }
+        const int s = (2 * i + kv) % NS;
+        if (i >= NS / 2 && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty(s), (i / (NS / 2) - 1) & 1, a.wait_ns)))) break;
+        if (lane == 0) mbar_arrive_expect_tx(full(s), bytes);
+        __syncwarp();
+        if (want) tma_load_3d(dst + s * L::SLOT, &map, half * 64, y, (page * 2 + kv) * a.Hk + hk, full(s));
+        __syncwarp();
+        ++i;
         page = page_n;
         want = want_n;
       }
@@ -261,7 +262,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     if (!ok) {
       // a wait ran out: let the copies in flight land before the CTA ends
       if (lane == 0) record_status(a.status, QWM_ERR_TIMEOUT);
-      for (int u = max(0, i - NS); u < i; ++u) mbar_wait(full(u % NS), (u / NS) & 1, kDrainNs);
+      for (int u = max(0, i - NS / 2); u < i; ++u) mbar_wait(full((2 * u + kv) % NS), (u / (NS / 2)) & 1, kDrainNs);
     }
     return;
   }
