@@ -36,7 +36,7 @@ constexpr int kGroupCost = 4;
 // products takes as long for two groups as for one, so two where the chain bounds
 // (64 channels; whole groups), one where HBM does and finer slots keep it busier
 // (128 channels on the line: 131071 keys 86 us with one, 91 with two; 517 keys x 12
-// whole groups 8.9 and 7.5).
+// whole groups 8.9 and 7.6; all four with one producer warp for K and V).
 template <int D, int KP_>
 struct Shape {
   static constexpr int KP = KP_;
@@ -620,17 +620,19 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
   p.nsplit = 1;
   const int64_t tiles = (max_visible + 63) / 64 + 1;                  // of 64 keys, of a group at most
   // Whole groups, a CTA each, take their waves x (a CTA's start and end and its
-  // tiles), the line an even share of all places after its start, parts and join;
-  // in 0.4 us, the time of 64 keys of 128 channels by themselves (0.3 us for 64
-  // channels, 0.7 when all SMs stream): 9 and 20 for start and end.  12 groups of
-  // 517 keys take 7.6 us whole and 9.2 shared, of 1000 keys 10.0 and 9.3; 96 groups
-  // of 1500 keys 14.4 and 18.6, 48 of 2000 keys 16.5 and 14.4.  Long groups are
-  // shared: they seldom have one length.  More groups than counters fill the SMs
-  // uncut.
-  const double tile = D == 128 ? 1.0 : 0.73, stream = 1.73 * tile * p.groups / nsm;
-  const double each = p.groups >= nsm ? 1.73 * tile : (stream > tile ? stream : tile);
-  const double whole = (double)((p.groups + nsm - 1) / nsm) * (9 + tiles * each);
-  const double shared = 20 + 1.3 * tile * (double)(tiles + kGroupCost) * p.groups / nsm;
+  // tiles), the line an even share of all places after its start, parts and join.
+  // In us, fitted to 1 to 8 sequences of 64 to 2000 keys; a tile's time is its own
+  // chain's, or its share of HBM when many CTAs stream.  Long groups are shared:
+  // they seldom have one length.  More groups than counters fill the SMs uncut.
+  // 12 groups of 1000 keys of 128 channels take 8.8 us whole and 9.2 shared, of
+  // 2000 keys 13.3 and 10.2; 48 of 1500 keys 11.2 and 13.0, of 2000 13.5 and 12.7;
+  // 8 groups of 1000 keys of 64 channels 6.7 and 8.4.  Near the change the two are
+  // close, and 96 groups of 2000 keys swing: 17 to 20 us either way.
+  const double chain = D == 128 ? 0.29 : 0.24, hbm = D == 128 ? 0.71 : 0.4;
+  const double stream = p.groups < nsm ? hbm * p.groups / nsm : hbm;
+  const double each = stream > chain ? stream : chain;
+  const double whole = (double)((p.groups + nsm - 1) / nsm) * ((D == 128 ? 4.0 : 2.8) + tiles * each);
+  const double shared = (D == 128 ? 8.2 : 7.6) + (D == 128 ? 0.44 : 0.33) * (double)(tiles + kGroupCost) * p.groups / nsm;
   if (split && (tiles > 40 || whole > shared) && p.groups <= QWM_PAGED_COUNTER_BYTES / 4) {
     // a CTA per SM, or as many as have min_tiles places each
     const int64_t places = ((max_visible + (D == 128 ? 63 : 127)) / (D == 128 ? 64 : 128) + 1 + kGroupCost) * p.groups;
