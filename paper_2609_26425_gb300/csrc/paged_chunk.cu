@@ -686,9 +686,14 @@ PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, 
   const int64_t tiles = (max_visible + TK - 1) / TK + 2;
   if (split) {
     // the split with the least waves x (tiles of a part + a CTA's fixed cost,
-    // about 6 tiles' time), 4 more for the join; parts of at least 4 tiles
+    // about 6 tiles' time), 4 more for the join; parts of at least 4 tiles.  Not
+    // past 8 waves, where a split evens out the last one only and the parts' fp32
+    // sums grow without end (170 to 256 MB in the first calls past it): 2500 Queries
+    // x 64 heads over 8192 keys take 502 us split and 457 whole, 3900 x 40 over 16384
+    // 854 either way, over 32768 1604 and 1672.
     int64_t best = 0;
     for (int64_t n = 1; n <= 64 && n * p.min_tiles <= tiles + p.min_tiles - 1; ++n) {
+      if (n > 1 && p.groups * n > 8 * (int64_t)nsm) break;
       const int64_t waves = ((int64_t)p.groups * n + nsm - 1) / nsm, cost = waves * ((tiles + n - 1) / n + 6) + (n > 1 ? 4 : 0);
       if (n == 1 || cost < best) {
         best = cost;
