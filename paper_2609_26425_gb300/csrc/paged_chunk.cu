@@ -144,40 +144,53 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   auto wait_all = [&](int i, uint32_t ph) -> bool {
     return __all_sync(0xFFFFFFFFu, mbar_wait(bar(i), ph, a.wait_ns));
   };
+  __syncthreads();                                    // the barriers are set up
   if (warp == W_MMA) {
     tmem_alloc(smem_u32(&s_tmem), 512);
     tmem_relinquish();
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tbase = s_tmem;
+  if (warp < W_MMA && (warp >> 2) < nqt) {
+    const int i = warp >> 2;
+    // Q_i: each warp its 32 rows, a row's 16-byte chunks over neighbouring lanes
+    uint8_t* sQ = sm + L::Q + i * NB * BLK;
+    constexpr int CH = D / 8;
+    {
+      uint4 v[CH];
+#pragma unroll
+      for (int k = 0; k < CH; ++k) {
+        const int idx = k * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
+        const uint32_t r = remA + min(i * 128 + rr, nrow - 1);
+        v[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (sq.q0 + tokA + r / G) * a.q_tok +
+                                               (hk * a.G + (int)(r % G)) * a.q_head + c * 8);
+      }
+#pragma unroll
+      for (int k = 0; k < CH; ++k) {
+        const int idx = k * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
+        if (i * 128 + rr >= nrow) v[k] = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[k];
+      }
+    }
+    fence_proxy_async_smem();
+  }
+  // The producers and the guard touch no TMEM: their first copies go out while it is
+  // being allocated and the Queries come in.  (All warps waiting for the allocation
+  // and the Queries loaded after it: 880 Queries x 12 heads 64.0 us against 62.5;
+  // three ragged prompts of 64 channels 79.5 against 80.5.)
+  uint32_t tbase = 0;
+  if (warp <= W_MMA) {
+    tc_fence_before();
+    named_bar_sync(1, (W_MMA + 1) * 32);
+    tc_fence_after();
+    tbase = s_tmem;
+  }
   const float sl2 = a.scale * 1.4426950408889634f;
 
   if (warp < W_MMA) {
     // ------------------------------------------------------------ softmax
     const int i = warp >> 2, row = tid & 127;
     if (i < nqt) {
-      // Q_i: each warp its 32 rows, a row's 16-byte chunks over neighbouring lanes
       uint8_t* sQ = sm + L::Q + i * NB * BLK;
       constexpr int CH = D / 8;
-      {
-        uint4 v[CH];
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-          const int idx = k * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
-          const uint32_t r = remA + min(i * 128 + rr, nrow - 1);
-          v[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (sq.q0 + tokA + r / G) * a.q_tok +
-                                                 (hk * a.G + (int)(r % G)) * a.q_head + c * 8);
-        }
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-          const int idx = k * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
-          if (i * 128 + rr >= nrow) v[k] = make_uint4(0, 0, 0, 0);
-          *reinterpret_cast<uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[k];
-        }
-      }
-      fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(B_QRDY + i));
 
