@@ -470,11 +470,9 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
         }
       }
       commit_e(bar(B_OFIN), e);
-      if (!ok) {
-        // a wait ran out: the MMAs already issued finish before TMEM is freed
-        mbar_wait(bar(B_OFIN), 0, kDrainNs);
-        s_err = 1;
-      }
+      // the MMAs issued finish before TMEM is freed: the softmax warps, which wait
+      // for them as well, may have given up
+      if (!mbar_wait(bar(B_OFIN), 0, kDrainNs) || !ok) s_err = 1;
     }
     __syncwarp();
   } else if (warp == W_K || warp == W_V) {
@@ -516,11 +514,10 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       page = page_n;
       want = want_n;
     }
-    if (!ok) {
-      // a wait ran out: let the copies in flight land before the CTA ends
-      s_err = 1;
-      for (int u = max(0, jt - ST); u < jt; ++u) mbar_wait(bar(full + (u & 1)), (u >> 1) & 1, kDrainNs);
-    }
+    if (!ok) s_err = 1;
+    // the last copies land before the CTA can end: the roles that wait for them may
+    // have given up on them
+    for (int u = max(0, jt - ST); u < jt; ++u) mbar_wait(bar(full + (u & 1)), (u >> 1) & 1, kDrainNs);
   } else {
     // ------------------------------------------------------------ guard of the Values
     bool ok = true;

@@ -259,11 +259,11 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         want = want_n;
       }
     } while (ok && next_group());
-    if (!ok) {
-      // a wait ran out: let the copies in flight land before the CTA ends
-      if (lane == 0) record_status(a.status, QWM_ERR_TIMEOUT);
-      for (int u = max(0, i - NS / 2); u < i; ++u) mbar_wait(full((2 * u + kv) % NS), (u / (NS / 2)) & 1, kDrainNs);
-    }
+    if (!ok && lane == 0) record_status(a.status, QWM_ERR_TIMEOUT);
+    // The last copies land before this warp ends, and so before the CTA can: the
+    // consumers may have given up on them.  Otherwise this is the wait the
+    // consumers are in as well.
+    for (int u = max(0, i - NS / 2); u < i; ++u) mbar_wait(full((2 * u + kv) % NS), (u / (NS / 2)) & 1, kDrainNs);
     return;
   }
 

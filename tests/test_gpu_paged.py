@@ -422,3 +422,27 @@ def test_calls_of_any_sizes_take_turns_on_one_workspace():
         for (c, b, q, _), w in list(zip(made, want)) + list(zip(made, want))[::-1]:
             assert torch.equal(qwm.qwm_paged_attend(c, b, q, workspace=shared), w)
     assert bool((shared[:65536] == 0).all())
+
+
+@pytest.mark.parametrize("new,held", [(1, 90), (1, 900), (4, 6000), (60, 100), (60, 900), (300, 5000)])
+@pytest.mark.parametrize("split", [False, True])
+def test_a_limit_near_a_copys_latency_leaves_nothing_in_flight(new, held, split):
+    """With the shortest limit some waits run out while their copies and MMAs are on
+    the way.  A CTA lets them land before it ends (its last tiles' too, which no
+    later wait of its own asks for), so the calls after it are exact."""
+    lens, Hk, D, page = [(new, held)], 2, 128, 16
+    q, keys, values, pages, table = make_case(71, lens, 4, Hk, D, BF, page)
+    cache, batch = build(lens, Hk, D, BF, page, pages, table)
+    ws = qwm.paged_attend_workspace(cache, batch, 4) if split else None
+    dq = q.cuda()
+    want = qwm.qwm_paged_attend(cache, batch, dq, workspace=ws).clone()
+    cold = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    for _ in range(12):
+        cold.zero_()                               # the pages leave the L2 cache
+        cache.set_wait_limit(1000)
+        qwm.qwm_paged_attend(cache, batch, dq, workspace=ws)
+        cache.set_wait_limit(2_000_000_000)
+        got = qwm.qwm_paged_attend(cache, batch, dq, workspace=ws)
+        assert cache.status() in (0, 5)
+        assert torch.equal(got, want)
+    assert cache.status() == 0
