@@ -87,7 +87,8 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   // tiles of a group of sequence b (one for a group that has rows and sees
   // nothing: its output is written all the same)
   auto tiles_of = [&](int b, Seq& sq, Tiles& tl) -> int {
-    if (!load_seq(a, b, sq) && blockIdx.x == 0) record_status(a.status, QWM_ERR_INVALID_ARG);
+    // on the line CTA 0 looks at every sequence, of whole groups each CTA at its own
+    if (!load_seq(a, b, sq) && (a.nsplit == 1 || blockIdx.x == 0)) record_status(a.status, QWM_ERR_INVALID_ARG);
     if (sq.qn == 0) return 0;
     tl = make_tiles<TK>(sq.kv - sq.qn, sq.kv - 1, sq.kv, a.block, a.window, a.sinks);
     return max(tl.n, 1);

@@ -446,3 +446,30 @@ def test_a_limit_near_a_copys_latency_leaves_nothing_in_flight(new, held, split)
         assert cache.status() in (0, 5)
         assert torch.equal(got, want)
     assert cache.status() == 0
+
+
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("b", [0, 1, 2])
+@pytest.mark.parametrize("fault", ["offset", "long", "negative", "page"])
+def test_step_calls_record_entries_out_of_range_of_every_sequence(fault, b, split):
+    lens, Hk, D, page = [(1, 3000), (2, 3000), (1, 3000)], 2, 128, 16
+    q, keys, values, pages, table = make_case(81, lens, 2, Hk, D, BF, page)
+    off, held = offsets(lens), torch.tensor([kv for _, kv in lens], dtype=torch.int32)
+    sound = {0, 1, 2} - {b}
+    if fault == "offset":                          # b's end past its bound, or before its start
+        off[b + 1 if b < 2 else b] += 9 if b < 2 else -9
+        sound = {0, 1, 2} - ({b, b + 1} if b < 2 else {1, 2})
+    elif fault == "page":
+        table[b, 150] = pages.shape[0]
+    else:
+        held[b] = 3001 if fault == "long" else -1
+    cache, _ = build(lens, Hk, D, BF, page, pages, table)
+    batch = qwm.PagedBatch(off.cuda(), held.cuda(), table.cuda(), 2, 3000)
+    ws = qwm.paged_attend_workspace(cache, batch, 2) if split else None
+    assert (ws is not None) == split
+    out = qwm.qwm_paged_attend(cache, batch, q.cuda(), workspace=ws).double().cpu()
+    assert cache.status() == 1 and cache.status() == 0
+    want = attend64(q, keys, values, lens, 1, 0, 0)
+    for i in sound:                                # the others are as they should be
+        r = slice(int(offsets(lens)[i]), int(offsets(lens)[i + 1]))
+        assert bool(((out[r] - want[0][r]).abs() <= want[2][r]).all())
