@@ -149,6 +149,12 @@ __device__ __forceinline__ bool load_seq(const A& a, int b, Seq& s) {
   return ok;
 }
 
+// Whether the offsets cover the call's rows: a row of no sequence is not written.
+template <class A>
+__device__ __forceinline__ bool rows_covered(const A& a) {
+  return a.q_off[0] == 0 && a.q_off[a.B] == a.N;
+}
+
 // The tokens a Query at token p sees: [0, min(sinks, hi)) and [lo, hi).
 struct Span {
   int32_t lo, hi;

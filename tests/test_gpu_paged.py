@@ -473,3 +473,22 @@ def test_step_calls_record_entries_out_of_range_of_every_sequence(fault, b, spli
     for i in sound:                                # the others are as they should be
         r = slice(int(offsets(lens)[i]), int(offsets(lens)[i + 1]))
         assert bool(((out[r] - want[0][r]).abs() <= want[2][r]).all())
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("off", [(0, 1, -1), (1, 1, 0), (0, 0, None)])
+@pytest.mark.parametrize("split", [False, True])
+def test_rows_of_no_sequence_are_recorded(new, off, split):
+    lens, Hk, D, page = [(new, 3000), (new, 3000)], 2, 128, 16
+    q, _, _, pages, table = make_case(82, lens, 2, Hk, D, BF, page)
+    cache, sound = build(lens, Hk, D, BF, page, pages, table)
+    offs = [off[0], off[1] * new, 0 if off[2] is None else 2 * new + off[2]]
+    batch = qwm.PagedBatch(torch.tensor(offs, dtype=torch.int32).cuda(), sound.tensors[1], sound.tensors[2], new, 3000)
+    ws = qwm.paged_attend_workspace(cache, batch, 2) if split else None
+    k = torch.zeros(2 * new, Hk, D, dtype=BF, device="cuda")
+    qwm.qwm_paged_attend(cache, sound, q.cuda(), workspace=ws)
+    assert cache.status() == 0
+    qwm.qwm_paged_attend(cache, batch, q.cuda(), workspace=ws)
+    assert cache.status() == 1 and cache.status() == 0
+    qwm.qwm_paged_append(cache, batch, k, k)
+    assert cache.status() == 1
