@@ -142,17 +142,13 @@ __device__ __forceinline__ bool load_seq(const A& a, int b, Seq& s) {
   const int64_t kv = a.kv_len[b];
   int64_t cap = (int64_t)a.table_stride << a.page_log2;
   if (cap > a.max_kv) cap = a.max_kv;
-  const bool ok = q0 >= 0 && q1 >= q0 && q1 <= a.N && q1 - q0 <= a.max_q && kv >= 0 && kv <= cap;
+  // the first sequence starts at row 0 and the last ends at N: no row is left out
+  const bool ok = (uint64_t)q0 <= (b > 0 ? (uint64_t)a.N : 0u) && q1 >= q0 && q1 <= a.N &&
+                  (b < a.B - 1 || q1 == a.N) && q1 - q0 <= a.max_q && kv >= 0 && kv <= cap;
   s.q0 = ok ? q0 : 0;
   s.qn = ok ? (int32_t)(q1 - q0) : 0;
   s.kv = ok ? (int32_t)kv : 0;
   return ok;
-}
-
-// Whether the offsets cover the call's rows: a row of no sequence is not written.
-template <class A>
-__device__ __forceinline__ bool rows_covered(const A& a) {
-  return a.q_off[0] == 0 && a.q_off[a.B] == a.N;
 }
 
 // The tokens a Query at token p sees: [0, min(sinks, hi)) and [lo, hi).

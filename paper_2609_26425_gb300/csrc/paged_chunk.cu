@@ -124,9 +124,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   // the row tiles with the most keys first
   const int rt = rtiles - 1 - (int)(blockIdx.x % rtiles), part = blockIdx.x / rtiles;
   Seq sq;
-  const bool sound = load_seq(a, b, sq);
-  if (blockIdx.x == 0 && hk == 0 && tid == 0 && !(sound && (b > 0 || rows_covered(a))))
-    record_status(a.status, QWM_ERR_INVALID_ARG);
+  if (!load_seq(a, b, sq) && blockIdx.x == 0 && hk == 0 && tid == 0) record_status(a.status, QWM_ERR_INVALID_ARG);
   const int64_t rows = (int64_t)sq.qn * a.G;
   const int64_t r0 = (int64_t)rt * ROWS;
   if (r0 >= rows) return;

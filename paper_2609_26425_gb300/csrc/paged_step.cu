@@ -111,7 +111,6 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   // each thread with a run of sequences.  Without a workspace, a CTA takes the
   // group of its number.
   const bool split = a.nsplit > 1;
-  const bool covered = blockIdx.x != 0 || tid != 0 || rows_covered(a);
   Seq sq;
   Tiles tl;
   int b, n, hk;
@@ -145,7 +144,6 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     before *= a.Hk;
     mine *= a.Hk;
     total *= a.Hk;
-    if (!covered) record_status(a.status, QWM_ERR_INVALID_ARG);
     share = max(divide(total + gridDim.x - 1, gridDim.x), (int64_t)a.min_tiles);
     x0 = blockIdx.x * share;
     if (x0 >= total) return;
@@ -197,7 +195,6 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     b = blockIdx.x / a.Hk;
     hk = blockIdx.x % a.Hk;
     n = tiles_of(b, sq, tl);
-    if (!covered) record_status(a.status, QWM_ERR_INVALID_ARG);
     if (n == 0) return;
     x0 = g0 = 0;
     x1 = n + kGroupCost;
