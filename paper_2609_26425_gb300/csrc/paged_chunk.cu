@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
           }
         }
         if (has && parts == 1 && a.lse)
-          a.lse[(int64_t)head * a.N + sq.q0 + tok] = m_run == -INFINITY ? -INFINITY : m_run * a.scale + logf(l_run);
+          a.lse[(int64_t)head * a.N + sq.q0 + tok] = m_run * a.scale + logf(l_run);   // -inf + log 0; NaN with a NaN l
         if (has && parts > 1) a.part_ml[pr] = make_float2(m_run, l_run);
       }
     }
@@ -669,7 +669,7 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
     *reinterpret_cast<uint4*>(dst + 32 * k) =
         make_uint4(Elem<T>::pack(v[k][0].x * inv, v[k][0].y * inv), Elem<T>::pack(v[k][0].z * inv, v[k][0].w * inv),
                    Elem<T>::pack(v[k][1].x * inv, v[k][1].y * inv), Elem<T>::pack(v[k][1].z * inv, v[k][1].w * inv));
-  if (a.lse && lane < 8) a.lse[(int64_t)head * a.N + sq.q0 + tok] = m == -INFINITY ? -INFINITY : m * a.scale + logf(l);
+  if (a.lse && lane < 8) a.lse[(int64_t)head * a.N + sq.q0 + tok] = m * a.scale + logf(l);
 }
 
 template <typename T, int D>

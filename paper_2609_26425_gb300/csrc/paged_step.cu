@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
       T* dst = static_cast<T*>(a.out) + (sq.q0 + tok) * a.o_tok + (int64_t)h * a.o_head + 4 * c;
       *reinterpret_cast<uint2*>(dst) = make_uint2(Elem<T>::pack(v.x * inv, v.y * inv), Elem<T>::pack(v.z * inv, v.w * inv));
-      if (a.lse && c == 0) a.lse[(int64_t)h * a.N + sq.q0 + tok] = m == -INFINITY ? -INFINITY : m * a.scale + logf(l);
+      if (a.lse && c == 0) a.lse[(int64_t)h * a.N + sq.q0 + tok] = m * a.scale + logf(l);   // -inf + log 0; NaN with a NaN l
     };
     // (m, l, O) of row r's channels 4c .. over the first `count` entries of s_ml and so
     auto merge = [&](int count, int r, int c, float& m, float& l, float4& v) {

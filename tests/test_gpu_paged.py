@@ -492,3 +492,24 @@ def test_rows_of_no_sequence_are_recorded(new, off, split):
     assert cache.status() == 1 and cache.status() == 0
     qwm.qwm_paged_append(cache, batch, k, k)
     assert cache.status() == 1
+
+
+@pytest.mark.parametrize("new,held", [(1, 40), (1, 3000), (3, 3000), (60, 3000)])
+@pytest.mark.parametrize("split", [False, True])
+def test_a_nan_logit_is_nan_in_the_lse(new, held, split):
+    """Also where every logit of a row is NaN, so that it has no running maximum: its
+    lse is not the -inf of a row that sees nothing."""
+    lens, Hk, D, page = [(new, held)], 2, 128, 16
+    q, keys, values, pages, table = make_case(83, lens, 4, Hk, D, BF, page)
+    q[0, 1, 5] = math.nan                          # one row: all of its logits
+    j = held - 1                                   # the last token's Key of head 1: the last rows' last logit
+    pages[int(table[0, j // page]), 0, 1, j % page, 3] = math.nan
+    cache, batch = build(lens, Hk, D, BF, page, pages, table)
+    ws = qwm.paged_attend_workspace(cache, batch, 4) if split else None
+    out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True, workspace=ws)
+    want = torch.zeros(new, 4, dtype=torch.bool)
+    want[0, 1] = True
+    want[-1, 2:] = True
+    assert torch.equal(out.isnan().cpu(), want[..., None].expand(new, 4, D))
+    assert torch.equal(lse.isnan().cpu(), want.t())
+    assert bool(torch.isfinite(lse.cpu()[~want.t()]).all()) and cache.status() == 0
