@@ -14,9 +14,9 @@
 // it: P is taken against the maximum known before the tile, one pass over S with
 // the exponentials (32 a cycle and SM) as its only bound.  P, l and O are
 // floating-point multiples of the same power of two, so a maximum that has grown
-// costs nothing until P could leave its type's range; a half tile whose sum is
-// above 2^kTau (no P above it can hide in a smaller sum) is taken again against
-// its rows' new maxima.
+// costs nothing until P has grown by 2^kTau; a half tile whose sum is above that
+// (no P above it can hide in a smaller sum) is taken again against its rows' new
+// maxima.
 // Few rows over many keys are split along the keys; the parts' O, m and l go
 // through global memory to a second kernel over all SMs, launched ahead so that
 // it stands ready.  (A join by a group's last CTA took 11 us of 69 at 880 Queries
@@ -87,6 +87,14 @@ __device__ __forceinline__ uint32_t bits(int a, int b) {
   const uint32_t hi = b <= 0 ? 0u : (b >= 32 ? 0xFFFFFFFFu : (1u << b) - 1u);
   const uint32_t lo = a <= 0 ? 0u : (a >= 32 ? 0xFFFFFFFFu : (1u << a) - 1u);
   return hi & ~lo;
+}
+
+constexpr float pow2(int e) { return e > 0 ? 2.0f * pow2(e - 1) : (e < 0 ? 0.5f * pow2(e + 1) : 1.0f); }
+// Natural-log sum-exp of a row: `m` is the power that its P were taken against, l
+// their sum.  -inf (and log 0) where nothing was seen, NaN with a NaN sum.
+template <typename T>
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return (m - (float)Elem<T>::kBias + log2f(l * pow2(Elem<T>::kBias))) * 0.69314718055994531f;
 }
 
 template <typename T, int D>
@@ -202,11 +210,13 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       const uint32_t tS = tbase + 128 * i + lrow, tO = tbase + 128 * NQ + D * i + lrow;
       float m_run = has ? -INFINITY : 0.0f, l_run = 0.0f;
       const uint64_t SL = f2pack(sl2, sl2);
-      const float kMost = exp2f(Elem<T>::kTau);
+      constexpr float kMost = pow2(Elem<T>::kTau - Elem<T>::kBias);
+      // P = 2^(s sl2 - power(m_run))
+      auto power = [&](float m) { return fmaf(m, sl2, (float)Elem<T>::kBias); };
       // Raises every row of the warp to its own maximum, and O with it (the P V
       // before it are complete)
       auto raise = [&](float mt, bool rescale) {
-        const float alpha = mt > m_run ? ex2f((m_run - mt) * sl2) : 1.0f;
+        const float alpha = mt > m_run ? ex2f(power(m_run) - power(mt)) : 1.0f;
         m_run = fmaxf(m_run, mt);
         l_run *= alpha;
         if (rescale) {
@@ -264,7 +274,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
         uint32_t pk[32];
         uint64_t sum, MB;
         auto begin_half = [&]() {
-          const float mb = m_run == -INFINITY ? 0.0f : m_run * sl2;
+          const float mb = m_run == -INFINITY ? 0.0f : power(m_run);
           MB = f2pack(-mb, -mb);
           sum = f2pack(0.0f, 0.0f);
         };
@@ -418,8 +428,8 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
           }
         }
         if (has && parts == 1 && a.lse)
-          a.lse[(int64_t)head * a.N + sq.q0 + tok] = m_run * a.scale + logf(l_run);   // -inf + log 0; NaN with a NaN l
-        if (has && parts > 1) a.part_ml[pr] = make_float2(m_run, l_run);
+          a.lse[(int64_t)head * a.N + sq.q0 + tok] = log_sum<T>(power(m_run), l_run);
+        if (has && parts > 1) a.part_ml[pr] = make_float2(power(m_run), l_run);
       }
     }
   } else if (warp == W_MMA) {
@@ -587,7 +597,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
 }
 
 // The parts of the groups that were cut, in part order: m = max m_p, l = sum l_p
-// 2^((m_p - m) c), O = sum O_p 2^((m_p - m) c) / l.  A CTA takes 64 rows, a warp 8
+// 2^(m_p - m), O = sum O_p 2^(m_p - m) / l, with m as powers of two.  A CTA takes 64 rows, a warp 8
 // of them; lanes 8 rows x 4 groups of 8 channels, so that reads (a part lies
 // [channels / 4][row]) and writes are whole sectors.
 constexpr int JR = 64;
@@ -613,7 +623,6 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
   const int64_t group = ((int64_t)b * a.Hk + hk) * rtiles + rt;
   const float2* ml = a.part_ml + group * a.nsplit * ROWS + r;
   const float4* po = reinterpret_cast<const float4*>(a.part_o) + group * a.nsplit * ROWS * (D / 4) + r;
-  const float sl2 = a.scale * 1.4426950408889634f;
   constexpr int CB = D / 32, PU = 4;                  // channel blocks of a lane, parts in flight
   float m = -INFINITY, l = 0.0f;
   float4 v[CB][2];
@@ -638,7 +647,7 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
 #pragma unroll
     for (int u = 0; u < PU; ++u) mn = fmaxf(mn, w[u].x);
     const float ref = mn == -INFINITY ? 0.0f : mn;
-    const float al = ex2f((m - ref) * sl2);
+    const float al = ex2f(m - ref);
     m = mn;
     l *= al;
 #pragma unroll
@@ -650,7 +659,7 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
 #pragma unroll
     for (int u = 0; u < PU; ++u) {
       if (pb + u >= parts) break;
-      const float f = ex2f((w[u].x - ref) * sl2);
+      const float f = ex2f(w[u].x - ref);
       l = fmaf(w[u].y, f, l);
 #pragma unroll
       for (int k = 0; k < CB; ++k)
@@ -669,7 +678,7 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
     *reinterpret_cast<uint4*>(dst + 32 * k) =
         make_uint4(Elem<T>::pack(v[k][0].x * inv, v[k][0].y * inv), Elem<T>::pack(v[k][0].z * inv, v[k][0].w * inv),
                    Elem<T>::pack(v[k][1].x * inv, v[k][1].y * inv), Elem<T>::pack(v[k][1].z * inv, v[k][1].w * inv));
-  if (a.lse && lane < 8) a.lse[(int64_t)head * a.N + sq.q0 + tok] = m * a.scale + logf(l);
+  if (a.lse && lane < 8) a.lse[(int64_t)head * a.N + sq.q0 + tok] = log_sum<T>(m, l);
 }
 
 template <typename T, int D>

@@ -513,3 +513,28 @@ def test_a_nan_logit_is_nan_in_the_lse(new, held, split):
     assert torch.equal(out.isnan().cpu(), want[..., None].expand(new, 4, D))
     assert torch.equal(lse.isnan().cpu(), want.t())
     assert bool(torch.isfinite(lse.cpu()[~want.t()]).all()) and cache.status() == 0
+
+
+@pytest.mark.parametrize("new", [3, 150])
+def test_large_values_under_a_rising_maximum(new):
+    """Logits that rise by 2^38 over the keys, and Values of 2^100: a sum kept against
+    a maximum that was left behind may not leave fp32's range."""
+    kv, D, page = 700, 128, 16
+    lens = [(new, kv)]
+    q, keys, values, pages, table = make_case(84, lens, 2, 1, D, BF, page)
+    keys[0] = 0.05 * keys[0].float()
+    keys[0][:, 0, 5] = torch.arange(kv, dtype=torch.float32) / 17
+    keys[0] = keys[0].to(BF)
+    q = 0.2 * q.float()
+    q[:, :, 5] = 1.0
+    q = q.to(BF)
+    values[0] = (values[0].float() * 2.0 ** 100).to(BF)
+    for i in range((kv + page - 1) // page):
+        n = min(page, kv - i * page)
+        pages[int(table[0, i]), 0, :, :n] = keys[0][i * page:i * page + n].permute(1, 0, 2)
+        pages[int(table[0, i]), 1, :, :n] = values[0][i * page:i * page + n].permute(1, 0, 2)
+    cache, batch = build(lens, 1, D, BF, page, pages, table)
+    want = attend64(q, keys, values, lens, 1, 0, 0, scale=1.0)
+    for ws in (None, qwm.paged_attend_workspace(cache, batch, 2)):
+        out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), sm_scale=1.0, want_lse=True, workspace=ws)
+        compare(out, lse, want)
