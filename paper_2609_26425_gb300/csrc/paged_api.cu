@@ -1,6 +1,7 @@
 // paged_api.cu -- host side of the rotary and paged entry points of
 // include/qwm.h: argument validation, the paged descriptor and launch plans.
 #include <new>
+#include <utility>
 
 #include "paged.cuh"
 
@@ -41,10 +42,33 @@ bool rows_ok(const qwm_rows* r) {
          (r->head_stride & 7) == 0 && r->token_stride >= 0 && r->head_stride >= 0 && r->heads >= 1 &&
          r->token_stride < (int64_t)1 << 31 && r->head_stride < (int64_t)1 << 31;
 }
+// Whether rows d + n ts + h hs and n' ts + h' hs of two tensors [N][H] share an
+// element for some |n - n'| < N and |h - h'| < H: by the differences of the shorter
+// axis, with those of the other that come nearest.  `self`: not a row and itself
+// (both strides are positive, or 0 with one row).
+bool rows_meet(int64_t d, int64_t N, int64_t ts, int64_t H, int64_t hs, int D, bool self) {
+  if (H > N) {
+    std::swap(H, N);
+    std::swap(hs, ts);
+  }
+  for (int64_t h = 1 - H; h < H; ++h) {
+    const int64_t x = d + h * hs;
+    for (int64_t near = ts > 0 ? -x / ts - 1 : 0, i = 0; i < (ts > 0 ? 3 : 1); ++i) {
+      const int64_t n = near + i;
+      if (n <= -N || n >= N || (self && n == 0 && h == 0)) continue;
+      const int64_t gap = x + n * ts;
+      if (gap < D && gap > -D) return true;
+    }
+  }
+  return false;
+}
 // A tensor that is written: no two (token, head) may share a row.
 bool out_ok(const qwm_rows* r, int64_t N, int D) {
   if (!rows_ok(r)) return false;
-  return (N <= 1 || r->token_stride >= D) && (r->heads <= 1 || r->head_stride >= D);
+  const int64_t H = r->heads, ts = N > 1 ? r->token_stride : 0, hs = H > 1 ? r->head_stride : 0;
+  if ((N > 1 && ts < D) || (H > 1 && hs < D)) return false;
+  // one axis's rows lie within a step of the other, or it takes a closer look
+  return N <= 1 || H <= 1 || ts >= (H - 1) * hs + D || hs >= (N - 1) * ts + D || !rows_meet(0, N, ts, H, hs, D, true);
 }
 
 qwm_status check_rope(const qwm_rope_config* c) {

@@ -168,3 +168,19 @@ def test_refusals():
         qwm.Rope(inv_freq(pairs), pairs)                                # not on the GPU
     with pytest.raises(ValueError):
         qwm.Rope(inv_freq(pairs).cuda(), (22, 21, 20))
+
+
+@pytest.mark.parametrize("token,head,heads,n", [
+    (256, 128, 2, 5), (128, 640, 2, 5), (264, 136, 2, 5),      # token-major, head-major, padded
+    (384, 256, 2, 4), (136, 272, 2, 2),                        # rows of one axis between those of the other
+    (8, 8, 1, 1), (128, 0, 1, 5)])                             # a stride that is never used
+def test_outputs_of_any_order_whose_rows_are_apart(token, head, heads, n):
+    pairs = (22, 21, 21)
+    freq, pos = inv_freq(pairs), positions(6, n)
+    rope = qwm.Rope(freq.cuda(), pairs)
+    x = torch.randn(n, heads, 128, generator=torch.Generator().manual_seed(8)).to(torch.bfloat16)
+    flat = torch.full(((n - 1) * token + (heads - 1) * head + 128,), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = flat.as_strided((n, heads, 128), (token, head, 1))
+    assert qwm.qwm_rope(rope, x.cuda(), pos.cuda(), q_out=out) is out
+    check(out, x, pos, freq, pairs, True, 1.0)
+    assert int((flat == 7.0).sum()) >= flat.numel() - x.numel()

@@ -58,3 +58,15 @@ def test_calls_without_a_cache_or_a_batch_are_refused(L):
     assert L.qwm_paged_init(ct.byref(h), paged.QwmPagedConfig(8, 80, 64, 0, 5), 4096, 1 << 30, None) == 2
     assert L.qwm_paged_init(ct.byref(h), paged.QwmPagedConfig(8, 128, 64, 0, 5), 4097, 1 << 30, None) == 1
     assert L.qwm_paged_init(ct.byref(h), paged.QwmPagedConfig(8, 128, 64, 0, 5), 4096, 256, None) == 3
+
+
+def test_written_rows_that_share_memory_are_refused(L):
+    def call(token, head, heads, n):
+        cfg = paged.QwmRopeConfig(128, 0, (ct.c_int32 * 3)(22, 21, 21), 1)
+        return L.qwm_rope(cfg, 4096, 4096, n, rows(heads), rows(heads, token=token, head=head), None, None, None)
+
+    assert call(128, 128, 2, 4) == 1                        # (n, 1) is (n + 1, 0)
+    assert call(256, 128, 3, 4) == 1                        # (n, 2) is (n + 1, 0)
+    assert call(128, 384, 2, 4) == 1                        # head-major, the last token is the next head's first
+    assert call(384, 256, 4, 4) == 1                        # (2, 0) is (0, 3)
+    assert call(120, 512, 2, 4) == 1 and call(512, 120, 2, 4) == 1
