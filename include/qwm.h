@@ -401,8 +401,8 @@ typedef struct qwm_rope_config {
  * reduced angle at every int32 position, the rotation is in fp32, the result
  * rounded once.  inv_freq: fp32 [P]; pos: int32 [N][3].  q_out and k_out have
  * the heads of q and k and may be the same tensors as q and k (same data and
- * strides: in place); they must not overlap them otherwise.  k and k_out may
- * both be NULL.  N = 0 is a no-op. */
+ * strides: in place); they must not overlap them otherwise (refused where base
+ * addresses or strides are equal).  k and k_out may both be NULL.  N = 0 is a no-op. */
 QWM_API qwm_status qwm_rope(const qwm_rope_config* cfg, const float* inv_freq, const int32_t* pos, int64_t N,
                             const qwm_rows* q, const qwm_rows* q_out, const qwm_rows* k, const qwm_rows* k_out,
                             void* stream);
@@ -489,9 +489,9 @@ typedef struct qwm_mask {
  * h / (q_heads / kv_heads)).  Logits, softmax statistics and sums are fp32; the
  * probabilities enter the tensor cores in the cache's type.  lse: fp32
  * [q_heads][tokens] natural-log sum-exp of the scaled logits, or NULL.  out must
- * not overlap q.  0 < sm_scale <= 1e38.  A row that sees nothing gets 0 and an
- * lse of -inf.  What a row does not see does
- * not reach it, infinities and NaN included.
+ * not overlap q (refused where base addresses or strides are equal).
+ * 0 < sm_scale <= 1e38.  A row that sees nothing gets 0 and an lse of -inf.  What a
+ * row does not see does not reach it, infinities and NaN included.
  * workspace: device scratch of at least qwm_paged_attend_workspace_bytes bytes
  * for the same arguments (256-byte aligned), its first QWM_PAGED_COUNTER_BYTES
  * zeroed once when it is made (each call leaves them at zero); the call then

@@ -71,6 +71,25 @@ bool out_ok(const qwm_rows* r, int64_t N, int D) {
   return N <= 1 || H <= 1 || ts >= (H - 1) * hs + D || hs >= (N - 1) * ts + D || !rows_meet(0, N, ts, H, hs, D, true);
 }
 
+// Whether an output [N][heads] overlaps its input.  Tensors of one base address, or of
+// equal strides, are told exactly; of others nothing is known here (false).
+bool overlaps(const qwm_rows* in, const qwm_rows* out, int64_t N, int D) {
+  const int64_t H = in->heads;
+  const int64_t ts = N > 1 ? in->token_stride : 0, hs = H > 1 ? in->head_stride : 0;
+  const int64_t to = N > 1 ? out->token_stride : 0, ho = H > 1 ? out->head_stride : 0;
+  const int64_t d = (static_cast<const char*>(out->data) - static_cast<const char*>(in->data)) / 2;
+  if (d == 0) return true;
+  if (d >= (N - 1) * ts + (H - 1) * hs + D || -d >= (N - 1) * to + (H - 1) * ho + D || ts != to || hs != ho) return false;
+  const int64_t w = (H - 1) * hs + D, r = ts >= w ? (d % ts + ts) % ts : 0;   // slices of one projection lie apart
+  return !(r >= w && ts - r >= w) && rows_meet(d, N, ts, H, hs, D, false);
+}
+// An output over its own input: the same rows, or none of them.
+bool in_place_ok(const qwm_rows* in, const qwm_rows* out, int64_t N, int D) {
+  const bool same = in->data == out->data && (N <= 1 || in->token_stride == out->token_stride) &&
+                    (in->heads <= 1 || in->head_stride == out->head_stride);
+  return same || !overlaps(in, out, N, D);
+}
+
 qwm_status check_rope(const qwm_rope_config* c) {
   if (c->dtype != QWM_BF16 && c->dtype != QWM_F16) return QWM_ERR_UNSUPPORTED;
   if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8) return QWM_ERR_UNSUPPORTED;
@@ -117,8 +136,12 @@ qwm_status rope_impl(const qwm_rope_config* cfg, const float* inv_freq, const in
   if (N == 0) return QWM_OK;
   if (!inv_freq || !pos) return QWM_ERR_INVALID_ARG;
   if (N > kMost) return QWM_ERR_UNSUPPORTED;
-  if (!rows_ok(q) || !out_ok(q_out, N, cfg->head_dim) || q->heads != q_out->heads) return QWM_ERR_INVALID_ARG;
-  if (k && (!rows_ok(k) || !out_ok(k_out, N, cfg->head_dim) || k->heads != k_out->heads)) return QWM_ERR_INVALID_ARG;
+  if (!rows_ok(q) || !out_ok(q_out, N, cfg->head_dim) || q->heads != q_out->heads ||
+      !in_place_ok(q, q_out, N, cfg->head_dim))
+    return QWM_ERR_INVALID_ARG;
+  if (k && (!rows_ok(k) || !out_ok(k_out, N, cfg->head_dim) || k->heads != k_out->heads ||
+            !in_place_ok(k, k_out, N, cfg->head_dim)))
+    return QWM_ERR_INVALID_ARG;
   qwm::RopeArgs a{};
   a.D = cfg->head_dim;
   a.N = N;
@@ -264,7 +287,9 @@ qwm_status qwm_paged_append(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   if (rope && (!inv_freq || !pos)) return QWM_ERR_INVALID_ARG;
   if (!rows_ok(k) || !rows_ok(v) || k->heads != c->cfg.kv_heads || v->heads != c->cfg.kv_heads)
     return QWM_ERR_INVALID_ARG;
-  if (q && (!rows_ok(q) || !out_ok(q_out, b->tokens, D) || q->heads != q_out->heads)) return QWM_ERR_INVALID_ARG;
+  if (q && (!rows_ok(q) || !out_ok(q_out, b->tokens, D) || q->heads != q_out->heads ||
+            !in_place_ok(q, q_out, b->tokens, D)))
+    return QWM_ERR_INVALID_ARG;
   qwm::RopeArgs a{};
   a.D = D;
   a.N = b->tokens;
@@ -309,7 +334,8 @@ qwm_status qwm_paged_attend(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return QWM_ERR_INVALID_ARG;
   if (b->tokens == 0) return QWM_OK;
   const int D = c->cfg.head_dim;
-  if (!rows_ok(q) || !out_ok(out, b->tokens, D) || q->heads != out->heads || q->heads % c->cfg.kv_heads)
+  if (!rows_ok(q) || !out_ok(out, b->tokens, D) || q->heads != out->heads || q->heads % c->cfg.kv_heads ||
+      overlaps(q, out, b->tokens, D))
     return QWM_ERR_INVALID_ARG;
   PagedPlan p = make_plan(c, b, q->heads, mask, workspace != nullptr);
   if (p.nsplit > 1 && workspace_bytes < carve(p, D).total) p = make_plan(c, b, q->heads, mask, false);

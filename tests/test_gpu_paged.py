@@ -538,3 +538,22 @@ def test_large_values_under_a_rising_maximum(new):
     for ws in (None, qwm.paged_attend_workspace(cache, batch, 2)):
         out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), sm_scale=1.0, want_lse=True, workspace=ws)
         compare(out, lse, want)
+
+
+@pytest.mark.parametrize("new,held", [(3, 40), (2, 3000), (70, 3000)])
+def test_an_output_over_the_queries_is_refused_and_one_beside_them_is_not(new, held):
+    lens, Hk, D, page = [(new, held)], 2, 128, 16
+    q, keys, values, pages, table = make_case(91, lens, 4, Hk, D, BF, page)
+    cache, batch = build(lens, Hk, D, BF, page, pages, table)
+    ws = qwm.paged_attend_workspace(cache, batch, 4)
+    wide = torch.zeros(new, 12, D, dtype=BF, device="cuda")
+    wide[:, :4] = q.cuda()
+    for out in (wide[:, :4], wide[:, 1:5]):
+        with pytest.raises(qwm.QwmError) as e:
+            qwm.qwm_paged_attend(cache, batch, wide[:, :4], out=out, workspace=ws)
+        assert e.value.status == 1
+    want = qwm.qwm_paged_attend(cache, batch, q.cuda(), workspace=ws)
+    for lo in (4, 8):                              # other heads of the same projection
+        got = qwm.qwm_paged_attend(cache, batch, wide[:, :4], out=wide[:, lo:lo + 4], workspace=ws)
+        assert torch.equal(got, want)
+    assert torch.equal(wide[:, :4].cpu(), q) and cache.status() == 0

@@ -70,3 +70,15 @@ def test_written_rows_that_share_memory_are_refused(L):
     assert call(128, 384, 2, 4) == 1                        # head-major, the last token is the next head's first
     assert call(384, 256, 4, 4) == 1                        # (2, 0) is (0, 3)
     assert call(120, 512, 2, 4) == 1 and call(512, 120, 2, 4) == 1
+
+
+def test_outputs_over_their_inputs_are_refused(L):
+    def call(at, token=256, head=128, token_out=256, head_out=128, n=4):
+        cfg = paged.QwmRopeConfig(128, 0, (ct.c_int32 * 3)(22, 21, 21), 1)
+        return L.qwm_rope(cfg, 4096, 4096, n, rows(2, data=1 << 20, token=token, head=head),
+                          rows(2, data=(1 << 20) + 2 * at, token=token_out, head=head_out), None, None, None)
+
+    assert call(128) == 1 and call(-256) == 1 and call(8) == 1         # a head, a token, a vector on
+    assert call(0, token_out=512) == 1                                 # the same place, other strides
+    assert call(64, token=1024, token_out=1024) == 1
+    assert call(128, token=128, head=1024, token_out=128, head_out=1024) == 1
