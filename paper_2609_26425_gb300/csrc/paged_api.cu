@@ -337,6 +337,7 @@ qwm_status qwm_paged_attend(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   if (!rows_ok(q) || !out_ok(out, b->tokens, D) || q->heads != out->heads || q->heads % c->cfg.kv_heads ||
       overlaps(q, out, b->tokens, D))
     return QWM_ERR_INVALID_ARG;
+  if ((int64_t)b->max_q * (q->heads / c->cfg.kv_heads) > (int64_t)1 << 38) return QWM_ERR_UNSUPPORTED;  // the grid's x
   PagedPlan p = make_plan(c, b, q->heads, mask, workspace != nullptr);
   if (p.nsplit > 1 && workspace_bytes < carve(p, D).total) p = make_plan(c, b, q->heads, mask, false);
   qwm::PagedArgs a{};

@@ -557,3 +557,17 @@ def test_an_output_over_the_queries_is_refused_and_one_beside_them_is_not(new, h
         got = qwm.qwm_paged_attend(cache, batch, wide[:, :4], out=wide[:, lo:lo + 4], workspace=ws)
         assert torch.equal(got, want)
     assert torch.equal(wide[:, :4].cpu(), q) and cache.status() == 0
+
+
+def test_a_bound_whose_row_tiles_pass_32_bits_is_refused():
+    """1024 grouped heads under a bound of 2^30 + 1 tokens are 2^32 + 4 row tiles; cut to
+    32 bits they would leave the second token's rows unwritten."""
+    lens, D, page = [(2, 40)], 128, 16
+    q, keys, values, pages, table = make_case(92, lens, 1024, 1, D, BF, page)
+    cache, batch = build(lens, 1, D, BF, page, pages, table)
+    with pytest.raises(qwm.QwmError) as e:
+        qwm.qwm_paged_attend(cache, qwm.PagedBatch(*batch.tensors, (1 << 30) + 1, 40), q.cuda())
+    assert e.value.status == 2
+    loose = qwm.PagedBatch(*batch.tensors, 5000, 1 << 20)             # a loose bound is no matter
+    assert torch.equal(qwm.qwm_paged_attend(cache, loose, q.cuda()), qwm.qwm_paged_attend(cache, batch, q.cuda()))
+    assert cache.status() == 0
