@@ -399,7 +399,7 @@ typedef struct qwm_rope_config {
  *   (x0, x1) -> (x0 cos t - x1 sin t, x0 sin t + x1 cos t).
  * The product and its reduction by turns are exact to fp32 rounding of the
  * reduced angle at every int32 position, the rotation is in fp32, the result
- * rounded once.  inv_freq: fp32 [P]; pos: int32 [N][3].  q_out and k_out have
+ * rounded once.  inv_freq: fp32 [P], below 2^24 in size (NaN comes of others); pos: int32 [N][3].  q_out and k_out have
  * the heads of q and k and may be the same tensors as q and k (same data and
  * strides: in place); they must not overlap them otherwise (refused where base
  * addresses or strides are equal).  k and k_out may both be NULL.  N = 0 is a no-op. */

@@ -15,38 +15,31 @@ using namespace ptx;
 
 constexpr int NT = 256;
 
-// (cos, sin) of pos * f.  The product is carried as hi + lo (exact for |pos| <
-// 2^24; the rest of a larger position adds its own product), then reduced by
-// whole turns with 2 pi in three fp32 parts (Cody and Waite's method), twice so
-// that a quotient above 2^23 leaves nothing behind.  The reduced angle is
-// within an fp32 rounding of the exact one, where the fast sine and cosine are
-// good to 2^-21 absolute: far below the output's 2^-9 or 2^-12.
+// (cos, sin) of pos * f, exact to the fp32 rounding of the reduced angle at every
+// position.  The angle is taken in turns, as a 64-bit fraction whose whole turns fall
+// off the top (after Payne and Hanek, who form only the bits of a product that a
+// reduction keeps): f = m 2^e with a 24-bit m, f / (2 pi) = m 2^e C with C = 1 / (2 pi) to 128
+// bits, cut below 2^-64 of a turn, times the position (2^-33 of a turn at 2^31).  What
+// is left beside the nearest quarter turn is at most pi / 4 in fp32, where the fast sine
+// and cosine are good to 2^-21: far below the output's 2^-9 or 2^-12.  An f of 2^24 or
+// more, an infinity or a NaN gives NaN.
 __device__ __forceinline__ float2 turn(int pos, float f, float sign) {
-  constexpr float kInv = 0.15915494309189535f;  // 1 / (2 pi)
-  // 2 pi = c1 + c2 + c3, each the fp32 rounding of what the ones before leave
-  constexpr double kTwoPi = 6.283185307179586476925286766559;
-  constexpr float c1 = (float)kTwoPi;
-  constexpr float c2 = (float)(kTwoPi - (double)c1);
-  constexpr float c3 = (float)(kTwoPi - (double)c1 - (double)c2);
-  const float p = (float)pos;
-  const float rest = (float)(pos - (int64_t)p);
-  const float hi = p * f;
-  float lo = fmaf(p, f, -hi);
-  lo = fmaf(rest, f, lo);
-  float r = hi;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float n = rintf(r * kInv);
-    r = fmaf(-n, c1, r);
-    lo = fmaf(-n, c2, lo);
-    lo = fmaf(-n, c3, lo);
-    const float s = r + lo;   // renormalise: r + lo is unchanged
-    lo = lo - (s - r);
-    r = s;
-  }
+  constexpr uint64_t kC1 = 0x28BE60DB9391054Aull, kC0 = 0x7F09D5F47D4D3770ull;   // floor(2^128 / (2 pi))
+  constexpr float kTurn = (float)(6.283185307179586476925286766559 / 18446744073709551616.0);
+  const uint32_t w = __float_as_uint(f), ex = (w >> 23) & 255u;
+  const uint64_t m = (w & 0x7FFFFFu) | (ex ? 0x800000u : 0u);
+  const int down = 150 - (int)max(ex, 1u);         // -e
+  const uint64_t c0 = __umul64hi(m, kC0), lo = m * kC1 + c0, hi = __umul64hi(m, kC1) + (lo < c0);
+  const uint64_t g = down <= 0 ? lo : (down < 64 ? (lo >> down) | (hi << (64 - down)) : (down < 128 ? hi >> (down - 64) : 0));
+  const uint64_t t = (uint64_t)(int64_t)pos * g;
+  const uint64_t q = (t + (1ull << 61)) >> 62;      // quarter turns
   float sn, cs;
-  __sincosf(r + lo, &sn, &cs);
-  return make_float2(cs, sign * sn);
+  __sincosf((float)(int64_t)(t - (q << 62)) * kTurn, &sn, &cs);
+  if (ex >= 127 + 24) cs = __uint_as_float(0x7FFFFFFFu);
+  const float c = q & 1 ? sn : cs, d = q & 1 ? cs : sn;
+  // a quarter turn on is (-sn, cs), and so forth
+  const float sc = (q + 1) & 2 ? -c : c, ss = q & 2 ? -d : d;
+  return make_float2(sc, (w >> 31) ? -(sign * ss) : sign * ss);
 }
 
 constexpr int kMaxTokens = 16;                     // tokens of a CTA
@@ -82,8 +75,10 @@ __device__ __forceinline__ Place place_of(const RopeArgs& a, int64_t n) {
   return r;
 }
 
+// 32 registers for neighbouring channels, so that 8 CTAs fit an SM (34 and 36: rotation of
+// 4680 x 80 heads 36.8 us, append of 4680 x 120 56.2; with 32 33.2 and 50.5).
 template <typename T, bool INTERLEAVED, bool PAGED>
-__global__ void __launch_bounds__(NT) rope_kernel(const RopeArgs a, int tokens_per_cta) {
+__global__ void __launch_bounds__(NT, INTERLEAVED ? 8 : 6) rope_kernel(const RopeArgs a, int tokens_per_cta) {
   extern __shared__ float4 table4[];               // (cos, sin) [tokens_per_cta][P]
   float2* table = reinterpret_cast<float2*>(table4);
   __shared__ Place places[kMaxTokens];

@@ -184,3 +184,30 @@ def test_outputs_of_any_order_whose_rows_are_apart(token, head, heads, n):
     assert qwm.qwm_rope(rope, x.cuda(), pos.cuda(), q_out=out) is out
     check(out, x, pos, freq, pairs, True, 1.0)
     assert int((flat == 7.0).sum()) >= flat.numel() - x.numel()
+
+
+@pytest.mark.parametrize("il", [True, False])
+@pytest.mark.parametrize("span,fastest", [(1 << 31, 1.0), (1 << 24, 1.0), (1 << 22, 900.0), (5000, 3.0e6), (1 << 31, 1e-7)])
+def test_every_position_is_turned_to_fp32_accuracy(span, fastest, il):
+    """The same bound as for small positions; the 64-bit formula's own product of a
+    position and a frequency is good to 2^-23 here."""
+    pairs, n = (32, 16, 16), 64
+    g = torch.Generator().manual_seed(5)
+    pos = torch.randint(-span, span, (n, 3), generator=g).to(torch.int32)
+    pos[0] = torch.tensor([span - 1, -span, 0])
+    x = torch.randn(n, 4, 128, generator=g).to(torch.float16)
+    freq = inv_freq(pairs) * fastest
+    freq[3] = -freq[3]
+    got = qwm.qwm_rope(qwm.Rope(freq.cuda(), pairs, interleaved=il), x.cuda(), pos.cuda())
+    check(got, x, pos, freq, pairs, il, 1.0)
+
+
+def test_a_frequency_that_is_not_finite_is_nan_in_its_pairs():
+    pairs = (22, 21, 21)
+    freq = inv_freq(pairs)
+    freq[3], freq[9] = math.inf, math.nan
+    x = torch.ones(2, 2, 128, dtype=torch.bfloat16, device="cuda")
+    y = qwm.qwm_rope(qwm.Rope(freq.cuda(), pairs), x, torch.ones(2, 3, dtype=torch.int32, device="cuda"))
+    bad = torch.zeros(128, dtype=torch.bool)
+    bad[6:8] = bad[18:20] = True
+    assert torch.equal(y.isnan().cpu(), bad.expand(2, 2, 128))
