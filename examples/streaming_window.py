@@ -2,12 +2,14 @@
 
 Frames arrive one after the other.  The last frames stay in bf16 pages: each new
 frame's Keys and Values are appended with their three-axis rotation applied on
-the way (qwm_paged_append), and its Queries attend to the window and to the first
-tokens of the stream (qwm_paged_attend).  A frame that leaves the window is
+the way (qwm_paged_append), and its Queries attend to the window
+(qwm_paged_attend).  A frame that leaves the window is
 compressed to the 2-bit cache (qwm_rope, qwm_fit_centroids, qwm_quantize_append)
 and its pages are given back; the Queries reach it through qwm_attend, and the two
 results are joined by their log-sum-exps.  At the end the stream is continued token
-by token with the same calls.
+by token with the same calls; what their window would leave behind without a whole
+frame to compress stays visible in the pages, so pages and history together are
+always the whole stream.
 
     python examples/streaming_window.py [--frames N] [--exact]
 
@@ -68,7 +70,8 @@ class Stream:
             self.history = qwm.Cache(self.cfg, FRAME, frames + 1)
 
     def step(self, q, k, v, block, keep=True):
-        """Append the new tokens and attend; block: tokens that see each other."""
+        """Append the new tokens and attend; block: tokens that see each other (the new
+        ones end a block).  ``lse`` keeps the log-sum-exps of the whole attention."""
         n = q.shape[0]
         pos = positions(self.len, n)
         for page in range(self.len // PAGE, (self.len + n - 1) // PAGE + 1):
@@ -80,7 +83,7 @@ class Stream:
         held = torch.tensor([self.len], dtype=torch.int32, device="cuda")
         batch = qwm.PagedBatch(offsets, held, self.table, n, self.len, tokens=n)
         q = qwm.qwm_paged_append(self.cache, batch, k, v, rope=self.rope, pos=pos, q=q)
-        window = self.window * FRAME
+        window = max(self.window * FRAME, self.len - self.oldest) if self.compress else self.window * FRAME
         ws = qwm.paged_attend_workspace(self.cache, batch, self.heads, window=window, block=block)
         out, lse = qwm.qwm_paged_attend(self.cache, batch, q, window=window, block=block, want_lse=True, workspace=ws)
         if self.compress and self.history.num_chunks:
@@ -88,6 +91,8 @@ class Stream:
             both = torch.logaddexp(lse, old_lse)
             out = (out.float() * torch.exp(lse - both).t()[..., None] +
                    old.float() * torch.exp(old_lse - both).t()[..., None]).to(out.dtype)
+            lse = both
+        self.lse = lse
         if keep and self.compress:
             self.old.append((qwm.qwm_rope(self.rope, k, pos), v.contiguous()))
         return out
