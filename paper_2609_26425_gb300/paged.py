@@ -168,8 +168,9 @@ class PagedCache:
         self.buffer = raw[off:off + n]
         self.pages = self.buffer[256:].view(dtype).view(num_pages, 2, kv_heads, page_tokens, head_dim)
         h = _P()
-        _check("qwm_paged_init", _lib().qwm_paged_init(ct.byref(h), self.cfg, self.buffer.data_ptr(), n,
-                                                      _stream(self.buffer)))
+        with torch.cuda.device(self.buffer.device):    # a default stream's handle is the current device's
+            _check("qwm_paged_init", _lib().qwm_paged_init(ct.byref(h), self.cfg, self.buffer.data_ptr(), n,
+                                                          _stream(self.buffer)))
         self.handle = h
         self._key = (h.value, head_dim, _DTYPES[dtype])
 
@@ -189,7 +190,8 @@ class PagedCache:
     def status(self) -> int:
         """Read and clear the device status word (synchronises the stream)."""
         v = ct.c_int32()
-        _check("qwm_paged_status", _lib().qwm_paged_status(self.handle, ct.byref(v), _stream(self.buffer)))
+        with torch.cuda.device(self.buffer.device):
+            _check("qwm_paged_status", _lib().qwm_paged_status(self.handle, ct.byref(v), _stream(self.buffer)))
         return v.value
 
 

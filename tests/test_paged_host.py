@@ -1,8 +1,11 @@
 """Host-only checks of the rotary and paged entry points: sizes and refusals that
 need no GPU (every call here returns before anything is launched)."""
+import contextlib
 import ctypes as ct
+import types
 
 import pytest
+import torch
 
 from paper_2609_26425_gb300 import paged
 
@@ -82,3 +85,56 @@ def test_outputs_over_their_inputs_are_refused(L):
     assert call(0, token_out=512) == 1                                 # the same place, other strides
     assert call(64, token=1024, token_out=1024) == 1
     assert call(128, token=128, head=1024, token_out=128, head_out=1024) == 1
+
+
+class Calls:
+    """Stand-in for the library and for CUDA: which device was current in each call."""
+
+    def __init__(self):
+        self.current, self.seen = 0, []
+
+    def qwm_paged_bytes(self, cfg):
+        return 4096
+
+    def qwm_paged_free(self, handle):
+        pass
+
+    def qwm_paged_init(self, handle, cfg, buf, n, stream):
+        self.seen.append(("init", self.current, stream))
+        handle._obj.value = 1
+        return 0
+
+    def qwm_paged_status(self, handle, v, stream):
+        self.seen.append(("status", self.current, stream))
+        return 0
+
+
+class Buffer:
+    device = torch.device("cuda:1")
+
+    def data_ptr(self):
+        return 1 << 20
+
+    def view(self, *a):
+        return self
+
+    __getitem__ = view
+
+
+def test_a_cache_is_made_and_read_with_its_own_device_current(monkeypatch):
+    calls = Calls()
+
+    @contextlib.contextmanager
+    def device(d):
+        before, calls.current = calls.current, torch.device(d).index
+        yield
+        calls.current = before
+
+    monkeypatch.setattr(paged, "_C", calls)
+    monkeypatch.setattr(torch, "empty", lambda *a, device, **k: Buffer() if device == Buffer.device else None)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d: types.SimpleNamespace(cuda_stream=0))
+    cache = paged.PagedCache(2, 4, device="cuda:1")
+    assert cache.status() == 0
+    assert calls.seen == [("init", 1, 0), ("status", 1, 0)] and calls.current == 0
+    cache.handle = None
