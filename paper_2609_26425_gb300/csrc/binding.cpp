@@ -109,15 +109,27 @@ bool integer(PyObject* o, const char* name, int64_t lo, int64_t hi, int64_t* v) 
   return true;
 }
 
-// (frequencies' address, time, height, width pairs, interleaved) of a rotation
-bool rotation(PyObject* o, int64_t d, at::ScalarType type, qwm_rope_config* c, const float** freq) {
-  int64_t v[5];
-  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 5) {
-    PyErr_SetString(PyExc_ValueError, "not a rotation");
+// What a rotation, a cache or a batch keeps for its calls: integers, the last of them
+// the device of what they stand for, which has to be the tensors'.
+template <int N>
+bool key(PyObject* o, const char* name, int device, int64_t (&v)[N]) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != N) {
+    PyErr_Format(PyExc_ValueError, "not a %s", name);
     return false;
   }
-  for (int i = 0; i < 5; ++i)
-    if (!integer(PyTuple_GET_ITEM(o, i), "a rotation's entry", INT64_MIN, INT64_MAX, &v[i])) return false;
+  for (int i = 0; i < N; ++i)
+    if (!integer(PyTuple_GET_ITEM(o, i), name, INT64_MIN, INT64_MAX, &v[i])) return false;
+  if (v[N - 1] != device) {
+    PyErr_Format(PyExc_ValueError, "the %s is on another device (%lld) than the tensors (%d)", name, (long long)v[N - 1], device);
+    return false;
+  }
+  return true;
+}
+
+// (frequencies' address, time, height, width pairs, interleaved, device) of a rotation
+bool rotation(PyObject* o, int64_t d, at::ScalarType type, int device, qwm_rope_config* c, const float** freq) {
+  int64_t v[6];
+  if (!key(o, "rotation", device, v)) return false;
   c->head_dim = (int32_t)d;
   c->dtype = type == at::kHalf ? QWM_F16 : QWM_BF16;
   for (int i = 0; i < 3; ++i) c->pairs[i] = (int32_t)v[1 + i];
@@ -148,7 +160,7 @@ PyObject* turn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!rows(*q, q->scalar_type(), -1, "q", -1, -1, &qr)) return nullptr;
   const int dev = q->get_device();
   const int64_t N = q->size(0), d = q->size(2);
-  if (!rotation(a[1], d, q->scalar_type(), &cfg, &freq) || !positions(a[3], N, dev, &pos)) return nullptr;
+  if (!rotation(a[1], d, q->scalar_type(), dev, &cfg, &freq) || !positions(a[3], N, dev, &pos)) return nullptr;
   const bool has_k = a[4] != Py_None;
   const at::Tensor* k = has_k ? tensor(a[4], "k") : nullptr;
   if (has_k && (!k || !rows(*k, q->scalar_type(), dev, "k", N, d, &kr))) return nullptr;
@@ -183,34 +195,25 @@ PyObject* turn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return both;
 }
 
-// A cache is (descriptor's address, head_dim, qwm_dtype), a batch (qwm_paged_batch's
-// address, rows or -1 for any).
+// A cache is (descriptor's address, head_dim, qwm_dtype, device), a batch
+// (qwm_paged_batch's address, rows or -1 for any, device).
 struct Cache {
   qwm_paged* handle;
   int64_t d;
   at::ScalarType type;
 };
-bool cache_of(PyObject* o, Cache* c) {
-  int64_t v[3];
-  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3) {
-    PyErr_SetString(PyExc_ValueError, "not a paged cache");
-    return false;
-  }
-  for (int i = 0; i < 3; ++i)
-    if (!integer(PyTuple_GET_ITEM(o, i), "a cache's entry", INT64_MIN, INT64_MAX, &v[i])) return false;
+// The cache for tensors of `like`'s device.
+bool cache_of(PyObject* o, const at::Tensor& like, Cache* c) {
+  int64_t v[4];
+  if (!key(o, "paged cache", like.is_cuda() ? like.get_device() : -1, v)) return false;
   c->handle = reinterpret_cast<qwm_paged*>(v[0]);
   c->d = v[1];
   c->type = v[2] == QWM_F16 ? at::kHalf : at::kBFloat16;
   return true;
 }
-bool batch_of(PyObject* o, int64_t n, qwm_paged_batch* b) {
-  int64_t v[2];
-  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 2) {
-    PyErr_SetString(PyExc_ValueError, "not a paged batch");
-    return false;
-  }
-  for (int i = 0; i < 2; ++i)
-    if (!integer(PyTuple_GET_ITEM(o, i), "a batch's entry", INT64_MIN, INT64_MAX, &v[i])) return false;
+bool batch_of(PyObject* o, int64_t n, int device, qwm_paged_batch* b) {
+  int64_t v[3];
+  if (!key(o, "paged batch", device, v)) return false;
   if (v[1] >= 0 && v[1] != n) {
     PyErr_Format(PyExc_ValueError, "the batch has %lld rows, the tensor %lld", (long long)v[1], (long long)n);
     return false;
@@ -223,19 +226,19 @@ bool batch_of(PyObject* o, int64_t n, qwm_paged_batch* b) {
 // append(cache, batch, k, v, rotation or None, pos or None, q or None, q_out or None)
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Cache c;
-  if (!count(n, 8) || !cache_of(a[0], &c)) return nullptr;
+  if (!count(n, 8)) return nullptr;
   const at::Tensor *k = tensor(a[2], "k"), *v = k ? tensor(a[3], "v") : nullptr;
   qwm_rows kr, vr, qr, qo;
-  if (!v || !rows(*k, c.type, -1, "k", -1, c.d, &kr)) return nullptr;
+  if (!v || !cache_of(a[0], *k, &c) || !rows(*k, c.type, -1, "k", -1, c.d, &kr)) return nullptr;
   const int64_t N = k->size(0);
   const int dev = k->get_device();
   qwm_paged_batch b;
-  if (!rows(*v, c.type, dev, "v", N, c.d, &vr) || !batch_of(a[1], N, &b)) return nullptr;
+  if (!rows(*v, c.type, dev, "v", N, c.d, &vr) || !batch_of(a[1], N, dev, &b)) return nullptr;
   qwm_rope_config cfg;
   const float* freq = nullptr;
   const int32_t* pos = nullptr;
   const bool turned = a[4] != Py_None, has_q = a[6] != Py_None;
-  if (turned && (!rotation(a[4], c.d, c.type, &cfg, &freq) || !positions(a[5], N, dev, &pos))) return nullptr;
+  if (turned && (!rotation(a[4], c.d, c.type, dev, &cfg, &freq) || !positions(a[5], N, dev, &pos))) return nullptr;
   PyObject* q_out = nullptr;
   if (has_q) {
     const at::Tensor* q = tensor(a[6], "q");
@@ -260,15 +263,15 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // attend(cache, batch, q, block, window, sinks, sm_scale, out or None, lse or None, want_lse, workspace or None)
 PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Cache c;
-  if (!count(n, 11) || !cache_of(a[0], &c)) return nullptr;
+  if (!count(n, 11)) return nullptr;
   const at::Tensor* q = tensor(a[2], "q");
   qwm_rows qr, orows;
-  if (!q || !rows(*q, c.type, -1, "q", -1, c.d, &qr)) return nullptr;
+  if (!q || !cache_of(a[0], *q, &c) || !rows(*q, c.type, -1, "q", -1, c.d, &qr)) return nullptr;
   const int64_t N = q->size(0), H = q->size(1);
   const int dev = q->get_device();
   qwm_paged_batch b;
   int64_t block, window, sinks;
-  if (!batch_of(a[1], N, &b) || !integer(a[3], "block", INT32_MIN, INT32_MAX, &block) ||
+  if (!batch_of(a[1], N, dev, &b) || !integer(a[3], "block", INT32_MIN, INT32_MAX, &block) ||
       !integer(a[4], "window", INT32_MIN, INT32_MAX, &window) || !integer(a[5], "sinks", INT32_MIN, INT32_MAX, &sinks))
     return nullptr;
   const qwm_mask mask{(int32_t)block, (int32_t)window, (int32_t)sinks};

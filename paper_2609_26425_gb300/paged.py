@@ -134,7 +134,7 @@ class Rope:
                 and inv_freq.is_contiguous() and tuple(inv_freq.shape) == (sum(pairs),)):
             raise ValueError(f"inv_freq must be a contiguous fp32 CUDA tensor [{sum(pairs)}]")
         self.inv_freq, self.pairs, self.interleaved = inv_freq, pairs, bool(interleaved)
-        self._key = (inv_freq.data_ptr(), *pairs, int(self.interleaved))
+        self._key = (inv_freq.data_ptr(), *pairs, int(self.interleaved), inv_freq.device.index)
 
 
 def qwm_rope(rope: Rope, q, pos, k=None, q_out=None, k_out=None):
@@ -172,7 +172,7 @@ class PagedCache:
             _check("qwm_paged_init", _lib().qwm_paged_init(ct.byref(h), self.cfg, self.buffer.data_ptr(), n,
                                                           _stream(self.buffer)))
         self.handle = h
-        self._key = (h.value, head_dim, _DTYPES[dtype])
+        self._key = (h.value, head_dim, _DTYPES[dtype], self.buffer.device.index)
 
     def __del__(self):
         h = getattr(self, "handle", None)
@@ -211,12 +211,14 @@ class PagedBatch:
         if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
             raise ValueError("page_table must be an int32 CUDA tensor [sequences][pages]")
         _ints(page_table, (B, page_table.shape[1]), "page_table")
+        if not q_offsets.device == kv_len.device == page_table.device:
+            raise ValueError("q_offsets, kv_len and page_table must be on one device")
         self.tensors = (q_offsets, kv_len, page_table)
         self.num_seqs, self.max_q, self.max_kv = B, int(max_q), int(max_kv)
         self.tokens = tokens
         self._c = QwmPagedBatch(B, page_table.shape[1], self.max_q, self.max_kv, -1 if tokens is None else tokens,
                                 q_offsets.data_ptr(), kv_len.data_ptr(), page_table.data_ptr())
-        self._key = (ct.addressof(self._c), self._c.tokens)
+        self._key = (ct.addressof(self._c), self._c.tokens, kv_len.device.index)
 
     def struct(self, tokens):
         """The C descriptor for a call of `tokens` rows."""

@@ -571,3 +571,25 @@ def test_a_bound_whose_row_tiles_pass_32_bits_is_refused():
     loose = qwm.PagedBatch(*batch.tensors, 5000, 1 << 20)             # a loose bound is no matter
     assert torch.equal(qwm.qwm_paged_attend(cache, loose, q.cuda()), qwm.qwm_paged_attend(cache, batch, q.cuda()))
     assert cache.status() == 0
+
+
+def test_parts_of_a_call_on_another_device_are_refused():
+    lens, Hk, D, page = [(3, 40)], 2, 128, 16
+    q, _, _, pages, table = make_case(93, lens, 4, Hk, D, BF, page)
+    cache, batch = build(lens, Hk, D, BF, page, pages, table)
+    rope = qwm.Rope(inv_freq((22, 21, 21)).cuda(), (22, 21, 21))
+    pos, dq, k = torch.zeros(3, 3, dtype=torch.int32).cuda(), q.cuda(), torch.zeros(3, Hk, D, dtype=BF, device="cuda")
+    for part in (cache, batch, rope):
+        sound = part._key
+        assert sound[-1] == dq.get_device()
+        part._key = (*sound[:-1], 1)               # as on a second GPU
+        calls = [] if part is rope else [lambda: qwm.qwm_paged_attend(cache, batch, dq)]
+        calls += [lambda: qwm.qwm_paged_append(cache, batch, k, k, rope=rope, pos=pos, q=dq)]
+        calls += [lambda: qwm.qwm_rope(rope, dq, pos)] if part is rope else []
+        for call in calls:
+            with pytest.raises(ValueError, match="on another device"):
+                call()
+        part._key = sound
+        for call in calls:
+            call()
+    assert cache.status() == 0

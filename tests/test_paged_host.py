@@ -138,3 +138,22 @@ def test_a_cache_is_made_and_read_with_its_own_device_current(monkeypatch):
     assert cache.status() == 0
     assert calls.seen == [("init", 1, 0), ("status", 1, 0)] and calls.current == 0
     cache.handle = None
+
+
+class OnDevice(torch.Tensor):
+    """An int32 tensor that is said to be on a device."""
+
+    @staticmethod
+    def __new__(cls, device, *shape):
+        return torch.Tensor._make_wrapper_subclass(cls, shape, dtype=torch.int32, device=device)
+
+    @classmethod
+    def __torch_dispatch__(cls, func, types, args=(), kwargs=None):
+        raise NotImplementedError
+
+
+@pytest.mark.parametrize("other", [0, 1, 2])
+def test_a_batchs_tensors_are_on_one_device(other):
+    t = [OnDevice("cuda:%d" % int(i == other), *shape) for i, shape in enumerate(((3,), (2,), (2, 5)))]
+    with pytest.raises(ValueError, match="one device"):
+        paged.PagedBatch(*t, 1, 64)
