@@ -14,6 +14,8 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <utility>
+
 #include "../../include/qwm.h"
 
 namespace {
@@ -38,6 +40,23 @@ const at::Tensor* tensor(PyObject* o, const char* name) {
     return nullptr;
   }
   return &THPVariable_Unpack(o);
+}
+
+// A reference that is given back on every way out, an exception's too.
+struct Ref {
+  PyObject* p = nullptr;
+  ~Ref() { Py_XDECREF(p); }
+  PyObject* release() { return std::exchange(p, nullptr); }
+};
+
+// The result of one output or of two.
+PyObject* result(Ref& a, Ref& b) {
+  if (!b.p) return a.release();
+  PyObject* both = PyTuple_New(2);
+  if (!both) return nullptr;
+  PyTuple_SET_ITEM(both, 0, a.release());
+  PyTuple_SET_ITEM(both, 1, b.release());
+  return both;
 }
 
 const char* type_name(at::ScalarType t) { return t == at::kHalf ? "torch.float16" : "torch.bfloat16"; }
@@ -66,7 +85,7 @@ bool rows(const at::Tensor& t, at::ScalarType type, int device, const char* name
 }
 
 // The output for `like`: the caller's tensor `o`, or a new contiguous one.
-bool output(PyObject* o, const at::Tensor& like, int device, const char* name, qwm_rows* r, PyObject** ret) {
+bool output(PyObject* o, const at::Tensor& like, int device, const char* name, qwm_rows* r, Ref* ret) {
   if (o != Py_None) {
     const at::Tensor* t = tensor(o, name);
     if (!t) return false;
@@ -75,7 +94,7 @@ bool output(PyObject* o, const at::Tensor& like, int device, const char* name, q
       return false;
     }
     if (!rows(*t, like.scalar_type(), device, name, -1, -1, r)) return false;
-    *ret = Py_NewRef(o);
+    ret->p = Py_NewRef(o);
     return true;
   }
   const at::Tensor t = at::empty(like.sizes(), like.options().memory_format(at::MemoryFormat::Contiguous));
@@ -83,8 +102,8 @@ bool output(PyObject* o, const at::Tensor& like, int device, const char* name, q
   r->head_stride = t.size(2);
   r->token_stride = t.size(1) * t.size(2);
   r->heads = (int32_t)t.size(1);
-  *ret = THPVariable_Wrap(t);
-  return *ret != nullptr;
+  ret->p = THPVariable_Wrap(t);
+  return ret->p != nullptr;
 }
 
 bool positions(PyObject* o, int64_t n, int device, const int32_t** p) {
@@ -164,12 +183,8 @@ PyObject* turn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const bool has_k = a[4] != Py_None;
   const at::Tensor* k = has_k ? tensor(a[4], "k") : nullptr;
   if (has_k && (!k || !rows(*k, q->scalar_type(), dev, "k", N, d, &kr))) return nullptr;
-  PyObject *q_out = nullptr, *k_out = nullptr;
-  if (!output(a[5], *q, dev, "q_out", &qo, &q_out)) return nullptr;
-  if (has_k && !output(a[6], *k, dev, "k_out", &ko, &k_out)) {
-    Py_DECREF(q_out);
-    return nullptr;
-  }
+  Ref q_out, k_out;
+  if (!output(a[5], *q, dev, "q_out", &qo, &q_out) || (has_k && !output(a[6], *k, dev, "k_out", &ko, &k_out))) return nullptr;
   qwm_status st;
   {
     const c10::cuda::CUDAGuard guard(dev);
@@ -178,21 +193,8 @@ PyObject* turn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     st = (backward ? qwm_rope_backward : qwm_rope)(&cfg, freq, pos, N, &qr, &qo, has_k ? &kr : nullptr, has_k ? &ko : nullptr, s);
     Py_END_ALLOW_THREADS
   }
-  if (st != QWM_OK) {
-    Py_DECREF(q_out);
-    Py_XDECREF(k_out);
-    return fail(backward ? "qwm_rope_backward" : "qwm_rope", st);
-  }
-  if (!has_k) return q_out;
-  PyObject* both = PyTuple_New(2);
-  if (!both) {
-    Py_DECREF(q_out);
-    Py_DECREF(k_out);
-    return nullptr;
-  }
-  PyTuple_SET_ITEM(both, 0, q_out);
-  PyTuple_SET_ITEM(both, 1, k_out);
-  return both;
+  if (st != QWM_OK) return fail(backward ? "qwm_rope_backward" : "qwm_rope", st);
+  return result(q_out, k_out);
 }
 
 // A cache is (descriptor's address, head_dim, qwm_dtype, device), a batch
@@ -239,7 +241,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int32_t* pos = nullptr;
   const bool turned = a[4] != Py_None, has_q = a[6] != Py_None;
   if (turned && (!rotation(a[4], c.d, c.type, dev, &cfg, &freq) || !positions(a[5], N, dev, &pos))) return nullptr;
-  PyObject* q_out = nullptr;
+  Ref q_out;
   if (has_q) {
     const at::Tensor* q = tensor(a[6], "q");
     if (!q || !rows(*q, c.type, dev, "q", N, c.d, &qr) || !output(a[7], *q, dev, "q_out", &qo, &q_out)) return nullptr;
@@ -253,11 +255,8 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
                           has_q ? &qo : nullptr, s);
     Py_END_ALLOW_THREADS
   }
-  if (st != QWM_OK) {
-    Py_XDECREF(q_out);
-    return fail("qwm_paged_append", st);
-  }
-  return has_q ? q_out : Py_NewRef(Py_None);
+  if (st != QWM_OK) return fail("qwm_paged_append", st);
+  return has_q ? q_out.release() : Py_NewRef(Py_None);
 }
 
 // attend(cache, batch, q, block, window, sinks, sm_scale, out or None, lse or None, want_lse, workspace or None)
@@ -289,7 +288,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     ws = t->data_ptr();
     ws_bytes = t->nbytes();
   }
-  PyObject *out = nullptr, *lse = nullptr;
+  Ref out, lse;
   float* lse_data = nullptr;
   if (a[8] != Py_None) {
     const at::Tensor* t = tensor(a[8], "lse");
@@ -300,17 +299,14 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
       return nullptr;
     }
     lse_data = static_cast<float*>(t->data_ptr());
-    lse = Py_NewRef(a[8]);
+    lse.p = Py_NewRef(a[8]);
   } else if (PyObject_IsTrue(a[9]) == 1) {
     const at::Tensor t = at::empty({H, N}, q->options().dtype(at::kFloat).memory_format(at::MemoryFormat::Contiguous));
     lse_data = static_cast<float*>(t.data_ptr());
-    lse = THPVariable_Wrap(t);
-    if (!lse) return nullptr;
+    lse.p = THPVariable_Wrap(t);
+    if (!lse.p) return nullptr;
   }
-  if (!output(a[7], *q, dev, "out", &orows, &out)) {
-    Py_XDECREF(lse);
-    return nullptr;
-  }
+  if (!output(a[7], *q, dev, "out", &orows, &out)) return nullptr;
   qwm_status st;
   {
     const c10::cuda::CUDAGuard guard(dev);
@@ -319,21 +315,8 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     st = qwm_paged_attend(c.handle, &b, &qr, &mask, (float)scale, &orows, lse_data, ws, ws_bytes, s);
     Py_END_ALLOW_THREADS
   }
-  if (st != QWM_OK) {
-    Py_DECREF(out);
-    Py_XDECREF(lse);
-    return fail("qwm_paged_attend", st);
-  }
-  if (!lse) return out;
-  PyObject* both = PyTuple_New(2);
-  if (!both) {
-    Py_DECREF(out);
-    Py_DECREF(lse);
-    return nullptr;
-  }
-  PyTuple_SET_ITEM(both, 0, out);
-  PyTuple_SET_ITEM(both, 1, lse);
-  return both;
+  if (st != QWM_OK) return fail("qwm_paged_attend", st);
+  return result(out, lse);
 }
 
 // set_error(class): what a status other than QWM_OK raises

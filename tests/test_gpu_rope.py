@@ -211,3 +211,17 @@ def test_a_frequency_that_is_not_finite_is_nan_in_its_pairs():
     bad = torch.zeros(128, dtype=torch.bool)
     bad[6:8] = bad[18:20] = True
     assert torch.equal(y.isnan().cpu(), bad.expand(2, 2, 128))
+
+
+def test_a_call_that_fails_gives_back_what_it_made():
+    """Keys too large to allocate an output for, after the Queries' output was made."""
+    pairs, n = (4, 0, 0), 1 << 20
+    rope = qwm.Rope(inv_freq(pairs).cuda(), pairs)
+    x = torch.zeros(1, 1, 8, dtype=torch.bfloat16, device="cuda")
+    pos = torch.zeros(n, 3, dtype=torch.int32, device="cuda")
+    before = torch.cuda.memory_allocated()
+    with pytest.raises(MemoryError):
+        qwm.qwm_rope(rope, x.expand(n, 1, 8), pos, k=x.expand(n, n, 8))
+    with pytest.raises(qwm.QwmError):
+        qwm.qwm_rope(qwm.Rope(rope.inv_freq, (4, 0, 0), interleaved=False), x.expand(n, 1, 8), pos)
+    assert torch.cuda.memory_allocated() == before
