@@ -18,6 +18,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT, "libqwm.so")
 BINDING = os.path.join(OUT, "qwm_binding.so")  # csrc/binding.cpp, against PyTorch's headers
+STAMP = os.path.join(OUT, "qwm_binding.txt")   # which PyTorch that was
 SOURCES = ["qwm_api.cu", "append.cu", "append_fused.cu", "append_fused_r8.cu", "append_fused_r16.cu",
            "append_fused_r32.cu", "append_generic.cu", "append_full.cu", "attend.cu", "fit.cu", "qstats.cu",
            "metrics.cu", "rope.cu", "paged_api.cu", "paged_step.cu", "paged_chunk.cu"]
@@ -42,8 +43,21 @@ def _deps():
     return files
 
 
+def _built_with() -> str:
+    """The PyTorch and the Python that the binding is compiled against."""
+    import torch
+    return "\n".join((torch.__version__, os.path.dirname(torch.__file__), str(torch._C._GLIBCXX_USE_CXX11_ABI),
+                      sys.version, sysconfig.get_paths()["include"]))
+
+
 def up_to_date() -> bool:
     if not os.path.exists(LIB) or not os.path.exists(BINDING):
+        return False
+    try:
+        with open(STAMP) as f:
+            if f.read() != _built_with():
+                return False
+    except FileNotFoundError:
         return False
     t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
     return all(os.path.getmtime(f) <= t for f in _deps())
@@ -96,6 +110,8 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, BINDING)
+    with open(STAMP, "w") as f:
+        f.write(_built_with())
     return LIB
 
 

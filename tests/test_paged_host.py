@@ -157,3 +157,15 @@ def test_a_batchs_tensors_are_on_one_device(other):
     t = [OnDevice("cuda:%d" % int(i == other), *shape) for i, shape in enumerate(((3,), (2,), (2, 5)))]
     with pytest.raises(ValueError, match="one device"):
         paged.PagedBatch(*t, 1, 64)
+
+
+def test_a_binding_of_another_pytorch_is_built_again(L, monkeypatch):
+    from paper_2609_26425_gb300 import build
+    assert build.up_to_date()
+    with monkeypatch.context() as m:
+        m.setattr(torch, "__version__", "0.0.0")
+        assert not build.up_to_date()
+    with monkeypatch.context() as m:
+        m.setattr(torch, "__file__", "/elsewhere/torch/__init__.py")
+        assert not build.up_to_date()
+    assert build.up_to_date()
