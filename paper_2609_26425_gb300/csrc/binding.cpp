@@ -10,6 +10,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -84,6 +85,11 @@ bool rows(const at::Tensor& t, at::ScalarType type, int device, const char* name
   return true;
 }
 
+// A caller's tensor that the call writes: autograd notices where it was saved.
+void written(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // The output for `like`: the caller's tensor `o`, or a new contiguous one.
 bool output(PyObject* o, const at::Tensor& like, int device, const char* name, qwm_rows* r, Ref* ret) {
   if (o != Py_None) {
@@ -94,6 +100,7 @@ bool output(PyObject* o, const at::Tensor& like, int device, const char* name, q
       return false;
     }
     if (!rows(*t, like.scalar_type(), device, name, -1, -1, r)) return false;
+    written(*t);
     ret->p = Py_NewRef(o);
     return true;
   }
@@ -162,9 +169,13 @@ bool count(Py_ssize_t n, Py_ssize_t want) {
   return n == want;
 }
 
-// turn(backward, rotation, q, pos, k or None, q_out or None, k_out or None)
+bool tracked(PyObject* o) { return THPVariable_Check(o) && THPVariable_Unpack(o).requires_grad(); }
+
+// turn(backward, rotation, q, pos, k or None, q_out or None, k_out or None); None, with
+// nothing done, if autograd has to record the call
 PyObject* turn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!count(n, 7)) return nullptr;
+  if (c10::GradMode::is_enabled() && (tracked(a[2]) || tracked(a[4]) || tracked(a[5]) || tracked(a[6]))) Py_RETURN_NONE;
   const bool backward = a[0] == Py_True;
   const at::Tensor* q = tensor(a[2], "q");
   if (!q) return nullptr;
@@ -299,6 +310,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
       return nullptr;
     }
     lse_data = static_cast<float*>(t->data_ptr());
+    written(*t);
     lse.p = Py_NewRef(a[8]);
   } else if (PyObject_IsTrue(a[9]) == 1) {
     const at::Tensor t = at::empty({H, N}, q->options().dtype(at::kFloat).memory_format(at::MemoryFormat::Contiguous));

@@ -137,15 +137,52 @@ class Rope:
         self._key = (inv_freq.data_ptr(), *pairs, int(self.interleaved), inv_freq.device.index)
 
 
+class _Recorded(torch.autograd.Function):
+    """The rotation as autograd sees it; its gradient is the rotation back."""
+
+    @staticmethod
+    def forward(ctx, rope, back, q, pos, k, q_out, k_out):
+        ctx.rope, ctx.back = rope, back
+        ctx.save_for_backward(pos, rope.inv_freq)
+        ctx.mark_dirty(*(t for t in (q if q_out is True else q_out, k if k_out is True else k_out) if t is not None))
+        return binding().turn(back, rope._key, q, pos, k, q if q_out is True else q_out, k if k_out is True else k_out)
+
+    @staticmethod
+    def backward(ctx, dq, dk=None):
+        pos = ctx.saved_tensors[0]
+        need = [g is not None and ctx.needs_input_grad[i] for g, i in ((dq, 2), (dk, 4))]
+        given = [_readable(g) for g, n in zip((dq, dk), need) if n]
+        turn = qwm_rope if ctx.back else qwm_rope_backward
+        got = turn(ctx.rope, given[0], pos, *given[1:]) if given else ()
+        got = iter(got if isinstance(got, tuple) else (got,))
+        dq, dk = (next(got) if n else None for n in need)
+        return None, None, dq, None, dk, None, None
+
+
+def _readable(g):
+    """A gradient in a layout that the kernels read (a sum's, say, has strides of zero)."""
+    return g if g.stride(2) == 1 and (g.stride(0) | g.stride(1)) % 8 == 0 and g.data_ptr() % 16 == 0 else g.contiguous()
+
+
+def _record(rope, back, q, pos, k, q_out, k_out):
+    # True: in place (a tensor is passed to autograd once)
+    return _Recorded.apply(rope, back, q, pos, k, True if q_out is q else q_out,
+                           True if k is not None and k_out is k else k_out)
+
+
 def qwm_rope(rope: Rope, q, pos, k=None, q_out=None, k_out=None):
     """Queries (and Keys) turned to their positions ``pos`` (int32 [tokens][3]);
-    ``q_out=q`` works in place.  Returns q_out, or (q_out, k_out) with Keys."""
-    return (_B or binding()).turn(False, rope._key, q, pos, k, q_out, k_out)
+    ``q_out=q`` works in place.  Returns q_out, or (q_out, k_out) with Keys.
+    Autograd records the call where it is on and q or k requires a gradient
+    (``inv_freq`` has none)."""
+    got = (_B or binding()).turn(False, rope._key, q, pos, k, q_out, k_out)
+    return got if got is not None else _record(rope, False, q, pos, k, q_out, k_out)
 
 
 def qwm_rope_backward(rope: Rope, dq, pos, dk=None, dq_out=None, dk_out=None):
     """Gradient of qwm_rope: the outputs' gradients turned back."""
-    return (_B or binding()).turn(True, rope._key, dq, pos, dk, dq_out, dk_out)
+    got = (_B or binding()).turn(True, rope._key, dq, pos, dk, dq_out, dk_out)
+    return got if got is not None else _record(rope, True, dq, pos, dk, dq_out, dk_out)
 
 
 # ------------------------------------------------------------------ pages

@@ -225,3 +225,89 @@ def test_a_call_that_fails_gives_back_what_it_made():
     with pytest.raises(qwm.QwmError):
         qwm.qwm_rope(qwm.Rope(rope.inv_freq, (4, 0, 0), interleaved=False), x.expand(n, 1, 8), pos)
     assert torch.cuda.memory_allocated() == before
+
+
+def formula(x, pos, freq, pairs, il):
+    """The rotation in torch operations in 64 bits, for autograd."""
+    axis = [a for a in range(3) for _ in range(pairs[a])]
+    t, P = (pos[:, axis].double() * freq.double())[:, None], sum(pairs)
+    ia = torch.arange(P) * (2 if il else 1)
+    ib = ia + (1 if il else P)
+    y = x.clone()
+    y[..., ia] = x[..., ia] * t.cos() - x[..., ib] * t.sin()
+    y[..., ib] = x[..., ia] * t.sin() + x[..., ib] * t.cos()
+    return y
+
+
+@pytest.mark.parametrize("il", [True, False])
+@pytest.mark.parametrize("wants", ["q", "k", "both"])
+@pytest.mark.parametrize("layout", ["dense", "slices", "head-major"])
+def test_autograd_records_the_rotation(layout, wants, il):
+    pairs, d, n, hq, hk = (12, 10, 10), 72, 7, 3, 2
+    freq, pos = inv_freq(pairs), positions(31, n)
+    rope = qwm.Rope(freq.cuda(), pairs, interleaved=il)
+    g = torch.Generator().manual_seed(32)
+    qkv = torch.randn(n, hq + hk, d, generator=g).to(torch.float16)
+    dy = torch.randn(n, hq + hk, d, generator=g).to(torch.float16)
+    q, k = qkv[:, :hq].clone(), qkv[:, hq:].clone()
+    if layout == "slices":
+        base = qkv.cuda()
+        dq, dk = base[:, :hq], base[:, hq:]
+    elif layout == "head-major":
+        dq, dk = (t.permute(1, 0, 2).contiguous().cuda().permute(1, 0, 2) for t in (q, k))
+    else:
+        dq, dk = q.cuda(), k.cuda()
+    dq, dk = dq.detach().requires_grad_(wants != "k"), dk.detach().requires_grad_(wants != "q")
+    a, b = qwm.qwm_rope(rope, dq, pos.cuda(), k=dk)
+    with torch.no_grad():
+        plain = qwm.qwm_rope(rope, dq, pos.cuda(), k=dk)
+    assert torch.equal(a, plain[0]) and torch.equal(b, plain[1])
+    assert not plain[0].requires_grad and a.requires_grad and b.requires_grad
+    ((a * dy[:, :hq].cuda()).sum() + (b * dy[:, hq:].cuda()).sum()).backward()
+    for x, got, w in ((q, dq.grad, dy[:, :hq]), (k, dk.grad, dy[:, hq:])):
+        if got is None:
+            continue
+        z = x.double().requires_grad_(True)
+        (formula(z, pos, freq, pairs, il) * w.double()).sum().backward()
+        bound = rope_bound(w, z.grad, torch.float16, pairs, il)
+        assert bool(((got.double().cpu() - z.grad).abs() <= bound).all())
+    assert (dq.grad is None) == (wants == "k") and (dk.grad is None) == (wants == "q")
+
+
+def test_autograd_in_place_and_through_expanded_gradients():
+    pairs, d, n, h = (22, 21, 21), 128, 5, 3
+    freq, pos = inv_freq(pairs), positions(33, n).cuda()
+    rope = qwm.Rope(freq.cuda(), pairs)
+    x = torch.randn(n, h, d, generator=torch.Generator().manual_seed(34)).to(torch.bfloat16).cuda().requires_grad_(True)
+    qwm.qwm_rope(rope, x, pos).sum().backward()                        # a gradient whose strides are 0
+    want, x.grad = x.grad, None
+    assert torch.equal(want, qwm.qwm_rope_backward(rope, torch.ones_like(x).detach(), pos))
+    y = x * 1.0
+    assert qwm.qwm_rope(rope, y, pos, q_out=y) is y                    # in place
+    y.sum().backward()
+    assert torch.equal(x.grad, want)
+    x.grad = None
+    z, given = x * 1.0, torch.empty_like(x).detach()
+    assert qwm.qwm_rope(rope, z, pos, q_out=given) is given            # into a tensor of the caller's
+    given.sum().backward()
+    assert torch.equal(x.grad, want)
+    with pytest.raises(RuntimeError, match="leaf"):
+        qwm.qwm_rope(rope, x, pos, q_out=x)
+    y = x * 1.0
+    square = y * y
+    with torch.no_grad():
+        qwm.qwm_rope(rope, y, pos, q_out=y)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        square.sum().backward()
+
+
+def test_the_gradient_has_a_gradient():
+    pairs, d, n, h = (8, 8, 8), 64, 4, 2
+    pos, rope = positions(35, n).cuda(), qwm.Rope(inv_freq(pairs).cuda(), pairs, interleaved=False)
+    g = torch.Generator().manual_seed(36)
+    x, v, w = (torch.randn(n, h, d, generator=g).to(torch.float16).cuda() for _ in range(3))
+    x.requires_grad_(True), v.requires_grad_(True)
+    back, = torch.autograd.grad(qwm.qwm_rope(rope, x, pos), x, v, create_graph=True)
+    assert torch.equal(back, qwm.qwm_rope_backward(rope, v.detach(), pos))
+    again, = torch.autograd.grad(back, v, w)
+    assert torch.equal(again, qwm.qwm_rope(rope, w, pos))
