@@ -491,8 +491,8 @@ typedef struct qwm_mask {
  * [q_heads][tokens] natural-log sum-exp of the scaled logits, or NULL.  out must
  * not overlap q (refused where base addresses or strides are equal).
  * 0 < sm_scale <= 1e38; max_q * (q_heads / kv_heads) <= 2^38.  A row that sees
- * nothing gets 0 and an lse of -inf.  What a row does not see does not reach it,
- * infinities and NaN included.
+ * nothing, or whose logits are all -inf, gets 0 and an lse of -inf.  What a row does
+ * not see does not reach it, infinities and NaN included.
  * workspace: device scratch of at least qwm_paged_attend_workspace_bytes bytes
  * for the same arguments (256-byte aligned), its first QWM_PAGED_COUNTER_BYTES
  * zeroed once when it is made (each call leaves them at zero); the call then

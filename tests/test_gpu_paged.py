@@ -593,3 +593,19 @@ def test_parts_of_a_call_on_another_device_are_refused():
         for call in calls:
             call()
     assert cache.status() == 0
+
+
+@pytest.mark.parametrize("new,held", [(1, 40), (1, 3000), (4, 3000), (60, 3000)])
+@pytest.mark.parametrize("split", [False, True])
+def test_a_row_whose_logits_are_all_minus_infinity_is_an_empty_one(new, held, split):
+    lens, Hk, D, page = [(new, held)], 1, 128, 16
+    q, keys, values, pages, table = make_case(94, lens, 2, Hk, D, BF, page)
+    for b in range(pages.shape[0]):
+        pages[b, 0, 0, :, 3] = -math.inf           # every Key's, of every page
+    q[:, 0, 3] = 0.5                               # head 0's logits are -inf,
+    q[:, 1, 3] = -0.5                              # head 1's are inf
+    cache, batch = build(lens, Hk, D, BF, page, pages, table)
+    ws = qwm.paged_attend_workspace(cache, batch, 2) if split else None
+    out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True, workspace=ws)
+    assert bool((out[:, 0] == 0).all()) and bool((lse[0] == -math.inf).all())
+    assert bool(out[:, 1].isnan().all()) and bool(lse[1].isnan().all()) and cache.status() == 0
