@@ -105,8 +105,7 @@ inline cudaError_t launch_ahead(void (*kernel)(P...), dim3 grid, int threads, si
   cfg.stream = s;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
-  return e != cudaSuccess ? e : cudaGetLastError();
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 // Rows (Query tokens x Query heads per cache head) up to which a sequence goes
 // to the step kernel.  With 16 rows of 128 channels it takes 67 us against the

@@ -27,6 +27,13 @@ int ilog2(int x) {
   return l;
 }
 
+// The status of a call whose CUDA call failed.  The runtime keeps such an error for
+// whoever asks next: it is taken here, so that no later call reports it as its own.
+qwm_status cuda_error() {
+  cudaGetLastError();
+  return QWM_ERR_CUDA;
+}
+
 bool paged_supported(const qwm_paged_config* c) {
   if (c->kv_heads < 1 || c->kv_heads > 4096) return false;
   if (c->head_dim != 64 && c->head_dim != 128) return false;
@@ -150,7 +157,7 @@ qwm_status rope_impl(const qwm_rope_config* cfg, const float* inv_freq, const in
   if (k) add_segment(a, k, k_out, true, -1);
   return qwm::launch_rope(a, cfg->dtype, cfg->interleaved != 0, static_cast<cudaStream_t>(stream)) == cudaSuccess
              ? QWM_OK
-             : QWM_ERR_CUDA;
+             : cuda_error();
 }
 
 qwm_status check_batch(const qwm_paged* c, const qwm_paged_batch* b) {
@@ -240,7 +247,7 @@ qwm_status qwm_paged_init(qwm_paged** out, const qwm_paged_config* cfg, void* de
                           cfg->page_tokens, cfg->head_dim, cfg->dtype) ||
       cudaMemsetAsync(dev_buf, 0, QWM_PAGED_HEADER_BYTES, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
     delete c;
-    return QWM_ERR_CUDA;
+    return cuda_error();
   }
   *out = c;
   return QWM_OK;
@@ -252,9 +259,9 @@ qwm_status qwm_paged_status(qwm_paged* c, int32_t* status, void* stream) {
   if (!c || !status) return QWM_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int32_t v = 0;
-  if (cudaMemcpyAsync(&v, c->base, sizeof v, cudaMemcpyDeviceToHost, s) != cudaSuccess) return QWM_ERR_CUDA;
-  if (cudaStreamSynchronize(s) != cudaSuccess) return QWM_ERR_CUDA;
-  if (v != 0 && cudaMemsetAsync(c->base, 0, sizeof v, s) != cudaSuccess) return QWM_ERR_CUDA;
+  if (cudaMemcpyAsync(&v, c->base, sizeof v, cudaMemcpyDeviceToHost, s) != cudaSuccess) return cuda_error();
+  if (cudaStreamSynchronize(s) != cudaSuccess) return cuda_error();
+  if (v != 0 && cudaMemsetAsync(c->base, 0, sizeof v, s) != cudaSuccess) return cuda_error();
   *status = v;
   return QWM_OK;
 }
@@ -312,7 +319,7 @@ qwm_status qwm_paged_append(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   return qwm::launch_rope(a, c->cfg.dtype, !rope || rope->interleaved, static_cast<cudaStream_t>(stream)) ==
                  cudaSuccess
              ? QWM_OK
-             : QWM_ERR_CUDA;
+             : cuda_error();
 }
 
 size_t qwm_paged_attend_workspace_bytes(const qwm_paged* c, const qwm_paged_batch* b, int32_t q_heads,
@@ -380,7 +387,7 @@ qwm_status qwm_paged_attend(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = p.step ? qwm::launch_paged_step(a, c->map, D, c->cfg.dtype, s)
                                : qwm::launch_paged_chunk(a, c->map, D, c->cfg.dtype, s);
-  return e == cudaSuccess ? QWM_OK : QWM_ERR_CUDA;
+  return e == cudaSuccess ? QWM_OK : cuda_error();
 }
 
 }  // extern "C"

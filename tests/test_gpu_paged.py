@@ -1,6 +1,7 @@
 """GPU: append into paged storage and attention over its pages, against the
 formulas in 64 bits (tests/paged_ref.py).  Every slot that holds no token is
 NaN, so a kernel that let one through would show it."""
+import ctypes
 import math
 
 import pytest
@@ -609,3 +610,26 @@ def test_a_row_whose_logits_are_all_minus_infinity_is_an_empty_one(new, held, sp
     out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True, workspace=ws)
     assert bool((out[:, 0] == 0).all()) and bool((lse[0] == -math.inf).all())
     assert bool(out[:, 1].isnan().all()) and bool(lse[1].isnan().all()) and cache.status() == 0
+
+
+def test_an_error_is_reported_by_the_call_that_met_it_only():
+    """Reading the status on a stream that is being captured fails; the calls after it do
+    not."""
+    lens, Hk, D, page = [(1, 40)], 2, 128, 16
+    q, _, _, pages, table = make_case(95, lens, 4, Hk, D, BF, page)
+    cache, batch = build(lens, Hk, D, BF, page, pages, table)
+    dq, k = q.cuda(), torch.zeros(1, Hk, D, dtype=BF, device="cuda")
+    want = qwm.qwm_paged_attend(cache, batch, dq)
+    torch.cuda.synchronize()
+    runtime = ctypes.CDLL("libcudart.so.%d" % int(torch.version.cuda.split(".")[0]))   # loaded by PyTorch
+    side, graph = torch.cuda.Stream(), ctypes.c_void_p()
+    for call in (lambda: torch.equal(qwm.qwm_paged_attend(cache, batch, dq), want),
+                 lambda: qwm.qwm_paged_append(cache, batch, k, k) is None):
+        assert runtime.cudaStreamBeginCapture(ctypes.c_void_p(side.cuda_stream), 2) == 0
+        with torch.cuda.stream(side), pytest.raises(qwm.QwmError) as e:
+            cache.status()
+        assert e.value.status == 4
+        assert runtime.cudaStreamEndCapture(ctypes.c_void_p(side.cuda_stream), ctypes.byref(graph)) != 0
+        runtime.cudaGetLastError()
+        assert call()
+    assert cache.status() == 0
