@@ -3,7 +3,8 @@
 // Only marshalling, like the ctypes binding of the other entry points: dtypes,
 // shapes, strides and devices are checked, outputs that the caller does not
 // give are allocated by PyTorch, and raw pointers and the current stream go to
-// the C ABI of include/qwm.h.  It is compiled because a single token's call is
+// the C ABI of include/qwm.h.  A rotation that autograd has to record is left to
+// paged.py.  It is compiled because a single token's call is
 // as long as its binding: through ctypes 12 to 17 us a call, of which the launch
 // is 3.
 #include <Python.h>

@@ -17,7 +17,9 @@
 // m, l and O through the group (no barrier between them in the loop); then they
 // are merged through shared memory.  The rows are the M = 16 side of mma.sync: a
 // tcgen05 tile would be 128 rows high for the 1 to 16 used here, and its TMEM
-// round trip is longer than the whole of a short step.
+// round trip is longer than the whole of a short step.  P is rounded to the cache's
+// type for the product, after its sum (error against 64 bits 1.0 to 1.1 times the
+// fp32 form's).
 // A group cut by the ends of stretches is joined by the CTA that finishes last,
 // in the order of the keys, so the result does not depend on which one that is.
 #include "paged.cuh"

@@ -6,7 +6,8 @@ the sequences of a step; the calls are qwm_rope, qwm_rope_backward,
 qwm_paged_append and qwm_paged_attend.  Like the rest of the binding these only
 marshal arguments (dtypes, shapes, strides and devices are checked, PyTorch is
 used for device memory); they go through the compiled csrc/binding.cpp, because
-a call for a single token is as long as its binding.
+a call for a single token is as long as its binding.  Autograd records qwm_rope; the
+paged calls leave no history.
 """
 from __future__ import annotations
 
