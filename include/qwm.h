@@ -446,9 +446,10 @@ QWM_API qwm_status qwm_paged_set_idle_role(qwm_paged* cache, int32_t role);
 /* The sequences of one call.  Sequence b has the new tokens (rows of the
  * call's tensors) q_offsets[b] .. q_offsets[b+1]-1, q_offsets[0] = 0 and
  * q_offsets[num_seqs] = tokens (rows of no sequence are undefined and
- * QWM_ERR_INVALID_ARG in the status word), and holds kv_len[b] tokens, the new ones at
- * its end: row q_offsets[b] + i is its token p = kv_len[b] - q_len + i.  Token j
- * lives in page page_table[b * table_stride + j / page_tokens], slot j %
+ * QWM_ERR_INVALID_ARG in the status word; the others are not affected), and
+ * holds kv_len[b] tokens, the new ones at its end: row q_offsets[b] + i is its
+ * token p = kv_len[b] - q_len + i.  Token j lives in page
+ * page_table[b * table_stride + j / page_tokens], slot j %
  * page_tokens.  A row with p < 0 is not stored and sees nothing.  Entries of
  * pages that no row of a call touches are not read (pages that a window has
  * left behind can be given back and their entries set to -1).  max_q and

@@ -131,7 +131,9 @@ __device__ __forceinline__ void record_status(int32_t* status, int code) {
 }
 
 // Sequence b of the batch: its rows [q0, q0 + qn) and length kv, held to the
-// ranges that the tensors and the page table have (false: something was out).
+// ranges that the tensors and the page table have.  False: something was out, or the
+// first sequence does not start at row 0 or the last one not end at N, so that rows are
+// left out (their sequences are as good as ever).
 struct Seq {
   int64_t q0;
   int32_t qn, kv;
@@ -142,13 +144,12 @@ __device__ __forceinline__ bool load_seq(const A& a, int b, Seq& s) {
   const int64_t kv = a.kv_len[b];
   int64_t cap = (int64_t)a.table_stride << a.page_log2;
   if (cap > a.max_kv) cap = a.max_kv;
-  // the first sequence starts at row 0 and the last ends at N: no row is left out
-  const bool ok = (uint64_t)q0 <= (b > 0 ? (uint64_t)a.N : 0u) && q1 >= q0 && q1 <= a.N &&
-                  (b < a.B - 1 || q1 == a.N) && q1 - q0 <= a.max_q && kv >= 0 && kv <= cap;
+  const bool ok = q0 >= 0 && q1 >= q0 && q1 <= a.N && q1 - q0 <= a.max_q && kv >= 0 && kv <= cap;
   s.q0 = ok ? q0 : 0;
   s.qn = ok ? (int32_t)(q1 - q0) : 0;
   s.kv = ok ? (int32_t)kv : 0;
-  return ok;
+  const int64_t left = (b == 0 ? q0 : 0) | (b == a.B - 1 ? a.N - q1 : 0);   // rows left out
+  return ok && left == 0;
 }
 
 // The tokens a Query at token p sees: [0, min(sinks, hi)) and [lo, hi).

@@ -633,3 +633,19 @@ def test_an_error_is_reported_by_the_call_that_met_it_only():
         runtime.cudaGetLastError()
         assert call()
     assert cache.status() == 0
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("split", [False, True])
+def test_rows_of_no_sequence_leave_the_others_as_they_are(new, split):
+    """A tensor with rows before the first sequence and after the last."""
+    lens, Hk, D, page = [(new, 3000), (new, 2000)], 2, 128, 16
+    q, keys, values, pages, table = make_case(96, lens, 2, Hk, D, BF, page)
+    cache, sound = build(lens, Hk, D, BF, page, pages, table)
+    pad = torch.ones(5, 2, D, dtype=BF)
+    wide = torch.cat([pad[:3], q, pad]).cuda()
+    batch = qwm.PagedBatch(sound.tensors[0] + 3, sound.tensors[1], sound.tensors[2], new, 3000)
+    ws = qwm.paged_attend_workspace(cache, batch, 2) if split else None
+    out, lse = qwm.qwm_paged_attend(cache, batch, wide, want_lse=True, workspace=ws)
+    assert cache.status() == 1
+    compare(out[3:-5], lse[:, 3:-5], attend64(q, keys, values, lens, 1, 0, 0))
