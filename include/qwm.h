@@ -354,12 +354,12 @@ QWM_API qwm_status qwm_top1_keys(const qwm_config* cfg, const void* q, int64_t N
 
 /* ---------------------------------------------------------------------------
  * The uncompressed side of the cache: rotary positions over three axes,
- * Keys and Values appended to paged storage with the rotation applied on the
- * way, and softmax attention over the pages (block-causal, with a sliding
- * window and first tokens that stay visible).  Not part of the paper, which
+ * Keys and Values appended to paged storage (16 bits, or 8) with the rotation
+ * applied on the way, read back, and softmax attention over the pages
+ * (block-causal, with a sliding window and first tokens that stay visible).  Not part of the paper, which
  * takes post-rotation Keys and compresses finished chunks: these are the
  * steps next to it in a streaming model (the rotation before
- * qwm_quantize_append, the recent tokens kept in bf16, single new tokens).
+ * qwm_quantize_append, the recent tokens kept in 16 or 8 bits, single new tokens).
  *
  * Conventions of these calls beside those at the top of this file:
  *   - bf16 or binary16 tensors (qwm_dtype), given as qwm_rows: any order of
@@ -432,6 +432,21 @@ QWM_API size_t qwm_paged_bytes(const qwm_paged_config* cfg);
  * they are.  Freed with qwm_paged_free; the buffer stays the caller's. */
 QWM_API qwm_status qwm_paged_init(qwm_paged** out, const qwm_paged_config* cfg, void* dev_buf, size_t bytes,
                                   void* stream);
+/* Paged storage in 8 bits, with the same configuration: dtype is the type of the
+ * tensors that come and go, the pages hold e4m3 codes [num_pages][Keys, Values]
+ * [kv_heads][page_tokens][head_dim] behind the header, and after all pages a
+ * binary16 scale for each row, [num_pages][Keys, Values][kv_heads][page_tokens].
+ * A row (token, head) stands for code x scale.  As it is appended (a Key after its
+ * rotation, in fp32) the scale is the least power of two 2^e, -15 <= e <= 8, with
+ * max |x| <= 448 x 2^e over the row's channels, and a code the nearest e4m3 number
+ * to x / 2^e, ties to even.  Every code x scale is then exact in binary16 and in
+ * bf16; the error is at most |x| / 16 (and 2^(e - 10) near zero).  A magnitude
+ * above 61440 = 240 x 2^8 is stored as 61440 and a NaN as a NaN; one above 65504
+ * (an infinity too) or a NaN records QWM_ERR_NONFINITE in the status word.  All
+ * calls below take either kind of pages; both functions are as those above. */
+QWM_API size_t qwm_paged_bytes_e4m3(const qwm_paged_config* cfg);
+QWM_API qwm_status qwm_paged_init_e4m3(qwm_paged** out, const qwm_paged_config* cfg, void* dev_buf, size_t bytes,
+                                       void* stream);
 QWM_API void qwm_paged_free(qwm_paged* cache);
 /* As qwm_cache_status and qwm_cache_set_wait_limit, for paged storage. */
 QWM_API qwm_status qwm_paged_status(qwm_paged* cache, int32_t* status, void* stream);
@@ -473,6 +488,17 @@ QWM_API qwm_status qwm_paged_append(qwm_paged* cache, const qwm_paged_batch* bat
                                     const qwm_rows* v, const qwm_rope_config* rope, const float* inv_freq,
                                     const int32_t* pos, const qwm_rows* q, const qwm_rows* q_out, void* stream);
 
+/* Read the batch's tokens back, as qwm_paged_append numbers them: row
+ * q_offsets[b] + i is token kv_len[b] - q_len + i of sequence b (a kv_len short of
+ * the sequence's end reads earlier tokens).  k_out and v_out are [tokens][kv_heads]
+ * [head_dim] of the cache's dtype; either may be NULL.  8-bit pages give code x
+ * scale rounded to that type, which is exact for rows that were appended; a row with
+ * p < 0, or whose entries are out of range, gives zeros.  The outputs must not
+ * overlap one another (refused where base addresses or strides are equal) or lie in
+ * the cache's buffer. */
+QWM_API qwm_status qwm_paged_read(qwm_paged* cache, const qwm_paged_batch* batch, const qwm_rows* k_out,
+                                  const qwm_rows* v_out, void* stream);
+
 /* Which tokens a Query at token p of its sequence sees: with the end of its
  * block e = (p / block + 1) * block, token j iff
  *   j < min(e, kv_len) and (window == 0 or j >= e - window or j < sinks).
@@ -488,7 +514,10 @@ typedef struct qwm_mask {
  * out = softmax(sm_scale q k^T) v over the visible tokens, with q of
  * q_heads = q->heads heads, a multiple of kv_heads (Query head h reads head
  * h / (q_heads / kv_heads)).  Logits, softmax statistics and sums are fp32; the
- * probabilities enter the tensor cores in the cache's type.  lse: fp32
+ * probabilities enter the tensor cores in the cache's type.  8-bit pages are
+ * multiplied in binary16, which holds their values exactly (code x scale rounded to
+ * it, where a caller wrote the scales itself), with bf16 Queries scaled to its range
+ * row by row.  lse: fp32
  * [q_heads][tokens] natural-log sum-exp of the scaled logits, or NULL.  out must
  * not overlap q (refused where base addresses or strides are equal).
  * 0 < sm_scale <= 1e38; max_q * (q_heads / kv_heads) <= 2^38.  A row that sees

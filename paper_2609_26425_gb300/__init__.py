@@ -30,7 +30,7 @@ import torch
 
 from . import paged as _paged
 from .paged import (PagedBatch, PagedCache, Rope, paged_attend_workspace, qwm_paged_append, qwm_paged_attend,
-                    qwm_paged_attend_workspace_bytes, qwm_rope, qwm_rope_backward)
+                    qwm_paged_attend_workspace_bytes, qwm_paged_read, qwm_rope, qwm_rope_backward)
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_build", "libqwm.so")

@@ -21,7 +21,7 @@ BINDING = os.path.join(OUT, "qwm_binding.so")  # csrc/binding.cpp, against PyTor
 STAMP = os.path.join(OUT, "qwm_binding.txt")   # which PyTorch that was
 SOURCES = ["qwm_api.cu", "append.cu", "append_fused.cu", "append_fused_r8.cu", "append_fused_r16.cu",
            "append_fused_r32.cu", "append_generic.cu", "append_full.cu", "attend.cu", "fit.cu", "qstats.cu",
-           "metrics.cu", "rope.cu", "paged_api.cu", "paged_step.cu", "paged_chunk.cu"]
+           "metrics.cu", "rope.cu", "paged_codes.cu", "paged_api.cu", "paged_step.cu", "paged_chunk.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
          "--expt-relaxed-constexpr"]

@@ -137,7 +137,9 @@ bool integer(PyObject* o, const char* name, int64_t lo, int64_t hi, int64_t* v) 
 }
 
 // What a rotation, a cache or a batch keeps for its calls: integers, the last of them
-// the device of what they stand for, which has to be the tensors'.
+// the device of what they stand for, which has to be the tensors' (kAnyDevice: it tells
+// the device).
+constexpr int kAnyDevice = -2;
 template <int N>
 bool key(PyObject* o, const char* name, int device, int64_t (&v)[N]) {
   if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != N) {
@@ -146,7 +148,7 @@ bool key(PyObject* o, const char* name, int device, int64_t (&v)[N]) {
   }
   for (int i = 0; i < N; ++i)
     if (!integer(PyTuple_GET_ITEM(o, i), name, INT64_MIN, INT64_MAX, &v[i])) return false;
-  if (v[N - 1] != device) {
+  if (device != kAnyDevice && v[N - 1] != device) {
     PyErr_Format(PyExc_ValueError, "the %s is on another device (%lld) than the tensors (%d)", name, (long long)v[N - 1], device);
     return false;
   }
@@ -216,15 +218,18 @@ struct Cache {
   int64_t d;
   at::ScalarType type;
 };
-// The cache for tensors of `like`'s device.
-bool cache_of(PyObject* o, const at::Tensor& like, Cache* c) {
+// The cache, for tensors of `device`; kAnyDevice, and `own` tells the cache's.
+bool cache_on(PyObject* o, int device, Cache* c, int* own = nullptr) {
   int64_t v[4];
-  if (!key(o, "paged cache", like.is_cuda() ? like.get_device() : -1, v)) return false;
+  if (!key(o, "paged cache", device, v)) return false;
   c->handle = reinterpret_cast<qwm_paged*>(v[0]);
   c->d = v[1];
   c->type = v[2] == QWM_F16 ? at::kHalf : at::kBFloat16;
+  if (own) *own = (int)v[3];
   return true;
 }
+// The cache for tensors of `like`'s device.
+bool cache_of(PyObject* o, const at::Tensor& like, Cache* c) { return cache_on(o, like.is_cuda() ? like.get_device() : -1, c); }
 bool batch_of(PyObject* o, int64_t n, int device, qwm_paged_batch* b) {
   int64_t v[3];
   if (!key(o, "paged batch", device, v)) return false;
@@ -269,6 +274,59 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   if (st != QWM_OK) return fail("qwm_paged_append", st);
   return has_q ? q_out.release() : Py_NewRef(Py_None);
+}
+
+// read(cache, batch, kv_heads, rows or -1, k_out or None or False, v_out or None or False);
+// None: a new tensor, False: not wanted (None in its place)
+PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Cache c;
+  int dev;
+  int64_t H, N, v[3];
+  if (!count(n, 6) || !cache_on(a[0], kAnyDevice, &c, &dev) || !integer(a[2], "kv_heads", 1, 4096, &H) ||
+      !integer(a[3], "tokens", -1, INT32_MAX, &N))
+    return nullptr;
+  const at::Tensor* given[2] = {nullptr, nullptr};
+  for (int i = 0; i < 2; ++i) {
+    PyObject* o = a[4 + i];
+    if (o == Py_None || o == Py_False) continue;
+    if (!(given[i] = tensor(o, i ? "v_out" : "k_out"))) return nullptr;
+    if (N < 0 && given[i]->dim() == 3) N = given[i]->size(0);
+  }
+  if (!key(a[1], "paged batch", dev, v)) return nullptr;
+  if (N < 0) N = v[1];
+  if (N < 0) {
+    PyErr_SetString(PyExc_ValueError, "the number of tokens to read is not known: give it, an output, or a batch made with it");
+    return nullptr;
+  }
+  qwm_paged_batch b;
+  if (!batch_of(a[1], N, dev, &b)) return nullptr;
+  qwm_rows r[2];
+  Ref ret[2];
+  for (int i = 0; i < 2; ++i) {
+    if (a[4 + i] == Py_False) {
+      ret[i].p = Py_NewRef(Py_None);
+    } else if (given[i]) {
+      if (!rows(*given[i], c.type, dev, i ? "v_out" : "k_out", N, c.d, &r[i])) return nullptr;
+      ret[i].p = Py_NewRef(a[4 + i]);
+    } else {
+      const at::Tensor t = at::empty({N, H, c.d}, at::TensorOptions().dtype(c.type).device(at::kCUDA, (c10::DeviceIndex)dev));
+      r[i] = qwm_rows{t.data_ptr(), H * c.d, c.d, (int32_t)H};
+      ret[i].p = THPVariable_Wrap(t);
+      if (!ret[i].p) return nullptr;
+    }
+  }
+  for (const at::Tensor* t : given)
+    if (t) written(*t);
+  qwm_status st;
+  {
+    const c10::cuda::CUDAGuard guard(dev);
+    void* s = c10::cuda::getCurrentCUDAStream(dev).stream();
+    Py_BEGIN_ALLOW_THREADS
+    st = qwm_paged_read(c.handle, &b, a[4] == Py_False ? nullptr : &r[0], a[5] == Py_False ? nullptr : &r[1], s);
+    Py_END_ALLOW_THREADS
+  }
+  if (st != QWM_OK) return fail("qwm_paged_read", st);
+  return result(ret[0], ret[1]);
 }
 
 // attend(cache, batch, q, block, window, sinks, sm_scale, out or None, lse or None, want_lse, workspace or None)
@@ -360,6 +418,7 @@ PyCFunction fast() {
 PyMethodDef methods[] = {
     {"turn", fast<turn>(), METH_FASTCALL, nullptr},
     {"append", fast<append>(), METH_FASTCALL, nullptr},
+    {"read", fast<read>(), METH_FASTCALL, nullptr},
     {"attend", fast<attend>(), METH_FASTCALL, nullptr},
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},

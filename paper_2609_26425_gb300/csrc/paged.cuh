@@ -30,9 +30,26 @@ struct RopeArgs {
   int32_t B, table_stride, page_log2, kv_heads, max_q, max_kv;
   int64_t num_pages;
   void* pages;
+  __half* scales;               // of the rows of 8-bit pages; null: 16-bit pages
   int32_t* status;
 };
 cudaError_t launch_rope(const RopeArgs& a, int dtype, bool interleaved, cudaStream_t s);
+cudaError_t launch_store(const RopeArgs& a, int dtype, bool interleaved, cudaStream_t s);
+
+// ------------------------------------------------------------ read-back
+struct ReadArgs {
+  const uint8_t* pages;
+  const __half* scales;         // null: 16-bit pages
+  void* out[2];                 // Keys, Values (null: not wanted)
+  int32_t o_tok[2], o_head[2];  // strides in elements
+  int32_t D;
+  int64_t N;
+  const int32_t *q_off, *kv_len, *table;
+  int32_t B, table_stride, page_log2, kv_heads, max_q, max_kv;
+  int64_t num_pages;
+  int32_t* status;
+};
+cudaError_t launch_read(const ReadArgs& a, int dtype, cudaStream_t s);
 
 // ------------------------------------------------------------ attention
 struct PagedArgs {
@@ -47,6 +64,7 @@ struct PagedArgs {
   int32_t page_log2;
   int64_t num_pages;
   const void* pages;
+  const __half* scales;                  // of the rows of 8-bit pages; null: 16-bit pages
   int32_t block, window, sinks;
   float scale;
   int32_t* status;
@@ -69,7 +87,7 @@ struct PagedPlan {
   int32_t rows;      // rows of a group
   int32_t nsplit, min_tiles;
 };
-PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split);
+PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split, bool codes);
 PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, bool split);
 cudaError_t launch_paged_step(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s);
 cudaError_t launch_paged_chunk(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s);
@@ -117,6 +135,9 @@ constexpr int kStepRows = 16;
 // Pages as rows of D channels, [num_pages * 2 * heads][page_tokens][D]: boxes of
 // 64 channels x min(page_tokens, 64) tokens, 128-byte swizzle.
 bool make_page_map(CUtensorMap* m, const void* pages, int64_t blocks, int page_tokens, int D, int dtype);
+// The same of 8-bit pages: boxes of D codes x min(page_tokens, 64) tokens, swizzled by the
+// row's length (128 or 64 bytes).
+bool make_code_map(CUtensorMap* m, const void* pages, int64_t blocks, int page_tokens, int D);
 
 // ------------------------------------------------------------ device helpers
 #ifdef __CUDACC__
@@ -128,6 +149,32 @@ __device__ __forceinline__ void grid_begin() {
 
 __device__ __forceinline__ void record_status(int32_t* status, int code) {
   if (status) atomicCAS(status, 0, code);
+}
+
+// The row of a token's first Key in the pages, as ((page * 2) * heads) * page_tokens + slot,
+// < 0: nowhere.  Row n of the call belongs to the last sequence that begins at or before it.
+template <class A>
+__device__ __forceinline__ int64_t place_of(const A& a, int64_t n) {
+  int lo = 0, hi = a.B;                            // last b with q_off[b] <= n
+  while (hi - lo > 1) {
+    const int m = (lo + hi) >> 1;
+    if (a.q_off[m] <= n) lo = m; else hi = m;
+  }
+  const int64_t q0 = a.q_off[lo], q1 = a.q_off[lo + 1], kv = a.kv_len[lo];
+  int64_t cap = (int64_t)a.table_stride << a.page_log2;
+  if (cap > a.max_kv) cap = a.max_kv;
+  if (!(n >= q0 && n < q1 && q1 <= a.N && q1 - q0 <= a.max_q && kv >= 0 && kv <= cap)) {
+    record_status(a.status, QWM_ERR_INVALID_ARG);
+    return -1;
+  }
+  const int64_t p = kv - q1 + n;
+  if (p < 0) return -1;
+  const int64_t page = a.table[(int64_t)lo * a.table_stride + (p >> a.page_log2)];
+  if (page < 0 || page >= a.num_pages) {
+    record_status(a.status, QWM_ERR_INVALID_ARG);
+    return -1;
+  }
+  return ((page * 2 * a.kv_heads) << a.page_log2) + (p & ((1 << a.page_log2) - 1));
 }
 
 // Sequence b of the batch: its rows [q0, q0 + qn) and length kv, held to the
@@ -253,6 +300,93 @@ struct Elem<__half> {
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
 };
+// ------------------------------------------------------------ 8-bit storage
+// A row (token, head) of 8-bit pages stands for code x scale: e4m3 codes and a binary16
+// power of two 2^e, -15 <= e <= 8, so that every product is a binary16 (and a bf16) number:
+// codes are multiples of 2^-9 and binary16 of 2^-24, and 240 x 2^8 is the largest e4m3
+// multiple of a power of two below 65504.
+constexpr float kCodeMost = 61440.0f;
+
+// The scale's biased exponent for a row whose largest magnitude is `most` <= kCodeMost: the
+// least e >= -15 with most <= 448 x 2^e (448 = 1.75 x 2^8: a mantissa above 0.75 carries).
+__device__ __forceinline__ uint32_t code_exponent(float most) {
+  const int e = (int)((__float_as_uint(most) + 0x1FFFFFu) >> 23) - 8;
+  return (uint32_t)max(e, 127 - 15);
+}
+// 2^e (and 2^-e) of a biased exponent 112 <= e <= 135
+__device__ __forceinline__ __half code_scale(uint32_t e) { return __float2half_rn(__uint_as_float(e << 23)); }
+__device__ __forceinline__ float code_inverse(uint32_t e) { return __uint_as_float((254u - e) << 23); }
+
+// Four values (already divided by their scale) as codes, the first in the low byte.
+__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
+  uint32_t w;
+  asm("{\n\t.reg .b16 l, h;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\t"
+      "mov.b32 %0, {l, h};\n\t}"
+      : "=r"(w)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
+  return w;
+}
+// Four codes as two pairs of binary16 numbers (exact; a NaN code gives NaN).
+__device__ __forceinline__ void from_codes(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\t"
+      "mov.b32 {l, h}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, l;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// The type that products over the pages are taken in.
+template <typename T, bool C8>
+struct OperandOf {
+  using type = T;
+};
+template <typename T>
+struct OperandOf<T, true> {
+  using type = __half;
+};
+template <typename T, bool C8>
+using Operand = typename OperandOf<T, C8>::type;
+
+// bf16 Queries as binary16: a row is taken times the power of two that brings its largest
+// finite magnitude to [2^14, 2^15), and its logits' scale by the inverse.  Exact but for
+// elements 2^-29 and less of the largest, which round to a multiple of 2^-39 of it.
+// The largest magnitude's bits of eight elements, infinities and NaN left out.
+__device__ __forceinline__ uint32_t finite_max(uint4 v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t lo = w[k] & 0x7FFFu, hi = (w[k] >> 16) & 0x7FFFu;
+    top = max(top, max(lo < 0x7F80u ? lo : 0u, hi < 0x7F80u ? hi : 0u));
+  }
+  return top;
+}
+__device__ __forceinline__ int row_power(uint32_t top) { return 14 + 127 - max((int)(top >> 7), 1); }   // -113 .. 140
+// x 2^up in two steps, each a normal number
+__device__ __forceinline__ float times_pow2(float x, int up) {
+  const int h = up >> 1;
+  return x * __uint_as_float((uint32_t)(127 + h) << 23) * __uint_as_float((uint32_t)(127 + up - h) << 23);
+}
+__device__ __forceinline__ uint32_t scaled_f16(uint32_t w, int up) {
+  const float2 f = Elem<__nv_bfloat16>::unpack(w);
+  return Elem<__half>::pack(times_pow2(f.x, up), times_pow2(f.y, up));
+}
+__device__ __forceinline__ uint4 scaled_f16(uint4 v, int up) {
+  return make_uint4(scaled_f16(v.x, up), scaled_f16(v.y, up), scaled_f16(v.z, up), scaled_f16(v.w, up));
+}
+// The scale of a row's logits, normal and finite (0 x inf and inf x 0 are not 0)
+__device__ __forceinline__ float row_scale(float sl2, int up) {
+  return fminf(fmaxf(times_pow2(sl2, -up), 1.2e-38f), 1.0e38f);
+}
+
 // Whether a word of two elements holds an infinity or a NaN.
 template <typename T>
 __device__ __forceinline__ bool nonfinite2(uint32_t w) {

@@ -7,6 +7,7 @@
 
 struct qwm_paged {
   qwm_paged_config cfg;
+  bool codes;                   // 8-bit pages
   uint8_t* base;
   CUtensorMap map;
   int32_t page_log2;
@@ -41,6 +42,45 @@ bool paged_supported(const qwm_paged_config* c) {
   if (c->dtype != QWM_BF16 && c->dtype != QWM_F16) return false;
   if (c->num_pages < 1 || c->num_pages > (((int64_t)1 << 31) - 1) / (2 * c->kv_heads)) return false;
   return true;
+}
+
+// Rows (token, head) of the pages
+int64_t page_rows(const qwm_paged_config* c) { return c->num_pages * 2 * c->kv_heads * c->page_tokens; }
+size_t paged_bytes(const qwm_paged_config* c, bool codes) {
+  if (!c || !paged_supported(c)) return 0;
+  const size_t rows = (size_t)page_rows(c);
+  return QWM_PAGED_HEADER_BYTES + (codes ? rows * (c->head_dim + 2) : rows * c->head_dim * 2);
+}
+uint8_t* pages_of(const qwm_paged* c) { return c->base + QWM_PAGED_HEADER_BYTES; }
+__half* scales_of(const qwm_paged* c) {
+  return c->codes ? reinterpret_cast<__half*>(pages_of(c) + (size_t)page_rows(&c->cfg) * c->cfg.head_dim) : nullptr;
+}
+
+qwm_status paged_init(qwm_paged** out, const qwm_paged_config* cfg, void* dev_buf, size_t bytes, bool codes, void* stream) {
+  if (!out || !cfg || !dev_buf) return QWM_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!paged_supported(cfg)) return QWM_ERR_UNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(dev_buf) & 255u) != 0) return QWM_ERR_INVALID_ARG;
+  if (bytes < paged_bytes(cfg, codes)) return QWM_ERR_CAPACITY;
+  qwm_paged* c = new (std::nothrow) qwm_paged();
+  if (!c) return QWM_ERR_INVALID_ARG;
+  c->cfg = *cfg;
+  c->codes = codes;
+  c->base = static_cast<uint8_t*>(dev_buf);
+  c->page_log2 = ilog2(cfg->page_tokens);
+  c->wait_ns = 2000000000ull;
+  const int64_t blocks = cfg->num_pages * 2 * cfg->kv_heads;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&c->nsm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+      !(codes ? qwm::make_code_map(&c->map, pages_of(c), blocks, cfg->page_tokens, cfg->head_dim)
+              : qwm::make_page_map(&c->map, pages_of(c), blocks, cfg->page_tokens, cfg->head_dim, cfg->dtype)) ||
+      cudaMemsetAsync(dev_buf, 0, QWM_PAGED_HEADER_BYTES, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+    delete c;
+    return cuda_error();
+  }
+  *out = c;
+  return QWM_OK;
 }
 
 // A tensor that the kernels can read in 16-byte vectors.
@@ -187,7 +227,7 @@ PagedPlan make_plan(const qwm_paged* c, const qwm_paged_batch* b, int32_t q_head
     if (w < seen) seen = w;
   }
   return rows <= qwm::kStepRows ? qwm::plan_step(b->num_seqs, c->cfg.kv_heads, c->cfg.head_dim, (int)rows, seen, c->nsm,
-                                               split)
+                                               split, c->codes)
                                 : qwm::plan_chunk(b->num_seqs, c->cfg.kv_heads, rows, seen, c->nsm, split);
 }
 
@@ -223,34 +263,14 @@ qwm_status qwm_rope_backward(const qwm_rope_config* cfg, const float* inv_freq, 
   return rope_impl(cfg, inv_freq, pos, N, dq, dq_out, dk, dk_out, -1.0f, stream);
 }
 
-size_t qwm_paged_bytes(const qwm_paged_config* c) {
-  if (!c || !paged_supported(c)) return 0;
-  return QWM_PAGED_HEADER_BYTES + (size_t)c->num_pages * 2 * c->kv_heads * c->page_tokens * c->head_dim * 2;
-}
+size_t qwm_paged_bytes(const qwm_paged_config* c) { return paged_bytes(c, false); }
+size_t qwm_paged_bytes_e4m3(const qwm_paged_config* c) { return paged_bytes(c, true); }
 
 qwm_status qwm_paged_init(qwm_paged** out, const qwm_paged_config* cfg, void* dev_buf, size_t bytes, void* stream) {
-  if (!out || !cfg || !dev_buf) return QWM_ERR_INVALID_ARG;
-  *out = nullptr;
-  if (!paged_supported(cfg)) return QWM_ERR_UNSUPPORTED;
-  if ((reinterpret_cast<uintptr_t>(dev_buf) & 255u) != 0) return QWM_ERR_INVALID_ARG;
-  if (bytes < qwm_paged_bytes(cfg)) return QWM_ERR_CAPACITY;
-  qwm_paged* c = new (std::nothrow) qwm_paged();
-  if (!c) return QWM_ERR_INVALID_ARG;
-  c->cfg = *cfg;
-  c->base = static_cast<uint8_t*>(dev_buf);
-  c->page_log2 = ilog2(cfg->page_tokens);
-  c->wait_ns = 2000000000ull;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&c->nsm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-      !qwm::make_page_map(&c->map, c->base + QWM_PAGED_HEADER_BYTES, cfg->num_pages * 2 * cfg->kv_heads,
-                          cfg->page_tokens, cfg->head_dim, cfg->dtype) ||
-      cudaMemsetAsync(dev_buf, 0, QWM_PAGED_HEADER_BYTES, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
-    delete c;
-    return cuda_error();
-  }
-  *out = c;
-  return QWM_OK;
+  return paged_init(out, cfg, dev_buf, bytes, false, stream);
+}
+qwm_status qwm_paged_init_e4m3(qwm_paged** out, const qwm_paged_config* cfg, void* dev_buf, size_t bytes, void* stream) {
+  return paged_init(out, cfg, dev_buf, bytes, true, stream);
 }
 
 void qwm_paged_free(qwm_paged* c) { delete c; }
@@ -314,12 +334,55 @@ qwm_status qwm_paged_append(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   a.page_log2 = c->page_log2;
   a.kv_heads = c->cfg.kv_heads;
   a.num_pages = c->cfg.num_pages;
-  a.pages = c->base + QWM_PAGED_HEADER_BYTES;
+  a.pages = pages_of(c);
+  a.scales = scales_of(c);
   a.status = reinterpret_cast<int32_t*>(c->base);
-  return qwm::launch_rope(a, c->cfg.dtype, !rope || rope->interleaved, static_cast<cudaStream_t>(stream)) ==
-                 cudaSuccess
+  return (c->codes ? qwm::launch_store : qwm::launch_rope)(a, c->cfg.dtype, !rope || rope->interleaved,
+                                                           static_cast<cudaStream_t>(stream)) == cudaSuccess
              ? QWM_OK
              : cuda_error();
+}
+
+qwm_status qwm_paged_read(qwm_paged* c, const qwm_paged_batch* b, const qwm_rows* k_out, const qwm_rows* v_out,
+                          void* stream) {
+  if (!c || !b || (!k_out && !v_out)) return QWM_ERR_INVALID_ARG;
+  const qwm_status st = check_batch(c, b);
+  if (st != QWM_OK) return st;
+  if (b->tokens == 0) return QWM_OK;
+  const int D = c->cfg.head_dim;
+  const qwm_rows* out[2] = {k_out, v_out};
+  for (const qwm_rows* r : out)
+    if (r && (!out_ok(r, b->tokens, D) || r->heads != c->cfg.kv_heads)) return QWM_ERR_INVALID_ARG;
+  if (k_out && v_out && overlaps(k_out, v_out, b->tokens, D)) return QWM_ERR_INVALID_ARG;
+  for (const qwm_rows* r : out) {                    // nor over the pages themselves
+    if (!r) continue;
+    const uint8_t *lo = static_cast<const uint8_t*>(r->data), *end = c->base + paged_bytes(&c->cfg, c->codes);
+    const int64_t ts = b->tokens > 1 ? r->token_stride : 0, hs = r->heads > 1 ? r->head_stride : 0;
+    if (lo < end && lo + 2 * ((b->tokens - 1) * ts + (r->heads - 1) * hs + D) > c->base) return QWM_ERR_INVALID_ARG;
+  }
+  qwm::ReadArgs a{};
+  for (int i = 0; i < 2; ++i) {
+    if (!out[i]) continue;
+    a.out[i] = out[i]->data;
+    a.o_tok[i] = (int32_t)out[i]->token_stride;
+    a.o_head[i] = (int32_t)out[i]->head_stride;
+  }
+  a.D = D;
+  a.N = b->tokens;
+  a.q_off = b->q_offsets;
+  a.kv_len = b->kv_len;
+  a.table = b->page_table;
+  a.B = b->num_seqs;
+  a.table_stride = b->table_stride;
+  a.max_q = b->max_q;
+  a.max_kv = b->max_kv;
+  a.page_log2 = c->page_log2;
+  a.kv_heads = c->cfg.kv_heads;
+  a.num_pages = c->cfg.num_pages;
+  a.pages = pages_of(c);
+  a.scales = scales_of(c);
+  a.status = reinterpret_cast<int32_t*>(c->base);
+  return qwm::launch_read(a, c->cfg.dtype, static_cast<cudaStream_t>(stream)) == cudaSuccess ? QWM_OK : cuda_error();
 }
 
 size_t qwm_paged_attend_workspace_bytes(const qwm_paged* c, const qwm_paged_batch* b, int32_t q_heads,
@@ -367,7 +430,8 @@ qwm_status qwm_paged_attend(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   a.G = q->heads / c->cfg.kv_heads;
   a.page_log2 = c->page_log2;
   a.num_pages = c->cfg.num_pages;
-  a.pages = c->base + QWM_PAGED_HEADER_BYTES;
+  a.pages = pages_of(c);
+  a.scales = scales_of(c);
   a.block = mask->block;
   a.window = mask->window;
   a.sinks = mask->sinks;

@@ -50,6 +50,7 @@ enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VRDY = 6, B_VEMPTY = 8, B_SFULL
 constexpr int NQ = 2, ROWS = 128 * NQ;               // row tiles and rows of a CTA
 constexpr int W_MMA = 4 * NQ, W_K = W_MMA + 1, W_V = W_MMA + 2;  // W_MMA + 3: the guard
 constexpr int NT = (4 * NQ + 4) * 32;
+constexpr int kRebuild = 3;                          // 8-bit pages: the last three warps make K and V from codes
 
 template <int D>
 struct Smem {
@@ -95,14 +96,137 @@ __device__ __forceinline__ uint32_t bits(int a, int b) {
 constexpr float pow2(int e) { return e > 0 ? 2.0f * pow2(e - 1) : (e < 0 ? 0.5f * pow2(e + 1) : 1.0f); }
 // Natural-log sum-exp of a row: `m` is the power that its P were taken against, l
 // their sum.  -inf (and log 0) where nothing was seen, NaN with a NaN sum.
-template <typename T>
+template <typename Op>
 __device__ __forceinline__ float log_sum(float m, float l) {
-  return (m - (float)Elem<T>::kBias + log2f(l * pow2(Elem<T>::kBias))) * 0.69314718055994531f;
+  return (m - (float)Elem<Op>::kBias + log2f(l * pow2(Elem<Op>::kBias))) * 0.69314718055994531f;
 }
 
-template <typename T, int D>
+// K and V of 8-bit pages: warp `rank` of three turns its share of each tile's codes
+// into binary16 where the TMA of 16-bit pages would have put them, so that the MMAs
+// are the same.  Codes go from global memory to registers, a tile ahead (through
+// shared memory they would take 64 KB more than it has, and a third of its
+// bandwidth, which the MMAs need); 16 of them a lane, D / 16 lanes a row.  Values that no
+// row of the CTA sees are cleared on the way, those that some see and others do not
+// searched (the guard's work).  False: a wait ran out.
+template <int D>
+__device__ __forceinline__ bool rebuild_tiles(const PagedArgs& a, uint8_t* sm, const Tiles& tl, int t0, int n, int b, int hk,
+                                              int rank, int* poison) {
+  using L = Smem<D>;
+  constexpr int NB = L::NB, LPR = D / 16, RPL = 32 / LPR;   // lanes of a row, rows of a load
+  constexpr int LOADS = TK / RPL, NL = (LOADS + kRebuild - 1) / kRebuild;
+  const int lane = threadIdx.x & 31, c = lane % LPR, sub = lane / LPR;
+  auto bar = [&](int i) { return smem_u32(sm + L::BAR) + 8u * i; };
+  auto wait_all = [&](int i, uint32_t ph) -> bool { return __all_sync(0xFFFFFFFFu, mbar_wait(bar(i), ph, a.wait_ns)); };
+  const int32_t* trow = a.table + (int64_t)b * a.table_stride;
+  const uint8_t* pages = static_cast<const uint8_t*>(a.pages);
+  const int64_t vrows = (int64_t)a.Hk << a.page_log2;       // from a token's Key to its Value, in rows
+  // Lane x (of 8, four times over) keeps the row of the Keys of the tile's tokens 16 x ..
+  // 16 x + 15, or -1 where no row of the CTA sees them.
+  auto look_up = [&](int jt) -> int64_t {
+    if (jt >= n) return -1;
+    const int j = tile_at(tl, t0 + jt) * TK + 16 * (lane & 7);
+    if (!any_sees(tl, j, j + 16, a.sinks)) return -1;
+    int64_t page = trow[j >> a.page_log2];
+    if (page < 0 || page >= a.num_pages) {            // not followed: the first page in its place
+      record_status(a.status, QWM_ERR_INVALID_ARG);
+      page = 0;
+    }
+    return ((page * 2 * a.Hk + hk) << a.page_log2) + (j & ((1 << a.page_log2) - 1));
+  };
+  struct Codes {
+    uint4 c[NL];
+    uint2 s;                                          // scales of the tile's rows 4 lane .. 4 lane + 3
+  };
+  auto fetch = [&](Codes& x, int64_t first, int64_t more) {
+    const int64_t mine = __shfl_sync(0xFFFFFFFFu, first, lane >> 2);
+    x.s = make_uint2(0, 0);
+    if (mine >= 0) x.s = *reinterpret_cast<const uint2*>(a.scales + mine + more + 4 * (lane & 3));
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int l = rank + kRebuild * i;
+      x.c[i] = make_uint4(0, 0, 0, 0);
+      if (l >= LOADS) continue;
+      const int64_t row = __shfl_sync(0xFFFFFFFFu, first, (l * RPL) >> 4);
+      if (row >= 0)
+        x.c[i] = *reinterpret_cast<const uint4*>(pages + (row + more + ((l * RPL) & 15) + sub) * D + 16 * c);
+    }
+  };
+  auto store = [&](Codes& x, uint8_t* tile, bool values, int j0) {
+    const bool open = !values || all_see(tl, j0, j0 + TK, a.sinks);
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int l = rank + kRebuild * i;
+      if (l >= LOADS) continue;
+      const int row = l * RPL + sub;
+      const uint32_t s01 = __shfl_sync(0xFFFFFFFFu, x.s.x, row >> 2), s23 = __shfl_sync(0xFFFFFFFFu, x.s.y, row >> 2);
+      const uint32_t s2 = __byte_perm(row & 2 ? s23 : s01, 0, row & 1 ? 0x3232 : 0x1010);
+      uint32_t h[8];
+      from_codes(x.c[i].x, h[0], h[1]);
+      from_codes(x.c[i].y, h[2], h[3]);
+      from_codes(x.c[i].z, h[4], h[5]);
+      from_codes(x.c[i].w, h[6], h[7]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) h[k] = mul_f16x2(h[k], s2);
+      if (!open) {
+        const int j = j0 + row;
+        if (!any_sees(tl, j, j + 1, a.sinks)) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) h[k] = 0u;
+        } else if (!all_see(tl, j, j + 1, a.sinks)) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            if (!nonfinite2<__half>(h[k])) continue;
+            if ((h[k] & 0x7C00u) == 0x7C00u) h[k] &= 0xFFFF0000u;
+            if ((h[k] & 0x7C000000u) == 0x7C000000u) h[k] &= 0xFFFFu;
+            odd = true;
+          }
+        }
+      }
+      const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
+      uint8_t* at = tile + (c >> 2) * BLK + row * 128;        // channels 16 c ..: chunks 2 c and 2 c + 1 of 8
+      const int k0 = (2 * c) & 7, sw = row & 7;
+      // the lanes of the upper channels write their second chunk first: no two of the
+      // eight lanes of a row on one bank
+      const bool flip = D == 128 && c >= 4;
+      *reinterpret_cast<uint4*>(at + (((k0 + flip) ^ sw) << 4)) = flip ? hi : lo;
+      *reinterpret_cast<uint4*>(at + (((k0 + !flip) ^ sw) << 4)) = flip ? lo : hi;
+    }
+    if (odd) *poison = 1;
+  };
+  bool ok = true;
+  if (a.idle) return true;
+  Codes k, v;
+  int64_t here = look_up(0), next = look_up(1);
+  if (n > 0) {
+    fetch(k, here, 0);
+    fetch(v, here, vrows);
+  }
+  for (int jt = 0; jt < n; ++jt) {
+    const int s = jt & 1, j0 = tile_at(tl, t0 + jt) * TK;
+    if (jt >= ST && !(ok = wait_all(B_KEMPTY + s, ((jt >> 1) - 1) & 1))) break;
+    store(k, sm + L::K + s * NB * BLK, false, j0);
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(B_KFULL + s));
+    if (jt + 1 < n) fetch(k, next, 0);
+    if (jt >= ST && !(ok = wait_all(B_VEMPTY + s, ((jt >> 1) - 1) & 1))) break;
+    store(v, sm + L::V + s * NB * BLK, true, j0);
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(B_VRDY + s));
+    if (jt + 1 < n) fetch(v, next, vrows);
+    next = look_up(jt + 2);
+  }
+  return ok;
+}
+
+// T: the type of Queries and output; C8: 8-bit pages, whose products are taken in
+// binary16 (every code x scale is one).
+template <typename T, int D, bool C8>
 __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
   using L = Smem<D>;
+  using Op = Operand<T, C8>;
   constexpr int NB = L::NB;
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -113,10 +237,10 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
   auto bar = [&](int i) { return smem_u32(sm + L::BAR) + 8u * i; };
   if (tid == 0) {
     for (int s = 0; s < 2; ++s) {
-      mbar_init(bar(B_KFULL + s), 1);
+      mbar_init(bar(B_KFULL + s), C8 ? kRebuild : 1);
       mbar_init(bar(B_KEMPTY + s), 1);
       mbar_init(bar(B_VFULL + s), 1);
-      mbar_init(bar(B_VRDY + s), 1);
+      mbar_init(bar(B_VRDY + s), C8 ? kRebuild : 1);
       mbar_init(bar(B_VEMPTY + s), 1);
       mbar_init(bar(B_SFULL + s), 1);
       mbar_init(bar(B_PV + s), 1);
@@ -160,6 +284,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
     tmem_alloc(smem_u32(&s_tmem), 512);
     tmem_relinquish();
   }
+  int q_up = 0;                                       // 8-bit pages: this thread's row was taken times 2^q_up
   if (warp < W_MMA && (warp >> 2) < nqt) {
     const int i = warp >> 2;
     // Q_i: each warp its 32 rows, a row's 16-byte chunks over neighbouring lanes
@@ -178,6 +303,20 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       for (int k = 0; k < CH; ++k) {
         const int idx = k * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
         if (i * 128 + rr >= nrow) v[k] = make_uint4(0, 0, 0, 0);
+        if constexpr (C8 && Elem<T>::bf16) {
+          // the CH lanes of a row agree on its power of two; the lane of the row's
+          // softmax thread keeps it
+          uint32_t top = finite_max(v[k]);
+#pragma unroll
+          for (int d = 1; d < CH; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+          const int up = row_power(top);
+          v[k] = scaled_f16(v[k], up);
+#pragma unroll
+          for (int x = 0; x < 32 / CH; ++x) {
+            const int p = __shfl_sync(0xFFFFFFFFu, up, x * CH);
+            if (lane == k * (32 / CH) + x) q_up = p;
+          }
+        }
         *reinterpret_cast<uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[k];
       }
     }
@@ -212,10 +351,11 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       const uint32_t lrow = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t tS = tbase + 128 * i + lrow, tO = tbase + 128 * NQ + D * i + lrow;
       float m_run = has ? -INFINITY : 0.0f, l_run = 0.0f;
-      const uint64_t SL = f2pack(sl2, sl2);
-      constexpr float kMost = pow2(Elem<T>::kTau - Elem<T>::kBias);
-      // P = 2^(s sl2 - power(m_run))
-      auto power = [&](float m) { return fmaf(m, sl2, (float)Elem<T>::kBias); };
+      const float sr = C8 && Elem<T>::bf16 ? row_scale(sl2, q_up) : sl2;
+      const uint64_t SL = f2pack(sr, sr);
+      constexpr float kMost = pow2(Elem<Op>::kTau - Elem<Op>::kBias);
+      // P = 2^(s sr - power(m_run))
+      auto power = [&](float m) { return fmaf(m, sr, (float)Elem<Op>::kBias); };
       // Raises every row of the warp to its own maximum, and O with it (the P V
       // before it are complete)
       auto raise = [&](float mt, bool rescale) {
@@ -300,7 +440,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
             x = ex2f(x);
             y = ex2f(y);
             sum = add2(sum, f2pack(x, y));
-            pk[16 * (blk & 1) + (e >> 1)] = Elem<T>::pack(x, y);
+            pk[16 * (blk & 1) + (e >> 1)] = Elem<Op>::pack(x, y);
           }
         };
         auto pass = [&](auto masked) {
@@ -386,14 +526,22 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
                 if (!sees(j, sp.lo, sp.hi, a.sinks) || all_see(tl, j, j + 1, a.sinks)) continue;
                 const int64_t page = a.table[(int64_t)b * a.table_stride + (j >> a.page_log2)];
                 if (page < 0 || page >= a.num_pages) continue;
-                const T* src = static_cast<const T*>(a.pages) +
-                               ((((page * 2 + 1) * a.Hk + hk) << a.page_log2) + (j & ((1 << a.page_log2) - 1))) * D + c0;
+                const int64_t at = (((page * 2 + 1) * a.Hk + hk) << a.page_log2) + (j & ((1 << a.page_log2) - 1));
+                uint32_t s2 = 0;
+                if (C8) s2 = *reinterpret_cast<const uint16_t*>(a.scales + at) * 0x10001u;
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
-                  const uint32_t w = *reinterpret_cast<const uint32_t*>(src + e);
-                  const float2 f = Elem<T>::unpack(w);
-                  if ((w & Elem<T>::kExp) == Elem<T>::kExp) v[e] += f.x;
-                  if (((w >> 16) & Elem<T>::kExp) == Elem<T>::kExp) v[e + 1] += f.y;
+                  uint32_t w;
+                  if (C8) {
+                    uint32_t none;
+                    from_codes(*reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(a.pages) + at * D + c0 + e), w, none);
+                    w = mul_f16x2(w, s2);
+                  } else {
+                    w = *reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.pages) + at * D + c0 + e);
+                  }
+                  const float2 f = Elem<Op>::unpack(w);
+                  if ((w & Elem<Op>::kExp) == Elem<Op>::kExp) v[e] += f.x;
+                  if (((w >> 16) & Elem<Op>::kExp) == Elem<Op>::kExp) v[e + 1] += f.y;
                 }
               }
             }
@@ -431,7 +579,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
           }
         }
         if (has && parts == 1 && a.lse)
-          a.lse[(int64_t)head * a.N + sq.q0 + tok] = log_sum<T>(power(m_run), l_run);
+          a.lse[(int64_t)head * a.N + sq.q0 + tok] = log_sum<Op>(power(m_run), l_run);
         if (has && parts > 1) a.part_ml[pr] = make_float2(power(m_run), l_run);
       }
     }
@@ -443,8 +591,8 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
     const uint64_t dQ = desc_sw128(smem_u32(sm + L::Q)), dK = desc_sw128(smem_u32(sm + L::K));
     const uint64_t dV = desc_sw128_mn(smem_u32(sm + L::V), BLK);
     auto off = [](int bytes) { return (uint64_t)(bytes >> 4); };
-    constexpr uint32_t idS = idesc_f16(128, TK, false, Elem<T>::bf16);
-    constexpr uint32_t idPV = idesc_f16(128, D, true, Elem<T>::bf16);
+    constexpr uint32_t idS = idesc_f16(128, TK, false, Elem<Op>::bf16);
+    constexpr uint32_t idPV = idesc_f16(128, D, true, Elem<Op>::bf16);
     bool ok = true;
     auto issue_S = [&](int i, int jt) -> bool {
       const int s = jt & 1;
@@ -488,6 +636,9 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       if (!mbar_wait(bar(B_OFIN), 0, kDrainNs) || !ok) s_err = 1;
     }
     __syncwarp();
+  } else if constexpr (C8) {
+    // ------------------------------------------------------------ K and V from codes
+    if (!rebuild_tiles<D>(a, sm, tl, t0, n, b, hk, warp - W_K, &s_poison)) s_err = 1;
   } else if (warp == W_K || warp == W_V) {
     // ------------------------------------------------------------ producers of K and V
     // lane = box * NB + channel block; a box is the part of a page (at most 64
@@ -604,7 +755,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
 // of them; lanes 8 rows x 4 groups of 8 channels, so that reads (a part lies
 // [channels / 4][row]) and writes are whole sectors.
 constexpr int JR = 64;
-template <typename T, int D>
+template <typename T, int D, typename Op>
 __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
   grid_begin();
   const int b = blockIdx.z, hk = blockIdx.y, rt = blockIdx.x / (ROWS / JR);
@@ -681,18 +832,22 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
     *reinterpret_cast<uint4*>(dst + 32 * k) =
         make_uint4(Elem<T>::pack(v[k][0].x * inv, v[k][0].y * inv), Elem<T>::pack(v[k][0].z * inv, v[k][0].w * inv),
                    Elem<T>::pack(v[k][1].x * inv, v[k][1].y * inv), Elem<T>::pack(v[k][1].z * inv, v[k][1].w * inv));
-  if (a.lse && lane < 8) a.lse[(int64_t)head * a.N + sq.q0 + tok] = log_sum<T>(m, l);
+  if (a.lse && lane < 8) a.lse[(int64_t)head * a.N + sq.q0 + tok] = log_sum<Op>(m, l);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool C8>
 cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   static bool done[64];
-  cudaError_t e = allow_smem(paged_chunk<T, D>, Smem<D>::TOTAL, done);
+  cudaError_t e = allow_smem(paged_chunk<T, D, C8>, Smem<D>::TOTAL, done);
   if (e != cudaSuccess) return e;
   const int64_t rtiles = ((int64_t)a.max_q * a.G + ROWS - 1) / ROWS;
-  e = launch_ahead(paged_chunk<T, D>, dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), NT, Smem<D>::TOTAL, s, map, a);
+  e = launch_ahead(paged_chunk<T, D, C8>, dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), NT, Smem<D>::TOTAL, s, map, a);
   if (e != cudaSuccess || a.nsplit == 1) return e;
-  return launch_ahead(paged_join<T, D>, dim3((unsigned)(rtiles * (ROWS / JR)), a.Hk, a.B), 256, 0, s, a);
+  return launch_ahead(paged_join<T, D, Operand<T, C8>>, dim3((unsigned)(rtiles * (ROWS / JR)), a.Hk, a.B), 256, 0, s, a);
+}
+template <typename T, bool C8>
+cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, int D, cudaStream_t s) {
+  return D == 64 ? go<T, 64, C8>(a, map, s) : go<T, 128, C8>(a, map, s);
 }
 
 }  // namespace
@@ -727,8 +882,8 @@ PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, 
 }
 
 cudaError_t launch_paged_chunk(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s) {
-  if (dtype == QWM_F16) return D == 64 ? go<__half, 64>(a, map, s) : go<__half, 128>(a, map, s);
-  return D == 64 ? go<__nv_bfloat16, 64>(a, map, s) : go<__nv_bfloat16, 128>(a, map, s);
+  if (a.scales) return dtype == QWM_F16 ? pick<__half, true>(a, map, D, s) : pick<__nv_bfloat16, true>(a, map, D, s);
+  return dtype == QWM_F16 ? pick<__half, false>(a, map, D, s) : pick<__nv_bfloat16, false>(a, map, D, s);
 }
 
 }  // namespace qwm

@@ -39,16 +39,18 @@ constexpr int kGroupCost = 4;
 // (64 channels; whole groups), one where HBM does and finer slots keep it busier
 // (128 channels on the line: 131071 keys 86 us with one, 91 with two; 517 keys x 12
 // whole groups 8.9 and 7.6; all four with one producer warp for K and V).
-template <int D, int KP_>
+// Of 8-bit pages two groups as well: a tile is half the bytes, and its chain the same.
+template <int D, int KP_, bool C8>
 struct Shape {
   static constexpr int KP = KP_;
   static constexpr int TK = 64 * KP;                           // keys per tile
-  static constexpr int SLOT = TK * D * 2;                      // bytes of a K or V tile
+  static constexpr int SLOT = TK * D * (C8 ? 1 : 2);           // bytes of a K or V tile
   static constexpr int NS = SLOT == 32768 ? 4 : 8;             // slots of the ring: K, V, K, V, ...
   static_assert(NS % 4 == 0, "an even number of tiles: a slot belongs to one warp group");
   static constexpr int MERGE = NS * SLOT;                      // the warps' O [warp][16][D], beside the ring so that
                                                                // the next group's tiles come in meanwhile
-  static constexpr int TOTAL = MERGE + kWarps * 16 * D * 4 + 1024;
+  static constexpr int SCALES = MERGE + kWarps * 16 * D * 4;   // 8-bit pages: the tiles' scales [slot][TK]
+  static constexpr int TOTAL = SCALES + (C8 ? NS * TK * 2 : 0) + 1024;
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
@@ -67,13 +69,26 @@ __device__ __forceinline__ uint32_t at(int key, int chunk) {
   return (uint32_t)((chunk >> 3) * (TK * 128) + key * 128 + (((chunk & 7) ^ (key & 7)) << 4));
 }
 
+// The same of a tile of codes [TK keys][D bytes]: 16 channels a chunk, swizzled by 128 or
+// 64 bytes.
+template <int D>
+__device__ __forceinline__ uint32_t at_code(int key, int chunk) {
+  return (uint32_t)(key * D + ((D == 128 ? chunk ^ (key & 7) : chunk ^ ((key >> 1) & 3)) << 4));
+}
+
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {   // a >= 0, b > 0
   return ((a | b) >> 32) ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
 }
 
-template <typename T, int D, int KP>
+// Codes enter the products as binary16: a lane's word of four Keys' channels is the B
+// fragment of one k16 step (the channels of a step in the order 4 tq .. 4 tq + 3 for Q and
+// K alike), a transposed word of Values two tokens' pairs of channels, which are put in
+// order before the conversion.  The Keys' scales multiply the logits, the Values' the
+// fragments (P times a scale would leave binary16's range).
+template <typename T, int D, int KP, bool C8>
 __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
-  using L = Shape<D, KP>;
+  using L = Shape<D, KP, C8>;
+  using Op = Operand<T, C8>;
   constexpr int NS = L::NS, TK = L::TK;
   constexpr int KS = D / 16;                       // k16 steps of Q K^T, n16 blocks of P V
   extern __shared__ uint8_t raw[];
@@ -226,8 +241,10 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     const int kv = warp - kWarps;
     const int box_log2 = min(a.page_log2, 6);
     const int box = lane >> 1, half = lane & 1;
-    const bool mine = box < (TK >> box_log2) && half * 64 < D;
-    const uint32_t dst = smem_u32(sm) + half * (TK * 128) + ((box << box_log2) * 128);
+    const bool mine = box < (TK >> box_log2) && half * 64 < D && !(C8 && half);
+    const uint32_t dst = smem_u32(sm) + (C8 ? (box << box_log2) * D : half * (TK * 128) + ((box << box_log2) * 128));
+    const uint32_t sdst = smem_u32(sm) + L::SCALES + ((box << box_log2) * 2);
+    const uint32_t box_bytes = (C8 ? D + 2u : 128u) << box_log2;
     bool ok = true;
     int i = 0;                                     // tiles sent
     do {
@@ -249,13 +266,17 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
           record_status(a.status, QWM_ERR_INVALID_ARG);
           page = 0;
         }
-        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, want)) * (128u << box_log2);
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, want)) * box_bytes;
         const int y = (tile_at(tl, t) * TK + (box << box_log2)) & ((1 << a.page_log2) - 1);
         const int s = (2 * i + kv) % NS;
         if (i >= NS / 2 && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty(s), (i / (NS / 2) - 1) & 1, a.wait_ns)))) break;
         if (lane == 0) mbar_arrive_expect_tx(full(s), bytes);
         __syncwarp();
-        if (want) tma_load_3d(dst + s * L::SLOT, &map, half * 64, y, (page * 2 + kv) * a.Hk + hk, full(s));
+        if (want) {
+          const int block = (page * 2 + kv) * a.Hk + hk;
+          tma_load_3d(dst + s * L::SLOT, &map, half * 64, y, block, full(s));
+          if (C8) bulk_g2s(sdst + s * (TK * 2), a.scales + (((int64_t)block << a.page_log2) + y), 2u << box_log2, full(s));
+        }
         __syncwarp();
         ++i;
         page = page_n;
@@ -276,7 +297,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   const int wg = warp >> 2, key0 = (warp & 3) * 16 * KP;                // tile parity, first key of the tile
   const int mrow = lane & 7, mi = lane >> 3;
   const int kkey = key0 + (mi >> 1) * 8 + mrow, kch = mi & 1;           // K: (keys 0-7 | 8-15) x (chunk, chunk + 1)
-  const int vkey = key0 + (mi & 1) * 8 + mrow, vch = mi >> 1;           // V: the same, keys innermost
+  const int vkey = key0 + (mi & 1) * 8 + mrow, vch = mi >> 1;           // V (and codes): the same, keys innermost
   const int maxrows = a.max_q * a.G;
   float* so = reinterpret_cast<float*>(sm + L::MERGE);                  // [warp][16][D]
   bool ok = true;                                                       // no wait of this warp has run out
@@ -295,6 +316,8 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     float o[2 * KS][4];
     float m_run[2], l_run[2];
     uint32_t qf[KS][4];
+    float slr[2] = {sl2, sl2};                                          // scale of a row's logits, as powers of two
+    float true_max[2] = {1.0f, 1.0f};                                   // from m_run to the rows' q k^T
     int hi[2], lo[2];
 #pragma unroll
     for (int k = 0; k < 2 * KS; ++k)
@@ -311,10 +334,33 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       hi[rr] = sp.hi;
       lo[rr] = sp.lo;
       const T* src = static_cast<const T*>(a.q) + (sq.q0 + tok) * a.q_tok + (int64_t)(hk * a.G + (has ? r % a.G : 0)) * a.q_head;
+      if constexpr (C8) {
+        uint32_t top = 0;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        qf[ks][rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + tq * 2) : 0u;
-        qf[ks][2 + rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8 + tq * 2) : 0u;
+        for (int ks = 0; ks < KS; ++ks) {
+          const uint2 w = has ? *reinterpret_cast<const uint2*>(src + ks * 16 + tq * 4) : make_uint2(0u, 0u);
+          qf[ks][rr] = w.x;
+          qf[ks][2 + rr] = w.y;
+          top = max(top, finite_max(make_uint4(w.x, w.y, 0u, 0u)));
+        }
+        if (Elem<T>::bf16) {
+          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+          const int up = row_power(top);
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            qf[ks][rr] = scaled_f16(qf[ks][rr], up);
+            qf[ks][2 + rr] = scaled_f16(qf[ks][2 + rr], up);
+          }
+          slr[rr] = row_scale(sl2, up);
+          true_max[rr] = times_pow2(1.0f, -up);
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          qf[ks][rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + tq * 2) : 0u;
+          qf[ks][2 + rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8 + tq * 2) : 0u;
+        }
       }
     }
     // This warp group's tiles are those of its parity in the CTA's count of tiles,
@@ -328,6 +374,25 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       const uint32_t kb = smem_u32(sm) + s * L::SLOT, vb = kb + L::SLOT;
       const bool open = all_see(tl, j0, j0 + 16 * KP, a.sinks), any = any_sees(tl, j0, j0 + 16 * KP, a.sinks);
       uint32_t pf[KP][4];
+      // scales of this lane's keys (2 tq, 2 tq + 1) of eight, as binary16
+      auto scales_at = [&](int slot, int key) -> uint32_t {
+        return *reinterpret_cast<const uint32_t*>(sm + L::SCALES + slot * (TK * 2) + 2 * (key0 + key + tq * 2));
+      };
+      // B fragments of P V for the channels of two n8 blocks, times their scales
+      auto values = [&](int kp, int nb, uint32_t (&bf)[4]) { ldsm4t(vb + at<TK>(vkey + 16 * kp, 2 * nb + vch), bf); };
+      // of four n8 blocks (nb even): block 2 nb has the even channels of 16, 2 nb + 1 the odd ones
+      auto code_values = [&](int kp, int nb, uint32_t (&bf)[2][4]) {
+        uint32_t w[4];                               // (keys 0-7 | 8-15) x (16 channels, the next 16)
+        ldsm4t(vb + at_code<D>(vkey + 16 * kp, nb + vch), w);
+        const uint32_t s0 = scales_at(s + 1, kp * 16), s1 = scales_at(s + 1, kp * 16 + 8);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          uint32_t even, odd;
+          from_codes(__byte_perm(w[x], 0, 0x3120), even, odd);
+          bf[x >> 1][x & 1] = mul_f16x2(even, x & 1 ? s1 : s0);
+          bf[x >> 1][2 + (x & 1)] = mul_f16x2(odd, x & 1 ? s1 : s0);
+        }
+      };
       if (any) {
         float sc[KP][2][4];
 #pragma unroll
@@ -336,15 +401,39 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
           for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int e = 0; e < 4; ++e) sc[kp][k][e] = 0.0f;
+        if constexpr (C8) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
+          for (int ks = 0; ks < KS; ks += 2)
 #pragma unroll
-          for (int kp = 0; kp < KP; ++kp) {
-            uint32_t bf[4];
-            ldsm4(kb + at<TK>(kkey + 16 * kp, 2 * ks + kch), bf);
-            Elem<T>::mma(sc[kp][0], qf[ks], bf[0], bf[1]);
-            Elem<T>::mma(sc[kp][1], qf[ks], bf[2], bf[3]);
-          }
+            for (int kp = 0; kp < KP; ++kp) {
+              uint32_t w[4];                         // (keys 0-7 | 8-15) x (step ks, ks + 1)
+              ldsm4(kb + at_code<D>(vkey + 16 * kp, ks + vch), w);
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                uint32_t b0, b1;
+                from_codes(w[x], b0, b1);
+                Elem<Op>::mma(sc[kp][x & 1], qf[ks + (x >> 1)], b0, b1);
+              }
+            }
+#pragma unroll
+          for (int kp = 0; kp < KP; ++kp)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const float2 f = Elem<Op>::unpack(scales_at(s, kp * 16 + k * 8));
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sc[kp][k][e] *= e & 1 ? f.y : f.x;
+            }
+        } else {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int kp = 0; kp < KP; ++kp) {
+              uint32_t bf[4];
+              ldsm4(kb + at<TK>(kkey + 16 * kp, 2 * ks + kch), bf);
+              Elem<Op>::mma(sc[kp][0], qf[ks], bf[0], bf[1]);
+              Elem<Op>::mma(sc[kp][1], qf[ks], bf[2], bf[3]);
+            }
+        }
         if (!open) {
 #pragma unroll
           for (int kp = 0; kp < KP; ++kp)
@@ -374,7 +463,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
             v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
             v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
             const float mn = fmaxf(m_run[rr], v);
-            const float al = mn == m_run[rr] ? 1.0f : ex2f((m_run[rr] - mn) * sl2);
+            const float al = mn == m_run[rr] ? 1.0f : ex2f((m_run[rr] - mn) * slr[rr]);
             m_run[rr] = mn;
             l_run[rr] *= al;
 #pragma unroll
@@ -385,18 +474,18 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
           }
         }
         // a row that has seen nothing yet keeps 0 as its reference: 2^-inf = 0
-        const float mb0 = m_run[0] == -INFINITY ? 0.0f : m_run[0] * sl2;
-        const float mb1 = m_run[1] == -INFINITY ? 0.0f : m_run[1] * sl2;
+        const float mb0 = m_run[0] == -INFINITY ? 0.0f : m_run[0] * slr[0];
+        const float mb1 = m_run[1] == -INFINITY ? 0.0f : m_run[1] * slr[1];
 #pragma unroll
         for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const float v0 = ex2f(fmaf(sc[kp][k][0], sl2, -mb0)), v1 = ex2f(fmaf(sc[kp][k][1], sl2, -mb0));
-            const float w0 = ex2f(fmaf(sc[kp][k][2], sl2, -mb1)), w1 = ex2f(fmaf(sc[kp][k][3], sl2, -mb1));
+            const float v0 = ex2f(fmaf(sc[kp][k][0], slr[0], -mb0)), v1 = ex2f(fmaf(sc[kp][k][1], slr[0], -mb0));
+            const float w0 = ex2f(fmaf(sc[kp][k][2], slr[1], -mb1)), w1 = ex2f(fmaf(sc[kp][k][3], slr[1], -mb1));
             l_run[0] += v0 + v1;
             l_run[1] += w0 + w1;
-            pf[kp][2 * k] = Elem<T>::pack(v0, v1);
-            pf[kp][2 * k + 1] = Elem<T>::pack(w0, w1);
+            pf[kp][2 * k] = Elem<Op>::pack(v0, v1);
+            pf[kp][2 * k + 1] = Elem<Op>::pack(w0, w1);
           }
       }
       __syncwarp();
@@ -406,11 +495,15 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
 #pragma unroll
         for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
-          for (int nb = 0; nb < KS; ++nb) {
-            uint32_t bf[4];
-            ldsm4t(vb + at<TK>(vkey + 16 * kp, 2 * nb + vch), bf);
-            Elem<T>::mma(o[2 * nb], pf[kp], bf[0], bf[1]);
-            Elem<T>::mma(o[2 * nb + 1], pf[kp], bf[2], bf[3]);
+          for (int nb = 0; nb < KS; nb += C8 ? 2 : 1) {
+            uint32_t bf[2][4];
+            if constexpr (C8) code_values(kp, nb, bf);
+            else values(kp, nb, bf[0]);
+#pragma unroll
+            for (int x = 0; x < (C8 ? 2 : 1); ++x) {
+              Elem<Op>::mma(o[2 * (nb + x)], pf[kp], bf[x][0], bf[x][1]);
+              Elem<Op>::mma(o[2 * (nb + x) + 1], pf[kp], bf[x][2], bf[x][3]);
+            }
           }
       } else if (any) {
         // Keys that no row sees may hold anything (0 x inf is not 0): their
@@ -428,11 +521,14 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
           bool odd = false;
           if (sq.qn > 1) {
 #pragma unroll
-            for (int nb = 0; nb < KS; ++nb) {
-              uint32_t bf[4];
-              ldsm4t(vb + at<TK>(vkey + 16 * kp, 2 * nb + vch), bf);
-              odd |= nonfinite2<T>(bf[0] & ma) || nonfinite2<T>(bf[1] & mb) || nonfinite2<T>(bf[2] & ma) ||
-                     nonfinite2<T>(bf[3] & mb);
+            for (int nb = 0; nb < KS; nb += C8 ? 2 : 1) {
+              uint32_t bf[2][4];
+              if constexpr (C8) code_values(kp, nb, bf);
+              else values(kp, nb, bf[0]);
+#pragma unroll
+              for (int x = 0; x < (C8 ? 2 : 1); ++x)
+                odd |= nonfinite2<Op>(bf[x][0] & ma) || nonfinite2<Op>(bf[x][1] & mb) || nonfinite2<Op>(bf[x][2] & ma) ||
+                       nonfinite2<Op>(bf[x][3] & mb);
             }
             odd = __any_sync(0xFFFFFFFFu, odd);
           }
@@ -448,15 +544,16 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
               wb = keep(sp.lo, sp.hi, ja + 8);
             }
 #pragma unroll
-            for (int nb = 0; nb < KS; ++nb) {
-              uint32_t bf[4];
-              ldsm4t(vb + at<TK>(vkey + 16 * kp, 2 * nb + vch), bf);
+            for (int nb = 0; nb < KS; nb += C8 ? 2 : 1) {
+              uint32_t bf[2][4];
+              if constexpr (C8) code_values(kp, nb, bf);
+              else values(kp, nb, bf[0]);
 #pragma unroll
-              for (int k = 0; k < 2; ++k) {
+              for (int k = 0; k < (C8 ? 4 : 2); ++k) {
                 float acc[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[e] = o[2 * nb + k][e];
-                Elem<T>::mma(acc, pf[kp], bf[2 * k] & wa, bf[2 * k + 1] & wb);
+                Elem<Op>::mma(acc, pf[kp], bf[k >> 1][2 * (k & 1)] & wa, bf[k >> 1][2 * (k & 1) + 1] & wb);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                   if (own[e >> 1]) o[2 * nb + k][e] = acc[e];
@@ -481,12 +578,19 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
       if (r >= rows) continue;
       if (tq == 0) {
-        s_ml[warp][r][0] = m_run[rr];
+        s_ml[warp][r][0] = C8 ? m_run[rr] * true_max[rr] : m_run[rr];
         s_ml[warp][r][1] = l;
       }
+      if constexpr (C8) {
 #pragma unroll
-      for (int k = 0; k < 2 * KS; ++k)
-        *reinterpret_cast<float2*>(so + ((warp * 16 + r) * D + k * 8 + tq * 2)) = make_float2(o[k][2 * rr], o[k][2 * rr + 1]);
+        for (int k = 0; k < 2 * KS; k += 2)
+          *reinterpret_cast<float4*>(so + ((warp * 16 + r) * D + k * 8 + tq * 4)) =
+              make_float4(o[k][2 * rr], o[k + 1][2 * rr], o[k][2 * rr + 1], o[k + 1][2 * rr + 1]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 2 * KS; ++k)
+          *reinterpret_cast<float2*>(so + ((warp * 16 + r) * D + k * 8 + tq * 2)) = make_float2(o[k][2 * rr], o[k][2 * rr + 1]);
+      }
     }
     named_bar_sync(1, kWarps * 32);
     auto emit = [&](int r, int c, float m, float l, float4 v) {
@@ -597,23 +701,24 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   } while (next_group());
 }
 
-template <typename T, int D, int KP>
+template <typename T, int D, int KP, bool C8>
 cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
-  constexpr int smem = Shape<D, KP>::TOTAL;
+  constexpr int smem = Shape<D, KP, C8>::TOTAL;
   static bool done[64];
-  cudaError_t e = allow_smem(paged_step<T, D, KP>, smem, done);
+  cudaError_t e = allow_smem(paged_step<T, D, KP, C8>, smem, done);
   if (e != cudaSuccess) return e;
-  return launch_ahead(paged_step<T, D, KP>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, map, a);
+  return launch_ahead(paged_step<T, D, KP, C8>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, map, a);
 }
 template <typename T>
 cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, int D, cudaStream_t s) {
-  if (D == 64) return go<T, 64, 2>(a, map, s);
-  return a.nsplit > 1 ? go<T, 128, 1>(a, map, s) : go<T, 128, 2>(a, map, s);
+  if (a.scales) return D == 64 ? go<T, 64, 2, true>(a, map, s) : go<T, 128, 2, true>(a, map, s);
+  if (D == 64) return go<T, 64, 2, false>(a, map, s);
+  return a.nsplit > 1 ? go<T, 128, 1, false>(a, map, s) : go<T, 128, 2, false>(a, map, s);
 }
 
 }  // namespace
 
-PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split) {
+PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split, bool codes) {
   PagedPlan p{};
   p.step = 1;
   p.groups = B * Hk;
@@ -638,7 +743,8 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
   const double shared = (D == 128 ? 8.2 : 7.6) + (D == 128 ? 0.44 : 0.33) * (double)(tiles + kGroupCost) * p.groups / nsm;
   if (split && (tiles > 40 || whole > shared) && p.groups <= QWM_PAGED_COUNTER_BYTES / 4) {
     // a CTA per SM, or as many as have min_tiles places each
-    const int64_t places = ((max_visible + (D == 128 ? 63 : 127)) / (D == 128 ? 64 : 128) + 1 + kGroupCost) * p.groups;
+    const int tk = D == 128 && !codes ? 64 : 128;
+    const int64_t places = ((max_visible + tk - 1) / tk + 1 + kGroupCost) * p.groups;
     const int64_t want = (places + p.min_tiles - 1) / p.min_tiles;
     p.nsplit = (int)(want < nsm ? want : nsm);
   }

@@ -7,7 +7,7 @@
 // token).  A CTA takes a few tokens: its threads fill a table of (cos t, sin t) of
 // those tokens, shared by all heads of Queries and Keys, then turn 16-byte
 // vectors, a row of 64 to 256 channels in neighbouring threads.
-#include "paged.cuh"
+#include "rope.cuh"
 
 namespace qwm {
 namespace {
@@ -15,65 +15,7 @@ using namespace ptx;
 
 constexpr int NT = 256;
 
-// (cos, sin) of pos * f, exact to the fp32 rounding of the reduced angle at every
-// position.  The angle is taken in turns, as a 64-bit fraction whose whole turns fall
-// off the top (after Payne and Hanek, who form only the bits of a product that a
-// reduction keeps): f = m 2^e with a 24-bit m, f / (2 pi) = m 2^e C with C = 1 / (2 pi) to 128
-// bits, cut below 2^-64 of a turn, times the position (2^-33 of a turn at 2^31).  What
-// is left beside the nearest quarter turn is at most pi / 4 in fp32, where the fast sine
-// and cosine are good to 2^-21: far below the output's 2^-9 or 2^-12.  An f of 2^24 or
-// more, an infinity or a NaN gives NaN.
-__device__ __forceinline__ float2 turn(int pos, float f, float sign) {
-  constexpr uint64_t kC1 = 0x28BE60DB9391054Aull, kC0 = 0x7F09D5F47D4D3770ull;   // floor(2^128 / (2 pi))
-  constexpr float kTurn = (float)(6.283185307179586476925286766559 / 18446744073709551616.0);
-  const uint32_t w = __float_as_uint(f), ex = (w >> 23) & 255u;
-  const uint64_t m = (w & 0x7FFFFFu) | (ex ? 0x800000u : 0u);
-  const int down = 150 - (int)max(ex, 1u);         // -e
-  const uint64_t c0 = __umul64hi(m, kC0), lo = m * kC1 + c0, hi = __umul64hi(m, kC1) + (lo < c0);
-  const uint64_t g = down <= 0 ? lo : (down < 64 ? (lo >> down) | (hi << (64 - down)) : (down < 128 ? hi >> (down - 64) : 0));
-  const uint64_t t = (uint64_t)(int64_t)pos * g;
-  const uint64_t q = (t + (1ull << 61)) >> 62;      // quarter turns
-  float sn, cs;
-  __sincosf((float)(int64_t)(t - (q << 62)) * kTurn, &sn, &cs);
-  if (ex >= 127 + 24) cs = __uint_as_float(0x7FFFFFFFu);
-  const float c = q & 1 ? sn : cs, d = q & 1 ? cs : sn;
-  // a quarter turn on is (-sn, cs), and so forth
-  const float sc = (q + 1) & 2 ? -c : c, ss = q & 2 ? -d : d;
-  return make_float2(sc, (w >> 31) ? -(sign * ss) : sign * ss);
-}
-
 constexpr int kMaxTokens = 16;                     // tokens of a CTA
-
-__device__ __forceinline__ int64_t wide(int a, int b) { return (int64_t)a * b; }
-
-// Where a token's first Key goes in the pages (elements), < 0: nowhere.
-struct Place {
-  int64_t at;
-};
-__device__ __forceinline__ Place place_of(const RopeArgs& a, int64_t n) {
-  int lo = 0, hi = a.B;                            // last b with q_off[b] <= n
-  while (hi - lo > 1) {
-    const int m = (lo + hi) >> 1;
-    if (a.q_off[m] <= n) lo = m; else hi = m;
-  }
-  const int64_t q0 = a.q_off[lo], q1 = a.q_off[lo + 1], kv = a.kv_len[lo];
-  int64_t cap = (int64_t)a.table_stride << a.page_log2;
-  if (cap > a.max_kv) cap = a.max_kv;
-  Place r{-1};
-  if (!(n >= q0 && n < q1 && q1 <= a.N && q1 - q0 <= a.max_q && kv >= 0 && kv <= cap)) {
-    record_status(a.status, QWM_ERR_INVALID_ARG);
-    return r;
-  }
-  const int64_t p = kv - q1 + n;
-  if (p < 0) return r;
-  const int64_t page = a.table[(int64_t)lo * a.table_stride + (p >> a.page_log2)];
-  if (page < 0 || page >= a.num_pages) {
-    record_status(a.status, QWM_ERR_INVALID_ARG);
-    return r;
-  }
-  r.at = (((page * 2 * a.kv_heads) << a.page_log2) + (p & ((1 << a.page_log2) - 1))) * a.D;
-  return r;
-}
 
 // 32 registers for neighbouring channels, so that 8 CTAs fit an SM (34 and 36: rotation of
 // 4680 x 80 heads 36.8 us, append of 4680 x 120 56.2; with 32 33.2 and 50.5).
@@ -81,7 +23,7 @@ template <typename T, bool INTERLEAVED, bool PAGED>
 __global__ void __launch_bounds__(NT, INTERLEAVED ? 8 : 6) rope_kernel(const RopeArgs a, int tokens_per_cta) {
   extern __shared__ float4 table4[];               // (cos, sin) [tokens_per_cta][P]
   float2* table = reinterpret_cast<float2*>(table4);
-  __shared__ Place places[kMaxTokens];
+  __shared__ int64_t places[kMaxTokens];
   const int tid = threadIdx.x;
   const int n0 = blockIdx.x * tokens_per_cta;      // (N <= 2^30)
   const int nt = (int)min((int64_t)tokens_per_cta, a.N - n0);
@@ -127,7 +69,7 @@ __global__ void __launch_bounds__(NT, INTERLEAVED ? 8 : 6) rope_kernel(const Rop
     }
   };
   fetch();
-  if (PAGED && tid < nt) places[tid] = place_of(a, n0 + tid);
+  if (PAGED && tid < nt) places[tid] = place_of(a, n0 + tid) * a.D;   // elements
   if (a.inv_freq) {
     for (int i = tid; i < nt * P; i += NT) {
       const int tt = i / P, j = i - tt * P;
@@ -142,9 +84,9 @@ __global__ void __launch_bounds__(NT, INTERLEAVED ? 8 : 6) rope_kernel(const Rop
     if (!PAGED || g.page < 0) {
       dst = static_cast<T*>(g.dst) + wide(n0 + rt, g.d_tok) + wide(rh, g.d_head);
     } else {
-      const Place pl = places[rt];
-      if (pl.at < 0) continue;
-      dst = static_cast<T*>(a.pages) + pl.at + wide(g.page * a.kv_heads + rh, a.D << a.page_log2);
+      const int64_t at = places[rt];
+      if (at < 0) continue;
+      dst = static_cast<T*>(a.pages) + at + wide(g.page * a.kv_heads + rh, a.D << a.page_log2);
     }
     if (turned && g.rotate) {
       uint32_t* xw = reinterpret_cast<uint32_t*>(&x);

@@ -1,9 +1,9 @@
 """Rotary positions over three axes and the uncompressed, paged side of the
 cache (binding of the qwm_rope* and qwm_paged* entry points of include/qwm.h).
 
-``Rope`` holds a rotation's frequencies, ``PagedCache`` the pages, ``PagedBatch``
-the sequences of a step; the calls are qwm_rope, qwm_rope_backward,
-qwm_paged_append and qwm_paged_attend.  Like the rest of the binding these only
+``Rope`` holds a rotation's frequencies, ``PagedCache`` the pages (16 bits, or 8),
+``PagedBatch`` the sequences of a step; the calls are qwm_rope, qwm_rope_backward,
+qwm_paged_append, qwm_paged_read and qwm_paged_attend.  Like the rest of the binding these only
 marshal arguments (dtypes, shapes, strides and devices are checked, PyTorch is
 used for device memory); they go through the compiled csrc/binding.cpp, because
 a call for a single token is as long as its binding.  Autograd records qwm_rope; the
@@ -63,6 +63,9 @@ def declare(L):
             ("qwm_rope", rope, ct.c_int), ("qwm_rope_backward", rope, ct.c_int),
             ("qwm_paged_bytes", [ct.POINTER(QwmPagedConfig)], ct.c_size_t),
             ("qwm_paged_init", [ct.POINTER(_P), ct.POINTER(QwmPagedConfig), _P, ct.c_size_t, _P], ct.c_int),
+            ("qwm_paged_bytes_e4m3", [ct.POINTER(QwmPagedConfig)], ct.c_size_t),
+            ("qwm_paged_init_e4m3", [ct.POINTER(_P), ct.POINTER(QwmPagedConfig), _P, ct.c_size_t, _P], ct.c_int),
+            ("qwm_paged_read", [_P, _BATCH, _ROWS, _ROWS, _P], ct.c_int),
             ("qwm_paged_free", [_P], None),
             ("qwm_paged_status", [_P, ct.POINTER(ct.c_int32), _P], ct.c_int),
             ("qwm_paged_set_wait_limit", [_P, ct.c_uint64], ct.c_int),
@@ -189,26 +192,36 @@ def qwm_rope_backward(rope: Rope, dq, pos, dk=None, dq_out=None, dk_out=None):
 # ------------------------------------------------------------------ pages
 class PagedCache:
     """Pages of bf16 or fp16 Keys and Values in a torch-allocated device buffer;
-    ``pages`` is [num_pages][Keys, Values][kv_heads][page_tokens][head_dim]."""
+    ``pages`` is [num_pages][Keys, Values][kv_heads][page_tokens][head_dim].  With
+    ``storage=torch.float8_e4m3fn`` the pages hold 8-bit codes, and ``scales`` (fp16,
+    the shape of ``pages`` without its channels) what each row is multiplied by;
+    ``dtype`` stays the type of the tensors that the calls take and give."""
 
-    def __init__(self, kv_heads, num_pages, page_tokens=64, head_dim=128, dtype=torch.bfloat16, device=None):
+    def __init__(self, kv_heads, num_pages, page_tokens=64, head_dim=128, dtype=torch.bfloat16, device=None, storage=None):
         if dtype not in _DTYPES:
             raise ValueError("pages hold bf16 or fp16")
+        codes = storage is torch.float8_e4m3fn
+        if not codes and storage is not None and storage is not dtype:
+            raise ValueError("storage is the pages' dtype (None) or torch.float8_e4m3fn")
+        size, init = ("qwm_paged_bytes_e4m3", "qwm_paged_init_e4m3") if codes else ("qwm_paged_bytes", "qwm_paged_init")
         self.cfg = QwmPagedConfig(kv_heads, head_dim, page_tokens, _DTYPES[dtype], num_pages)
         self.dtype, self.head_dim, self.kv_heads, self.page_tokens = dtype, head_dim, kv_heads, page_tokens
         self.num_pages, self.scale = num_pages, 1.0 / math.sqrt(head_dim) if head_dim > 0 else 1.0
-        n = int(_lib().qwm_paged_bytes(self.cfg))
+        n = int(getattr(_lib(), size)(self.cfg))
         if n == 0:
-            _check("qwm_paged_bytes", 2)
+            _check(size, 2)
         dev = torch.device(device) if device is not None else torch.device("cuda", torch.cuda.current_device())
         raw = torch.empty(n + 1024, dtype=torch.uint8, device=dev)
         off = (-raw.data_ptr()) % 1024
         self.buffer = raw[off:off + n]
-        self.pages = self.buffer[256:].view(dtype).view(num_pages, 2, kv_heads, page_tokens, head_dim)
+        rows = num_pages * 2 * kv_heads * page_tokens
+        held = self.buffer[256:256 + rows * head_dim * (1 if codes else 2)]
+        self.pages = held.view(storage if codes else dtype).view(num_pages, 2, kv_heads, page_tokens, head_dim)
+        self.storage = storage if codes else dtype
+        self.scales = self.buffer[256 + rows * head_dim:].view(torch.float16).view(self.pages.shape[:-1]) if codes else None
         h = _P()
         with torch.cuda.device(self.buffer.device):    # a default stream's handle is the current device's
-            _check("qwm_paged_init", _lib().qwm_paged_init(ct.byref(h), self.cfg, self.buffer.data_ptr(), n,
-                                                          _stream(self.buffer)))
+            _check(init, getattr(_lib(), init)(ct.byref(h), self.cfg, self.buffer.data_ptr(), n, _stream(self.buffer)))
         self.handle = h
         self._key = (h.value, head_dim, _DTYPES[dtype], self.buffer.device.index)
 
@@ -270,6 +283,15 @@ def qwm_paged_append(cache: PagedCache, batch: PagedBatch, k, v, rope: Rope = No
     are turned to ``pos`` on the way, and ``q`` is turned beside them.  Returns
     the Queries (a new tensor, or q_out), or None without q."""
     return (_B or binding()).append(cache._key, batch._key, k, v, None if rope is None else rope._key, pos, q, q_out)
+
+
+def qwm_paged_read(cache: PagedCache, batch: PagedBatch, tokens=None, k_out=None, v_out=None, keys=True, values=True):
+    """The batch's tokens read back from their pages: (Keys, Values), each [tokens][kv_heads][head_dim]
+    of the cache's dtype, the newest ``q_offsets`` tokens of each sequence as ``kv_len`` ends it (a
+    ``kv_len`` short of the sequence's end reads earlier ones).  ``tokens``: the number of rows, where
+    neither the batch nor an output tells it.  ``keys=False`` or ``values=False`` leaves one out (None)."""
+    return (_B or binding()).read(cache._key, batch._key, cache.kv_heads, -1 if tokens is None else tokens,
+                                  k_out if keys else False, v_out if values else False)
 
 
 def qwm_paged_attend_workspace_bytes(cache: PagedCache, batch: PagedBatch, q_heads, tokens, window=0, sinks=0,
