@@ -52,11 +52,13 @@ def test_storage_is_the_dtype_or_e4m3():
 def test_a_read_of_unknown_length_or_of_wrong_outputs_is_refused():
     read = paged.binding().read
     cache = types.SimpleNamespace(_key=(0, 128, 0, 0), kv_heads=2)
-    any_rows, three = (0, -1, 0), (0, 3, 0)
+    b = paged.QwmPagedBatch(1, 1, 1, 1, 1, 4096, 4096, 4096)
+    at = ct.addressof(b)
+    any_rows, three = (at, -1, 0), (at, 3, 0)
     with pytest.raises(ValueError, match="not known"):
         read(cache._key, any_rows, 2, -1, None, None)
     with pytest.raises(ValueError, match="another device"):
-        read(cache._key, (0, 3, 1), 2, -1, None, None)
+        read(cache._key, (at, 3, 1), 2, -1, None, None)
     for bad in (7, "k", torch.zeros(3, 2, 128)):           # not a tensor; not on the GPU
         with pytest.raises(ValueError):
             read(cache._key, any_rows, 2, 3, bad, False)
