@@ -49,8 +49,13 @@ enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VRDY = 6, B_VEMPTY = 8, B_SFULL
 
 constexpr int NQ = 2, ROWS = 128 * NQ;               // row tiles and rows of a CTA
 constexpr int W_MMA = 4 * NQ, W_K = W_MMA + 1, W_V = W_MMA + 2;  // W_MMA + 3: the guard
+constexpr int W_CODES = W_MMA + 4;                   // 8-bit pages: 4 warps for K and V (W_MMA + 1 .. 3 idle)
 constexpr int NT = (4 * NQ + 4) * 32;
-constexpr int kRebuild = 3;                          // 8-bit pages: the last three warps make K and V from codes
+// 8-bit pages: a fourth warpgroup makes K and V from codes, and the warps share out the
+// registers (65536 in all): softmax, the MMAs' warpgroup, the codes'.
+constexpr int kRebuild = 4, NT8 = NT + 128;
+constexpr int kRegSoftmax = 168, kRegMma = 32, kRegCodes = 144;
+static_assert(128 * (NQ * kRegSoftmax + kRegMma + kRegCodes) <= 128 * NT8, "registers of the launch: 128 a thread");
 
 template <int D>
 struct Smem {
@@ -101,130 +106,162 @@ __device__ __forceinline__ float log_sum(float m, float l) {
   return (m - (float)Elem<Op>::kBias + log2f(l * pow2(Elem<Op>::kBias))) * 0.69314718055994531f;
 }
 
-// K and V of 8-bit pages: warp `rank` of three turns its share of each tile's codes
-// into binary16 where the TMA of 16-bit pages would have put them, so that the MMAs
-// are the same.  Codes go from global memory to registers, a tile ahead (through
-// shared memory they would take 64 KB more than it has, and a third of its
-// bandwidth, which the MMAs need); 16 of them a lane, D / 16 lanes a row.  Values that no
-// row of the CTA sees are cleared on the way, those that some see and others do not
-// searched (the guard's work).  False: a wait ran out.
+// A warpgroup's registers a thread: more than the launch's, once others have given theirs, or fewer.
+template <int N>
+__device__ __forceinline__ void reg_take() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void reg_give() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// Loads that stay where they are written: a tile ahead of their use.
+__device__ __forceinline__ uint4 load16(const uint8_t* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint32_t load4(const __half* p) {
+  uint32_t v;
+  asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+
+// K and V of 8-bit pages: warp `rank` of four turns the codes of two boxes of 16 tokens of
+// each tile into binary16 where the TMA of 16-bit pages would have put them, so that the
+// MMAs are the same.  Codes go from global memory to registers, a tile ahead (through
+// shared memory they would take bandwidth that the MMAs need); 16 of them a lane, D / 16
+// lanes a row, a lane's rows of a box side by side so that it has their scales in one
+// load.  Values that no row of the CTA sees are cleared on the way, those that some
+// see and others do not searched (the guard's work).  False: a wait ran out.
 template <int D>
 __device__ __forceinline__ bool rebuild_tiles(const PagedArgs& a, uint8_t* sm, const Tiles& tl, int t0, int n, int b, int hk,
                                               int rank, int* poison) {
   using L = Smem<D>;
-  constexpr int NB = L::NB, LPR = D / 16, RPL = 32 / LPR;   // lanes of a row, rows of a load
-  constexpr int LOADS = TK / RPL, NL = (LOADS + kRebuild - 1) / kRebuild;
+  constexpr int NB = L::NB, LPR = D / 16, R = LPR / 2;      // lanes of a row; rows of a lane in a box
+  constexpr int BOXES = TK / 16 / kRebuild;                 // of a warp
   const int lane = threadIdx.x & 31, c = lane % LPR, sub = lane / LPR;
   auto bar = [&](int i) { return smem_u32(sm + L::BAR) + 8u * i; };
   auto wait_all = [&](int i, uint32_t ph) -> bool { return __all_sync(0xFFFFFFFFu, mbar_wait(bar(i), ph, a.wait_ns)); };
   const int32_t* trow = a.table + (int64_t)b * a.table_stride;
   const uint8_t* pages = static_cast<const uint8_t*>(a.pages);
   const int64_t vrows = (int64_t)a.Hk << a.page_log2;       // from a token's Key to its Value, in rows
-  // Lane x (of 8, four times over) keeps the row of the Keys of the tile's tokens 16 x ..
-  // 16 x + 15, or -1 where no row of the CTA sees them.
-  auto look_up = [&](int jt) -> int64_t {
-    if (jt >= n) return -1;
-    const int j = tile_at(tl, t0 + jt) * TK + 16 * (lane & 7);
-    if (!any_sees(tl, j, j + 16, a.sinks)) return -1;
-    int64_t page = trow[j >> a.page_log2];
-    if (page < 0 || page >= a.num_pages) {            // not followed: the first page in its place
-      record_status(a.status, QWM_ERR_INVALID_ARG);
-      page = 0;
+  // A box's page is asked for a tile before its codes.  Tokens that no row of the CTA sees
+  // are not followed: the first row stands in, and is cleared or masked like any hidden token.
+  auto token = [&](int jt, int box) { return tile_at(tl, t0 + jt) * TK + 16 * (rank * BOXES + box); };
+  auto wants = [&](int j) { return any_sees(tl, j, j + 16, a.sinks); };
+  int page[BOXES];
+  auto ask = [&](int jt) {
+#pragma unroll
+    for (int x = 0; x < BOXES; ++x) {
+      const int j = token(jt, x);
+      page[x] = jt < n && wants(j) ? trow[j >> a.page_log2] : 0;
     }
-    return ((page * 2 * a.Hk + hk) << a.page_log2) + (j & ((1 << a.page_log2) - 1));
+  };
+  int64_t first[BOXES];                                     // row of the box's first Key
+  auto place = [&](int jt) {
+#pragma unroll
+    for (int x = 0; x < BOXES; ++x) {
+      const int j = token(jt, x);
+      first[x] = 0;
+      if (!wants(j)) continue;
+      if (page[x] < 0 || page[x] >= a.num_pages) {          // not followed either
+        record_status(a.status, QWM_ERR_INVALID_ARG);
+        page[x] = 0;
+      }
+      first[x] = (((int64_t)page[x] * 2 * a.Hk + hk) << a.page_log2) + (j & ((1 << a.page_log2) - 1));
+    }
   };
   struct Codes {
-    uint4 c[NL];
-    uint2 s;                                          // scales of the tile's rows 4 lane .. 4 lane + 3
+    uint4 c[BOXES][R];
+    uint32_t s[BOXES][R / 2];                               // scales of this lane's rows
   };
-  auto fetch = [&](Codes& x, int64_t first, int64_t more) {
-    const int64_t mine = __shfl_sync(0xFFFFFFFFu, first, lane >> 2);
-    x.s = make_uint2(0, 0);
-    if (mine >= 0) x.s = *reinterpret_cast<const uint2*>(a.scales + mine + more + 4 * (lane & 3));
+  auto fetch = [&](Codes& x, int64_t more) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int l = rank + kRebuild * i;
-      x.c[i] = make_uint4(0, 0, 0, 0);
-      if (l >= LOADS) continue;
-      const int64_t row = __shfl_sync(0xFFFFFFFFu, first, (l * RPL) >> 4);
-      if (row >= 0)
-        x.c[i] = *reinterpret_cast<const uint4*>(pages + (row + more + ((l * RPL) & 15) + sub) * D + 16 * c);
+    for (int i = 0; i < BOXES; ++i) {
+      const int64_t row = first[i] + more + sub * R;
+#pragma unroll
+      for (int r = 0; r < R; ++r) x.c[i][r] = load16(pages + (row + r) * D + 16 * c);
+#pragma unroll
+      for (int r = 0; r < R; r += 2) x.s[i][r / 2] = load4(a.scales + row + r);
     }
   };
-  auto store = [&](Codes& x, uint8_t* tile, bool values, int j0) {
-    const bool open = !values || all_see(tl, j0, j0 + TK, a.sinks);
+  auto store = [&](auto masked, const Codes& x, uint8_t* tile, int j0) {
     bool odd = false;
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int l = rank + kRebuild * i;
-      if (l >= LOADS) continue;
-      const int row = l * RPL + sub;
-      const uint32_t s01 = __shfl_sync(0xFFFFFFFFu, x.s.x, row >> 2), s23 = __shfl_sync(0xFFFFFFFFu, x.s.y, row >> 2);
-      const uint32_t s2 = __byte_perm(row & 2 ? s23 : s01, 0, row & 1 ? 0x3232 : 0x1010);
-      uint32_t h[8];
-      from_codes(x.c[i].x, h[0], h[1]);
-      from_codes(x.c[i].y, h[2], h[3]);
-      from_codes(x.c[i].z, h[4], h[5]);
-      from_codes(x.c[i].w, h[6], h[7]);
+    for (int i = 0; i < BOXES; ++i)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) h[k] = mul_f16x2(h[k], s2);
-      if (!open) {
-        const int j = j0 + row;
-        if (!any_sees(tl, j, j + 1, a.sinks)) {
+      for (int r = 0; r < R; ++r) {
+        const int row = (rank * BOXES + i) * 16 + sub * R + r;
+        const uint32_t s2 = __byte_perm(x.s[i][r / 2], 0, r & 1 ? 0x3232 : 0x1010);
+        uint32_t h[8];
+        from_codes(x.c[i][r].x, h[0], h[1]);
+        from_codes(x.c[i][r].y, h[2], h[3]);
+        from_codes(x.c[i][r].z, h[4], h[5]);
+        from_codes(x.c[i][r].w, h[6], h[7]);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) h[k] = 0u;
-        } else if (!all_see(tl, j, j + 1, a.sinks)) {
+        for (int k = 0; k < 8; ++k) h[k] = mul_f16x2(h[k], s2);
+        if constexpr (masked) {
+          const int j = j0 + row;
+          if (!any_sees(tl, j, j + 1, a.sinks)) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            if (!nonfinite2<__half>(h[k])) continue;
-            if ((h[k] & 0x7C00u) == 0x7C00u) h[k] &= 0xFFFF0000u;
-            if ((h[k] & 0x7C000000u) == 0x7C000000u) h[k] &= 0xFFFFu;
-            odd = true;
+            for (int k = 0; k < 8; ++k) h[k] = 0u;
+          } else if (!all_see(tl, j, j + 1, a.sinks)) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              if (!nonfinite2<__half>(h[k])) continue;
+              if ((h[k] & 0x7C00u) == 0x7C00u) h[k] &= 0xFFFF0000u;
+              if ((h[k] & 0x7C000000u) == 0x7C000000u) h[k] &= 0xFFFFu;
+              odd = true;
+            }
           }
         }
+        const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
+        uint8_t* at = tile + (c >> 2) * BLK + row * 128;    // channels 16 c ..: chunks 2 c and 2 c + 1 of 8
+        const int k0 = (2 * c) & 7, sw = row & 7;
+        // half of the lanes write their second chunk first: no two of eight on one bank
+        const bool flip = D == 128 ? c >= 4 : sub & 1;
+        *reinterpret_cast<uint4*>(at + (((k0 + flip) ^ sw) << 4)) = flip ? hi : lo;
+        *reinterpret_cast<uint4*>(at + (((k0 + !flip) ^ sw) << 4)) = flip ? lo : hi;
       }
-      const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
-      uint8_t* at = tile + (c >> 2) * BLK + row * 128;        // channels 16 c ..: chunks 2 c and 2 c + 1 of 8
-      const int k0 = (2 * c) & 7, sw = row & 7;
-      // the lanes of the upper channels write their second chunk first: no two of the
-      // eight lanes of a row on one bank
-      const bool flip = D == 128 && c >= 4;
-      *reinterpret_cast<uint4*>(at + (((k0 + flip) ^ sw) << 4)) = flip ? hi : lo;
-      *reinterpret_cast<uint4*>(at + (((k0 + !flip) ^ sw) << 4)) = flip ? lo : hi;
-    }
     if (odd) *poison = 1;
   };
-  bool ok = true;
-  if (a.idle) return true;
+  if (a.idle || n == 0) return true;
   Codes k, v;
-  int64_t here = look_up(0), next = look_up(1);
-  if (n > 0) {
-    fetch(k, here, 0);
-    fetch(v, here, vrows);
-  }
+  ask(0);
+  place(0);
+  ask(1);
+  fetch(k, 0);
+  fetch(v, vrows);
   for (int jt = 0; jt < n; ++jt) {
     const int s = jt & 1, j0 = tile_at(tl, t0 + jt) * TK;
-    if (jt >= ST && !(ok = wait_all(B_KEMPTY + s, ((jt >> 1) - 1) & 1))) break;
-    store(k, sm + L::K + s * NB * BLK, false, j0);
+    if (jt >= ST && !wait_all(B_KEMPTY + s, ((jt >> 1) - 1) & 1)) return false;
+    store(std::false_type{}, k, sm + L::K + s * NB * BLK, j0);
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(B_KFULL + s));
-    if (jt + 1 < n) fetch(k, next, 0);
-    if (jt >= ST && !(ok = wait_all(B_VEMPTY + s, ((jt >> 1) - 1) & 1))) break;
-    store(v, sm + L::V + s * NB * BLK, true, j0);
+    if (jt + 1 < n) {
+      place(jt + 1);
+      ask(jt + 2);
+      fetch(k, 0);
+    }
+    if (jt >= ST && !wait_all(B_VEMPTY + s, ((jt >> 1) - 1) & 1)) return false;
+    uint8_t* tile = sm + L::V + s * NB * BLK;
+    if (all_see(tl, j0, j0 + TK, a.sinks)) store(std::false_type{}, v, tile, j0);
+    else store(std::true_type{}, v, tile, j0);
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(B_VRDY + s));
-    if (jt + 1 < n) fetch(v, next, vrows);
-    next = look_up(jt + 2);
+    if (jt + 1 < n) fetch(v, vrows);
   }
-  return ok;
+  return true;
 }
 
 // T: the type of Queries and output; C8: 8-bit pages, whose products are taken in
 // binary16 (every code x scale is one).
 template <typename T, int D, bool C8>
-__global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
+__global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
   using L = Smem<D>;
   using Op = Operand<T, C8>;
   constexpr int NB = L::NB;
@@ -337,6 +374,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
 
   if (warp < W_MMA) {
     // ------------------------------------------------------------ softmax
+    if constexpr (C8) reg_take<kRegSoftmax>();
     const int i = warp >> 2, row = tid & 127;
     if (i < nqt) {
       uint8_t* sQ = sm + L::Q + i * NB * BLK;
@@ -583,7 +621,15 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
         if (has && parts > 1) a.part_ml[pr] = make_float2(power(m_run), l_run);
       }
     }
-  } else if (warp == W_MMA) {
+  } else if (C8 && warp >= W_CODES) {
+    // ------------------------------------------------------------ K and V from codes
+    if constexpr (C8) {
+      reg_take<kRegCodes>();
+      if (!rebuild_tiles<D>(a, sm, tl, t0, n, b, hk, warp - W_CODES, &s_poison)) s_err = 1;
+    }
+  } else {
+    if constexpr (C8) reg_give<kRegMma>();
+    if (warp == W_MMA) {
     // ------------------------------------------------------------ MMA issue
     // Order per K/V tile j: P0 V(j) in two halves, S0(j+1), P1 V(j), S1(j+1); S_i(j+1) may
     // overwrite P_i(j) because the MMAs of one thread run in issue order.
@@ -636,10 +682,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       if (!mbar_wait(bar(B_OFIN), 0, kDrainNs) || !ok) s_err = 1;
     }
     __syncwarp();
-  } else if constexpr (C8) {
-    // ------------------------------------------------------------ K and V from codes
-    if (!rebuild_tiles<D>(a, sm, tl, t0, n, b, hk, warp - W_K, &s_poison)) s_err = 1;
-  } else if (warp == W_K || warp == W_V) {
+    } else if (!C8 && (warp == W_K || warp == W_V)) {
     // ------------------------------------------------------------ producers of K and V
     // lane = box * NB + channel block; a box is the part of a page (at most 64
     // tokens of it) that lies in the tile.  Boxes no row sees are not read.
@@ -682,7 +725,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
     // the last copies land before the CTA can end: the roles that wait for them may
     // have given up on them
     for (int u = max(0, jt - ST); u < jt; ++u) mbar_wait(bar(full + (u & 1)), (u >> 1) & 1, kDrainNs);
-  } else {
+    } else if (!C8) {
     // ------------------------------------------------------------ guard of the Values
     bool ok = true;
     for (int jt = 0; jt < n; ++jt) {
@@ -739,6 +782,7 @@ __global__ void __launch_bounds__(NT, 1) paged_chunk(const __grid_constant__ CUt
       if (lane == 0) mbar_arrive(bar(B_VRDY + s));
     }
     if (!ok) s_err = 1;
+    }
   }
 
   tc_fence_before();
@@ -841,7 +885,7 @@ cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   cudaError_t e = allow_smem(paged_chunk<T, D, C8>, Smem<D>::TOTAL, done);
   if (e != cudaSuccess) return e;
   const int64_t rtiles = ((int64_t)a.max_q * a.G + ROWS - 1) / ROWS;
-  e = launch_ahead(paged_chunk<T, D, C8>, dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), NT, Smem<D>::TOTAL, s, map, a);
+  e = launch_ahead(paged_chunk<T, D, C8>, dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), C8 ? NT8 : NT, Smem<D>::TOTAL, s, map, a);
   if (e != cudaSuccess || a.nsplit == 1) return e;
   return launch_ahead(paged_join<T, D, Operand<T, C8>>, dim3((unsigned)(rtiles * (ROWS / JR)), a.Hk, a.B), 256, 0, s, a);
 }
