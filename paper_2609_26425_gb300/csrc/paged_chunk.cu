@@ -45,25 +45,29 @@ constexpr int ST = 2;                     // K tiles and V tiles in flight
 constexpr int BLK = 16384;                // 128 rows x 128 bytes
 
 enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VRDY = 6, B_VEMPTY = 8, B_SFULL = 10, B_QRDY = 12, B_PV = 14,
-       B_PFULL = 16 /* tile, half */, B_OFIN = 20 };
+       B_PFULL = 16 /* tile, half */, B_OFIN = 20, B_CFULL = 22 /* codes: K, V, stage */, B_CEMPTY = 26 };
 
 constexpr int NQ = 2, ROWS = 128 * NQ;               // row tiles and rows of a CTA
 constexpr int W_MMA = 4 * NQ, W_K = W_MMA + 1, W_V = W_MMA + 2;  // W_MMA + 3: the guard
-constexpr int W_CODES = W_MMA + 4;                   // 8-bit pages: 4 warps for K and V (W_MMA + 1 .. 3 idle)
+constexpr int W_CODES = W_MMA + 4;                   // 8-bit pages: 4 warps for K and V
 constexpr int NT = (4 * NQ + 4) * 32;
 // 8-bit pages: a fourth warpgroup makes K and V from codes, and the warps share out the
-// registers (65536 in all): softmax, the MMAs' warpgroup, the codes'.
+// registers (65536 in all): softmax, the MMAs' and the producers' warpgroup, the codes'.
 constexpr int kRebuild = 4, NT8 = NT + 128;
-constexpr int kRegSoftmax = 168, kRegMma = 32, kRegCodes = 144;
-static_assert(128 * (NQ * kRegSoftmax + kRegMma + kRegCodes) <= 128 * NT8, "registers of the launch: 128 a thread");
+constexpr int kRegLaunch = 65536 / NT8, kRegSoftmax = 168, kRegMma = 80, kRegCodes = 96;
+static_assert(NT8 == 512 && NQ * kRegSoftmax + kRegMma + kRegCodes <= 4 * kRegLaunch, "what the launch has");
 
-template <int D>
+template <int D, bool C8 = false>
 struct Smem {
   static constexpr int NB = D / 64;                  // 64-channel blocks of a tile
   static constexpr int Q = 0;                        // tile i, block k at (i * NB + k) * BLK
   static constexpr int K = NQ * NB * BLK;            // stage s, block k at (s * NB + k) * BLK
   static constexpr int V = K + ST * NB * BLK;
-  static constexpr int BAR = V + ST * NB * BLK;
+  // 8-bit pages: tiles of codes [K, V][stage], and their scales
+  static constexpr int CS = C8 ? (D == 64 ? 2 : 1) : 0;
+  static constexpr int CODES = V + ST * NB * BLK;
+  static constexpr int SCALES = CODES + 2 * CS * TK * D;
+  static constexpr int BAR = SCALES + 2 * CS * TK * 2;
   static constexpr int TOTAL = BAR + 256 + 1024;
 };
 
@@ -106,154 +110,96 @@ __device__ __forceinline__ float log_sum(float m, float l) {
   return (m - (float)Elem<Op>::kBias + log2f(l * pow2(Elem<Op>::kBias))) * 0.69314718055994531f;
 }
 
-// A warpgroup's registers a thread: more than the launch's, once others have given theirs, or fewer.
+// A warpgroup's registers a thread from here on: fewer than at the launch, or more, for which
+// it waits until others have given theirs.
 template <int N>
-__device__ __forceinline__ void reg_take() {
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-}
-template <int N>
-__device__ __forceinline__ void reg_give() {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+__device__ __forceinline__ void set_registers() {
+  static_assert(N % 8 == 0 && N >= 24 && N <= 256, "");
+  if constexpr (N < kRegLaunch) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
 }
 
-// Loads that stay where they are written: a tile ahead of their use.
-__device__ __forceinline__ uint4 load16(const uint8_t* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ uint32_t load4(const __half* p) {
-  uint32_t v;
-  asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));
-  return v;
-}
-
-// K and V of 8-bit pages: warp `rank` of four turns the codes of two boxes of 16 tokens of
-// each tile into binary16 where the TMA of 16-bit pages would have put them, so that the
-// MMAs are the same.  Codes go from global memory to registers, a tile ahead (through
-// shared memory they would take bandwidth that the MMAs need); 16 of them a lane, D / 16
-// lanes a row, a lane's rows of a box side by side so that it has their scales in one
-// load.  Values that no row of the CTA sees are cleared on the way, those that some
-// see and others do not searched (the guard's work).  False: a wait ran out.
+// K and V of 8-bit pages: warp `rank` of four turns a quarter of each tile's codes into
+// binary16 where the TMA of 16-bit pages would have put them, so that the MMAs are the
+// same: 16 codes a lane, D / 16 lanes a row.  Values that no row of the CTA sees are cleared
+// on the way, those that some see and others do not searched (the guard's work).  False: a
+// wait ran out.
 template <int D>
-__device__ __forceinline__ bool rebuild_tiles(const PagedArgs& a, uint8_t* sm, const Tiles& tl, int t0, int n, int b, int hk,
-                                              int rank, int* poison) {
-  using L = Smem<D>;
-  constexpr int NB = L::NB, LPR = D / 16, R = LPR / 2;      // lanes of a row; rows of a lane in a box
-  constexpr int BOXES = TK / 16 / kRebuild;                 // of a warp
-  const int lane = threadIdx.x & 31, c = lane % LPR, sub = lane / LPR;
+__device__ __forceinline__ bool rebuild_tiles(const PagedArgs& a, uint8_t* sm, const Tiles& tl, int t0, int n, int rank,
+                                              int* poison) {
+  using L = Smem<D, true>;
+  constexpr int NB = L::NB, LPR = D / 16, RPL = 32 / LPR;   // lanes of a row, rows of a load
+  constexpr int LOADS = TK / RPL / kRebuild;
+  const int lane = threadIdx.x & 31, c = lane % LPR, row0 = rank * (TK / kRebuild) + lane / LPR;
   auto bar = [&](int i) { return smem_u32(sm + L::BAR) + 8u * i; };
   auto wait_all = [&](int i, uint32_t ph) -> bool { return __all_sync(0xFFFFFFFFu, mbar_wait(bar(i), ph, a.wait_ns)); };
-  const int32_t* trow = a.table + (int64_t)b * a.table_stride;
-  const uint8_t* pages = static_cast<const uint8_t*>(a.pages);
-  const int64_t vrows = (int64_t)a.Hk << a.page_log2;       // from a token's Key to its Value, in rows
-  // A box's page is asked for a tile before its codes.  Tokens that no row of the CTA sees
-  // are not followed: the first row stands in, and is cleared or masked like any hidden token.
-  auto token = [&](int jt, int box) { return tile_at(tl, t0 + jt) * TK + 16 * (rank * BOXES + box); };
-  auto wants = [&](int j) { return any_sees(tl, j, j + 16, a.sinks); };
-  int page[BOXES];
-  auto ask = [&](int jt) {
+  // Tile jt of K or V: from codes to its place in the ring
+  auto rebuild = [&](auto masked, int kv, int jt, uint8_t* tile) {
+    const int st = kv * L::CS + jt % L::CS;
+    const uint8_t* codes = sm + L::CODES + st * (TK * D);
+    const uint16_t* scales = reinterpret_cast<const uint16_t*>(sm + L::SCALES) + st * TK;
+    uint4 x[LOADS];
+    uint32_t s2[LOADS];
 #pragma unroll
-    for (int x = 0; x < BOXES; ++x) {
-      const int j = token(jt, x);
-      page[x] = jt < n && wants(j) ? trow[j >> a.page_log2] : 0;
+    for (int i = 0; i < LOADS; ++i) {
+      const int row = row0 + i * RPL;
+      x[i] = *reinterpret_cast<const uint4*>(codes + row * D + ((D == 128 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4));
+      s2[i] = scales[row] * 0x10001u;
     }
-  };
-  int64_t first[BOXES];                                     // row of the box's first Key
-  auto place = [&](int jt) {
-#pragma unroll
-    for (int x = 0; x < BOXES; ++x) {
-      const int j = token(jt, x);
-      first[x] = 0;
-      if (!wants(j)) continue;
-      if (page[x] < 0 || page[x] >= a.num_pages) {          // not followed either
-        record_status(a.status, QWM_ERR_INVALID_ARG);
-        page[x] = 0;
-      }
-      first[x] = (((int64_t)page[x] * 2 * a.Hk + hk) << a.page_log2) + (j & ((1 << a.page_log2) - 1));
-    }
-  };
-  struct Codes {
-    uint4 c[BOXES][R];
-    uint32_t s[BOXES][R / 2];                               // scales of this lane's rows
-  };
-  auto fetch = [&](Codes& x, int64_t more) {
-#pragma unroll
-    for (int i = 0; i < BOXES; ++i) {
-      const int64_t row = first[i] + more + sub * R;
-#pragma unroll
-      for (int r = 0; r < R; ++r) x.c[i][r] = load16(pages + (row + r) * D + 16 * c);
-#pragma unroll
-      for (int r = 0; r < R; r += 2) x.s[i][r / 2] = load4(a.scales + row + r);
-    }
-  };
-  auto store = [&](auto masked, const Codes& x, uint8_t* tile, int j0) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(B_CEMPTY + st));
     bool odd = false;
 #pragma unroll
-    for (int i = 0; i < BOXES; ++i)
+    for (int i = 0; i < LOADS; ++i) {
+      const int row = row0 + i * RPL;
+      uint32_t h[8];
+      from_codes(x[i].x, h[0], h[1]);
+      from_codes(x[i].y, h[2], h[3]);
+      from_codes(x[i].z, h[4], h[5]);
+      from_codes(x[i].w, h[6], h[7]);
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int row = (rank * BOXES + i) * 16 + sub * R + r;
-        const uint32_t s2 = __byte_perm(x.s[i][r / 2], 0, r & 1 ? 0x3232 : 0x1010);
-        uint32_t h[8];
-        from_codes(x.c[i][r].x, h[0], h[1]);
-        from_codes(x.c[i][r].y, h[2], h[3]);
-        from_codes(x.c[i][r].z, h[4], h[5]);
-        from_codes(x.c[i][r].w, h[6], h[7]);
+      for (int k = 0; k < 8; ++k) h[k] = mul_f16x2(h[k], s2[i]);
+      if constexpr (masked) {
+        const int j = tile_at(tl, t0 + jt) * TK + row;
+        if (!any_sees(tl, j, j + 1, a.sinks)) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) h[k] = mul_f16x2(h[k], s2);
-        if constexpr (masked) {
-          const int j = j0 + row;
-          if (!any_sees(tl, j, j + 1, a.sinks)) {
+          for (int k = 0; k < 8; ++k) h[k] = 0u;
+        } else if (!all_see(tl, j, j + 1, a.sinks)) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) h[k] = 0u;
-          } else if (!all_see(tl, j, j + 1, a.sinks)) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              if (!nonfinite2<__half>(h[k])) continue;
-              if ((h[k] & 0x7C00u) == 0x7C00u) h[k] &= 0xFFFF0000u;
-              if ((h[k] & 0x7C000000u) == 0x7C000000u) h[k] &= 0xFFFFu;
-              odd = true;
-            }
+          for (int k = 0; k < 8; ++k) {
+            if (!nonfinite2<__half>(h[k])) continue;
+            if ((h[k] & 0x7C00u) == 0x7C00u) h[k] &= 0xFFFF0000u;
+            if ((h[k] & 0x7C000000u) == 0x7C000000u) h[k] &= 0xFFFFu;
+            odd = true;
           }
         }
-        const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
-        uint8_t* at = tile + (c >> 2) * BLK + row * 128;    // channels 16 c ..: chunks 2 c and 2 c + 1 of 8
-        const int k0 = (2 * c) & 7, sw = row & 7;
-        // half of the lanes write their second chunk first: no two of eight on one bank
-        const bool flip = D == 128 ? c >= 4 : sub & 1;
-        *reinterpret_cast<uint4*>(at + (((k0 + flip) ^ sw) << 4)) = flip ? hi : lo;
-        *reinterpret_cast<uint4*>(at + (((k0 + !flip) ^ sw) << 4)) = flip ? lo : hi;
       }
+      const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
+      uint8_t* at = tile + (c >> 2) * BLK + row * 128;      // channels 16 c ..: chunks 2 c and 2 c + 1 of 8
+      const int k0 = (2 * c) & 7, sw = row & 7;
+      // the lanes of the upper channels write their second chunk first: no two of the
+      // eight lanes of a row on one bank
+      const bool flip = D == 128 && c >= 4;
+      *reinterpret_cast<uint4*>(at + (((k0 + flip) ^ sw) << 4)) = flip ? hi : lo;
+      *reinterpret_cast<uint4*>(at + (((k0 + !flip) ^ sw) << 4)) = flip ? lo : hi;
+    }
     if (odd) *poison = 1;
-  };
-  if (a.idle || n == 0) return true;
-  Codes k, v;
-  ask(0);
-  place(0);
-  ask(1);
-  fetch(k, 0);
-  fetch(v, vrows);
-  for (int jt = 0; jt < n; ++jt) {
-    const int s = jt & 1, j0 = tile_at(tl, t0 + jt) * TK;
-    if (jt >= ST && !wait_all(B_KEMPTY + s, ((jt >> 1) - 1) & 1)) return false;
-    store(std::false_type{}, k, sm + L::K + s * NB * BLK, j0);
     fence_proxy_async_smem();
     __syncwarp();
+  };
+  for (int jt = 0; jt < n; ++jt) {
+    const int s = jt & 1, j0 = tile_at(tl, t0 + jt) * TK, cs = jt % L::CS;
+    const uint32_t ph = (jt / L::CS) & 1;
+    if (!wait_all(B_CFULL + cs, ph)) return false;
+    if (jt >= ST && !wait_all(B_KEMPTY + s, ((jt >> 1) - 1) & 1)) return false;
+    rebuild(std::false_type{}, 0, jt, sm + L::K + s * NB * BLK);
     if (lane == 0) mbar_arrive(bar(B_KFULL + s));
-    if (jt + 1 < n) {
-      place(jt + 1);
-      ask(jt + 2);
-      fetch(k, 0);
-    }
+    if (!wait_all(B_CFULL + L::CS + cs, ph)) return false;
     if (jt >= ST && !wait_all(B_VEMPTY + s, ((jt >> 1) - 1) & 1)) return false;
     uint8_t* tile = sm + L::V + s * NB * BLK;
-    if (all_see(tl, j0, j0 + TK, a.sinks)) store(std::false_type{}, v, tile, j0);
-    else store(std::true_type{}, v, tile, j0);
-    fence_proxy_async_smem();
-    __syncwarp();
+    if (all_see(tl, j0, j0 + TK, a.sinks)) rebuild(std::false_type{}, 1, jt, tile);
+    else rebuild(std::true_type{}, 1, jt, tile);
     if (lane == 0) mbar_arrive(bar(B_VRDY + s));
-    if (jt + 1 < n) fetch(v, vrows);
   }
   return true;
 }
@@ -262,7 +208,7 @@ __device__ __forceinline__ bool rebuild_tiles(const PagedArgs& a, uint8_t* sm, c
 // binary16 (every code x scale is one).
 template <typename T, int D, bool C8>
 __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
-  using L = Smem<D>;
+  using L = Smem<D, C8>;
   using Op = Operand<T, C8>;
   constexpr int NB = L::NB;
   extern __shared__ uint8_t raw[];
@@ -284,6 +230,12 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
       mbar_init(bar(B_PFULL + 2 * s), 4);
       mbar_init(bar(B_PFULL + 2 * s + 1), 4);
       mbar_init(bar(B_QRDY + s), 4);
+    }
+    if constexpr (C8) {
+      for (int s = 0; s < 2 * L::CS; ++s) {
+        mbar_init(bar(B_CFULL + s), 1);
+        mbar_init(bar(B_CEMPTY + s), kRebuild);
+      }
     }
     mbar_init(bar(B_OFIN), 1);
     s_err = 0;
@@ -374,7 +326,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
 
   if (warp < W_MMA) {
     // ------------------------------------------------------------ softmax
-    if constexpr (C8) reg_take<kRegSoftmax>();
+    if constexpr (C8) set_registers<kRegSoftmax>();
     const int i = warp >> 2, row = tid & 127;
     if (i < nqt) {
       uint8_t* sQ = sm + L::Q + i * NB * BLK;
@@ -624,11 +576,11 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
   } else if (C8 && warp >= W_CODES) {
     // ------------------------------------------------------------ K and V from codes
     if constexpr (C8) {
-      reg_take<kRegCodes>();
-      if (!rebuild_tiles<D>(a, sm, tl, t0, n, b, hk, warp - W_CODES, &s_poison)) s_err = 1;
+      set_registers<kRegCodes>();
+      if (!rebuild_tiles<D>(a, sm, tl, t0, n, warp - W_CODES, &s_poison)) s_err = 1;
     }
   } else {
-    if constexpr (C8) reg_give<kRegMma>();
+    if constexpr (C8) set_registers<kRegMma>();
     if (warp == W_MMA) {
     // ------------------------------------------------------------ MMA issue
     // Order per K/V tile j: P0 V(j) in two halves, S0(j+1), P1 V(j), S1(j+1); S_i(j+1) may
@@ -682,18 +634,24 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
       if (!mbar_wait(bar(B_OFIN), 0, kDrainNs) || !ok) s_err = 1;
     }
     __syncwarp();
-    } else if (!C8 && (warp == W_K || warp == W_V)) {
+    } else if (warp == W_K || warp == W_V) {
     // ------------------------------------------------------------ producers of K and V
     // lane = box * NB + channel block; a box is the part of a page (at most 64
     // tokens of it) that lies in the tile.  Boxes no row sees are not read.
     const int kv = warp == W_V;
-    const int full = kv ? B_VFULL : B_KFULL, empty = kv ? B_VEMPTY : B_KEMPTY;
+    // (of 8-bit pages: a box's codes and its scales, CS tiles of each in flight)
+    constexpr int STAGES = C8 ? L::CS : ST;
+    const int full = C8 ? B_CFULL + kv * L::CS : (kv ? B_VFULL : B_KFULL);
+    const int empty = C8 ? B_CEMPTY + kv * L::CS : (kv ? B_VEMPTY : B_KEMPTY);
     const int box_log2 = min(a.page_log2, 6);
     const int boxes = TK >> box_log2;
-    const int box = lane / NB, blk = lane % NB;
+    const int box = C8 ? lane : lane / NB, blk = C8 ? 0 : lane % NB;
     const bool mine = box < boxes;
     const int32_t* trow = a.table + (int64_t)b * a.table_stride;
-    const uint32_t ring = smem_u32(sm + (kv ? L::V : L::K)) + blk * BLK + ((box << box_log2) * 128);
+    const uint32_t ring = C8 ? smem_u32(sm + L::CODES) + kv * L::CS * TK * D + ((box << box_log2) * D)
+                             : smem_u32(sm + (kv ? L::V : L::K)) + blk * BLK + ((box << box_log2) * 128);
+    const uint32_t sring = C8 ? smem_u32(sm + L::SCALES) + kv * L::CS * TK * 2 + ((box << box_log2) * 2) : 0u;
+    const uint32_t box_bytes = (C8 ? D + 2u : 128u) << box_log2;
     auto page_of = [&](int jt, bool& want) -> int {
       const int j0 = tile_at(tl, t0 + jt) * TK + (box << box_log2);
       want = mine && any_sees(tl, j0, j0 + (1 << box_log2), a.sinks);
@@ -703,7 +661,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
     int page = n > 0 ? page_of(0, want) : 0;
     int jt = 0;
     for (; jt < n && !a.idle; ++jt) {
-      const int s = jt & 1;
+      const int s = jt % STAGES;
       bool want_n = false;
       int page_n = 0;
       if (jt + 1 < n) page_n = page_of(jt + 1, want_n);   // its latency runs beside the copies
@@ -711,12 +669,16 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
         record_status(a.status, QWM_ERR_INVALID_ARG);
         page = 0;
       }
-      const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, want)) * (128u << box_log2);
+      const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, want)) * box_bytes;
       const int y = (tile_at(tl, t0 + jt) * TK + (box << box_log2)) & ((1 << a.page_log2) - 1);
-      if (jt >= ST && !(ok = wait_all(empty + s, ((jt >> 1) - 1) & 1))) break;
+      if (jt >= STAGES && !(ok = wait_all(empty + s, (jt / STAGES - 1) & 1))) break;
       if (lane == 0) mbar_arrive_expect_tx(bar(full + s), bytes);
       __syncwarp();
-      if (want) tma_load_3d(ring + s * NB * BLK, &map, blk * 64, y, (page * 2 + kv) * a.Hk + hk, bar(full + s));
+      if (want) {
+        const int block = (page * 2 + kv) * a.Hk + hk;
+        tma_load_3d(ring + s * (C8 ? TK * D : NB * BLK), &map, blk * 64, y, block, bar(full + s));
+        if (C8) bulk_g2s(sring + s * TK * 2, a.scales + (((int64_t)block << a.page_log2) + y), 2u << box_log2, bar(full + s));
+      }
       __syncwarp();
       page = page_n;
       want = want_n;
@@ -724,7 +686,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
     if (!ok) s_err = 1;
     // the last copies land before the CTA can end: the roles that wait for them may
     // have given up on them
-    for (int u = max(0, jt - ST); u < jt; ++u) mbar_wait(bar(full + (u & 1)), (u >> 1) & 1, kDrainNs);
+    for (int u = max(0, jt - STAGES); u < jt; ++u) mbar_wait(bar(full + u % STAGES), (u / STAGES) & 1, kDrainNs);
     } else if (!C8) {
     // ------------------------------------------------------------ guard of the Values
     bool ok = true;
@@ -882,10 +844,10 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
 template <typename T, int D, bool C8>
 cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   static bool done[64];
-  cudaError_t e = allow_smem(paged_chunk<T, D, C8>, Smem<D>::TOTAL, done);
+  cudaError_t e = allow_smem(paged_chunk<T, D, C8>, Smem<D, C8>::TOTAL, done);
   if (e != cudaSuccess) return e;
   const int64_t rtiles = ((int64_t)a.max_q * a.G + ROWS - 1) / ROWS;
-  e = launch_ahead(paged_chunk<T, D, C8>, dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), C8 ? NT8 : NT, Smem<D>::TOTAL, s, map, a);
+  e = launch_ahead(paged_chunk<T, D, C8>, dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), C8 ? NT8 : NT, Smem<D, C8>::TOTAL, s, map, a);
   if (e != cudaSuccess || a.nsplit == 1) return e;
   return launch_ahead(paged_join<T, D, Operand<T, C8>>, dim3((unsigned)(rtiles * (ROWS / JR)), a.Hk, a.B), 256, 0, s, a);
 }
