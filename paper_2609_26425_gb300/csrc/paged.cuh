@@ -88,9 +88,11 @@ struct PagedPlan {
   int32_t nsplit, min_tiles;
 };
 PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split, bool codes);
-PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, bool split);
+PagedPlan plan_chunk(int B, int Hk, int D, int64_t rows, int64_t max_visible, int nsm, bool split, bool codes);
 cudaError_t launch_paged_step(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s);
-cudaError_t launch_paged_chunk(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s);
+// (half_map: of 8-bit pages of 128 channels, boxes of 64 of them)
+cudaError_t launch_paged_chunk(const PagedArgs& a, const CUtensorMap& map, const CUtensorMap& half_map, int D, int dtype,
+                               cudaStream_t s);
 // Limit of the waits that let copies and MMAs in flight finish after another
 // wait has run out, before a CTA gives up its shared memory and TMEM.
 constexpr uint64_t kDrainNs = 1000000000ull;
@@ -111,18 +113,23 @@ inline cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64]) {
 // grid_begin() before its first access to global memory: it waits for that
 // kernel's end, then lets the next one be set up.  Back to back this hides the
 // launch and the start of a CTA, 1 to 2 us of a short step's 5 to 12.
+// `cluster`: CTAs of a cluster, along x.
 template <class... P, class... A>
-inline cudaError_t launch_ahead(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A&&... args) {
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
+inline cudaError_t launch_ahead(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, int cluster,
+                                A&&... args) {
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 // Rows (Query tokens x Query heads per cache head) up to which a sequence goes
@@ -135,9 +142,9 @@ constexpr int kStepRows = 16;
 // Pages as rows of D channels, [num_pages * 2 * heads][page_tokens][D]: boxes of
 // 64 channels x min(page_tokens, 64) tokens, 128-byte swizzle.
 bool make_page_map(CUtensorMap* m, const void* pages, int64_t blocks, int page_tokens, int D, int dtype);
-// The same of 8-bit pages: boxes of D codes x min(page_tokens, 64) tokens, swizzled by the
-// row's length (128 or 64 bytes).
-bool make_code_map(CUtensorMap* m, const void* pages, int64_t blocks, int page_tokens, int D);
+// The same of 8-bit pages: boxes of `width` (64 or 128) codes x min(page_tokens, 64) tokens,
+// swizzled by that many bytes.
+bool make_code_map(CUtensorMap* m, const void* pages, int64_t blocks, int page_tokens, int D, int width);
 
 // ------------------------------------------------------------ device helpers
 #ifdef __CUDACC__

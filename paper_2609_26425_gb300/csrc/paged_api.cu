@@ -9,7 +9,7 @@ struct qwm_paged {
   qwm_paged_config cfg;
   bool codes;                   // 8-bit pages
   uint8_t* base;
-  CUtensorMap map;
+  CUtensorMap map, half_map;    // half_map: of 8-bit pages of 128 channels, boxes of 64 of them
   int32_t page_log2;
   int nsm;
   uint64_t wait_ns;
@@ -73,7 +73,8 @@ qwm_status paged_init(qwm_paged** out, const qwm_paged_config* cfg, void* dev_bu
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess ||
       cudaDeviceGetAttribute(&c->nsm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-      !(codes ? qwm::make_code_map(&c->map, pages_of(c), blocks, cfg->page_tokens, cfg->head_dim)
+      !(codes ? qwm::make_code_map(&c->map, pages_of(c), blocks, cfg->page_tokens, cfg->head_dim, cfg->head_dim) &&
+                    qwm::make_code_map(&c->half_map, pages_of(c), blocks, cfg->page_tokens, cfg->head_dim, 64)
               : qwm::make_page_map(&c->map, pages_of(c), blocks, cfg->page_tokens, cfg->head_dim, cfg->dtype)) ||
       cudaMemsetAsync(dev_buf, 0, QWM_PAGED_HEADER_BYTES, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
     delete c;
@@ -228,7 +229,8 @@ PagedPlan make_plan(const qwm_paged* c, const qwm_paged_batch* b, int32_t q_head
   }
   return rows <= qwm::kStepRows ? qwm::plan_step(b->num_seqs, c->cfg.kv_heads, c->cfg.head_dim, (int)rows, seen, c->nsm,
                                                split, c->codes)
-                                : qwm::plan_chunk(b->num_seqs, c->cfg.kv_heads, rows, seen, c->nsm, split);
+                                : qwm::plan_chunk(b->num_seqs, c->cfg.kv_heads, c->cfg.head_dim, rows, seen, c->nsm, split,
+                                                  c->codes);
 }
 
 // A workspace: counters, at the same place for every call (they stay zero between
@@ -450,7 +452,7 @@ qwm_status qwm_paged_attend(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = p.step ? qwm::launch_paged_step(a, c->map, D, c->cfg.dtype, s)
-                               : qwm::launch_paged_chunk(a, c->map, D, c->cfg.dtype, s);
+                               : qwm::launch_paged_chunk(a, c->map, c->half_map, D, c->cfg.dtype, s);
   return e == cudaSuccess ? QWM_OK : cuda_error();
 }
 

@@ -45,7 +45,8 @@ constexpr int ST = 2;                     // K tiles and V tiles in flight
 constexpr int BLK = 16384;                // 128 rows x 128 bytes
 
 enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VRDY = 6, B_VEMPTY = 8, B_SFULL = 10, B_QRDY = 12, B_PV = 14,
-       B_PFULL = 16 /* tile, half */, B_OFIN = 20, B_CFULL = 22 /* codes: K, V, stage */, B_CEMPTY = 26 };
+       B_PFULL = 16 /* tile, half */, B_OFIN = 20, B_CFULL = 22 /* codes: K, V, stage */, B_CEMPTY = 26,
+       B_KREL = 30, B_VREL = 32 /* the second CTA's K and V, to be told to the first */, N_BAR = 34 };
 
 constexpr int NQ = 2, ROWS = 128 * NQ;               // row tiles and rows of a CTA
 constexpr int W_MMA = 4 * NQ, W_K = W_MMA + 1, W_V = W_MMA + 2;  // W_MMA + 3: the guard
@@ -57,18 +58,25 @@ constexpr int kRebuild = 4, NT8 = NT + 128;
 constexpr int kRegLaunch = 65536 / NT8, kRegSoftmax = 168, kRegMma = 80, kRegCodes = 96;
 static_assert(NT8 == 512 && NQ * kRegSoftmax + kRegMma + kRegCodes <= 4 * kRegLaunch, "what the launch has");
 
-template <int D, bool C8 = false>
+template <int D, bool C8>
 struct Smem {
+  // 8-bit pages of 128 channels: a pair of CTAs shares its MMAs, and each has half of
+  // the keys of a K tile and half of the channels of a V tile
+  static constexpr bool PAIR = C8 && D == 128;
+  static constexpr int GR = PAIR ? 2 * ROWS : ROWS;  // rows of a group (a CTA's, or a pair's)
   static constexpr int NB = D / 64;                  // 64-channel blocks of a tile
+  static constexpr int KROWS = PAIR ? TK / 2 : TK, KBLK = KROWS * 128, KST = NB * KBLK;   // of a CTA: keys, bytes
+  static constexpr int VCH = PAIR ? D / 2 : D, VST = VCH / 64 * BLK;                      // channels, bytes
   static constexpr int Q = 0;                        // tile i, block k at (i * NB + k) * BLK
-  static constexpr int K = NQ * NB * BLK;            // stage s, block k at (s * NB + k) * BLK
-  static constexpr int V = K + ST * NB * BLK;
-  // 8-bit pages: tiles of codes [K, V][stage], and their scales
-  static constexpr int CS = C8 ? (D == 64 ? 2 : 1) : 0;
-  static constexpr int CODES = V + ST * NB * BLK;
-  static constexpr int SCALES = CODES + 2 * CS * TK * D;
+  static constexpr int K = NQ * NB * BLK;            // stage s, block k at s * KST + k * KBLK
+  static constexpr int V = K + ST * KST;
+  // 8-bit pages: tiles of codes [K, V][stage], and their scales [K, V][stage][TK]
+  static constexpr int CS = C8 ? 2 : 0, CT = TK * VCH;
+  static_assert(KROWS * D == CT, "K and V codes of a CTA");
+  static constexpr int CODES = V + ST * VST;
+  static constexpr int SCALES = CODES + 2 * CS * CT;
   static constexpr int BAR = SCALES + 2 * CS * TK * 2;
-  static constexpr int TOTAL = BAR + 256 + 1024;
+  static constexpr int TOTAL = BAR + N_BAR * 8 + 1024;
 };
 
 __device__ __forceinline__ void umma_ss_e(uint32_t d, uint64_t ad, uint64_t bd, uint32_t id, uint32_t acc, uint32_t e) {
@@ -119,36 +127,37 @@ __device__ __forceinline__ void set_registers() {
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
 }
 
-// K and V of 8-bit pages: warp `rank` of four turns a quarter of each tile's codes into
-// binary16 where the TMA of 16-bit pages would have put them, so that the MMAs are the
-// same: 16 codes a lane, D / 16 lanes a row.  Values that no row of the CTA sees are cleared
-// on the way, those that some see and others do not searched (the guard's work).  False: a
-// wait ran out.
-template <int D>
-__device__ __forceinline__ bool rebuild_tiles(const PagedArgs& a, uint8_t* sm, const Tiles& tl, int t0, int n, int rank,
-                                              int* poison) {
+// K and V of 8-bit pages: warp `w` of four turns a quarter of the CTA's share of each
+// tile from codes into binary16, where the TMA of 16-bit pages would have put it, so that
+// the MMAs are the same: 16 codes a lane.  Values that no row sees are cleared on the way,
+// those that some see and others do not searched (the guard's work; true in *odd where
+// something was taken out).  `done` hands a stage of K or V on.  False: a wait ran out.
+template <int D, class Done>
+__device__ __forceinline__ bool rebuild_tiles(const PagedArgs& a, uint8_t* sm, const Tiles& tl, int t0, int n, int w,
+                                              bool* odd, Done done) {
   using L = Smem<D, true>;
-  constexpr int NB = L::NB, LPR = D / 16, RPL = 32 / LPR;   // lanes of a row, rows of a load
-  constexpr int LOADS = TK / RPL / kRebuild;
-  const int lane = threadIdx.x & 31, c = lane % LPR, row0 = rank * (TK / kRebuild) + lane / LPR;
+  const int lane = threadIdx.x & 31;
   auto bar = [&](int i) { return smem_u32(sm + L::BAR) + 8u * i; };
   auto wait_all = [&](int i, uint32_t ph) -> bool { return __all_sync(0xFFFFFFFFu, mbar_wait(bar(i), ph, a.wait_ns)); };
-  // Tile jt of K or V: from codes to its place in the ring
-  auto rebuild = [&](auto masked, int kv, int jt, uint8_t* tile) {
+  // Tile jt of K (NR keys x NC channels here) or V: from codes to its place in the ring,
+  // blocks of 64 channels `stride` bytes apart
+  auto rebuild = [&](auto rows_, auto channels_, auto masked, int kv, int jt, uint8_t* tile, int stride) {
+    constexpr int NR = rows_, NC = channels_, LPR = NC / 16, RPL = 32 / LPR;   // lanes of a row, rows of a load
+    constexpr int LOADS = NR / RPL / kRebuild;
+    const int c = lane % LPR, row0 = w * (NR / kRebuild) + lane / LPR;
     const int st = kv * L::CS + jt % L::CS;
-    const uint8_t* codes = sm + L::CODES + st * (TK * D);
+    const uint8_t* codes = sm + L::CODES + st * L::CT;
     const uint16_t* scales = reinterpret_cast<const uint16_t*>(sm + L::SCALES) + st * TK;
     uint4 x[LOADS];
     uint32_t s2[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int row = row0 + i * RPL;
-      x[i] = *reinterpret_cast<const uint4*>(codes + row * D + ((D == 128 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4));
+      x[i] = *reinterpret_cast<const uint4*>(codes + row * NC + ((NC == 128 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4));
       s2[i] = scales[row] * 0x10001u;
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(B_CEMPTY + st));
-    bool odd = false;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int row = row0 + i * RPL;
@@ -170,36 +179,39 @@ __device__ __forceinline__ bool rebuild_tiles(const PagedArgs& a, uint8_t* sm, c
             if (!nonfinite2<__half>(h[k])) continue;
             if ((h[k] & 0x7C00u) == 0x7C00u) h[k] &= 0xFFFF0000u;
             if ((h[k] & 0x7C000000u) == 0x7C000000u) h[k] &= 0xFFFFu;
-            odd = true;
+            *odd = true;
           }
         }
       }
       const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
-      uint8_t* at = tile + (c >> 2) * BLK + row * 128;      // channels 16 c ..: chunks 2 c and 2 c + 1 of 8
+      uint8_t* at = tile + (c >> 2) * stride + row * 128;   // channels 16 c ..: chunks 2 c and 2 c + 1 of 8
       const int k0 = (2 * c) & 7, sw = row & 7;
       // the lanes of the upper channels write their second chunk first: no two of the
       // eight lanes of a row on one bank
-      const bool flip = D == 128 && c >= 4;
+      const bool flip = NC == 128 && c >= 4;
       *reinterpret_cast<uint4*>(at + (((k0 + flip) ^ sw) << 4)) = flip ? hi : lo;
       *reinterpret_cast<uint4*>(at + (((k0 + !flip) ^ sw) << 4)) = flip ? lo : hi;
     }
-    if (odd) *poison = 1;
     fence_proxy_async_smem();
     __syncwarp();
   };
+  using KRows = std::integral_constant<int, L::KROWS>;
+  using VChannels = std::integral_constant<int, L::VCH>;
+  using All = std::integral_constant<int, D>;
+  using Keys = std::integral_constant<int, TK>;
   for (int jt = 0; jt < n; ++jt) {
     const int s = jt & 1, j0 = tile_at(tl, t0 + jt) * TK, cs = jt % L::CS;
     const uint32_t ph = (jt / L::CS) & 1;
     if (!wait_all(B_CFULL + cs, ph)) return false;
     if (jt >= ST && !wait_all(B_KEMPTY + s, ((jt >> 1) - 1) & 1)) return false;
-    rebuild(std::false_type{}, 0, jt, sm + L::K + s * NB * BLK);
-    if (lane == 0) mbar_arrive(bar(B_KFULL + s));
+    rebuild(KRows{}, All{}, std::false_type{}, 0, jt, sm + L::K + s * L::KST, L::KBLK);
+    done(0, s);
     if (!wait_all(B_CFULL + L::CS + cs, ph)) return false;
     if (jt >= ST && !wait_all(B_VEMPTY + s, ((jt >> 1) - 1) & 1)) return false;
-    uint8_t* tile = sm + L::V + s * NB * BLK;
-    if (all_see(tl, j0, j0 + TK, a.sinks)) rebuild(std::false_type{}, 1, jt, tile);
-    else rebuild(std::true_type{}, 1, jt, tile);
-    if (lane == 0) mbar_arrive(bar(B_VRDY + s));
+    uint8_t* tile = sm + L::V + s * L::VST;
+    if (all_see(tl, j0, j0 + TK, a.sinks)) rebuild(Keys{}, VChannels{}, std::false_type{}, 1, jt, tile, BLK);
+    else rebuild(Keys{}, VChannels{}, std::true_type{}, 1, jt, tile, BLK);
+    done(1, s);
   }
   return true;
 }
@@ -207,8 +219,11 @@ __device__ __forceinline__ bool rebuild_tiles(const PagedArgs& a, uint8_t* sm, c
 // T: the type of Queries and output; C8: 8-bit pages, whose products are taken in
 // binary16 (every code x scale is one).
 template <typename T, int D, bool C8>
-__global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
+__global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_constant__ CUtensorMap map,
+                                                                 const __grid_constant__ CUtensorMap half_map,
+                                                                 const PagedArgs a) {
   using L = Smem<D, C8>;
+  constexpr bool PAIR = L::PAIR;
   using Op = Operand<T, C8>;
   constexpr int NB = L::NB;
   extern __shared__ uint8_t raw[];
@@ -218,18 +233,24 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   auto bar = [&](int i) { return smem_u32(sm + L::BAR) + 8u * i; };
+  const uint32_t rank = PAIR ? cluster_rank() : 0;    // 0: the CTA that issues the pair's MMAs
   if (tid == 0) {
     for (int s = 0; s < 2; ++s) {
-      mbar_init(bar(B_KFULL + s), C8 ? kRebuild : 1);
+      // (of a pair: this CTA's warps, and for K and V one arrival for all of the other's)
+      mbar_init(bar(B_KFULL + s), C8 ? kRebuild + PAIR : 1);
       mbar_init(bar(B_KEMPTY + s), 1);
       mbar_init(bar(B_VFULL + s), 1);
-      mbar_init(bar(B_VRDY + s), C8 ? kRebuild : 1);
+      mbar_init(bar(B_VRDY + s), C8 ? kRebuild + PAIR : 1);
       mbar_init(bar(B_VEMPTY + s), 1);
       mbar_init(bar(B_SFULL + s), 1);
       mbar_init(bar(B_PV + s), 1);
-      mbar_init(bar(B_PFULL + 2 * s), 4);
-      mbar_init(bar(B_PFULL + 2 * s + 1), 4);
-      mbar_init(bar(B_QRDY + s), 4);
+      mbar_init(bar(B_PFULL + 2 * s), PAIR ? 8 : 4);
+      mbar_init(bar(B_PFULL + 2 * s + 1), PAIR ? 8 : 4);
+      mbar_init(bar(B_QRDY + s), PAIR ? 8 : 4);
+      if constexpr (PAIR) {
+        mbar_init(bar(B_KREL + s), kRebuild);
+        mbar_init(bar(B_VREL + s), kRebuild);
+      }
     }
     if constexpr (C8) {
       for (int s = 0; s < 2 * L::CS; ++s) {
@@ -244,16 +265,18 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
   }
   grid_begin();
   const int b = blockIdx.z, hk = blockIdx.y;
-  const int rtiles = gridDim.x / a.nsplit;
+  const int gx = PAIR ? blockIdx.x >> 1 : blockIdx.x, rtiles = (PAIR ? gridDim.x >> 1 : gridDim.x) / a.nsplit;
   // the row tiles with the most keys first
-  const int rt = rtiles - 1 - (int)(blockIdx.x % rtiles), part = blockIdx.x / rtiles;
+  const int rt = rtiles - 1 - gx % rtiles, part = gx / rtiles;
   Seq sq;
   if (!load_seq(a, b, sq) && blockIdx.x == 0 && hk == 0 && tid == 0) record_status(a.status, QWM_ERR_INVALID_ARG);
   const int64_t rows = (int64_t)sq.qn * a.G;
-  const int64_t r0 = (int64_t)rt * ROWS;
+  const int64_t r0 = (int64_t)rt * L::GR;
   if (r0 >= rows) return;
-  const int nrow = (int)min((int64_t)ROWS, rows - r0);
-  const int nqt = nrow > 128 ? 2 : 1;
+  const int nrow = (int)min((int64_t)L::GR, rows - r0);
+  const int nqt = nrow > L::GR / 2 ? 2 : 1;
+  // row tile i holds the group's rows row_at(i) ..: of a pair, 128 of the first CTA, then of the second
+  auto row_at = [&](int i) { return PAIR ? 256 * i + 128 * (int)rank : 128 * i; };
   const int p0 = sq.kv - sq.qn;                       // token of the sequence's first row
   // row r0 + i is new token tokA + (remA + i) / G, grouped head (remA + i) % G
   const int tokA = (int)(r0 / a.G);
@@ -270,8 +293,13 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
   };
   __syncthreads();                                    // the barriers are set up
   if (warp == W_MMA) {
-    tmem_alloc(smem_u32(&s_tmem), 512);
-    tmem_relinquish();
+    if constexpr (PAIR) {
+      tmem_alloc2(smem_u32(&s_tmem), 512);
+      tmem_relinquish2();
+    } else {
+      tmem_alloc(smem_u32(&s_tmem), 512);
+      tmem_relinquish();
+    }
   }
   int q_up = 0;                                       // 8-bit pages: this thread's row was taken times 2^q_up
   if (warp < W_MMA && (warp >> 2) < nqt) {
@@ -284,14 +312,14 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
 #pragma unroll
       for (int k = 0; k < CH; ++k) {
         const int idx = k * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
-        const uint32_t r = remA + min(i * 128 + rr, nrow - 1);
+        const uint32_t r = remA + min(row_at(i) + rr, nrow - 1);
         v[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (sq.q0 + tokA + r / G) * a.q_tok +
                                                (hk * a.G + (int)(r % G)) * a.q_head + c * 8);
       }
 #pragma unroll
       for (int k = 0; k < CH; ++k) {
         const int idx = k * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
-        if (i * 128 + rr >= nrow) v[k] = make_uint4(0, 0, 0, 0);
+        if (row_at(i) + rr >= nrow) v[k] = make_uint4(0, 0, 0, 0);
         if constexpr (C8 && Elem<T>::bf16) {
           // the CH lanes of a row agree on its power of two; the lane of the row's
           // softmax thread keeps it
@@ -315,8 +343,14 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
   // being allocated and the Queries come in.  (All warps waiting for the allocation
   // and the Queries loaded after it: 880 Queries x 12 heads 64.0 us against 62.5;
   // three ragged prompts of 64 channels 79.5 against 80.5.)
+  // (A pair's warps all wait: the other CTA's barriers and TMEM have to be there.)
   uint32_t tbase = 0;
-  if (warp <= W_MMA) {
+  if constexpr (PAIR) {
+    tc_fence_before();
+    cluster_sync();
+    tc_fence_after();
+    tbase = s_tmem;
+  } else if (warp <= W_MMA) {
     tc_fence_before();
     named_bar_sync(1, (W_MMA + 1) * 32);
     tc_fence_after();
@@ -332,11 +366,14 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
       uint8_t* sQ = sm + L::Q + i * NB * BLK;
       constexpr int CH = D / 8;
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B_QRDY + i));
+      if (lane == 0) {
+        if (rank == 0) mbar_arrive(bar(B_QRDY + i));
+        else mbar_arrive_cluster(mapa(bar(B_QRDY + i), 0));
+      }
 
-      const bool has = i * 128 + row < nrow;
-      const int tok = has ? tokA + (int)((remA + i * 128 + row) / G) : tokB;
-      const int head = hk * a.G + (has ? (int)((remA + i * 128 + row) % G) : 0);
+      const bool has = row_at(i) + row < nrow;
+      const int tok = has ? tokA + (int)((remA + row_at(i) + row) / G) : tokB;
+      const int head = hk * a.G + (has ? (int)((remA + row_at(i) + row) % G) : 0);
       const Span sp = has ? row_span(p0 + tok, sq.kv, a.block, a.window) : Span{0, 0};
       const uint32_t lrow = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t tS = tbase + 128 * i + lrow, tO = tbase + 128 * NQ + D * i + lrow;
@@ -482,7 +519,11 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(B_PFULL + 2 * i + half));
+            // (P is tensor memory, stored and fenced: the other CTA's arrival has nothing to release)
+            if (lane == 0) {
+              if (rank == 0) mbar_arrive(bar(B_PFULL + 2 * i + half));
+              else mbar_arrive_cluster_relaxed(mapa(bar(B_PFULL + 2 * i + half), 0));
+            }
           }
         };
         if (open) pass(std::false_type{});
@@ -491,10 +532,11 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
       }
       if (ok && n > 0) ok = wait_all(B_OFIN, 0);
       if (!ok) s_err = 1;
+      if constexpr (PAIR) cluster_sync();             // what either CTA took out of the Values is known
       if (ok) {
         tc_fence_after();
         const int64_t group = ((int64_t)b * a.Hk + hk) * rtiles + rt;
-        const int64_t pr = (group * a.nsplit + part) * ROWS + i * 128 + row;
+        const int64_t pr = (group * a.nsplit + part) * L::GR + row_at(i) + row;
         const float inv = l_run > 0.0f || l_run != l_run ? 1.0f / l_run : 0.0f;
         const bool poison = *(volatile int*)&s_poison != 0;
 #pragma unroll 1
@@ -550,10 +592,10 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
             }
           } else if (has) {
             // a part: [channels / 4][row], so that a warp writes whole lines
-            float4* d4 = reinterpret_cast<float4*>(a.part_o) + (group * a.nsplit + part) * ROWS * (D / 4) +
-                         (int64_t)(c0 / 4) * ROWS + i * 128 + row;
+            float4* d4 = reinterpret_cast<float4*>(a.part_o) + (group * a.nsplit + part) * L::GR * (D / 4) +
+                         (int64_t)(c0 / 4) * L::GR + row_at(i) + row;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) d4[k * ROWS] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+            for (int k = 0; k < 8; ++k) d4[k * L::GR] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
           }
         }
         if (parts == 1) {
@@ -561,8 +603,8 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
 #pragma unroll 4
           for (int it = 0; it < CH; ++it) {
             const int idx = it * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
-            if (i * 128 + rr >= nrow) continue;
-            const uint32_t r = remA + i * 128 + rr;
+            if (row_at(i) + rr >= nrow) continue;
+            const uint32_t r = remA + row_at(i) + rr;
             *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + (sq.q0 + tokA + r / G) * a.o_tok +
                                       (int64_t)(hk * a.G + (int)(r % G)) * a.o_head + c * 8) =
                 *reinterpret_cast<const uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4));
@@ -572,63 +614,91 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
           a.lse[(int64_t)head * a.N + sq.q0 + tok] = log_sum<Op>(power(m_run), l_run);
         if (has && parts > 1) a.part_ml[pr] = make_float2(power(m_run), l_run);
       }
+    } else if constexpr (PAIR) {
+      cluster_sync();
     }
   } else if (C8 && warp >= W_CODES) {
     // ------------------------------------------------------------ K and V from codes
     if constexpr (C8) {
       set_registers<kRegCodes>();
-      if (!rebuild_tiles<D>(a, sm, tl, t0, n, warp - W_CODES, &s_poison)) s_err = 1;
+      bool odd = false;
+      auto done = [&](int kv, int s) {
+        if (odd) s_poison = 1;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar((rank == 0 ? (kv ? B_VRDY : B_KFULL) : (kv ? B_VREL : B_KREL)) + s));
+      };
+      if (!rebuild_tiles<D>(a, sm, tl, t0, n, warp - W_CODES, &odd, done)) s_err = 1;
+      if constexpr (PAIR) {
+        if (odd) st_cluster(mapa(smem_u32(&s_poison), rank ^ 1), 1);
+        __syncwarp();
+        cluster_sync();
+      }
     }
   } else {
     if constexpr (C8) set_registers<kRegMma>();
-    if (warp == W_MMA) {
+    if (warp == W_MMA && rank == 0) {
     // ------------------------------------------------------------ MMA issue
     // Order per K/V tile j: P0 V(j) in two halves, S0(j+1), P1 V(j), S1(j+1); S_i(j+1) may
     // overwrite P_i(j) because the MMAs of one thread run in issue order.
     const uint32_t e = elect_one();
     const uint64_t dQ = desc_sw128(smem_u32(sm + L::Q)), dK = desc_sw128(smem_u32(sm + L::K));
-    const uint64_t dV = desc_sw128_mn(smem_u32(sm + L::V), BLK);
+    const uint64_t dV = PAIR ? desc_sw128(smem_u32(sm + L::V)) : desc_sw128_mn(smem_u32(sm + L::V), BLK);
     auto off = [](int bytes) { return (uint64_t)(bytes >> 4); };
-    constexpr uint32_t idS = idesc_f16(128, TK, false, Elem<Op>::bf16);
-    constexpr uint32_t idPV = idesc_f16(128, D, true, Elem<Op>::bf16);
+    constexpr uint32_t idS = idesc_f16(PAIR ? 256 : 128, TK, false, Elem<Op>::bf16);
+    constexpr uint32_t idPV = idesc_f16(PAIR ? 256 : 128, D, true, Elem<Op>::bf16);
+    auto mma_ss = [&](uint32_t d, uint64_t x, uint64_t y, uint32_t acc) {
+      if constexpr (PAIR) umma2_ss_e(d, x, y, idS, acc, e);
+      else umma_ss_e(d, x, y, idS, acc, e);
+    };
+    auto mma_ts = [&](uint32_t d, uint32_t x, uint64_t y, uint32_t acc) {
+      if constexpr (PAIR) umma2_ts_e(d, x, y, idPV, acc, e);
+      else umma_ts_e(d, x, y, idPV, acc, e);
+    };
+    auto commit = [&](int i) {
+      if constexpr (PAIR) umma2_commit_both_e(bar(i), e);
+      else commit_e(bar(i), e);
+    };
+    auto wait_mma = [&](int i, uint32_t ph) -> bool {
+      if constexpr (PAIR) return __all_sync(0xFFFFFFFFu, mbar_wait_cluster(bar(i), ph, a.wait_ns));
+      else return wait_all(i, ph);
+    };
     bool ok = true;
     auto issue_S = [&](int i, int jt) -> bool {
       const int s = jt & 1;
-      if (i == 0 && !wait_all(B_KFULL + s, (jt >> 1) & 1)) return false;
-      if (jt == 0 && !wait_all(B_QRDY + i, 0)) return false;
+      if (i == 0 && !wait_mma(B_KFULL + s, (jt >> 1) & 1)) return false;
+      if (jt == 0 && !wait_mma(B_QRDY + i, 0)) return false;
       tc_fence_after();
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
-          umma_ss_e(tbase + 128 * i, dQ + off((i * NB + kb) * BLK + ks * 32), dK + off((s * NB + kb) * BLK + ks * 32),
-                    idS, (kb | ks) != 0, e);
-      commit_e(bar(B_SFULL + i), e);
-      if (i == nqt - 1) commit_e(bar(B_KEMPTY + s), e);
+          mma_ss(tbase + 128 * i, dQ + off((i * NB + kb) * BLK + ks * 32), dK + off(s * L::KST + kb * L::KBLK + ks * 32),
+                 (kb | ks) != 0);
+      commit(B_SFULL + i);
+      if (i == nqt - 1) commit(B_KEMPTY + s);
       return true;
     };
     if (n > 0) {
       for (int i = 0; i < nqt && ok; ++i) ok = issue_S(i, 0);
       for (int jt = 0; jt < n && ok; ++jt) {
         const int s = jt & 1;
-        if (!(ok = wait_all(B_VRDY + s, (jt >> 1) & 1))) break;
+        if (!(ok = wait_mma(B_VRDY + s, (jt >> 1) & 1))) break;
         for (int i = 0; i < nqt; ++i) {
 #pragma unroll
           for (int half = 0; half < 2 && ok; ++half) {
-            if (!(ok = wait_all(B_PFULL + 2 * i + half, jt & 1))) break;
+            if (!(ok = wait_mma(B_PFULL + 2 * i + half, jt & 1))) break;
             tc_fence_after();
 #pragma unroll
             for (int ks = 4 * half; ks < 4 * half + 4; ++ks)
-              umma_ts_e(tbase + 128 * NQ + D * i, tbase + 128 * i + 8 * ks, dV + off(s * NB * BLK + ks * 2048), idPV,
-                        (jt | ks) != 0, e);
-            if (half == 0) commit_e(bar(B_PV + i), e);
+              mma_ts(tbase + 128 * NQ + D * i, tbase + 128 * i + 8 * ks, dV + off(s * L::VST + ks * 2048), (jt | ks) != 0);
+            if (half == 0) commit(B_PV + i);
           }
           if (!ok) break;
-          if (i == nqt - 1) commit_e(bar(B_VEMPTY + s), e);
+          if (i == nqt - 1) commit(B_VEMPTY + s);
           if (jt + 1 < n && !(ok = issue_S(i, jt + 1))) break;
         }
       }
-      commit_e(bar(B_OFIN), e);
+      commit(B_OFIN);
       // the MMAs issued finish before TMEM is freed: the softmax warps, which wait
       // for them as well, may have given up
       if (!mbar_wait(bar(B_OFIN), 0, kDrainNs) || !ok) s_err = 1;
@@ -639,21 +709,24 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
     // lane = box * NB + channel block; a box is the part of a page (at most 64
     // tokens of it) that lies in the tile.  Boxes no row sees are not read.
     const int kv = warp == W_V;
-    // (of 8-bit pages: a box's codes and its scales, CS tiles of each in flight)
+    // Of 8-bit pages: a box's codes and its scales, CS tiles of each in flight; a CTA of
+    // a pair takes its half of a tile's Keys, or its half of the Values' channels.
     constexpr int STAGES = C8 ? L::CS : ST;
     const int full = C8 ? B_CFULL + kv * L::CS : (kv ? B_VFULL : B_KFULL);
     const int empty = C8 ? B_CEMPTY + kv * L::CS : (kv ? B_VEMPTY : B_KEMPTY);
     const int box_log2 = min(a.page_log2, 6);
-    const int boxes = TK >> box_log2;
+    const int k0 = PAIR && !kv ? (int)rank * L::KROWS : 0;   // the CTA's first key of a tile
+    const int row_bytes = kv ? L::VCH : D;                   // (of codes)
+    const int boxes = (kv ? TK : L::KROWS) >> box_log2;
     const int box = C8 ? lane : lane / NB, blk = C8 ? 0 : lane % NB;
     const bool mine = box < boxes;
     const int32_t* trow = a.table + (int64_t)b * a.table_stride;
-    const uint32_t ring = C8 ? smem_u32(sm + L::CODES) + kv * L::CS * TK * D + ((box << box_log2) * D)
-                             : smem_u32(sm + (kv ? L::V : L::K)) + blk * BLK + ((box << box_log2) * 128);
+    const uint32_t ring = C8 ? smem_u32(sm + L::CODES) + kv * L::CS * L::CT + ((box << box_log2) * row_bytes)
+                             : smem_u32(sm + (kv ? L::V : L::K)) + blk * BLK + ((box << box_log2) * 128);   // (KBLK is BLK)
     const uint32_t sring = C8 ? smem_u32(sm + L::SCALES) + kv * L::CS * TK * 2 + ((box << box_log2) * 2) : 0u;
-    const uint32_t box_bytes = (C8 ? D + 2u : 128u) << box_log2;
+    const uint32_t box_bytes = (C8 ? row_bytes + 2u : 128u) << box_log2;
     auto page_of = [&](int jt, bool& want) -> int {
-      const int j0 = tile_at(tl, t0 + jt) * TK + (box << box_log2);
+      const int j0 = tile_at(tl, t0 + jt) * TK + k0 + (box << box_log2);
       want = mine && any_sees(tl, j0, j0 + (1 << box_log2), a.sinks);
       return want ? trow[j0 >> a.page_log2] : 0;
     };
@@ -670,13 +743,14 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
         page = 0;
       }
       const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, want)) * box_bytes;
-      const int y = (tile_at(tl, t0 + jt) * TK + (box << box_log2)) & ((1 << a.page_log2) - 1);
+      const int y = (tile_at(tl, t0 + jt) * TK + k0 + (box << box_log2)) & ((1 << a.page_log2) - 1);
       if (jt >= STAGES && !(ok = wait_all(empty + s, (jt / STAGES - 1) & 1))) break;
       if (lane == 0) mbar_arrive_expect_tx(bar(full + s), bytes);
       __syncwarp();
       if (want) {
         const int block = (page * 2 + kv) * a.Hk + hk;
-        tma_load_3d(ring + s * (C8 ? TK * D : NB * BLK), &map, blk * 64, y, block, bar(full + s));
+        if (PAIR && kv) tma_load_3d(ring + s * L::CT, &half_map, (int)rank * L::VCH, y, block, bar(full + s));
+        else tma_load_3d(ring + s * (C8 ? L::CT : NB * BLK), &map, blk * 64, y, block, bar(full + s));
         if (C8) bulk_g2s(sring + s * TK * 2, a.scales + (((int64_t)block << a.page_log2) + y), 2u << box_log2, bar(full + s));
       }
       __syncwarp();
@@ -687,6 +761,19 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
     // the last copies land before the CTA can end: the roles that wait for them may
     // have given up on them
     for (int u = max(0, jt - STAGES); u < jt; ++u) mbar_wait(bar(full + u % STAGES), (u / STAGES) & 1, kDrainNs);
+    } else if (PAIR && rank == 1) {
+      // ------------------------------------------------------------ relays
+      // Of the second CTA, W_MMA and the last warp tell the first that a stage of K or V is
+      // there: a release over the cluster waits for what the SM has in flight, and the
+      // warps that make the stages go on meanwhile.
+      const int kv = warp != W_MMA;
+      bool ok = true;
+      for (int jt = 0; jt < n && ok; ++jt) {
+        const int s = jt & 1;
+        ok = wait_all((kv ? B_VREL : B_KREL) + s, (jt >> 1) & 1);
+        if (ok && lane == 0) mbar_arrive_cluster(mapa(bar((kv ? B_VRDY : B_KFULL) + s), 0));
+      }
+      if (!ok) s_err = 1;
     } else if (!C8) {
     // ------------------------------------------------------------ guard of the Values
     bool ok = true;
@@ -745,13 +832,19 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
     }
     if (!ok) s_err = 1;
     }
+    if constexpr (PAIR) {
+      __syncwarp();
+      cluster_sync();
+    }
   }
 
   tc_fence_before();
   __syncthreads();
+  if constexpr (PAIR) cluster_sync();                 // neither frees the pair's TMEM while the other reads it
   if (warp == W_MMA) {
     tc_fence_after();
-    tmem_dealloc(tbase, 512);
+    if constexpr (PAIR) tmem_dealloc2(tbase, 512);
+    else tmem_dealloc(tbase, 512);
   }
   if (tid == 0 && s_err) record_status(a.status, QWM_ERR_TIMEOUT);
 }
@@ -761,16 +854,16 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
 // of them; lanes 8 rows x 4 groups of 8 channels, so that reads (a part lies
 // [channels / 4][row]) and writes are whole sectors.
 constexpr int JR = 64;
-template <typename T, int D, typename Op>
+template <typename T, int D, typename Op, int GR>
 __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
   grid_begin();
-  const int b = blockIdx.z, hk = blockIdx.y, rt = blockIdx.x / (ROWS / JR);
-  const int rtiles = gridDim.x / (ROWS / JR);
+  const int b = blockIdx.z, hk = blockIdx.y, rt = blockIdx.x / (GR / JR);
+  const int rtiles = gridDim.x / (GR / JR);
   Seq sq;
   load_seq(a, b, sq);
-  const int64_t rows = (int64_t)sq.qn * a.G, r0 = (int64_t)rt * ROWS;
+  const int64_t rows = (int64_t)sq.qn * a.G, r0 = (int64_t)rt * GR;
   if (r0 >= rows) return;
-  const int nrow = (int)min((int64_t)ROWS, rows - r0);
+  const int nrow = (int)min((int64_t)GR, rows - r0);
   const int tokA = (int)(r0 / a.G), p0 = sq.kv - sq.qn;
   const uint32_t G = (uint32_t)a.G, remA = (uint32_t)(r0 - (int64_t)tokA * a.G);
   const int tokB = tokA + (int)((remA + (uint32_t)nrow - 1) / G);
@@ -778,11 +871,11 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
   const int per = max((tl.n + a.nsplit - 1) / a.nsplit, a.min_tiles);
   const int parts = max(1, (tl.n + per - 1) / per);
   const int lane = threadIdx.x & 31;
-  const int r = (blockIdx.x % (ROWS / JR)) * JR + (threadIdx.x >> 5) * 8 + (lane & 7);
+  const int r = (blockIdx.x % (GR / JR)) * JR + (threadIdx.x >> 5) * 8 + (lane & 7);
   if (parts == 1 || r >= nrow) return;
   const int64_t group = ((int64_t)b * a.Hk + hk) * rtiles + rt;
-  const float2* ml = a.part_ml + group * a.nsplit * ROWS + r;
-  const float4* po = reinterpret_cast<const float4*>(a.part_o) + group * a.nsplit * ROWS * (D / 4) + r;
+  const float2* ml = a.part_ml + group * a.nsplit * GR + r;
+  const float4* po = reinterpret_cast<const float4*>(a.part_o) + group * a.nsplit * GR * (D / 4) + r;
   constexpr int CB = D / 32, PU = 4;                  // channel blocks of a lane, parts in flight
   float m = -INFINITY, l = 0.0f;
   float4 v[CB][2];
@@ -794,13 +887,13 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
 #pragma unroll
     for (int u = 0; u < PU; ++u) {
       const int p = min(pb + u, parts - 1);
-      w[u] = __ldcg(ml + p * ROWS);
+      w[u] = __ldcg(ml + p * GR);
       if (pb + u >= parts) w[u] = make_float2(-INFINITY, 0.0f);
 #pragma unroll
       for (int k = 0; k < CB; ++k) {
-        const float4* src = po + ((int64_t)p * (D / 4) + 2 * (4 * k + (lane >> 3))) * ROWS;
+        const float4* src = po + ((int64_t)p * (D / 4) + 2 * (4 * k + (lane >> 3))) * GR;
         x[u][k][0] = __ldcg(src);
-        x[u][k][1] = __ldcg(src + ROWS);
+        x[u][k][1] = __ldcg(src + GR);
       }
     }
     float mn = m;
@@ -842,25 +935,29 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
 }
 
 template <typename T, int D, bool C8>
-cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
+cudaError_t go(const PagedArgs& a, const CUtensorMap& map, const CUtensorMap& half_map, cudaStream_t s) {
+  using L = Smem<D, C8>;
   static bool done[64];
-  cudaError_t e = allow_smem(paged_chunk<T, D, C8>, Smem<D, C8>::TOTAL, done);
+  cudaError_t e = allow_smem(paged_chunk<T, D, C8>, L::TOTAL, done);
   if (e != cudaSuccess) return e;
-  const int64_t rtiles = ((int64_t)a.max_q * a.G + ROWS - 1) / ROWS;
-  e = launch_ahead(paged_chunk<T, D, C8>, dim3((unsigned)(rtiles * a.nsplit), a.Hk, a.B), C8 ? NT8 : NT, Smem<D, C8>::TOTAL, s, map, a);
+  const int64_t rtiles = ((int64_t)a.max_q * a.G + L::GR - 1) / L::GR;
+  e = launch_ahead(paged_chunk<T, D, C8>, dim3((unsigned)(rtiles * a.nsplit * (L::PAIR ? 2 : 1)), a.Hk, a.B),
+                   C8 ? NT8 : NT, L::TOTAL, s, L::PAIR ? 2 : 1, map, half_map, a);
   if (e != cudaSuccess || a.nsplit == 1) return e;
-  return launch_ahead(paged_join<T, D, Operand<T, C8>>, dim3((unsigned)(rtiles * (ROWS / JR)), a.Hk, a.B), 256, 0, s, a);
+  return launch_ahead(paged_join<T, D, Operand<T, C8>, L::GR>, dim3((unsigned)(rtiles * (L::GR / JR)), a.Hk, a.B), 256, 0, s, 1, a);
 }
 template <typename T, bool C8>
-cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, int D, cudaStream_t s) {
-  return D == 64 ? go<T, 64, C8>(a, map, s) : go<T, 128, C8>(a, map, s);
+cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, const CUtensorMap& half_map, int D, cudaStream_t s) {
+  return D == 64 ? go<T, 64, C8>(a, map, half_map, s) : go<T, 128, C8>(a, map, half_map, s);
 }
 
 }  // namespace
 
-PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, bool split) {
+PagedPlan plan_chunk(int B, int Hk, int D, int64_t rows, int64_t max_visible, int nsm, bool split, bool codes) {
   PagedPlan p{};
-  p.rows = ROWS;
+  const bool pair = codes && D == 128;                                // a group is a pair of CTAs'
+  p.rows = pair ? 2 * ROWS : ROWS;
+  if (pair) nsm /= 2;
   const int64_t rtiles = (rows + p.rows - 1) / p.rows;
   const int64_t groups = rtiles * B * Hk;
   p.groups = (int)(groups < 1 << 30 ? groups : 1 << 30);   // (as many are not split)
@@ -887,9 +984,11 @@ PagedPlan plan_chunk(int B, int Hk, int64_t rows, int64_t max_visible, int nsm, 
   return p;
 }
 
-cudaError_t launch_paged_chunk(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s) {
-  if (a.scales) return dtype == QWM_F16 ? pick<__half, true>(a, map, D, s) : pick<__nv_bfloat16, true>(a, map, D, s);
-  return dtype == QWM_F16 ? pick<__half, false>(a, map, D, s) : pick<__nv_bfloat16, false>(a, map, D, s);
+cudaError_t launch_paged_chunk(const PagedArgs& a, const CUtensorMap& map, const CUtensorMap& half_map, int D, int dtype,
+                               cudaStream_t s) {
+  if (a.scales)
+    return dtype == QWM_F16 ? pick<__half, true>(a, map, half_map, D, s) : pick<__nv_bfloat16, true>(a, map, half_map, D, s);
+  return dtype == QWM_F16 ? pick<__half, false>(a, map, half_map, D, s) : pick<__nv_bfloat16, false>(a, map, half_map, D, s);
 }
 
 }  // namespace qwm

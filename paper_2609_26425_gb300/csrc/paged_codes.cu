@@ -171,7 +171,7 @@ cudaError_t go(const RopeArgs& a, cudaStream_t s) {
   if (tpc > kMaxTokens) tpc = kMaxTokens;
   if (tpc < 1) tpc = 1;
   const unsigned grid = (unsigned)((a.N + tpc - 1) / tpc);
-  return launch_ahead(store_kernel<T, IL, D>, dim3(grid), NT, (size_t)tpc * a.P * sizeof(float2), s, a, (int)tpc);
+  return launch_ahead(store_kernel<T, IL, D>, dim3(grid), NT, (size_t)tpc * a.P * sizeof(float2), s, 1, a, (int)tpc);
 }
 template <typename T>
 cudaError_t pick(const RopeArgs& a, bool il, cudaStream_t s) {
@@ -248,7 +248,7 @@ cudaError_t go_read(const ReadArgs& a, cudaStream_t s) {
   if (tpc > kMaxTokens) tpc = kMaxTokens;
   if (tpc < 1) tpc = 1;
   const unsigned grid = (unsigned)((a.N + tpc - 1) / tpc);
-  return launch_ahead(a.scales ? read_kernel<T, true> : read_kernel<T, false>, dim3(grid), NT, 0, s, a, (int)tpc);
+  return launch_ahead(a.scales ? read_kernel<T, true> : read_kernel<T, false>, dim3(grid), NT, 0, s, 1, a, (int)tpc);
 }
 
 }  // namespace

@@ -707,7 +707,7 @@ cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   static bool done[64];
   cudaError_t e = allow_smem(paged_step<T, D, KP, C8>, smem, done);
   if (e != cudaSuccess) return e;
-  return launch_ahead(paged_step<T, D, KP, C8>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, map, a);
+  return launch_ahead(paged_step<T, D, KP, C8>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, 1, map, a);
 }
 template <typename T>
 cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, int D, cudaStream_t s) {

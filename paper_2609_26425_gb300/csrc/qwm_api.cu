@@ -61,15 +61,15 @@ bool make_page_map(CUtensorMap* m, const void* pages, int64_t blocks, int page_t
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool make_code_map(CUtensorMap* m, const void* pages, int64_t blocks, int page_tokens, int D) {
+bool make_code_map(CUtensorMap* m, const void* pages, int64_t blocks, int page_tokens, int D, int width) {
   PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
   if (!fn || blocks < 1) return false;
   cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)page_tokens, (cuuint64_t)blocks};
   cuuint64_t strides[2] = {(cuuint64_t)D, (cuuint64_t)D * page_tokens};
-  cuuint32_t box[3] = {(cuuint32_t)D, (cuuint32_t)(page_tokens < 64 ? page_tokens : 64), 1};
+  cuuint32_t box[3] = {(cuuint32_t)width, (cuuint32_t)(page_tokens < 64 ? page_tokens : 64), 1};
   cuuint32_t es[3] = {1, 1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(pages), dims, strides, box, es,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

@@ -128,7 +128,7 @@ cudaError_t go(const RopeArgs& a, cudaStream_t s) {
   if (tpc < 1) tpc = 1;
   const unsigned grid = (unsigned)((a.N + tpc - 1) / tpc);
   const size_t smem = (size_t)tpc * a.P * sizeof(float2);
-  return launch_ahead(a.pages ? rope_kernel<T, IL, true> : rope_kernel<T, IL, false>, dim3(grid), NT, smem, s, a, (int)tpc);
+  return launch_ahead(a.pages ? rope_kernel<T, IL, true> : rope_kernel<T, IL, false>, dim3(grid), NT, smem, s, 1, a, (int)tpc);
 }
 
 }  // namespace
