@@ -31,25 +31,32 @@ using namespace ptx;
 constexpr int kWarps = 8;                // consumer warps
 constexpr int NT = (kWarps + 2) * 32;    // and two producers, of K and of V
 // What a group costs a CTA beside its tiles (Queries, merge, output: about 5 K
-// cycles), in tiles' time (1.3 K cycles when all CTAs stream).
-constexpr int kGroupCost = 4;
+// cycles, and as much again where 8-bit pages have to be unpacked at the mask's edges),
+// in tiles' time (1.3 K cycles when all CTAs stream).  Of 8-bit pages, 32 sequences of 100
+// to 30000 keys x 8 heads, window 8192: 52 us with 4, 45.4 with 6, 44.5 with 8, 50.6 with 14.
+template <bool C8>
+constexpr int group_cost() { return C8 ? 8 : 4; }
 
 // KP 16-key groups of a warp.  A tile's chain of products, exponentials and
 // products takes as long for two groups as for one, so two where the chain bounds
 // (64 channels; whole groups), one where HBM does and finer slots keep it busier
 // (128 channels on the line: 131071 keys 86 us with one, 91 with two; 517 keys x 12
 // whole groups 8.9 and 7.6; all four with one producer warp for K and V).
-// Of 8-bit pages two groups as well: a tile is half the bytes, and its chain the same.
-template <int D, int KP_, bool C8>
+// Of 8-bit pages two groups as well: a tile is half the bytes, and its chain the same
+// (131071 keys 56 us, with one 69).
+// N8: at most 8 rows, which are the N side of the products then.
+template <int D, int KP_, bool C8, bool N8>
 struct Shape {
+  static_assert(C8 || !N8, "");
   static constexpr int KP = KP_;
   static constexpr int TK = 64 * KP;                           // keys per tile
   static constexpr int SLOT = TK * D * (C8 ? 1 : 2);           // bytes of a K or V tile
-  static constexpr int NS = SLOT == 32768 ? 4 : 8;             // slots of the ring: K, V, K, V, ...
+  static constexpr int NS = C8 ? 131072 / SLOT : (SLOT == 32768 ? 4 : 8);   // slots of the ring: K, V, K, V, ...
   static_assert(NS % 4 == 0, "an even number of tiles: a slot belongs to one warp group");
-  static constexpr int MERGE = NS * SLOT;                      // the warps' O [warp][16][D], beside the ring so that
+  static constexpr int ROWS = N8 ? 8 : 16;
+  static constexpr int MERGE = NS * SLOT;                      // the warps' O [warp][ROWS][D], beside the ring so that
                                                                // the next group's tiles come in meanwhile
-  static constexpr int SCALES = MERGE + kWarps * 16 * D * 4;   // 8-bit pages: the tiles' scales [slot][TK]
+  static constexpr int SCALES = MERGE + kWarps * ROWS * D * 4; // 8-bit pages: the tiles' scales [slot][TK]
   static constexpr int TOTAL = SCALES + (C8 ? NS * TK * 2 : 0) + 1024;
 };
 
@@ -80,21 +87,32 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {   // a >= 0, b
   return ((a | b) >> 32) ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
 }
 
-// Codes enter the products as binary16: a lane's word of four Keys' channels is the B
+// An 8 x 8 block of 16-bit values over the warp, transposed.
+__device__ __forceinline__ uint32_t transpose8(uint32_t w) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(w));
+  return r;
+}
+
+// Codes enter the products as binary16: a lane's word of four of a Key's channels is its
 // fragment of one k16 step (the channels of a step in the order 4 tq .. 4 tq + 3 for Q and
 // K alike), a transposed word of Values two tokens' pairs of channels, which are put in
 // order before the conversion.  The Keys' scales multiply the logits, the Values' the
-// fragments (P times a scale would leave binary16's range).
-template <typename T, int D, int KP, bool C8>
+// fragments (P times a scale would leave binary16's range).  Up to 8 rows (N8) are the
+// N = 8 side, keys and channels M = 16 (S^T = K Q^T, O^T += V^T P^T): a conversion then feeds
+// half as many MMAs and no half of a fragment is idle rows (131071 keys, 8 rows: 56 us
+// against 59 with the rows as M; 32 sequences, 5 rows: 44.5 against 48; 9 to 12 rows in two
+// such blocks took 28.6 us where rows as M take 26).  More warps lost: 12 59 us, 16 76.
+template <typename T, int D, int KP, bool C8, bool N8>
 __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
-  using L = Shape<D, KP, C8>;
+  using L = Shape<D, KP, C8, N8>;
   using Op = Operand<T, C8>;
-  constexpr int NS = L::NS, TK = L::TK;
+  constexpr int NS = L::NS, TK = L::TK, ROWS = L::ROWS, kGroupCost = group_cost<C8>();
   constexpr int KS = D / 16;                       // k16 steps of Q K^T, n16 blocks of P V
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   __shared__ uint64_t bars[2 * NS];
-  __shared__ float s_ml[kWarps][16][2];
+  __shared__ float s_ml[kWarps][ROWS][2];
   __shared__ int64_t s_scan[kWarps + 2], s_first;
   __shared__ Seq s_sq;
   __shared__ Tiles s_tl;
@@ -299,7 +317,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   const int kkey = key0 + (mi >> 1) * 8 + mrow, kch = mi & 1;           // K: (keys 0-7 | 8-15) x (chunk, chunk + 1)
   const int vkey = key0 + (mi & 1) * 8 + mrow, vch = mi >> 1;           // V (and codes): the same, keys innermost
   const int maxrows = a.max_q * a.G;
-  float* so = reinterpret_cast<float*>(sm + L::MERGE);                  // [warp][16][D]
+  float* so = reinterpret_cast<float*>(sm + L::MERGE);                  // [warp][ROWS][D]
   bool ok = true;                                                       // no wait of this warp has run out
   int filled = 0;                                                       // slots of the pieces before
   do {
@@ -312,284 +330,516 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     const int64_t c0 = whole ? 0 : divide(first, share), c1 = whole ? 0 : divide(first + n - 1, share);   // its CTAs
     const int parts = (int)(c1 - c0) + 1;
     const int p0 = sq.kv - sq.qn;
-    // the fragments of mma.sync: this lane has rows g and g + 8 (index rr)
-    float o[2 * KS][4];
-    float m_run[2], l_run[2];
-    uint32_t qf[KS][4];
-    float slr[2] = {sl2, sl2};                                          // scale of a row's logits, as powers of two
-    float true_max[2] = {1.0f, 1.0f};                                   // from m_run to the rows' q k^T
-    int hi[2], lo[2];
+    if constexpr (N8) {
+      // S^T and O^T: this lane has rows 2 tq + x (index x), of keys g and g + 8 and of
+      // channels 2 g and 2 g + 1 of 16
+      float o[KS][4], m_run[2], l_run[2], slr[2];
+      uint32_t qf[KS][2];
+      int hi[2], lo[2];
 #pragma unroll
-    for (int k = 0; k < 2 * KS; ++k)
+      for (int k = 0; k < KS; ++k)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[k][e] = 0.0f;
-#pragma unroll
-    for (int rr = 0; rr < 2; ++rr) {
-      m_run[rr] = -INFINITY;
-      l_run[rr] = 0.0f;
-      const int r = rr * 8 + g;
-      const bool has = r < rows;
-      const int tok = has ? r / a.G : 0;
-      const Span sp = has ? row_span(p0 + tok, sq.kv, a.block, a.window) : Span{0, 0};
-      hi[rr] = sp.hi;
-      lo[rr] = sp.lo;
-      const T* src = static_cast<const T*>(a.q) + (sq.q0 + tok) * a.q_tok + (int64_t)(hk * a.G + (has ? r % a.G : 0)) * a.q_head;
-      if constexpr (C8) {
-        uint32_t top = 0;
+        for (int e = 0; e < 4; ++e) o[k][e] = 0.0f;
+      {
+        // Queries as B: this lane row g's channels 4 tq .. of each k16 step
+        const bool has = g < rows;
+        const int tok = has ? g / a.G : 0;
+        const T* src = static_cast<const T*>(a.q) + (sq.q0 + tok) * a.q_tok + (int64_t)(hk * a.G + (has ? g % a.G : 0)) * a.q_head;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           const uint2 w = has ? *reinterpret_cast<const uint2*>(src + ks * 16 + tq * 4) : make_uint2(0u, 0u);
-          qf[ks][rr] = w.x;
-          qf[ks][2 + rr] = w.y;
-          top = max(top, finite_max(make_uint4(w.x, w.y, 0u, 0u)));
+          qf[ks][0] = w.x;
+          qf[ks][1] = w.y;
         }
-        if (Elem<T>::bf16) {
+        int up = 0;
+        if constexpr (Elem<T>::bf16) {
+          uint32_t top = 0;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) top = max(top, finite_max(make_uint4(qf[ks][0], qf[ks][1], 0u, 0u)));
           top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
           top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-          const int up = row_power(top);
+          up = row_power(top);
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
-            qf[ks][rr] = scaled_f16(qf[ks][rr], up);
-            qf[ks][2 + rr] = scaled_f16(qf[ks][2 + rr], up);
+            qf[ks][0] = scaled_f16(qf[ks][0], up);
+            qf[ks][1] = scaled_f16(qf[ks][1], up);
           }
-          slr[rr] = row_scale(sl2, up);
-          true_max[rr] = times_pow2(1.0f, -up);
         }
-      } else {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          qf[ks][rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + tq * 2) : 0u;
-          qf[ks][2 + rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8 + tq * 2) : 0u;
+        for (int x = 0; x < 2; ++x) {
+          const int r = 2 * tq + x;
+          m_run[x] = -INFINITY;
+          l_run[x] = 0.0f;
+          slr[x] = sl2;
+          if constexpr (Elem<T>::bf16) slr[x] = row_scale(sl2, __shfl_sync(0xFFFFFFFFu, up, 4 * r));
+          const Span sp = r < rows ? row_span(p0 + r / a.G, sq.kv, a.block, a.window) : Span{0, 0};
+          hi[x] = sp.hi;
+          lo[x] = sp.lo;
         }
       }
-    }
-    // This warp group's tiles are those of its parity in the CTA's count of tiles,
-    // so that a slot of the ring is always the same group's: a group that did not
-    // wait for every use of a slot could take the phase before the one it waits
-    // for as done (a parity tells only two apart).
-    for (int t = t0 + (((filled >> 1) + wg) & 1); t < t_end && ok; t += 2) {
-      const int i = filled + 2 * (t - t0), s = i % NS;                   // slots s and s + 1
-      const int j0 = tile_at(tl, t) * TK + key0;                         // this warp's keys: j0 .. j0 + 16 KP - 1
-      if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full(s), (i / NS) & 1, a.wait_ns)))) break;
-      const uint32_t kb = smem_u32(sm) + s * L::SLOT, vb = kb + L::SLOT;
-      const bool open = all_see(tl, j0, j0 + 16 * KP, a.sinks), any = any_sees(tl, j0, j0 + 16 * KP, a.sinks);
-      uint32_t pf[KP][4];
-      // scales of this lane's keys (2 tq, 2 tq + 1) of eight, as binary16
-      auto scales_at = [&](int slot, int key) -> uint32_t {
-        return *reinterpret_cast<const uint32_t*>(sm + L::SCALES + slot * (TK * 2) + 2 * (key0 + key + tq * 2));
-      };
-      // B fragments of P V for the channels of two n8 blocks, times their scales
-      auto values = [&](int kp, int nb, uint32_t (&bf)[4]) { ldsm4t(vb + at<TK>(vkey + 16 * kp, 2 * nb + vch), bf); };
-      // of four n8 blocks (nb even): block 2 nb has the even channels of 16, 2 nb + 1 the odd ones
-      auto code_values = [&](int kp, int nb, uint32_t (&bf)[2][4]) {
-        uint32_t w[4];                               // (keys 0-7 | 8-15) x (16 channels, the next 16)
-        ldsm4t(vb + at_code<D>(vkey + 16 * kp, nb + vch), w);
-        const uint32_t s0 = scales_at(s + 1, kp * 16), s1 = scales_at(s + 1, kp * 16 + 8);
+      // (this warp group's tiles: as below)
+      for (int t = t0 + (((filled >> 1) + wg) & 1); t < t_end && ok; t += 2) {
+        const int i = filled + 2 * (t - t0), s = i % NS;                   // slots s and s + 1
+        const int j0 = tile_at(tl, t) * TK + key0;                         // this warp's keys: j0 .. j0 + 16 KP - 1
+        if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full(s), (i / NS) & 1, a.wait_ns)))) break;
+        const uint32_t kb = smem_u32(sm) + s * L::SLOT, vb = kb + L::SLOT;
+        const uint8_t* sc_k = sm + L::SCALES + s * (TK * 2) + 2 * key0;
+        const uint8_t* sc_v = sc_k + TK * 2;
+        const bool open = all_see(tl, j0, j0 + 16 * KP, a.sinks), any = any_sees(tl, j0, j0 + 16 * KP, a.sinks);
+        uint32_t pf[KP][2];
+        if (any) {
+          float sc[KP][2][4];                          // two sums each: half the chain of MMAs
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          uint32_t even, odd;
-          from_codes(__byte_perm(w[x], 0, 0x3120), even, odd);
-          bf[x >> 1][x & 1] = mul_f16x2(even, x & 1 ? s1 : s0);
-          bf[x >> 1][2 + (x & 1)] = mul_f16x2(odd, x & 1 ? s1 : s0);
-        }
-      };
-      if (any) {
-        float sc[KP][2][4];
+          for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
-        for (int kp = 0; kp < KP; ++kp)
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sc[kp][k][e] = 0.0f;
-        if constexpr (C8) {
+            for (int e = 0; e < 4; ++e) sc[kp][0][e] = sc[kp][1][e] = 0.0f;
 #pragma unroll
           for (int ks = 0; ks < KS; ks += 2)
 #pragma unroll
             for (int kp = 0; kp < KP; ++kp) {
-              uint32_t w[4];                         // (keys 0-7 | 8-15) x (step ks, ks + 1)
+              uint32_t w[4];                           // (keys 0-7 | 8-15) x (step ks, ks + 1)
               ldsm4(kb + at_code<D>(vkey + 16 * kp, ks + vch), w);
 #pragma unroll
-              for (int x = 0; x < 4; ++x) {
-                uint32_t b0, b1;
-                from_codes(w[x], b0, b1);
-                Elem<Op>::mma(sc[kp][x & 1], qf[ks + (x >> 1)], b0, b1);
+              for (int x = 0; x < 2; ++x) {
+                uint32_t af[4];
+                from_codes(w[2 * x], af[0], af[2]);
+                from_codes(w[2 * x + 1], af[1], af[3]);
+                Elem<Op>::mma(sc[kp][x], af, qf[ks + x][0], qf[ks + x][1]);
               }
             }
+          bool grow = false;
+          float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+          for (int kp = 0; kp < KP; ++kp) {
+            const float f0 = __half2float(*reinterpret_cast<const __half*>(sc_k + 2 * (kp * 16 + g)));
+            const float f1 = __half2float(*reinterpret_cast<const __half*>(sc_k + 2 * (kp * 16 + g + 8)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float& v = sc[kp][0][e];
+              v = (v + sc[kp][1][e]) * (e < 2 ? f0 : f1);
+              if (!open && !sees(j0 + kp * 16 + g + (e < 2 ? 0 : 8), lo[e & 1], hi[e & 1], a.sinks)) v = -INFINITY;
+              top[e & 1] = fmaxf(top[e & 1], v);
+            }
+          }
+          // running maximum of each row, moved only when a key of this slice is above it: the
+          // eight lanes of a row agree through three shuffles then
+          grow = top[0] > m_run[0] || top[1] > m_run[1];
+          if (__any_sync(0xFFFFFFFFu, grow)) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              float v = top[x];
+              v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 4));
+              v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 8));
+              v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 16));
+              const float mn = fmaxf(m_run[x], v);
+              const float al = mn == m_run[x] ? 1.0f : ex2f((m_run[x] - mn) * slr[x]);
+              m_run[x] = mn;
+              l_run[x] *= al;
+#pragma unroll
+              for (int k = 0; k < KS; ++k) {
+                o[k][x] *= al;
+                o[k][2 + x] *= al;
+              }
+            }
+          }
+          // a row that has seen nothing yet keeps 0 as its reference: 2^-inf = 0
+          const float mb[2] = {m_run[0] == -INFINITY ? 0.0f : m_run[0] * slr[0], m_run[1] == -INFINITY ? 0.0f : m_run[1] * slr[1]};
+#pragma unroll
+          for (int kp = 0; kp < KP; ++kp) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = ex2f(fmaf(sc[kp][0][e], slr[e & 1], -mb[e & 1]));
+            l_run[0] += v[0] + v[2];
+            l_run[1] += v[1] + v[3];
+            pf[kp][0] = transpose8(Elem<Op>::pack(v[0], v[1]));   // to B: row g, keys 2 tq and 2 tq + 1
+            pf[kp][1] = transpose8(Elem<Op>::pack(v[2], v[3]));
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(s));
+        if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full(s + 1), (i / NS) & 1, a.wait_ns)))) break;
+        // Values as A, times their scales: channels 2 g and 2 g + 1 of 16 (blocks nb and nb + 1),
+        // keys 2 tq, 2 tq + 1 and those plus 8
+        auto values = [&](int kp, int nb, uint32_t (&af)[2][4]) {
+          uint32_t w[4];                               // (keys 0-7 | 8-15) x (16 channels, the next 16)
+          ldsm4t(vb + at_code<D>(vkey + 16 * kp, nb + vch), w);
+          const uint32_t s0 = *reinterpret_cast<const uint32_t*>(sc_v + 2 * (kp * 16 + tq * 2));
+          const uint32_t s1 = *reinterpret_cast<const uint32_t*>(sc_v + 2 * (kp * 16 + 8 + tq * 2));
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            uint32_t even, odd;
+            from_codes(__byte_perm(w[x], 0, 0x3120), even, odd);
+            af[x >> 1][2 * (x & 1)] = mul_f16x2(even, x & 1 ? s1 : s0);
+            af[x >> 1][2 * (x & 1) + 1] = mul_f16x2(odd, x & 1 ? s1 : s0);
+          }
+        };
+        if (open) {
 #pragma unroll
           for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const float2 f = Elem<Op>::unpack(scales_at(s, kp * 16 + k * 8));
+            for (int nb = 0; nb < KS; nb += 2) {
+              uint32_t af[2][4];
+              values(kp, nb, af);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) sc[kp][k][e] *= e & 1 ? f.y : f.x;
+              for (int x = 0; x < 2; ++x) Elem<Op>::mma(o[nb + x], af[x], pf[kp][0], pf[kp][1]);
             }
+        } else if (any) {
+          // as below: what no row sees is cleared, what some see and others do not is taken
+          // token by token where it is not finite
+          auto keep = [&](int klo, int khi, int j) -> uint32_t {
+            return (sees(j, klo, khi, a.sinks) ? 0xFFFFu : 0u) | (sees(j + 1, klo, khi, a.sinks) ? 0xFFFF0000u : 0u);
+          };
+#pragma unroll 1
+          for (int kp = 0; kp < KP; ++kp) {
+            const int ja = j0 + kp * 16 + tq * 2;
+            const uint32_t ma = keep(tl.lo_min, tl.hi_max, ja), mb = keep(tl.lo_min, tl.hi_max, ja + 8);
+            const uint32_t b0 = kp == 0 ? pf[0][0] : pf[KP - 1][0], b1 = kp == 0 ? pf[0][1] : pf[KP - 1][1];
+            static_assert(KP <= 2, "");
+            bool odd = false;
+            if (sq.qn > 1) {
+#pragma unroll 1
+              for (int nb = 0; nb < KS; nb += 2) {
+                uint32_t af[2][4];
+                values(kp, nb, af);
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) odd |= nonfinite2<Op>(af[x][e] & (e < 2 ? ma : mb));
+              }
+              odd = __any_sync(0xFFFFFFFFu, odd);
+            }
+            const int turns = odd ? sq.qn : 1;
+            for (int tk = 0; tk < turns; ++tk) {
+              uint32_t wa = ma, wb = mb;
+              if (odd) {
+                const Span sp = row_span(p0 + tk, sq.kv, a.block, a.window);
+                wa = keep(sp.lo, sp.hi, ja);
+                wb = keep(sp.lo, sp.hi, ja + 8);
+              }
+              const bool own[2] = {!odd || (2 * tq) / a.G == tk, !odd || (2 * tq + 1) / a.G == tk};
+#pragma unroll
+              for (int nb = 0; nb < KS; nb += 2) {
+                uint32_t af[2][4];
+                values(kp, nb, af);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                  af[x][0] &= wa; af[x][1] &= wa; af[x][2] &= wb; af[x][3] &= wb;
+                  float acc[4];
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) acc[e] = o[nb + x][e];
+                  Elem<Op>::mma(acc, af[x], b0, b1);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    if (own[e & 1]) o[nb + x][e] = acc[e];
+                }
+              }
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(s + 1));
+      }
+      filled += 2 * max(0, t_end - t0);
+      if (!ok && lane == 0) record_status(a.status, QWM_ERR_TIMEOUT);
+
+      // -------------------------------------------------------- the warps' (max, sum, O) of the piece
+      named_bar_sync(1, kWarps * 32);                  // the last piece's have been read
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int r = 2 * tq + x;
+        float l = l_run[x];                            // the eight lanes of a row hold its sum in parts
+        l += __shfl_xor_sync(0xFFFFFFFFu, l, 4);
+        l += __shfl_xor_sync(0xFFFFFFFFu, l, 8);
+        l += __shfl_xor_sync(0xFFFFFFFFu, l, 16);
+        if (r >= rows) continue;
+        if (g == 0) {
+          s_ml[warp][r][0] = m_run[x] * (slr[x] / sl2);   // in the units of q k^T
+          s_ml[warp][r][1] = l;
+        }
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+          *reinterpret_cast<float2*>(so + ((warp * ROWS + r) * D + k * 16 + g * 2)) = make_float2(o[k][x], o[k][2 + x]);
+      }
+    } else {
+      // the fragments of mma.sync: this lane has rows g and g + 8 (index rr)
+      float o[2 * KS][4];
+      float m_run[2], l_run[2];
+      uint32_t qf[KS][4];
+      float slr[2] = {sl2, sl2};                                          // scale of a row's logits, as powers of two
+      float true_max[2] = {1.0f, 1.0f};                                   // from m_run to the rows' q k^T
+      int hi[2], lo[2];
+#pragma unroll
+      for (int k = 0; k < 2 * KS; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[k][e] = 0.0f;
+#pragma unroll
+      for (int rr = 0; rr < 2; ++rr) {
+        m_run[rr] = -INFINITY;
+        l_run[rr] = 0.0f;
+        const int r = rr * 8 + g;
+        const bool has = r < rows;
+        const int tok = has ? r / a.G : 0;
+        const Span sp = has ? row_span(p0 + tok, sq.kv, a.block, a.window) : Span{0, 0};
+        hi[rr] = sp.hi;
+        lo[rr] = sp.lo;
+        const T* src = static_cast<const T*>(a.q) + (sq.q0 + tok) * a.q_tok + (int64_t)(hk * a.G + (has ? r % a.G : 0)) * a.q_head;
+        if constexpr (C8) {
+          uint32_t top = 0;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            const uint2 w = has ? *reinterpret_cast<const uint2*>(src + ks * 16 + tq * 4) : make_uint2(0u, 0u);
+            qf[ks][rr] = w.x;
+            qf[ks][2 + rr] = w.y;
+            top = max(top, finite_max(make_uint4(w.x, w.y, 0u, 0u)));
+          }
+          if (Elem<T>::bf16) {
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            const int up = row_power(top);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+              qf[ks][rr] = scaled_f16(qf[ks][rr], up);
+              qf[ks][2 + rr] = scaled_f16(qf[ks][2 + rr], up);
+            }
+            slr[rr] = row_scale(sl2, up);
+            true_max[rr] = times_pow2(1.0f, -up);
+          }
         } else {
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-            for (int kp = 0; kp < KP; ++kp) {
-              uint32_t bf[4];
-              ldsm4(kb + at<TK>(kkey + 16 * kp, 2 * ks + kch), bf);
-              Elem<Op>::mma(sc[kp][0], qf[ks], bf[0], bf[1]);
-              Elem<Op>::mma(sc[kp][1], qf[ks], bf[2], bf[3]);
-            }
+          for (int ks = 0; ks < KS; ++ks) {
+            qf[ks][rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + tq * 2) : 0u;
+            qf[ks][2 + rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8 + tq * 2) : 0u;
+          }
         }
-        if (!open) {
+      }
+      // This warp group's tiles are those of its parity in the CTA's count of tiles,
+      // so that a slot of the ring is always the same group's: a group that did not
+      // wait for every use of a slot could take the phase before the one it waits
+      // for as done (a parity tells only two apart).
+      for (int t = t0 + (((filled >> 1) + wg) & 1); t < t_end && ok; t += 2) {
+        const int i = filled + 2 * (t - t0), s = i % NS;                   // slots s and s + 1
+        const int j0 = tile_at(tl, t) * TK + key0;                         // this warp's keys: j0 .. j0 + 16 KP - 1
+        if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full(s), (i / NS) & 1, a.wait_ns)))) break;
+        const uint32_t kb = smem_u32(sm) + s * L::SLOT, vb = kb + L::SLOT;
+        const bool open = all_see(tl, j0, j0 + 16 * KP, a.sinks), any = any_sees(tl, j0, j0 + 16 * KP, a.sinks);
+        uint32_t pf[KP][4];
+        // scales of this lane's keys (2 tq, 2 tq + 1) of eight, as binary16
+        auto scales_at = [&](int slot, int key) -> uint32_t {
+          return *reinterpret_cast<const uint32_t*>(sm + L::SCALES + slot * (TK * 2) + 2 * (key0 + key + tq * 2));
+        };
+        // B fragments of P V for the channels of two n8 blocks, times their scales
+        auto values = [&](int kp, int nb, uint32_t (&bf)[4]) { ldsm4t(vb + at<TK>(vkey + 16 * kp, 2 * nb + vch), bf); };
+        // of four n8 blocks (nb even): block 2 nb has the even channels of 16, 2 nb + 1 the odd ones
+        auto code_values = [&](int kp, int nb, uint32_t (&bf)[2][4]) {
+          uint32_t w[4];                               // (keys 0-7 | 8-15) x (16 channels, the next 16)
+          ldsm4t(vb + at_code<D>(vkey + 16 * kp, nb + vch), w);
+          const uint32_t s0 = scales_at(s + 1, kp * 16), s1 = scales_at(s + 1, kp * 16 + 8);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            uint32_t even, odd;
+            from_codes(__byte_perm(w[x], 0, 0x3120), even, odd);
+            bf[x >> 1][x & 1] = mul_f16x2(even, x & 1 ? s1 : s0);
+            bf[x >> 1][2 + (x & 1)] = mul_f16x2(odd, x & 1 ? s1 : s0);
+          }
+        };
+        if (any) {
+          float sc[KP][2][4];
 #pragma unroll
           for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (!sees(j0 + kp * 16 + k * 8 + tq * 2 + (e & 1), lo[e >> 1], hi[e >> 1], a.sinks)) sc[kp][k][e] = -INFINITY;
-        }
-        // running maximum of each row, moved only when a key of this slice is
-        // above it: the four lanes of a row agree through two shuffles then
-        bool grow = false;
-        float top[2];
+              for (int e = 0; e < 4; ++e) sc[kp][k][e] = 0.0f;
+          if constexpr (C8) {
 #pragma unroll
-        for (int rr = 0; rr < 2; ++rr) {
-          top[rr] = -INFINITY;
+            for (int ks = 0; ks < KS; ks += 2)
 #pragma unroll
-          for (int kp = 0; kp < KP; ++kp)
-            top[rr] = fmaxf(top[rr], fmaxf(fmaxf(sc[kp][0][2 * rr], sc[kp][0][2 * rr + 1]),
-                                           fmaxf(sc[kp][1][2 * rr], sc[kp][1][2 * rr + 1])));
-          grow |= top[rr] > m_run[rr];
-        }
-        if (__any_sync(0xFFFFFFFFu, grow)) {
+              for (int kp = 0; kp < KP; ++kp) {
+                uint32_t w[4];                         // (keys 0-7 | 8-15) x (step ks, ks + 1)
+                ldsm4(kb + at_code<D>(vkey + 16 * kp, ks + vch), w);
 #pragma unroll
-          for (int rr = 0; rr < 2; ++rr) {
-            float v = top[rr];
-            v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
-            v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
-            const float mn = fmaxf(m_run[rr], v);
-            const float al = mn == m_run[rr] ? 1.0f : ex2f((m_run[rr] - mn) * slr[rr]);
-            m_run[rr] = mn;
-            l_run[rr] *= al;
+                for (int x = 0; x < 4; ++x) {
+                  uint32_t b0, b1;
+                  from_codes(w[x], b0, b1);
+                  Elem<Op>::mma(sc[kp][x & 1], qf[ks + (x >> 1)], b0, b1);
+                }
+              }
 #pragma unroll
-            for (int k = 0; k < 2 * KS; ++k) {
-              o[k][2 * rr] *= al;
-              o[k][2 * rr + 1] *= al;
-            }
+            for (int kp = 0; kp < KP; ++kp)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const float2 f = Elem<Op>::unpack(scales_at(s, kp * 16 + k * 8));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[kp][k][e] *= e & 1 ? f.y : f.x;
+              }
+          } else {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+              for (int kp = 0; kp < KP; ++kp) {
+                uint32_t bf[4];
+                ldsm4(kb + at<TK>(kkey + 16 * kp, 2 * ks + kch), bf);
+                Elem<Op>::mma(sc[kp][0], qf[ks], bf[0], bf[1]);
+                Elem<Op>::mma(sc[kp][1], qf[ks], bf[2], bf[3]);
+              }
           }
-        }
-        // a row that has seen nothing yet keeps 0 as its reference: 2^-inf = 0
-        const float mb0 = m_run[0] == -INFINITY ? 0.0f : m_run[0] * slr[0];
-        const float mb1 = m_run[1] == -INFINITY ? 0.0f : m_run[1] * slr[1];
+          if (!open) {
 #pragma unroll
-        for (int kp = 0; kp < KP; ++kp)
+            for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float v0 = ex2f(fmaf(sc[kp][k][0], slr[0], -mb0)), v1 = ex2f(fmaf(sc[kp][k][1], slr[0], -mb0));
-            const float w0 = ex2f(fmaf(sc[kp][k][2], slr[1], -mb1)), w1 = ex2f(fmaf(sc[kp][k][3], slr[1], -mb1));
-            l_run[0] += v0 + v1;
-            l_run[1] += w0 + w1;
-            pf[kp][2 * k] = Elem<Op>::pack(v0, v1);
-            pf[kp][2 * k + 1] = Elem<Op>::pack(w0, w1);
-          }
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(empty(s));
-      if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full(s + 1), (i / NS) & 1, a.wait_ns)))) break;
-      if (open) {
-#pragma unroll
-        for (int kp = 0; kp < KP; ++kp)
-#pragma unroll
-          for (int nb = 0; nb < KS; nb += C8 ? 2 : 1) {
-            uint32_t bf[2][4];
-            if constexpr (C8) code_values(kp, nb, bf);
-            else values(kp, nb, bf[0]);
-#pragma unroll
-            for (int x = 0; x < (C8 ? 2 : 1); ++x) {
-              Elem<Op>::mma(o[2 * (nb + x)], pf[kp], bf[x][0], bf[x][1]);
-              Elem<Op>::mma(o[2 * (nb + x) + 1], pf[kp], bf[x][2], bf[x][3]);
-            }
-          }
-      } else if (any) {
-        // Keys that no row sees may hold anything (0 x inf is not 0): their
-        // Values are cleared in the fragments.  Keys that some rows see and
-        // others do not (drafts of several tokens): if one holds an infinity
-        // or a NaN, the product is taken token by token and only that
-        // token's rows keep it.
-        auto keep = [&](int klo, int khi, int j) -> uint32_t {
-          return (sees(j, klo, khi, a.sinks) ? 0xFFFFu : 0u) | (sees(j + 1, klo, khi, a.sinks) ? 0xFFFF0000u : 0u);
-        };
-#pragma unroll
-        for (int kp = 0; kp < KP; ++kp) {
-          const int ja = j0 + kp * 16 + tq * 2;
-          const uint32_t ma = keep(tl.lo_min, tl.hi_max, ja), mb = keep(tl.lo_min, tl.hi_max, ja + 8);
-          bool odd = false;
-          if (sq.qn > 1) {
-#pragma unroll
-            for (int nb = 0; nb < KS; nb += C8 ? 2 : 1) {
-              uint32_t bf[2][4];
-              if constexpr (C8) code_values(kp, nb, bf);
-              else values(kp, nb, bf[0]);
-#pragma unroll
-              for (int x = 0; x < (C8 ? 2 : 1); ++x)
-                odd |= nonfinite2<Op>(bf[x][0] & ma) || nonfinite2<Op>(bf[x][1] & mb) || nonfinite2<Op>(bf[x][2] & ma) ||
-                       nonfinite2<Op>(bf[x][3] & mb);
-            }
-            odd = __any_sync(0xFFFFFFFFu, odd);
-          }
-          const int turns = odd ? sq.qn : 1;
-          for (int tk = 0; tk < turns; ++tk) {
-            uint32_t wa = ma, wb = mb;
-            bool own[2];
-#pragma unroll
-            for (int rr = 0; rr < 2; ++rr) own[rr] = !odd || (rr * 8 + g) / a.G == tk;
-            if (odd) {
-              const Span sp = row_span(p0 + tk, sq.kv, a.block, a.window);
-              wa = keep(sp.lo, sp.hi, ja);
-              wb = keep(sp.lo, sp.hi, ja + 8);
-            }
-#pragma unroll
-            for (int nb = 0; nb < KS; nb += C8 ? 2 : 1) {
-              uint32_t bf[2][4];
-              if constexpr (C8) code_values(kp, nb, bf);
-              else values(kp, nb, bf[0]);
-#pragma unroll
-              for (int k = 0; k < (C8 ? 4 : 2); ++k) {
-                float acc[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = o[2 * nb + k][e];
-                Elem<Op>::mma(acc, pf[kp], bf[k >> 1][2 * (k & 1)] & wa, bf[k >> 1][2 * (k & 1) + 1] & wb);
+              for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                  if (own[e >> 1]) o[2 * nb + k][e] = acc[e];
+                  if (!sees(j0 + kp * 16 + k * 8 + tq * 2 + (e & 1), lo[e >> 1], hi[e >> 1], a.sinks)) sc[kp][k][e] = -INFINITY;
+          }
+          // running maximum of each row, moved only when a key of this slice is
+          // above it: the four lanes of a row agree through two shuffles then
+          bool grow = false;
+          float top[2];
+#pragma unroll
+          for (int rr = 0; rr < 2; ++rr) {
+            top[rr] = -INFINITY;
+#pragma unroll
+            for (int kp = 0; kp < KP; ++kp)
+              top[rr] = fmaxf(top[rr], fmaxf(fmaxf(sc[kp][0][2 * rr], sc[kp][0][2 * rr + 1]),
+                                             fmaxf(sc[kp][1][2 * rr], sc[kp][1][2 * rr + 1])));
+            grow |= top[rr] > m_run[rr];
+          }
+          if (__any_sync(0xFFFFFFFFu, grow)) {
+#pragma unroll
+            for (int rr = 0; rr < 2; ++rr) {
+              float v = top[rr];
+              v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
+              v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
+              const float mn = fmaxf(m_run[rr], v);
+              const float al = mn == m_run[rr] ? 1.0f : ex2f((m_run[rr] - mn) * slr[rr]);
+              m_run[rr] = mn;
+              l_run[rr] *= al;
+#pragma unroll
+              for (int k = 0; k < 2 * KS; ++k) {
+                o[k][2 * rr] *= al;
+                o[k][2 * rr + 1] *= al;
+              }
+            }
+          }
+          // a row that has seen nothing yet keeps 0 as its reference: 2^-inf = 0
+          const float mb0 = m_run[0] == -INFINITY ? 0.0f : m_run[0] * slr[0];
+          const float mb1 = m_run[1] == -INFINITY ? 0.0f : m_run[1] * slr[1];
+#pragma unroll
+          for (int kp = 0; kp < KP; ++kp)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const float v0 = ex2f(fmaf(sc[kp][k][0], slr[0], -mb0)), v1 = ex2f(fmaf(sc[kp][k][1], slr[0], -mb0));
+              const float w0 = ex2f(fmaf(sc[kp][k][2], slr[1], -mb1)), w1 = ex2f(fmaf(sc[kp][k][3], slr[1], -mb1));
+              l_run[0] += v0 + v1;
+              l_run[1] += w0 + w1;
+              pf[kp][2 * k] = Elem<Op>::pack(v0, v1);
+              pf[kp][2 * k + 1] = Elem<Op>::pack(w0, w1);
+            }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(s));
+        if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full(s + 1), (i / NS) & 1, a.wait_ns)))) break;
+        if (open) {
+#pragma unroll
+          for (int kp = 0; kp < KP; ++kp)
+#pragma unroll
+            for (int nb = 0; nb < KS; nb += C8 ? 2 : 1) {
+              uint32_t bf[2][4];
+              if constexpr (C8) code_values(kp, nb, bf);
+              else values(kp, nb, bf[0]);
+#pragma unroll
+              for (int x = 0; x < (C8 ? 2 : 1); ++x) {
+                Elem<Op>::mma(o[2 * (nb + x)], pf[kp], bf[x][0], bf[x][1]);
+                Elem<Op>::mma(o[2 * (nb + x) + 1], pf[kp], bf[x][2], bf[x][3]);
+              }
+            }
+        } else if (any) {
+          // Keys that no row sees may hold anything (0 x inf is not 0): their
+          // Values are cleared in the fragments.  Keys that some rows see and
+          // others do not (drafts of several tokens): if one holds an infinity
+          // or a NaN, the product is taken token by token and only that
+          // token's rows keep it.
+          auto keep = [&](int klo, int khi, int j) -> uint32_t {
+            return (sees(j, klo, khi, a.sinks) ? 0xFFFFu : 0u) | (sees(j + 1, klo, khi, a.sinks) ? 0xFFFF0000u : 0u);
+          };
+#pragma unroll
+          for (int kp = 0; kp < KP; ++kp) {
+            const int ja = j0 + kp * 16 + tq * 2;
+            const uint32_t ma = keep(tl.lo_min, tl.hi_max, ja), mb = keep(tl.lo_min, tl.hi_max, ja + 8);
+            bool odd = false;
+            if (sq.qn > 1) {
+#pragma unroll
+              for (int nb = 0; nb < KS; nb += C8 ? 2 : 1) {
+                uint32_t bf[2][4];
+                if constexpr (C8) code_values(kp, nb, bf);
+                else values(kp, nb, bf[0]);
+#pragma unroll
+                for (int x = 0; x < (C8 ? 2 : 1); ++x)
+                  odd |= nonfinite2<Op>(bf[x][0] & ma) || nonfinite2<Op>(bf[x][1] & mb) || nonfinite2<Op>(bf[x][2] & ma) ||
+                         nonfinite2<Op>(bf[x][3] & mb);
+              }
+              odd = __any_sync(0xFFFFFFFFu, odd);
+            }
+            const int turns = odd ? sq.qn : 1;
+            for (int tk = 0; tk < turns; ++tk) {
+              uint32_t wa = ma, wb = mb;
+              bool own[2];
+#pragma unroll
+              for (int rr = 0; rr < 2; ++rr) own[rr] = !odd || (rr * 8 + g) / a.G == tk;
+              if (odd) {
+                const Span sp = row_span(p0 + tk, sq.kv, a.block, a.window);
+                wa = keep(sp.lo, sp.hi, ja);
+                wb = keep(sp.lo, sp.hi, ja + 8);
+              }
+#pragma unroll
+              for (int nb = 0; nb < KS; nb += C8 ? 2 : 1) {
+                uint32_t bf[2][4];
+                if constexpr (C8) code_values(kp, nb, bf);
+                else values(kp, nb, bf[0]);
+#pragma unroll
+                for (int k = 0; k < (C8 ? 4 : 2); ++k) {
+                  float acc[4];
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) acc[e] = o[2 * nb + k][e];
+                  Elem<Op>::mma(acc, pf[kp], bf[k >> 1][2 * (k & 1)] & wa, bf[k >> 1][2 * (k & 1) + 1] & wb);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    if (own[e >> 1]) o[2 * nb + k][e] = acc[e];
+                }
               }
             }
           }
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(s + 1));
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(empty(s + 1));
-    }
-    filled += 2 * max(0, t_end - t0);
-    if (!ok && lane == 0) record_status(a.status, QWM_ERR_TIMEOUT);
+      filled += 2 * max(0, t_end - t0);
+      if (!ok && lane == 0) record_status(a.status, QWM_ERR_TIMEOUT);
 
-    // -------------------------------------------------------- the warps' (max, sum, O) of the piece
-    named_bar_sync(1, kWarps * 32);                  // the last piece's have been read
+      // -------------------------------------------------------- the warps' (max, sum, O) of the piece
+      named_bar_sync(1, kWarps * 32);                  // the last piece's have been read
 #pragma unroll
-    for (int rr = 0; rr < 2; ++rr) {
-      const int r = rr * 8 + g;
-      float l = l_run[rr];                           // the four lanes of a row hold its sum in parts
-      l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
-      l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
-      if (r >= rows) continue;
-      if (tq == 0) {
-        s_ml[warp][r][0] = C8 ? m_run[rr] * true_max[rr] : m_run[rr];
-        s_ml[warp][r][1] = l;
-      }
-      if constexpr (C8) {
+      for (int rr = 0; rr < 2; ++rr) {
+        const int r = rr * 8 + g;
+        float l = l_run[rr];                           // the four lanes of a row hold its sum in parts
+        l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
+        l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
+        if (r >= rows) continue;
+        if (tq == 0) {
+          s_ml[warp][r][0] = C8 ? m_run[rr] * true_max[rr] : m_run[rr];
+          s_ml[warp][r][1] = l;
+        }
+        if constexpr (C8) {
 #pragma unroll
-        for (int k = 0; k < 2 * KS; k += 2)
-          *reinterpret_cast<float4*>(so + ((warp * 16 + r) * D + k * 8 + tq * 4)) =
-              make_float4(o[k][2 * rr], o[k + 1][2 * rr], o[k][2 * rr + 1], o[k + 1][2 * rr + 1]);
-      } else {
+          for (int k = 0; k < 2 * KS; k += 2)
+            *reinterpret_cast<float4*>(so + ((warp * ROWS + r) * D + k * 8 + tq * 4)) =
+                make_float4(o[k][2 * rr], o[k + 1][2 * rr], o[k][2 * rr + 1], o[k + 1][2 * rr + 1]);
+        } else {
 #pragma unroll
-        for (int k = 0; k < 2 * KS; ++k)
-          *reinterpret_cast<float2*>(so + ((warp * 16 + r) * D + k * 8 + tq * 2)) = make_float2(o[k][2 * rr], o[k][2 * rr + 1]);
+          for (int k = 0; k < 2 * KS; ++k)
+            *reinterpret_cast<float2*>(so + ((warp * ROWS + r) * D + k * 8 + tq * 2)) = make_float2(o[k][2 * rr], o[k][2 * rr + 1]);
+        }
       }
     }
     named_bar_sync(1, kWarps * 32);
@@ -610,7 +860,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
 #pragma unroll 4
       for (int w = 0; w < count; ++w) {
         const float f = ex2f((s_ml[w][r][0] - ref) * sl2);
-        const float4 x = *reinterpret_cast<const float4*>(so + ((w * 16 + r) * D + 4 * c));
+        const float4 x = *reinterpret_cast<const float4*>(so + ((w * ROWS + r) * D + 4 * c));
         l = fmaf(s_ml[w][r][1], f, l);
         v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
       }
@@ -680,7 +930,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       if (slices == 1) {
         emit(r, c, m, l, v);
       } else {
-        *reinterpret_cast<float4*>(so + ((sl * 16 + r) * D + 4 * c)) = v;
+        *reinterpret_cast<float4*>(so + ((sl * ROWS + r) * D + 4 * c)) = v;
         if (c == 0) {
           s_ml[sl][r][0] = m;
           s_ml[sl][r][1] = l;
@@ -701,19 +951,20 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   } while (next_group());
 }
 
-template <typename T, int D, int KP, bool C8>
+template <typename T, int D, int KP, bool C8, bool N8>
 cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
-  constexpr int smem = Shape<D, KP, C8>::TOTAL;
+  constexpr int smem = Shape<D, KP, C8, N8>::TOTAL;
   static bool done[64];
-  cudaError_t e = allow_smem(paged_step<T, D, KP, C8>, smem, done);
+  cudaError_t e = allow_smem(paged_step<T, D, KP, C8, N8>, smem, done);
   if (e != cudaSuccess) return e;
-  return launch_ahead(paged_step<T, D, KP, C8>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, 1, map, a);
+  return launch_ahead(paged_step<T, D, KP, C8, N8>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, 1,
+                      map, a);
 }
-template <typename T>
-cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, int D, cudaStream_t s) {
-  if (a.scales) return D == 64 ? go<T, 64, 2, true>(a, map, s) : go<T, 128, 2, true>(a, map, s);
-  if (D == 64) return go<T, 64, 2, false>(a, map, s);
-  return a.nsplit > 1 ? go<T, 128, 1, false>(a, map, s) : go<T, 128, 2, false>(a, map, s);
+template <typename T, int D>
+cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
+  if (a.scales) return (int64_t)a.max_q * a.G <= 8 ? go<T, D, 2, true, true>(a, map, s) : go<T, D, 2, true, false>(a, map, s);
+  if (D == 64) return go<T, D, 2, false, false>(a, map, s);
+  return a.nsplit > 1 ? go<T, D, 1, false, false>(a, map, s) : go<T, D, 2, false, false>(a, map, s);
 }
 
 }  // namespace
@@ -740,11 +991,11 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
   const double stream = p.groups < nsm ? hbm * p.groups / nsm : hbm;
   const double each = stream > chain ? stream : chain;
   const double whole = (double)((p.groups + nsm - 1) / nsm) * ((D == 128 ? 4.0 : 2.8) + tiles * each);
-  const double shared = (D == 128 ? 8.2 : 7.6) + (D == 128 ? 0.44 : 0.33) * (double)(tiles + kGroupCost) * p.groups / nsm;
+  const double shared = (D == 128 ? 8.2 : 7.6) + (D == 128 ? 0.44 : 0.33) * (double)(tiles + group_cost<false>()) * p.groups / nsm;
   if (split && (tiles > 40 || whole > shared) && p.groups <= QWM_PAGED_COUNTER_BYTES / 4) {
     // a CTA per SM, or as many as have min_tiles places each
     const int tk = D == 128 && !codes ? 64 : 128;
-    const int64_t places = ((max_visible + tk - 1) / tk + 1 + kGroupCost) * p.groups;
+    const int64_t places = ((max_visible + tk - 1) / tk + 1 + (codes ? group_cost<true>() : group_cost<false>())) * p.groups;
     const int64_t want = (places + p.min_tiles - 1) / p.min_tiles;
     p.nsplit = (int)(want < nsm ? want : nsm);
   }
@@ -752,8 +1003,8 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
 }
 
 cudaError_t launch_paged_step(const PagedArgs& a, const CUtensorMap& map, int D, int dtype, cudaStream_t s) {
-  if (dtype == QWM_F16) return pick<__half>(a, map, D, s);
-  return pick<__nv_bfloat16>(a, map, D, s);
+  if (dtype == QWM_F16) return D == 64 ? pick<__half, 64>(a, map, s) : pick<__half, 128>(a, map, s);
+  return D == 64 ? pick<__nv_bfloat16, 64>(a, map, s) : pick<__nv_bfloat16, 128>(a, map, s);
 }
 
 }  // namespace qwm
