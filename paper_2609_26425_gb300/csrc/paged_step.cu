@@ -254,12 +254,14 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
 
   if (warp >= kWarps) {
     // ---------------------------------------------------------- producers of K and V
-    // lane = box * 2 + channel half; a box is the part of a page (at most 64 tokens
-    // of it) that lies in the tile.  Boxes that no row sees are not read.
+    // lane = box * 2 + channel half (of codes: box); a box is the part of a page (at most 64
+    // tokens of it) that lies in the tile.  Boxes that no row sees are not read.  The table
+    // is read for as many tiles at once as there are lanes for their boxes, while those
+    // before are sent: with a lookup for each tile its latency set the pace of short tiles.
     const int kv = warp - kWarps;
-    const int box_log2 = min(a.page_log2, 6);
-    const int box = lane >> 1, half = lane & 1;
-    const bool mine = box < (TK >> box_log2) && half * 64 < D && !(C8 && half);
+    const int box_log2 = min(a.page_log2, 6), boxes = TK >> box_log2, per = 32 / boxes;
+    const int box = C8 ? lane : lane >> 1, half = C8 ? 0 : lane & 1;
+    const bool mine = box < boxes && half * 64 < D;
     const uint32_t dst = smem_u32(sm) + (C8 ? (box << box_log2) * D : half * (TK * 128) + ((box << box_log2) * 128));
     const uint32_t sdst = smem_u32(sm) + L::SCALES + ((box << box_log2) * 2);
     const uint32_t box_bytes = (C8 ? D + 2u : 128u) << box_log2;
@@ -269,21 +271,29 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       piece();
       t1 = min(t1, tl.n);
       const int32_t* trow = a.table + (int64_t)b * a.table_stride;
-      auto page_of = [&](int t, bool& want) -> int {
-        const int j0 = tile_at(tl, t) * TK + (box << box_log2);
-        want = mine && any_sees(tl, j0, j0 + (1 << box_log2), a.sinks);
+      // this lane's entry: box lane % boxes of tile t + lane / boxes
+      auto ask = [&](int t, bool& want) -> int {
+        t += lane / boxes;
+        const int j0 = tile_at(tl, t) * TK + ((lane % boxes) << box_log2);
+        want = t < t1 && any_sees(tl, j0, j0 + (1 << box_log2), a.sinks);
         return want ? trow[j0 >> a.page_log2] : 0;
       };
-      bool want = false;
-      int page = t0 < t1 ? page_of(t0, want) : 0;
-      for (int t = t0; t < t1 && !a.idle; ++t) {
-        bool want_n = false;
-        int page_n = 0;
-        if (t + 1 < t1) page_n = page_of(t + 1, want_n);   // its latency runs beside the copies
-        if (want && (page < 0 || page >= a.num_pages)) {   // not followed: the first page in its place
-          record_status(a.status, QWM_ERR_INVALID_ARG);
-          page = 0;
+      bool wants = false, wants_n = false;
+      int pages = 0, pages_n = t0 < t1 ? ask(t0, wants_n) : 0, at = per;
+      for (int t = t0; t < t1 && !a.idle; ++t, ++at) {
+        if (at == per) {
+          at = 0;
+          wants = wants_n;
+          pages = pages_n;
+          pages_n = ask(t + per, wants_n);
+          if (wants && (pages < 0 || pages >= a.num_pages)) {   // not followed: the first page in its place
+            record_status(a.status, QWM_ERR_INVALID_ARG);
+            pages = 0;
+          }
         }
+        const int src = at * boxes + box;          // (< 32 where mine)
+        const int page = __shfl_sync(0xFFFFFFFFu, pages, src & 31);
+        const bool want = __shfl_sync(0xFFFFFFFFu, (int)wants, src & 31) && mine;
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, want)) * box_bytes;
         const int y = (tile_at(tl, t) * TK + (box << box_log2)) & ((1 << a.page_log2) - 1);
         const int s = (2 * i + kv) % NS;
@@ -297,8 +307,6 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         }
         __syncwarp();
         ++i;
-        page = page_n;
-        want = want_n;
       }
     } while (ok && next_group());
     if (!ok && lane == 0) record_status(a.status, QWM_ERR_TIMEOUT);
