@@ -899,11 +899,13 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     auto place = [&](int p) { return (2 * (c0 + p) + (p == 0 ? 1 : 0)) * maxrows; };
     // A warp takes whole rows (where there are fewer rows than warps and more
     // parts than a warp has in flight, the warps share a row's parts out), a lane
-    // four channels.
+    // four channels.  Of 8-bit pages the warps always share: one trip to memory for
+    // ten parts (16384 keys x 8 heads, joins of 19 parts: 16.8 us a call with 20 parts in flight
+    // and one warp a row, 14.9).
     constexpr int LPR = D / 4, RPW = 32 / LPR;        // lanes per row, rows per warp at a time
-    constexpr int PU = 20;                            // parts in flight
+    constexpr int PU = C8 ? 10 : 20;                  // parts in flight
     const int rr = (rows + RPW - 1) / RPW;
-    const int slices = rr > 4 || parts <= PU ? 1 : (rr > 2 ? 2 : (rr > 1 ? 4 : 8)), sl = warp % slices;
+    const int slices = rr > 4 || parts <= (C8 ? 2 : PU) ? 1 : (rr > 2 ? 2 : (rr > 1 ? 4 : 8)), sl = warp % slices;
     const int q0 = parts * sl / slices, q1 = parts * (sl + 1) / slices;
     for (int rb = (warp / slices) * RPW; rb < rows; rb += (kWarps / slices) * RPW) {
       const int r = rb + lane / LPR, c = lane % LPR;
