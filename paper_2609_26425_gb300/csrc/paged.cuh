@@ -74,6 +74,8 @@ struct PagedArgs {
   // min_tiles tiles; step: nsplit CTAs share the line of all tiles, at least
   // min_tiles places each.  nsplit 1: no split
   int32_t nsplit, min_tiles;
+  int32_t whole, rtiles;                 // chunk: >= 0: groups in one line, of which so many first ones are not cut;
+                                         // row tiles of a sequence and head
   float* part_o;                         // chunk [group][nsplit][D / 4][row][4]; step [CTA][2][row][D]
   float2* part_ml;                       // running (max, sum): chunk [group][nsplit][row], the maximum as the
                                          // power that P is taken against; step [CTA][2][row]
@@ -86,6 +88,7 @@ struct PagedPlan {
   int32_t groups;    // (sequence, head, row tile) triples of the grid
   int32_t rows;      // rows of a group
   int32_t nsplit, min_tiles;
+  int32_t whole;     // chunk: groups not cut (-1: none, or all if nsplit is 1)
 };
 PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split, bool codes);
 PagedPlan plan_chunk(int B, int Hk, int D, int64_t rows, int64_t max_visible, int nsm, bool split, bool codes);
@@ -363,20 +366,25 @@ template <typename T, bool C8>
 using Operand = typename OperandOf<T, C8>::type;
 
 // bf16 Queries as binary16: a row is taken times the power of two that brings its largest
-// finite magnitude to [2^14, 2^15), and its logits' scale by the inverse.  Exact but for
-// elements 2^-29 and less of the largest, which round to a multiple of 2^-39 of it.
+// finite magnitude to [2^14, 2^15) (2^127 at the most), and its logits' scale by the inverse.
+// Exact but for elements 2^-29 and less of the largest, which round to a multiple of 2^-39 of
+// it (rows below 2^-113: of 2^-152).
 // The largest magnitude's bits of eight elements, infinities and NaN left out.
 __device__ __forceinline__ uint32_t finite_max(uint4 v) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t top = 0;
+  const uint32_t w[4] = {v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu, v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu};
+  const uint32_t both = ptx::vmax_u16x2(ptx::vmax_u16x2(w[0], w[1]), ptx::vmax_u16x2(w[2], w[3]));
+  uint32_t top = max(both & 0xFFFFu, both >> 16);
+  if (top >= 0x7F80u) {
+    top = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t lo = w[k] & 0x7FFFu, hi = (w[k] >> 16) & 0x7FFFu;
-    top = max(top, max(lo < 0x7F80u ? lo : 0u, hi < 0x7F80u ? hi : 0u));
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t lo = w[k] & 0x7FFFu, hi = w[k] >> 16;
+      top = max(top, max(lo < 0x7F80u ? lo : 0u, hi < 0x7F80u ? hi : 0u));
+    }
   }
   return top;
 }
-__device__ __forceinline__ int row_power(uint32_t top) { return 14 + 127 - max((int)(top >> 7), 1); }   // -113 .. 140
+__device__ __forceinline__ int row_power(uint32_t top) { return min(14 + 127 - (int)(top >> 7), 127); }   // -113 .. 127
 // x 2^up in two steps, each a normal number
 __device__ __forceinline__ float times_pow2(float x, int up) {
   const int h = up >> 1;
@@ -384,7 +392,8 @@ __device__ __forceinline__ float times_pow2(float x, int up) {
 }
 __device__ __forceinline__ uint32_t scaled_f16(uint32_t w, int up) {
   const float2 f = Elem<__nv_bfloat16>::unpack(w);
-  return Elem<__half>::pack(times_pow2(f.x, up), times_pow2(f.y, up));
+  const float s = __uint_as_float((uint32_t)(127 + up) << 23);
+  return Elem<__half>::pack(f.x * s, f.y * s);
 }
 __device__ __forceinline__ uint4 scaled_f16(uint4 v, int up) {
   return make_uint4(scaled_f16(v.x, up), scaled_f16(v.y, up), scaled_f16(v.z, up), scaled_f16(v.w, up));

@@ -242,7 +242,7 @@ struct Carve {
 };
 Carve carve(const PagedPlan& p, int D) {
   Carve w{};
-  const size_t rows = (size_t)(p.step ? 2 : p.groups) * p.nsplit * p.rows;
+  const size_t rows = (size_t)(p.step ? 2 : p.groups - (p.whole > 0 ? p.whole : 0)) * p.nsplit * p.rows;
   w.ml = QWM_PAGED_COUNTER_BYTES;
   w.o = w.ml + (rows * 8 + 255) / 256 * 256;
   w.total = w.o + rows * D * 4;
@@ -443,6 +443,7 @@ qwm_status qwm_paged_attend(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   a.idle = c->idle_role == QWM_ROLE_PAGE_LOADS;
   a.nsplit = p.nsplit;
   a.min_tiles = p.nsplit > 1 ? p.min_tiles : 1 << 24;
+  a.whole = p.step ? -1 : p.whole;
   if (p.nsplit > 1) {
     const Carve w = carve(p, D);
     uint8_t* ws = static_cast<uint8_t*>(workspace);

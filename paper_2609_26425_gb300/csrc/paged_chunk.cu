@@ -264,12 +264,27 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
     fence_mbar_init();
   }
   grid_begin();
-  const int b = blockIdx.z, hk = blockIdx.y;
-  const int gx = PAIR ? blockIdx.x >> 1 : blockIdx.x, rtiles = (PAIR ? gridDim.x >> 1 : gridDim.x) / a.nsplit;
-  // the row tiles with the most keys first
-  const int rt = rtiles - 1 - gx % rtiles, part = gx / rtiles;
+  int b = blockIdx.z, hk = blockIdx.y;
+  const int gx = PAIR ? blockIdx.x >> 1 : blockIdx.x;
+  int rtiles, rt, part, nsplit = a.nsplit, cut;         // cut: the group's number among those in parts
+  if (C8 && a.whole >= 0) {
+    // groups in one line: the first `whole` of them as they are, the others in parts
+    rtiles = a.rtiles;
+    const int y = gx - a.whole, group = y < 0 ? gx : a.whole + y / nsplit;
+    part = y < 0 ? 0 : y % nsplit;
+    if (y < 0) nsplit = 1;
+    cut = group - a.whole;
+    rt = rtiles - 1 - group % rtiles;
+    b = group / rtiles / a.Hk;
+    hk = group / rtiles % a.Hk;
+  } else {
+    rtiles = (PAIR ? gridDim.x >> 1 : gridDim.x) / nsplit;
+    rt = rtiles - 1 - gx % rtiles;                      // the row tiles with the most keys first
+    part = gx / rtiles;
+    cut = (b * a.Hk + hk) * rtiles + rt;
+  }
   Seq sq;
-  if (!load_seq(a, b, sq) && blockIdx.x == 0 && hk == 0 && tid == 0) record_status(a.status, QWM_ERR_INVALID_ARG);
+  if (!load_seq(a, b, sq) && rt == rtiles - 1 && part == 0 && hk == 0 && tid == 0) record_status(a.status, QWM_ERR_INVALID_ARG);
   const int64_t rows = (int64_t)sq.qn * a.G;
   const int64_t r0 = (int64_t)rt * L::GR;
   if (r0 >= rows) return;
@@ -283,7 +298,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
   const uint32_t G = (uint32_t)a.G, remA = (uint32_t)(r0 - (int64_t)tokA * a.G);
   const int tokB = tokA + (int)((remA + (uint32_t)nrow - 1) / G);
   const Tiles tl = make_tiles<TK>(p0 + tokA, p0 + tokB, sq.kv, a.block, a.window, a.sinks);
-  const int per = max((tl.n + a.nsplit - 1) / a.nsplit, a.min_tiles);
+  const int per = nsplit == 1 ? max(tl.n, 1) : max((tl.n + nsplit - 1) / nsplit, a.min_tiles);
   const int parts = max(1, (tl.n + per - 1) / per);
   if (part >= parts) return;
   const int t0 = part * per, n = max(0, min(tl.n, t0 + per) - t0);   // this part's tiles: t0 .. t0 + n - 1
@@ -301,41 +316,54 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
       tmem_relinquish();
     }
   }
+  if constexpr (PAIR) {
+    tc_fence_before();
+    cluster_arrive();                                 // this CTA's barriers and TMEM are there
+  }
   int q_up = 0;                                       // 8-bit pages: this thread's row was taken times 2^q_up
   if (warp < W_MMA && (warp >> 2) < nqt) {
     const int i = warp >> 2;
-    // Q_i: each warp its 32 rows, a row's 16-byte chunks over neighbouring lanes
+    // Q_i: each warp its 32 rows, a row's 16-byte chunks over neighbouring lanes, RPK rows a load
     uint8_t* sQ = sm + L::Q + i * NB * BLK;
-    constexpr int CH = D / 8;
+    constexpr int CH = D / 8, RPK = 32 / CH;
+    uint4 v[CH];
     {
-      uint4 v[CH];
+      const int rr0 = (warp & 3) * 32 + lane / CH;
+      const uint32_t r = remA + row_at(i) + rr0, step_t = RPK / G, step_g = RPK % G;
+      uint32_t t = r / G, g = r % G;
 #pragma unroll
       for (int k = 0; k < CH; ++k) {
-        const int idx = k * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
-        const uint32_t r = remA + min(row_at(i) + rr, nrow - 1);
-        v[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (sq.q0 + tokA + r / G) * a.q_tok +
-                                               (hk * a.G + (int)(r % G)) * a.q_head + c * 8);
+        v[k] = make_uint4(0, 0, 0, 0);
+        if (row_at(i) + rr0 + k * RPK < nrow)
+          v[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (sq.q0 + tokA + t) * a.q_tok +
+                                                 (hk * a.G + (int)g) * a.q_head + (lane % CH) * 8);
+        t += step_t;
+        g += step_g;
+        if (g >= G) { g -= G; ++t; }
       }
+    }
+    if constexpr (C8 && Elem<T>::bf16) {
+      // A row's power of two: each lane has the maxima of CH rows' chunks; they are halved
+      // with a lane's at a time, until lane c of CH has row c's.
+      uint32_t top[CH];
 #pragma unroll
-      for (int k = 0; k < CH; ++k) {
-        const int idx = k * 32 + lane, rr = (warp & 3) * 32 + idx / CH, c = idx % CH;
-        if (row_at(i) + rr >= nrow) v[k] = make_uint4(0, 0, 0, 0);
-        if constexpr (C8 && Elem<T>::bf16) {
-          // the CH lanes of a row agree on its power of two; the lane of the row's
-          // softmax thread keeps it
-          uint32_t top = finite_max(v[k]);
+      for (int k = 0; k < CH; ++k) top[k] = finite_max(v[k]);
 #pragma unroll
-          for (int d = 1; d < CH; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-          const int up = row_power(top);
-          v[k] = scaled_f16(v[k], up);
+      for (int s = CH / 2; s > 0; s >>= 1)
 #pragma unroll
-          for (int x = 0; x < 32 / CH; ++x) {
-            const int p = __shfl_sync(0xFFFFFFFFu, up, x * CH);
-            if (lane == k * (32 / CH) + x) q_up = p;
-          }
+        for (int k = 0; k < s; ++k) {
+          const uint32_t mine = lane & s ? top[k + s] : top[k], other = lane & s ? top[k] : top[k + s];
+          top[k] = max(mine, __shfl_xor_sync(0xFFFFFFFFu, other, s));
         }
-        *reinterpret_cast<uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[k];
-      }
+      const int up = row_power(top[0]);
+      q_up = __shfl_sync(0xFFFFFFFFu, up, (lane % RPK) * CH + lane / RPK);   // of the softmax thread's row
+#pragma unroll
+      for (int k = 0; k < CH; ++k) v[k] = scaled_f16(v[k], __shfl_sync(0xFFFFFFFFu, up, (lane & ~(CH - 1)) + k));
+    }
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int rr = (warp & 3) * 32 + k * RPK + lane / CH, c = lane % CH;
+      *reinterpret_cast<uint4*>(sQ + (c >> 3) * BLK + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[k];
     }
     fence_proxy_async_smem();
   }
@@ -343,13 +371,16 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
   // being allocated and the Queries come in.  (All warps waiting for the allocation
   // and the Queries loaded after it: 880 Queries x 12 heads 64.0 us against 62.5;
   // three ragged prompts of 64 channels 79.5 against 80.5.)
-  // (A pair's warps all wait: the other CTA's barriers and TMEM have to be there.)
+  // (Of a pair, who reaches into the other CTA waits for its barriers and TMEM; the others
+  // before they meet it again.)
   uint32_t tbase = 0;
+  const bool reaches = warp <= W_MMA || (warp == W_MMA + 3 && rank == 1);
   if constexpr (PAIR) {
-    tc_fence_before();
-    cluster_sync();
-    tc_fence_after();
-    tbase = s_tmem;
+    if (reaches) {
+      cluster_wait();
+      tc_fence_after();
+      tbase = s_tmem;
+    }
   } else if (warp <= W_MMA) {
     tc_fence_before();
     named_bar_sync(1, (W_MMA + 1) * 32);
@@ -535,8 +566,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
       if constexpr (PAIR) cluster_sync();             // what either CTA took out of the Values is known
       if (ok) {
         tc_fence_after();
-        const int64_t group = ((int64_t)b * a.Hk + hk) * rtiles + rt;
-        const int64_t pr = (group * a.nsplit + part) * L::GR + row_at(i) + row;
+        const int64_t pr = ((int64_t)cut * nsplit + part) * L::GR + row_at(i) + row;
         const float inv = l_run > 0.0f || l_run != l_run ? 1.0f / l_run : 0.0f;
         const bool poison = *(volatile int*)&s_poison != 0;
 #pragma unroll 1
@@ -592,7 +622,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
             }
           } else if (has) {
             // a part: [channels / 4][row], so that a warp writes whole lines
-            float4* d4 = reinterpret_cast<float4*>(a.part_o) + (group * a.nsplit + part) * L::GR * (D / 4) +
+            float4* d4 = reinterpret_cast<float4*>(a.part_o) + ((int64_t)cut * nsplit + part) * L::GR * (D / 4) +
                          (int64_t)(c0 / 4) * L::GR + row_at(i) + row;
 #pragma unroll
             for (int k = 0; k < 8; ++k) d4[k * L::GR] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
@@ -629,6 +659,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
       };
       if (!rebuild_tiles<D>(a, sm, tl, t0, n, warp - W_CODES, &odd, done)) s_err = 1;
       if constexpr (PAIR) {
+        cluster_wait();
         if (odd) st_cluster(mapa(smem_u32(&s_poison), rank ^ 1), 1);
         __syncwarp();
         cluster_sync();
@@ -834,6 +865,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
     }
     if constexpr (PAIR) {
       __syncwarp();
+      if (!reaches) cluster_wait();
       cluster_sync();
     }
   }
@@ -857,8 +889,18 @@ constexpr int JR = 64;
 template <typename T, int D, typename Op, int GR>
 __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
   grid_begin();
-  const int b = blockIdx.z, hk = blockIdx.y, rt = blockIdx.x / (GR / JR);
-  const int rtiles = gridDim.x / (GR / JR);
+  int b = blockIdx.z, hk = blockIdx.y, rt = blockIdx.x / (GR / JR), rtiles = gridDim.x / (GR / JR);
+  int64_t group;
+  if (a.whole >= 0) {                                 // a line of the groups that were cut
+    const int g = a.whole + rt;
+    group = rt;
+    rtiles = a.rtiles;
+    rt = rtiles - 1 - g % rtiles;
+    b = g / rtiles / a.Hk;
+    hk = g / rtiles % a.Hk;
+  } else {
+    group = ((int64_t)b * a.Hk + hk) * rtiles + rt;
+  }
   Seq sq;
   load_seq(a, b, sq);
   const int64_t rows = (int64_t)sq.qn * a.G, r0 = (int64_t)rt * GR;
@@ -873,7 +915,6 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
   const int lane = threadIdx.x & 31;
   const int r = (blockIdx.x % (GR / JR)) * JR + (threadIdx.x >> 5) * 8 + (lane & 7);
   if (parts == 1 || r >= nrow) return;
-  const int64_t group = ((int64_t)b * a.Hk + hk) * rtiles + rt;
   const float2* ml = a.part_ml + group * a.nsplit * GR + r;
   const float4* po = reinterpret_cast<const float4*>(a.part_o) + group * a.nsplit * GR * (D / 4) + r;
   constexpr int CB = D / 32, PU = 4;                  // channel blocks of a lane, parts in flight
@@ -935,16 +976,22 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
 }
 
 template <typename T, int D, bool C8>
-cudaError_t go(const PagedArgs& a, const CUtensorMap& map, const CUtensorMap& half_map, cudaStream_t s) {
+cudaError_t go(PagedArgs a, const CUtensorMap& map, const CUtensorMap& half_map, cudaStream_t s) {
   using L = Smem<D, C8>;
   static bool done[64];
   cudaError_t e = allow_smem(paged_chunk<T, D, C8>, L::TOTAL, done);
   if (e != cudaSuccess) return e;
-  const int64_t rtiles = ((int64_t)a.max_q * a.G + L::GR - 1) / L::GR;
-  e = launch_ahead(paged_chunk<T, D, C8>, dim3((unsigned)(rtiles * a.nsplit * (L::PAIR ? 2 : 1)), a.Hk, a.B),
-                   C8 ? NT8 : NT, L::TOTAL, s, L::PAIR ? 2 : 1, map, half_map, a);
+  const int64_t rtiles = ((int64_t)a.max_q * a.G + L::GR - 1) / L::GR, groups = rtiles * a.Hk * a.B;
+  const unsigned wide = L::PAIR ? 2 : 1;
+  a.rtiles = (int)rtiles;
+  dim3 grid((unsigned)(rtiles * a.nsplit * wide), a.Hk, a.B), join((unsigned)(rtiles * (L::GR / JR)), a.Hk, a.B);
+  if (a.whole >= 0) {
+    grid = dim3((unsigned)((a.whole + (groups - a.whole) * a.nsplit) * wide));
+    join = dim3((unsigned)((groups - a.whole) * (L::GR / JR)));
+  }
+  e = launch_ahead(paged_chunk<T, D, C8>, grid, C8 ? NT8 : NT, L::TOTAL, s, (int)wide, map, half_map, a);
   if (e != cudaSuccess || a.nsplit == 1) return e;
-  return launch_ahead(paged_join<T, D, Operand<T, C8>, L::GR>, dim3((unsigned)(rtiles * (L::GR / JR)), a.Hk, a.B), 256, 0, s, 1, a);
+  return launch_ahead(paged_join<T, D, Operand<T, C8>, L::GR>, join, 256, 0, s, 1, a);
 }
 template <typename T, bool C8>
 cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, const CUtensorMap& half_map, int D, cudaStream_t s) {
@@ -963,6 +1010,7 @@ PagedPlan plan_chunk(int B, int Hk, int D, int64_t rows, int64_t max_visible, in
   p.groups = (int)(groups < 1 << 30 ? groups : 1 << 30);   // (as many are not split)
   p.min_tiles = 4;
   p.nsplit = 1;
+  p.whole = -1;
   const int64_t tiles = (max_visible + TK - 1) / TK + 2;
   if (split) {
     // the split with the least waves x (tiles of a part + a CTA's fixed cost,
@@ -978,6 +1026,21 @@ PagedPlan plan_chunk(int B, int Hk, int D, int64_t rows, int64_t max_visible, in
       if (n == 1 || cost < best) {
         best = cost;
         p.nsplit = (int)n;
+      }
+    }
+  }
+  // Of 8-bit pages also: full waves of whole groups, and only what would be a part of a
+  // wave cut (4680 Queries x 40 heads, 400 pairs in 5.3 waves: @@ us against @@).
+  const int64_t full = p.groups / nsm * nsm, tail = p.groups - full;
+  if (split && codes && p.groups < 1 << 28 && full > 0 && tail > 0) {
+    int64_t best = (int64_t)((p.groups * (int64_t)p.nsplit + nsm - 1) / nsm) * ((tiles + p.nsplit - 1) / p.nsplit + 6) +
+                   (p.nsplit > 1 ? 4 : 0);
+    for (int64_t n = 2; n <= 64 && n * p.min_tiles <= tiles + p.min_tiles - 1; ++n) {
+      const int64_t cost = full / nsm * (tiles + 6) + (tail * n + nsm - 1) / nsm * ((tiles + n - 1) / n + 6) + 4;
+      if (cost < best) {
+        best = cost;
+        p.nsplit = (int)n;
+        p.whole = (int)full;
       }
     }
   }
