@@ -1,17 +1,17 @@
 """A streaming model's attention layer over both sides of the cache.
 
-Frames arrive one after the other.  The last frames stay in bf16 pages: each new
-frame's Keys and Values are appended with their three-axis rotation applied on
-the way (qwm_paged_append), and its Queries attend to the window
-(qwm_paged_attend).  A frame that leaves the window is
-compressed to the 2-bit cache (qwm_rope, qwm_fit_centroids, qwm_quantize_append)
-and its pages are given back; the Queries reach it through qwm_attend, and the two
+Frames arrive one after the other.  The last frames stay in pages, in bf16 or (--codes)
+in 8 bits: each new frame's Keys and Values are appended with their three-axis rotation
+applied on the way (qwm_paged_append), and its Queries attend to the window
+(qwm_paged_attend).  A frame that leaves the window is read back from its pages
+(qwm_paged_read) and compressed to the 2-bit cache (qwm_fit_centroids,
+qwm_quantize_append), and its pages are given back; the Queries reach it through qwm_attend, and the two
 results are joined by their log-sum-exps.  At the end the stream is continued token
 by token with the same calls; what their window would leave behind without a whole
 frame to compress stays visible in the pages, so pages and history together are
 always the whole stream.
 
-    python examples/streaming_window.py [--frames N] [--exact]
+    python examples/streaming_window.py [--frames N] [--exact] [--codes]
 
 prints the time of each frame's calls; --exact keeps every frame in pages instead
 and checks the outputs against plain attention.
@@ -54,17 +54,17 @@ def projected(seed, n, heads):
 class Stream:
     """One sequence: its pages, page table and length, and what has been compressed."""
 
-    def __init__(self, heads, frames, window, compress):
+    def __init__(self, heads, frames, window, compress, storage=None):
         self.heads, self.window, self.compress = heads, window, compress
         total = (frames + 1) * FRAME
         held = ((window + 1) * FRAME if compress else total) // PAGE + 2
-        self.cache = qwm.PagedCache(heads, held, page_tokens=PAGE, head_dim=DIM)
+        self.cache = qwm.PagedCache(heads, held, page_tokens=PAGE, head_dim=DIM, storage=storage)
         self.free = list(range(held))
         self.table = torch.full((1, total // PAGE + 1), -1, dtype=torch.int32, device="cuda")
         self.rope = qwm.Rope(frequencies(), PAIRS)
         self.len = self.oldest = 0                 # tokens so far; first token still in pages
         self.pages = {}
-        self.old = []                              # Keys (rotated) and Values of the frames in the window
+        self.whole = 0                             # frames in pages that can be compressed
         if compress:
             self.cfg = qwm.config(heads, 64, psac_rank=0)
             self.history = qwm.Cache(self.cfg, FRAME, frames + 1)
@@ -93,14 +93,18 @@ class Stream:
                    old.float() * torch.exp(old_lse - both).t()[..., None]).to(out.dtype)
             lse = both
         self.lse = lse
-        if keep and self.compress:
-            self.old.append((qwm.qwm_rope(self.rope, k, pos), v.contiguous()))
+        self.whole += keep
         return out
 
     def leave(self):
         """Compress the frame that the next one's window leaves behind and give its pages back."""
         while self.compress and self.len + FRAME - self.window * FRAME >= self.oldest + FRAME:
-            k, v = self.old.pop(0)
+            assert self.whole > 0
+            self.whole -= 1
+            offsets = torch.tensor([0, FRAME], dtype=torch.int32, device="cuda")
+            end = torch.tensor([self.oldest + FRAME], dtype=torch.int32, device="cuda")
+            batch = qwm.PagedBatch(offsets, end, self.table, FRAME, self.len, tokens=FRAME)
+            k, v = qwm.qwm_paged_read(self.cache, batch)       # Keys as they were rotated
             qwm.qwm_quantize_append(self.cfg, self.history, k, v, qwm.qwm_fit_centroids(self.cfg, k),
                                     qwm.qwm_fit_centroids(self.cfg, v))
             self.oldest += FRAME
@@ -127,9 +131,9 @@ def plain(heads, frames, tokens, window):
     return torch.einsum("hqk,khd->qhd", torch.softmax(s, -1), vs.float())
 
 
-def run(heads=4, frames=5, tokens=3, window=3, compress=True):
+def run(heads=4, frames=5, tokens=3, window=3, compress=True, storage=None):
     """Outputs [frames * FRAME + tokens][heads][DIM] and the milliseconds of each step."""
-    s, outs, times = Stream(heads, frames, window, compress), [], []
+    s, outs, times = Stream(heads, frames, window, compress, storage), [], []
     for i in range(frames + tokens):
         frame = i < frames
         q, k, v = projected(i, FRAME, heads) if frame else projected(1000 + i - frames, 1, heads)
@@ -150,9 +154,11 @@ def main():
     ap.add_argument("--frames", type=int, default=5)
     ap.add_argument("--heads", type=int, default=4)
     ap.add_argument("--exact", action="store_true")
+    ap.add_argument("--codes", action="store_true", help="pages in 8 bits")
     a = ap.parse_args()
-    run(heads=a.heads, compress=not a.exact)       # kernels are loaded on their first use
-    out, times = run(heads=a.heads, frames=a.frames, compress=not a.exact)
+    storage = torch.float8_e4m3fn if a.codes else None
+    run(heads=a.heads, compress=not a.exact, storage=storage)       # kernels are loaded on their first use
+    out, times = run(heads=a.heads, frames=a.frames, compress=not a.exact, storage=storage)
     for i, t in enumerate(times):
         print("%s %d: %.3f ms" % ("frame" if i < a.frames else "token", i if i < a.frames else i - a.frames, t))
     if a.exact:

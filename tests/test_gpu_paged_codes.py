@@ -299,6 +299,31 @@ def test_step_over_many_sequences(D, dtype, Hq, Hk, new):
     run_case(300 + D, lens, Hq, Hk, D, dtype, 16, 1, 600, 9)
 
 
+@pytest.mark.parametrize("D,dtype,B,Hk,new", [(128, BF, 10, 8, 40), (64, HF, 20, 8, 33), (128, HF, 4, 20, 300)])
+def test_groups_past_a_full_wave_are_cut(D, dtype, B, Hk, new):
+    """A little more work than the GPU has places for: the first groups whole, the rest in parts."""
+    lens = [(new, 1500 - 7 * i) for i in range(B)]
+    q, keys, values, c, s, table = make_code_case(41, lens, Hk, Hk, D, dtype, 64)
+    cache, batch = made(Hk, c.shape[0], 64, D, dtype, c, s), batch_of(lens, table)
+    ws = qwm.paged_attend_workspace(cache, batch, Hk)
+    assert ws is not None
+    out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True, workspace=ws)
+    again, _ = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True, workspace=ws)
+    assert torch.equal(out, again)
+    # every sequence's first and last rows against 64 bits, all of them against the call that is not split
+    plain, plain_lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True)
+    u = 2.0 ** -8 if dtype == BF else 2.0 ** -11
+    size = torch.cat([v.abs().amax(0)[None].expand(new, -1, -1) for v in values])
+    assert bool(((out.double() - plain.double()).abs().cpu() <= 4 * u * size).all())
+    assert bool(((lse - plain_lse).abs() <= 2.0 ** -18 * (1 + plain_lse.abs())).all())
+    for b, (_, kv) in enumerate(lens):
+        for r in (0, new - 1):
+            i, p = b * new + r, kv - new + r + 1
+            want = attend_codes64(q[i:i + 1], [keys[b][:p]], [values[b][:p]], [(1, p)], 1, 0, 0)
+            compare(out[i:i + 1], lse[:, i:i + 1], want)
+    assert cache.status() == 0
+
+
 @pytest.mark.parametrize("new", [1, 3, 150])
 @pytest.mark.parametrize("q_size,k_size", [(2.0 ** 100, 1e-3), (2.0 ** -100, 6e4), (2.0 ** 20, 1.0), (2.0 ** -126, 1.0)])
 def test_queries_of_any_size(new, q_size, k_size):
@@ -612,6 +637,20 @@ def test_another_stream_and_two_graphs_on_one_workspace():
             g.replay()
     torch.cuda.synchronize()
     assert torch.equal(outs[0], ref) and torch.equal(outs[1], ref)
+
+
+@pytest.mark.parametrize("compress", [False, True])
+def test_the_streaming_example_runs_on_8_bit_pages(compress):
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import streaming_window as ex
+    out, _ = ex.run(heads=2, frames=4, tokens=2, compress=compress, storage=E4)
+    wide, _ = ex.run(heads=2, frames=4, tokens=2, compress=compress)
+    assert out.shape == wide.shape and bool(torch.isfinite(out).all())
+    # the first frame sees itself only: Keys' relative error of at most 2^-4 a channel, independent, of logits that
+    # spread by 1, and Values' of 2^-4 (uniform in sign): well under half of the outputs' size
+    assert (out - wide)[:ex.FRAME].float().norm() <= 0.5 * wide[:ex.FRAME].float().norm()
 
 
 def test_refusals():
