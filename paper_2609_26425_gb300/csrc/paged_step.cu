@@ -997,11 +997,20 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
   // 2000 keys 13.3 and 10.2; 48 of 1500 keys 11.2 and 13.0, of 2000 13.5 and 12.7;
   // 8 groups of 1000 keys of 64 channels 6.7 and 8.4.  Near the change the two are
   // close, and 96 groups of 2000 keys swing: 17 to 20 us either way.
-  const double chain = D == 128 ? 0.29 : 0.24, hbm = D == 128 ? 0.71 : 0.4;
-  const double stream = p.groups < nsm ? hbm * p.groups / nsm : hbm;
-  const double each = stream > chain ? stream : chain;
-  const double whole = (double)((p.groups + nsm - 1) / nsm) * ((D == 128 ? 4.0 : 2.8) + tiles * each);
-  const double shared = (D == 128 ? 8.2 : 7.6) + (D == 128 ? 0.44 : 0.33) * (double)(tiles + group_cost<false>()) * p.groups / nsm;
+  // 8-bit pages (4 to 320 groups of 130 to 4000 keys): 12 groups of 1000 keys of 128
+  // channels 9.0 whole and 9.6 shared, of 1500 11.3 and 10.1; 96 of 2000 14.5 and 15.9; 192 of 1500
+  // 24.0 and 23.8; of 64 channels 48 of 2000 11.1 and 10.7, 192 of 1000 14.6 and 17.2.
+  struct Costs {
+    double chain, hbm, start, line, place;   // a tile, a whole group's start; the line's start, a place
+    int group;
+  };
+  const Costs u = codes ? (D == 128 ? Costs{0.267, 0.308, 4.75, 8.6, 0.31, 12} : Costs{0.228, 0.24, 4.2, 8.0, 0.238, 14})
+                        : (D == 128 ? Costs{0.29, 0.71, 4.0, 8.2, 0.44, group_cost<false>()}
+                                    : Costs{0.24, 0.4, 2.8, 7.6, 0.33, group_cost<false>()});
+  const double stream = p.groups < nsm ? u.hbm * p.groups / nsm : u.hbm;
+  const double each = stream > u.chain ? stream : u.chain;
+  const double whole = (double)((p.groups + nsm - 1) / nsm) * (u.start + tiles * each);
+  const double shared = u.line + u.place * (double)(tiles + u.group) * p.groups / nsm;
   if (split && (tiles > 40 || whole > shared) && p.groups <= QWM_PAGED_COUNTER_BYTES / 4) {
     // a CTA per SM, or as many as have min_tiles places each
     const int tk = D == 128 && !codes ? 64 : 128;
