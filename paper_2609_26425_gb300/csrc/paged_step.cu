@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   if (tid == 0) {
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      mbar_init(full(s), 1);
+      mbar_init(full(s), C8 ? 33 : 1);               // (the producer's, and of 8-bit pages each lane's scales)
       mbar_init(empty(s), kWarps / 2);
     }
     fence_mbar_init();
@@ -263,8 +263,8 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     const int box = C8 ? lane : lane >> 1, half = C8 ? 0 : lane & 1;
     const bool mine = box < boxes && half * 64 < D;
     const uint32_t dst = smem_u32(sm) + (C8 ? (box << box_log2) * D : half * (TK * 128) + ((box << box_log2) * 128));
-    const uint32_t sdst = smem_u32(sm) + L::SCALES + ((box << box_log2) * 2);
-    const uint32_t box_bytes = (C8 ? D + 2u : 128u) << box_log2;
+    const uint32_t box_bytes = (C8 ? D : 128u) << box_log2;
+    const int skey = 8 * lane, sbox = skey >> box_log2;   // scales: eight keys a lane, 16 bytes
     bool ok = true;
     int i = 0;                                     // tiles sent
     do {
@@ -303,7 +303,18 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         if (want) {
           const int block = (page * 2 + kv) * a.Hk + hk;
           tma_load_3d(dst + s * L::SLOT, &map, half * 64, y, block, full(s));
-          if (C8) bulk_g2s(sdst + s * (TK * 2), a.scales + (((int64_t)block << a.page_log2) + y), 2u << box_log2, full(s));
+        }
+        if constexpr (C8) {
+          // A copy of its own for each box's scales costs as much as its codes: 131071 keys in
+          // pages of 16 tokens 62.6 us, so 55.9; 517 keys x 12 heads 7.9 and 7.5; in pages of 64 with 64
+          // channels 37.0 and 38.0.
+          const int spage = __shfl_sync(0xFFFFFFFFu, pages, (at * boxes + sbox) & 31);
+          const bool swant = __shfl_sync(0xFFFFFFFFu, (int)wants, (at * boxes + sbox) & 31) && skey < TK;
+          if (swant)
+            cp_async16(smem_u32(sm) + L::SCALES + s * (TK * 2) + 2 * skey,
+                       a.scales + ((((int64_t)spage * 2 + kv) * a.Hk + hk) << a.page_log2) +
+                           ((tile_at(tl, t) * TK + skey) & ((1 << a.page_log2) - 1)));
+          cp_async_arrive(full(s));
         }
         __syncwarp();
         ++i;
