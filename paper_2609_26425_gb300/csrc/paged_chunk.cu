@@ -55,7 +55,7 @@ constexpr int NT = (4 * NQ + 4) * 32;
 // 8-bit pages: a fourth warpgroup makes K and V from codes, and the warps share out the
 // registers (65536 in all): softmax, the MMAs' and the producers' warpgroup, the codes'.
 constexpr int kRebuild = 4, NT8 = NT + 128;
-constexpr int kRegLaunch = 65536 / NT8, kRegSoftmax = 168, kRegMma = 80, kRegCodes = 96;
+constexpr int kRegLaunch = 65536 / NT8, kRegSoftmax = 176, kRegMma = 64, kRegCodes = 96;
 static_assert(NT8 == 512 && NQ * kRegSoftmax + kRegMma + kRegCodes <= 4 * kRegLaunch, "what the launch has");
 
 template <int D, bool C8>
@@ -431,12 +431,20 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
           }
         }
       };
+      // What all rows of the warp see: tiles that end at all_hi, and begin at all_lo or end in the first tokens
+      int all_lo = has ? sp.lo : 0, all_hi = has ? sp.hi : INT32_MAX;
+      bool fresh = true;                                // some row may have no maximum yet
+      if constexpr (C8) {
+        all_lo = __reduce_max_sync(0xFFFFFFFFu, all_lo);
+        all_hi = __reduce_min_sync(0xFFFFFFFFu, all_hi);
+      }
       bool ok = true;
       for (int jt = 0; jt < n; ++jt) {
         if (!(ok = wait_all(B_SFULL + i, jt & 1))) break;
         tc_fence_after();
         const int j0 = tile_at(tl, t0 + jt) * TK;
-        const bool open = __all_sync(0xFFFFFFFFu, !has || (j0 + TK <= sp.hi && (j0 >= sp.lo || j0 + TK <= a.sinks)));
+        const bool open = C8 ? j0 + TK <= all_hi && (j0 >= all_lo || j0 + TK <= a.sinks)
+                             : __all_sync(0xFFFFFFFFu, !has || (j0 + TK <= sp.hi && (j0 >= sp.lo || j0 + TK <= a.sinks)));
         // Which keys of each 32-key block this row sees; a warp whose rows all
         // see a whole block, or none of it, takes it without the selection.
         enum { kNone, kSome, kAll };
@@ -451,7 +459,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
           for (int e = 0; e < 32; ++e) w[e] = (see >> e) & 1 ? w[e] : 0xFF800000u;
         };
         // where a row has no maximum yet, the tile's comes first
-        if (__any_sync(0xFFFFFFFFu, m_run == -INFINITY)) {
+        if ((!C8 || fresh) && __any_sync(0xFFFFFFFFu, m_run == -INFINITY)) {
           float mt = -INFINITY;
           if (open) {
             mt = tmem_max128(tS);
@@ -469,6 +477,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
             }
           }
           if (__any_sync(0xFFFFFFFFu, mt > m_run)) raise(mt, jt > 0);
+          if constexpr (C8) fresh = __any_sync(0xFFFFFFFFu, m_run == -INFINITY);
         }
         // One pass over S in two halves of 64 keys, each handed on as soon as it is
         // done: P against m_run, and its sum.
