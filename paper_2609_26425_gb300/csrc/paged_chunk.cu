@@ -32,6 +32,21 @@
 // not 0 in the MMA) in the tiles at the edges of the mask, and waves the others
 // through; infinities and NaN in Values that some rows see and others do not
 // are taken out of the product and added to the rows that see them at the end.
+//
+// 8-bit pages: the producers bring codes, and a fourth warpgroup makes binary16 tiles of
+// them, the Values' guard in one.  What was found on the way (4680 Queries x 40 heads over 34320
+// keys; 880 x 12 over 14080): codes through registers, a tile ahead, by three warps of the twelve
+// 9465 and 288 us, their loads waited for one after the other; a warpgroup of its own, with
+// registers shared out by role, 2643 and 93; codes by TMA 2476 and 95: shared memory then
+// is the MMAs' bound, who read 192 KB a tile pair of 128 channels while 64 KB are written.  So
+// at 128 channels two CTAs share their MMAs (cta_group::2, M = 256): each makes and holds half of
+// a tile's Keys, and half of the Values' channels, and reads 128 KB where 32 KB are written: 2432 and
+// 84 (less than the gain a tile, 3.5 K to 3.2 K cycles, for 400 pairs are 5.3 waves of 76);
+// with only the last wave cut along the keys 2330, with the registers shared out anew 2260.
+// What is left is the chain S, softmax, P V: without softmax and rebuilding the MMAs take 1690
+// us (100% of a library product's rate), without exponentials 2200, without rebuilding 2190.
+// S in halves of 64 keys, each made while the other half is worked on, reads the Queries twice
+// and lost what it won (2500).  At 64 channels a CTA works alone, as with 16-bit pages.
 #include <type_traits>
 
 #include "paged.cuh"
@@ -220,7 +235,7 @@ __device__ __forceinline__ bool rebuild_tiles(const PagedArgs& a, uint8_t* sm, c
 // binary16 (every code x scale is one).
 template <typename T, int D, bool C8>
 __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_constant__ CUtensorMap map,
-                                                                 const __grid_constant__ CUtensorMap half_map,
+                                                                 const __grid_constant__ CUtensorMap half_map,   // pairs: 64 channels
                                                                  const PagedArgs a) {
   using L = Smem<D, C8>;
   constexpr bool PAIR = L::PAIR;
@@ -266,7 +281,8 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
   grid_begin();
   int b = blockIdx.z, hk = blockIdx.y;
   const int gx = PAIR ? blockIdx.x >> 1 : blockIdx.x;
-  int rtiles, rt, part, nsplit = a.nsplit, cut;         // cut: the group's number among those in parts
+  int rtiles, rt, part, nsplit = a.nsplit;
+  int64_t cut;                                          // the group's number among those in parts
   if (C8 && a.whole >= 0) {
     // groups in one line: the first `whole` of them as they are, the others in parts
     rtiles = a.rtiles;
@@ -281,7 +297,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
     rtiles = (PAIR ? gridDim.x >> 1 : gridDim.x) / nsplit;
     rt = rtiles - 1 - gx % rtiles;                      // the row tiles with the most keys first
     part = gx / rtiles;
-    cut = (b * a.Hk + hk) * rtiles + rt;
+    cut = ((int64_t)b * a.Hk + hk) * rtiles + rt;
   }
   Seq sq;
   if (!load_seq(a, b, sq) && rt == rtiles - 1 && part == 0 && hk == 0 && tid == 0) record_status(a.status, QWM_ERR_INVALID_ARG);
@@ -575,7 +591,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
       if constexpr (PAIR) cluster_sync();             // what either CTA took out of the Values is known
       if (ok) {
         tc_fence_after();
-        const int64_t pr = ((int64_t)cut * nsplit + part) * L::GR + row_at(i) + row;
+        const int64_t pr = (cut * nsplit + part) * L::GR + row_at(i) + row;
         const float inv = l_run > 0.0f || l_run != l_run ? 1.0f / l_run : 0.0f;
         const bool poison = *(volatile int*)&s_poison != 0;
 #pragma unroll 1
@@ -631,7 +647,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
             }
           } else if (has) {
             // a part: [channels / 4][row], so that a warp writes whole lines
-            float4* d4 = reinterpret_cast<float4*>(a.part_o) + ((int64_t)cut * nsplit + part) * L::GR * (D / 4) +
+            float4* d4 = reinterpret_cast<float4*>(a.part_o) + (cut * nsplit + part) * L::GR * (D / 4) +
                          (int64_t)(c0 / 4) * L::GR + row_at(i) + row;
 #pragma unroll
             for (int k = 0; k < 8; ++k) d4[k * L::GR] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
@@ -1039,7 +1055,7 @@ PagedPlan plan_chunk(int B, int Hk, int D, int64_t rows, int64_t max_visible, in
     }
   }
   // Of 8-bit pages also: full waves of whole groups, and only what would be a part of a
-  // wave cut (4680 Queries x 40 heads, 400 pairs in 5.3 waves: @@ us against @@).
+  // wave cut (4680 Queries x 40 heads, 400 pairs in 5.3 waves: 2330 us against 2432).
   const int64_t full = p.groups / nsm * nsm, tail = p.groups - full;
   if (split && codes && p.groups < 1 << 28 && full > 0 && tail > 0) {
     int64_t best = (int64_t)((p.groups * (int64_t)p.nsplit + nsm - 1) / nsm) * ((tiles + p.nsplit - 1) / p.nsplit + 6) +

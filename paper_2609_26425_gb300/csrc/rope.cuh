@@ -13,6 +13,9 @@ namespace qwm {
 // is left beside the nearest quarter turn is at most pi / 4 in fp32, where the fast sine
 // and cosine are good to 2^-21: far below the output's 2^-9 or 2^-12.  An f of 2^24 or
 // more, an infinity or a NaN gives NaN.
+// FINE: with the full sine and cosine, for results that are rounded to less than they are good
+// for: next to a border between two codes every bit counts.
+template <bool FINE = false>
 __device__ __forceinline__ float2 turn(int pos, float f, float sign) {
   constexpr uint64_t kC1 = 0x28BE60DB9391054Aull, kC0 = 0x7F09D5F47D4D3770ull;   // floor(2^128 / (2 pi))
   constexpr float kTurn = (float)(6.283185307179586476925286766559 / 18446744073709551616.0);
@@ -24,7 +27,9 @@ __device__ __forceinline__ float2 turn(int pos, float f, float sign) {
   const uint64_t t = (uint64_t)(int64_t)pos * g;
   const uint64_t q = (t + (1ull << 61)) >> 62;      // quarter turns
   float sn, cs;
-  __sincosf((float)(int64_t)(t - (q << 62)) * kTurn, &sn, &cs);
+  const float left = (float)(int64_t)(t - (q << 62)) * kTurn;
+  if (FINE) sincosf(left, &sn, &cs);
+  else __sincosf(left, &sn, &cs);
   if (ex >= 127 + 24) cs = __uint_as_float(0x7FFFFFFFu);
   const float c = q & 1 ? sn : cs, d = q & 1 ? cs : sn;
   // a quarter turn on is (-sn, cs), and so forth
