@@ -14,9 +14,9 @@ Functions carry the C names:
 qwm_cache_layout / qwm_cache_chunk_info, ``QueryStats`` wraps a Query
 statistics buffer (qwm_query_stats_bytes / _reset / _update / _read and
 qwm_query_basis), and qwm_dequant_chunk / qwm_top1_keys serve the
-token-selection shift measurement.  ``paged`` binds the uncompressed side:
-rotary positions (``Rope``, qwm_rope*) and paged storage (``PagedCache``,
-``PagedBatch``, qwm_paged_*).
+token-selection shift measurement.  ``paged`` binds the paged side: rotary
+positions (``Rope``, qwm_rope*) and paged storage in 16 or 8 bits
+(``PagedCache``, ``PagedBatch``, qwm_paged_*).
 """
 from __future__ import annotations
 

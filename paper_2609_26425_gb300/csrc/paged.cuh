@@ -139,7 +139,8 @@ inline cudaError_t launch_ahead(void (*kernel)(P...), dim3 grid, int threads, si
 // to the step kernel.  With 16 rows of 128 channels it takes 67 us against the
 // chunk kernel's 77 (one sequence of 131071 tokens, 4 cache heads), 20 against 16
 // (4000 tokens); a step kernel with a second tile of 16 rows lost on nearly every
-// length (24 rows: 88 against 79 us and 27 against 16).
+// length (24 rows: 88 against 79 us and 27 against 16).  Over codes the step
+// kernel wins at every length: 61 against 103 us, 20 against 23.
 constexpr int kStepRows = 16;
 
 // Pages as rows of D channels, [num_pages * 2 * heads][page_tokens][D]: boxes of

@@ -1,4 +1,4 @@
-"""Rotary positions over three axes and the uncompressed, paged side of the
+"""Rotary positions over three axes and the paged side (16 or 8 bits) of the
 cache (binding of the qwm_rope* and qwm_paged* entry points of include/qwm.h).
 
 ``Rope`` holds a rotation's frequencies, ``PagedCache`` the pages (16 bits, or 8),
