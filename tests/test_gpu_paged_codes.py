@@ -441,6 +441,30 @@ def test_attention_over_codes_is_attention_over_what_they_stand_for(new):
     assert bool(((la - lb).abs().cpu() <= 2 * want[3]).all())
 
 
+def test_every_pass_gives_the_same_bits():
+    """Tiles at the mask's edges (first tokens, then the window's start) amid a long list of
+    tiles, whose making takes longer than their neighbours', in more groups than the SMs hold."""
+    new, kv, H, D, page = 4680, 23400, 20, 128, 128
+    g = torch.Generator(device="cuda").manual_seed(5)
+    num = (kv + page - 1) // page
+    cache = qwm.PagedCache(H, num, page_tokens=page, head_dim=D, dtype=BF, storage=torch.float8_e4m3fn)
+    cache.pages.copy_(torch.randn(cache.pages.shape, generator=g, device="cuda").to(torch.float8_e4m3fn))
+    cache.scales.copy_(torch.exp2(torch.randint(-2, 2, cache.scales.shape, generator=g, device="cuda").float()))
+    table = torch.randperm(num, generator=torch.Generator().manual_seed(6)).int()[None]
+    batch = batch_of([(new, kv)], table)
+    q = torch.randn(new, H, D, generator=g, device="cuda").to(BF)
+    mask = dict(window=18720, sinks=1560, block=new)
+    ws = qwm.paged_attend_workspace(cache, batch, H, **mask)
+    first, first_lse = qwm.qwm_paged_attend(cache, batch, q, want_lse=True, workspace=ws, **mask)
+    differ = torch.zeros((), dtype=torch.int64, device="cuda")
+    out, lse = torch.empty_like(first), torch.empty_like(first_lse)
+    for _ in range(400):
+        qwm.qwm_paged_attend(cache, batch, q, out=out, lse=lse, workspace=ws, **mask)
+        differ += (out.view(torch.int16) != first.view(torch.int16)).any() | (lse != first_lse).any()
+    assert int(differ) == 0
+    assert cache.status() == 0
+
+
 def test_offsets_beyond_32_bits():
     Hk, page, D = 8, 128, 128
     num = (1 << 32) // (2 * Hk * page * D) + 9                 # the last pages' codes start past 2^32 bytes
