@@ -130,11 +130,26 @@ __device__ __forceinline__ uint32_t bits(int a, int b) {
 }
 
 constexpr float pow2(int e) { return e > 0 ? 2.0f * pow2(e - 1) : (e < 0 ? 0.5f * pow2(e + 1) : 1.0f); }
+// P of a new maximum is 2^-kBias, and may grow until 64 of them sum up to kMost before the
+// maximum moves.  8-bit pages: binary16 keeps all bits of P down to 2^-16 of the maximum of a
+// row's first tile, and none below 2^-27.  Less room to grow costs time: 2^11 (then 2^-19)
+// 86 and 2288 us where 2^14 takes 83 and 2276, 2^9 95 and 2317, 2^7 103 and 2395 (880 Queries x
+// 12 heads; 4680 x 40).
+template <typename T, bool C8>
+struct Range {
+  static constexpr int kBias = Elem<T>::kBias;
+  static constexpr float kMost = pow2(Elem<T>::kTau - kBias);
+};
+template <typename T>
+struct Range<T, true> {
+  static constexpr int kBias = -2;
+  static constexpr float kMost = 65504.0f;
+};
 // Natural-log sum-exp of a row: `m` is the power that its P were taken against, l
 // their sum.  -inf (and log 0) where nothing was seen, NaN with a NaN sum.
-template <typename Op>
+template <int BIAS>
 __device__ __forceinline__ float log_sum(float m, float l) {
-  return (m - (float)Elem<Op>::kBias + log2f(l * pow2(Elem<Op>::kBias))) * 0.69314718055994531f;
+  return (m - (float)BIAS + log2f(l * pow2(BIAS))) * 0.69314718055994531f;
 }
 
 // A warpgroup's registers a thread from here on: fewer than at the launch, or more, for which
@@ -433,9 +448,9 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
       float m_run = has ? -INFINITY : 0.0f, l_run = 0.0f;
       const float sr = C8 && Elem<T>::bf16 ? row_scale(sl2, q_up) : sl2;
       const uint64_t SL = f2pack(sr, sr);
-      constexpr float kMost = pow2(Elem<Op>::kTau - Elem<Op>::kBias);
+      using P = Range<T, C8>;
       // P = 2^(s sr - power(m_run))
-      auto power = [&](float m) { return fmaf(m, sr, (float)Elem<Op>::kBias); };
+      auto power = [&](float m) { return fmaf(m, sr, (float)P::kBias); };
       // Raises every row of the warp to its own maximum, and O with it (the P V
       // before it are complete)
       auto raise = [&](float mt, bool rescale) {
@@ -545,7 +560,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
             const int half = blk >> 1;
             float sx, sy;
             f2unpack(sum, sx, sy);
-            if (__any_sync(0xFFFFFFFFu, sx + sy > kMost)) {
+            if (__any_sync(0xFFFFFFFFu, sx + sy > P::kMost)) {
               // again against the new maximum; the first half's P V has to be in O
               // before O is scaled for the second's
               if (half == 1) {
@@ -672,7 +687,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
           }
         }
         if (has && parts == 1 && a.lse)
-          a.lse[(int64_t)head * a.N + sq.q0 + tok] = log_sum<Op>(power(m_run), l_run);
+          a.lse[(int64_t)head * a.N + sq.q0 + tok] = log_sum<P::kBias>(power(m_run), l_run);
         if (has && parts > 1) a.part_ml[pr] = make_float2(power(m_run), l_run);
       }
     } else if constexpr (PAIR) {
@@ -917,7 +932,7 @@ __global__ void __launch_bounds__(C8 ? NT8 : NT, 1) paged_chunk(const __grid_con
 // of them; lanes 8 rows x 4 groups of 8 channels, so that reads (a part lies
 // [channels / 4][row]) and writes are whole sectors.
 constexpr int JR = 64;
-template <typename T, int D, typename Op, int GR>
+template <typename T, int D, int BIAS, int GR>
 __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
   grid_begin();
   int b = blockIdx.z, hk = blockIdx.y, rt = blockIdx.x / (GR / JR), rtiles = gridDim.x / (GR / JR);
@@ -1003,7 +1018,7 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a) {
     *reinterpret_cast<uint4*>(dst + 32 * k) =
         make_uint4(Elem<T>::pack(v[k][0].x * inv, v[k][0].y * inv), Elem<T>::pack(v[k][0].z * inv, v[k][0].w * inv),
                    Elem<T>::pack(v[k][1].x * inv, v[k][1].y * inv), Elem<T>::pack(v[k][1].z * inv, v[k][1].w * inv));
-  if (a.lse && lane < 8) a.lse[(int64_t)head * a.N + sq.q0 + tok] = log_sum<Op>(m, l);
+  if (a.lse && lane < 8) a.lse[(int64_t)head * a.N + sq.q0 + tok] = log_sum<BIAS>(m, l);
 }
 
 template <typename T, int D, bool C8>
@@ -1022,7 +1037,7 @@ cudaError_t go(PagedArgs a, const CUtensorMap& map, const CUtensorMap& half_map,
   }
   e = launch_ahead(paged_chunk<T, D, C8>, grid, C8 ? NT8 : NT, L::TOTAL, s, (int)wide, map, half_map, a);
   if (e != cudaSuccess || a.nsplit == 1) return e;
-  return launch_ahead(paged_join<T, D, Operand<T, C8>, L::GR>, join, 256, 0, s, 1, a);
+  return launch_ahead(paged_join<T, D, Range<T, C8>::kBias, L::GR>, join, 256, 0, s, 1, a);
 }
 template <typename T, bool C8>
 cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, const CUtensorMap& half_map, int D, cudaStream_t s) {

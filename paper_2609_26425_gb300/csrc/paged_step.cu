@@ -37,6 +37,15 @@ constexpr int NT = (kWarps + 2) * 32;    // and two producers, of K and of V
 template <bool C8>
 constexpr int group_cost() { return C8 ? 8 : 4; }
 
+// Of 8-bit pages P enters the products as binary16, 2^15 at a row's maximum: from 2^-29 of
+// it on with all its bits, down to 2^-39 at all (with 1 at the maximum from 2^-14 on, which
+// the many keys beside a first token that draws most of the weight can lie below).  A piece's
+// sums are brought back when they are written.
+template <bool C8>
+constexpr float kTop = C8 ? 15.0f : 0.0f;
+template <bool C8>
+constexpr float kUnit = C8 ? 0x1p-15f : 1.0f;
+
 // KP 16-key groups of a warp.  A tile's chain of products, exponentials and
 // products takes as long for two groups as for one, so two where the chain bounds
 // (64 channels; whole groups), one where HBM does and finer slots keep it busier
@@ -462,7 +471,8 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
             }
           }
           // a row that has seen nothing yet keeps 0 as its reference: 2^-inf = 0
-          const float mb[2] = {m_run[0] == -INFINITY ? 0.0f : m_run[0] * slr[0], m_run[1] == -INFINITY ? 0.0f : m_run[1] * slr[1]};
+          const float mb[2] = {m_run[0] == -INFINITY ? 0.0f : fmaf(m_run[0], slr[0], -kTop<C8>),
+                               m_run[1] == -INFINITY ? 0.0f : fmaf(m_run[1], slr[1], -kTop<C8>)};
 #pragma unroll
           for (int kp = 0; kp < KP; ++kp) {
             float v[4];
@@ -573,11 +583,12 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         if (r >= rows) continue;
         if (g == 0) {
           s_ml[warp][r][0] = m_run[x] * (slr[x] / sl2);   // in the units of q k^T
-          s_ml[warp][r][1] = l;
+          s_ml[warp][r][1] = l * kUnit<C8>;
         }
 #pragma unroll
         for (int k = 0; k < KS; ++k)
-          *reinterpret_cast<float2*>(so + ((warp * ROWS + r) * D + k * 16 + g * 2)) = make_float2(o[k][x], o[k][2 + x]);
+          *reinterpret_cast<float2*>(so + ((warp * ROWS + r) * D + k * 16 + g * 2)) =
+              make_float2(o[k][x] * kUnit<C8>, o[k][2 + x] * kUnit<C8>);
       }
     } else {
       // the fragments of mma.sync: this lane has rows g and g + 8 (index rr)
@@ -742,8 +753,8 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
             }
           }
           // a row that has seen nothing yet keeps 0 as its reference: 2^-inf = 0
-          const float mb0 = m_run[0] == -INFINITY ? 0.0f : m_run[0] * slr[0];
-          const float mb1 = m_run[1] == -INFINITY ? 0.0f : m_run[1] * slr[1];
+          const float mb0 = m_run[0] == -INFINITY ? 0.0f : fmaf(m_run[0], slr[0], -kTop<C8>);
+          const float mb1 = m_run[1] == -INFINITY ? 0.0f : fmaf(m_run[1], slr[1], -kTop<C8>);
 #pragma unroll
           for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
@@ -847,13 +858,14 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         if (r >= rows) continue;
         if (tq == 0) {
           s_ml[warp][r][0] = C8 ? m_run[rr] * true_max[rr] : m_run[rr];
-          s_ml[warp][r][1] = l;
+          s_ml[warp][r][1] = l * kUnit<C8>;
         }
         if constexpr (C8) {
 #pragma unroll
           for (int k = 0; k < 2 * KS; k += 2)
             *reinterpret_cast<float4*>(so + ((warp * ROWS + r) * D + k * 8 + tq * 4)) =
-                make_float4(o[k][2 * rr], o[k + 1][2 * rr], o[k][2 * rr + 1], o[k + 1][2 * rr + 1]);
+                make_float4(o[k][2 * rr] * kUnit<C8>, o[k + 1][2 * rr] * kUnit<C8>, o[k][2 * rr + 1] * kUnit<C8>,
+                            o[k + 1][2 * rr + 1] * kUnit<C8>);
         } else {
 #pragma unroll
           for (int k = 0; k < 2 * KS; ++k)

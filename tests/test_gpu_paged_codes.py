@@ -426,6 +426,39 @@ def test_running_maxima_that_move(new, dtype, D, order):
         compare(out, lse, want)
 
 
+@pytest.mark.parametrize("new,G,gap", [(1, 2, 16.0), (3, 2, 16.0), (5, 3, 16.0), (150, 2, 11.0)])
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 64)])
+def test_many_keys_beside_one_that_draws_most_of_the_weight(new, G, gap, dtype, D):
+    """A first token whose Value is zero and whose logit is above all others by 16 (steps:
+    P 2^-23 of the largest) or 11 (chunks: 2^-15.9): the others are the output.  Their P keeps
+    all its bits (2^-12 relative of binary16), so the output is off by that, its own
+    rounding, and 2^-14 for the exponentials of arguments below 32 in fp32 and the sums."""
+    kv, page = 900, 16
+    lens = [(new, kv)]
+    q, keys, values, c, s, table = make_code_case(67, lens, G, 1, D, dtype, page)
+    q = torch.zeros_like(q)
+    q[:, :, 5] = 1.0                                           # a logit is one channel of the Key
+    keys[0][:, 0, 5] = 0.0
+    keys[0][0, 0, 5] = gap
+    values[0] = values[0].abs() + 0.5
+    values[0][0] = 0.0
+    for x, rows in enumerate((keys, values)):
+        cc, cs = quantise64(rows[0].to(dtype))
+        rows[0] = stands_for(cc, cs)
+        for i in range((kv + page - 1) // page):
+            n = min(page, kv - i * page)
+            c[int(table[0, i]), x, :, :n] = cc[i * page:i * page + n].permute(1, 0, 2)
+            s[int(table[0, i]), x, :, :n] = cs[i * page:i * page + n].t().half()
+    assert float(keys[0][0, 0, 5]) == gap
+    cache, batch = made(1, c.shape[0], page, D, dtype, c, s), batch_of(lens, table)
+    want = attend_codes64(q, keys, values, lens, 1, 0, 0, scale=1.0)[0]
+    bound = want.abs() * (2.0 ** -12 + torch.finfo(dtype).eps / 2 * 1.01 + 2.0 ** -14) + (2.0 ** -25 if dtype == HF else 0)
+    for ws in (None, qwm.paged_attend_workspace(cache, batch, G)):
+        out = qwm.qwm_paged_attend(cache, batch, q.cuda(), sm_scale=1.0, workspace=ws)
+        out = out[0] if isinstance(out, tuple) else out
+        assert bool(((out.double().cpu() - want).abs() <= bound).all())
+
+
 @pytest.mark.parametrize("new", [1, 40])
 def test_attention_over_codes_is_attention_over_what_they_stand_for(new):
     """The same bits' worth of tokens in 8-bit and in 16-bit pages."""
