@@ -74,6 +74,7 @@ struct PagedArgs {
   // min_tiles tiles; step: nsplit CTAs share the line of all tiles, at least
   // min_tiles places each.  nsplit 1: no split
   int32_t nsplit, min_tiles;
+  int32_t wide;                          // step: tiles of 256 keys
   int32_t whole, rtiles;                 // chunk: >= 0: groups in one line, of which so many first ones are not cut;
                                          // row tiles of a sequence and head
   float* part_o;                         // chunk [group][nsplit][D / 4][row][4]; step [CTA][2][row][D]
@@ -89,6 +90,7 @@ struct PagedPlan {
   int32_t rows;      // rows of a group
   int32_t nsplit, min_tiles;
   int32_t whole;     // chunk: groups not cut (-1: none, or all if nsplit is 1)
+  int32_t wide;      // step: tiles of 256 keys (8-bit pages of 64 channels)
 };
 PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split, bool codes);
 PagedPlan plan_chunk(int B, int Hk, int D, int64_t rows, int64_t max_visible, int nsm, bool split, bool codes);

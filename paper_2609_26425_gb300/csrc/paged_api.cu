@@ -444,6 +444,7 @@ qwm_status qwm_paged_attend(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   a.nsplit = p.nsplit;
   a.min_tiles = p.nsplit > 1 ? p.min_tiles : 1 << 24;
   a.whole = p.step ? -1 : p.whole;
+  a.wide = p.wide;
   if (p.nsplit > 1) {
     const Carve w = carve(p, D);
     uint8_t* ws = static_cast<uint8_t*>(workspace);

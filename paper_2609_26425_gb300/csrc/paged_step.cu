@@ -33,9 +33,10 @@ constexpr int NT = (kWarps + 2) * 32;    // and two producers, of K and of V
 // What a group costs a CTA beside its tiles (Queries, merge, output: about 5 K
 // cycles, and as much again where 8-bit pages have to be unpacked at the mask's edges),
 // in tiles' time (1.3 K cycles when all CTAs stream).  Of 8-bit pages, 32 sequences of 100
-// to 30000 keys x 8 heads, window 8192: 52 us with 4, 45.4 with 6, 44.5 with 8, 50.6 with 14.
-template <bool C8>
-constexpr int group_cost() { return C8 ? 8 : 4; }
+// to 30000 keys x 8 heads, window 8192: 52 us with 4, 45.4 with 6, 44.5 with 8, 50.6 with 14
+// (tiles of 128 keys; of 256, 21 drafts of 4 tokens over 64 to 20000 keys: 24.3 with 4, 22.4 with 5).
+template <bool C8, int KP = 2>
+constexpr int group_cost() { return !C8 ? 4 : KP == 4 ? 5 : 8; }
 
 // Of 8-bit pages P enters the products as binary16, 2^15 at a row's maximum: from 2^-29 of
 // it on with all its bits, down to 2^-39 at all (with 1 at the maximum from 2^-14 on, which
@@ -52,7 +53,7 @@ constexpr float kUnit = C8 ? 0x1p-15f : 1.0f;
 // (128 channels on the line: 131071 keys 86 us with one, 91 with two; 517 keys x 12
 // whole groups 8.9 and 7.6; all four with one producer warp for K and V).
 // Of 8-bit pages two groups as well: a tile is half the bytes, and its chain the same
-// (131071 keys 56 us, with one 69).
+// (131071 keys 56 us, with one 69); of 64 channels four where groups are long (plan_step).
 // N8: at most 8 rows, which are the N side of the products then.
 template <int D, int KP_, bool C8, bool N8>
 struct Shape {
@@ -66,7 +67,11 @@ struct Shape {
   static constexpr int MERGE = NS * SLOT;                      // the warps' O [warp][ROWS][D], beside the ring so that
                                                                // the next group's tiles come in meanwhile
   static constexpr int SCALES = MERGE + kWarps * ROWS * D * 4; // 8-bit pages: the tiles' scales [slot][TK]
-  static constexpr int TOTAL = SCALES + (C8 ? NS * TK * 2 : 0) + 1024;
+  // Queries of 9 to 16 rows of 128 channels lie in shared memory as fragments [k16 step][lane]:
+  // in registers, others spill (21 drafts of 4 tokens over 64 to 20000 keys 38.9 us, so 36.4)
+  static constexpr bool QS = C8 && !N8 && D == 128;
+  static constexpr int QUERIES = SCALES + (C8 ? NS * TK * 2 : 0);
+  static constexpr int TOTAL = QUERIES + (QS ? (D / 16) * 32 * 16 : 0) + 1024;
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
@@ -116,7 +121,7 @@ template <typename T, int D, int KP, bool C8, bool N8>
 __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUtensorMap map, const PagedArgs a) {
   using L = Shape<D, KP, C8, N8>;
   using Op = Operand<T, C8>;
-  constexpr int NS = L::NS, TK = L::TK, ROWS = L::ROWS, kGroupCost = group_cost<C8>();
+  constexpr int NS = L::NS, TK = L::TK, ROWS = L::ROWS, kGroupCost = group_cost<C8, KP>();
   constexpr int KS = D / 16;                       // k16 steps of Q K^T, n16 blocks of P V
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -522,8 +527,13 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
           for (int kp = 0; kp < KP; ++kp) {
             const int ja = j0 + kp * 16 + tq * 2;
             const uint32_t ma = keep(tl.lo_min, tl.hi_max, ja), mb = keep(tl.lo_min, tl.hi_max, ja + 8);
-            const uint32_t b0 = kp == 0 ? pf[0][0] : pf[KP - 1][0], b1 = kp == 0 ? pf[0][1] : pf[KP - 1][1];
-            static_assert(KP <= 2, "");
+            uint32_t b0 = pf[0][0], b1 = pf[0][1];
+#pragma unroll
+            for (int k = 1; k < KP; ++k)
+              if (kp == k) {
+                b0 = pf[k][0];
+                b1 = pf[k][1];
+              }
             bool odd = false;
             if (sq.qn > 1) {
 #pragma unroll 1
@@ -596,7 +606,6 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       float m_run[2], l_run[2];
       uint32_t qf[KS][4];
       float slr[2] = {sl2, sl2};                                          // scale of a row's logits, as powers of two
-      float true_max[2] = {1.0f, 1.0f};                                   // from m_run to the rows' q k^T
       int hi[2], lo[2];
 #pragma unroll
       for (int k = 0; k < 2 * KS; ++k)
@@ -614,25 +623,11 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         lo[rr] = sp.lo;
         const T* src = static_cast<const T*>(a.q) + (sq.q0 + tok) * a.q_tok + (int64_t)(hk * a.G + (has ? r % a.G : 0)) * a.q_head;
         if constexpr (C8) {
-          uint32_t top = 0;
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
             const uint2 w = has ? *reinterpret_cast<const uint2*>(src + ks * 16 + tq * 4) : make_uint2(0u, 0u);
             qf[ks][rr] = w.x;
             qf[ks][2 + rr] = w.y;
-            top = max(top, finite_max(make_uint4(w.x, w.y, 0u, 0u)));
-          }
-          if (Elem<T>::bf16) {
-            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            const int up = row_power(top);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-              qf[ks][rr] = scaled_f16(qf[ks][rr], up);
-              qf[ks][2 + rr] = scaled_f16(qf[ks][2 + rr], up);
-            }
-            slr[rr] = row_scale(sl2, up);
-            true_max[rr] = times_pow2(1.0f, -up);
           }
         } else {
 #pragma unroll
@@ -641,6 +636,32 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
             qf[ks][2 + rr] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8 + tq * 2) : 0u;
           }
         }
+      }
+      if constexpr (C8 && Elem<T>::bf16) {
+        // (after all loads: its branch for infinities would hold up each of them; the drafts above
+        // 36.4 us, so 31.0)
+#pragma unroll
+        for (int rr = 0; rr < 2; ++rr) {
+          uint32_t top = 0;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) top = max(top, finite_max(make_uint4(qf[ks][rr], qf[ks][2 + rr], 0u, 0u)));
+          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+          const int up = row_power(top);
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            qf[ks][rr] = scaled_f16(qf[ks][rr], up);
+            qf[ks][2 + rr] = scaled_f16(qf[ks][2 + rr], up);
+          }
+          slr[rr] = row_scale(sl2, up);
+        }
+      }
+      uint4* qs = reinterpret_cast<uint4*>(sm + L::QUERIES) + lane;
+      if constexpr (L::QS) {
+        // each warp writes all of them, the same values (nobody reads the last piece's any more)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qs[32 * ks] = make_uint4(qf[ks][0], qf[ks][1], qf[ks][2], qf[ks][3]);
+        __syncwarp();
       }
       // This warp group's tiles are those of its parity in the CTA's count of tiles,
       // so that a slot of the ring is always the same group's: a group that did not
@@ -682,7 +703,18 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
               for (int e = 0; e < 4; ++e) sc[kp][k][e] = 0.0f;
           if constexpr (C8) {
 #pragma unroll
-            for (int ks = 0; ks < KS; ks += 2)
+            for (int ks = 0; ks < KS; ks += 2) {
+              uint32_t qa[2][4];
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                if constexpr (L::QS) {
+                  const uint4 v = qs[32 * (ks + x)];
+                  qa[x][0] = v.x; qa[x][1] = v.y; qa[x][2] = v.z; qa[x][3] = v.w;
+                } else {
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) qa[x][e] = qf[ks + x][e];
+                }
+              }
 #pragma unroll
               for (int kp = 0; kp < KP; ++kp) {
                 uint32_t w[4];                         // (keys 0-7 | 8-15) x (step ks, ks + 1)
@@ -691,9 +723,10 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
                 for (int x = 0; x < 4; ++x) {
                   uint32_t b0, b1;
                   from_codes(w[x], b0, b1);
-                  Elem<Op>::mma(sc[kp][x & 1], qf[ks + (x >> 1)], b0, b1);
+                  Elem<Op>::mma(sc[kp][x & 1], qa[x >> 1], b0, b1);
                 }
               }
+            }
 #pragma unroll
             for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
@@ -793,8 +826,17 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
           auto keep = [&](int klo, int khi, int j) -> uint32_t {
             return (sees(j, klo, khi, a.sinks) ? 0xFFFFu : 0u) | (sees(j + 1, klo, khi, a.sinks) ? 0xFFFF0000u : 0u);
           };
-#pragma unroll
+          constexpr int kTurns = C8 ? 1 : KP;          // (unrolled, 8-bit pages spill)
+#pragma unroll kTurns
           for (int kp = 0; kp < KP; ++kp) {
+            uint32_t pr[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              pr[e] = pf[0][e];
+#pragma unroll
+              for (int k = 1; k < KP; ++k)
+                if (kp == k) pr[e] = pf[k][e];
+            }
             const int ja = j0 + kp * 16 + tq * 2;
             const uint32_t ma = keep(tl.lo_min, tl.hi_max, ja), mb = keep(tl.lo_min, tl.hi_max, ja + 8);
             bool odd = false;
@@ -832,7 +874,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
                   float acc[4];
 #pragma unroll
                   for (int e = 0; e < 4; ++e) acc[e] = o[2 * nb + k][e];
-                  Elem<Op>::mma(acc, pf[kp], bf[k >> 1][2 * (k & 1)] & wa, bf[k >> 1][2 * (k & 1) + 1] & wb);
+                  Elem<Op>::mma(acc, pr, bf[k >> 1][2 * (k & 1)] & wa, bf[k >> 1][2 * (k & 1) + 1] & wb);
 #pragma unroll
                   for (int e = 0; e < 4; ++e)
                     if (own[e >> 1]) o[2 * nb + k][e] = acc[e];
@@ -857,7 +899,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
         if (r >= rows) continue;
         if (tq == 0) {
-          s_ml[warp][r][0] = C8 ? m_run[rr] * true_max[rr] : m_run[rr];
+          s_ml[warp][r][0] = C8 ? m_run[rr] * (slr[rr] / sl2) : m_run[rr];   // in the units of q k^T
           s_ml[warp][r][1] = l * kUnit<C8>;
         }
         if constexpr (C8) {
@@ -995,7 +1037,12 @@ cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
 }
 template <typename T, int D>
 cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
-  if (a.scales) return (int64_t)a.max_q * a.G <= 8 ? go<T, D, 2, true, true>(a, map, s) : go<T, D, 2, true, false>(a, map, s);
+  if (a.scales) {
+    const bool few = (int64_t)a.max_q * a.G <= 8;
+    if constexpr (D == 64)
+      if (a.wide) return few ? go<T, D, 4, true, true>(a, map, s) : go<T, D, 4, true, false>(a, map, s);
+    return few ? go<T, D, 2, true, true>(a, map, s) : go<T, D, 2, true, false>(a, map, s);
+  }
   if (D == 64) return go<T, D, 2, false, false>(a, map, s);
   return a.nsplit > 1 ? go<T, D, 1, false, false>(a, map, s) : go<T, D, 2, false, false>(a, map, s);
 }
@@ -1010,6 +1057,13 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
   // the shortest stretch, in places (3 and 6 were no better from 300 to 4000 keys)
   p.min_tiles = 4;
   p.nsplit = 1;
+  // Tiles of 256 keys (8-bit pages of 64 channels): a chain for four 16-key groups instead
+  // of two.  Up to 8 rows: 512 groups of 300 keys take 22.5 us so and 21.0 with 128, of 600 24.1
+  // and 24.5, of 4000 61.7 and 75.1; shared out, 4 groups of 4000 9.9 and 9.4, 32 11.8 and 12.3.  9 to 16
+  // rows: 512 of 1000 37.7 and 33.0, of 2500 53.9 and 57.0, 32 of 4000 14.3 and 13.9.
+  const int64_t load = p.groups * max_visible;
+  p.wide = codes && D == 64 && (rows <= 8 ? max_visible > 500 && (max_visible <= 2500 || load > 40000)
+                                          : max_visible > 2000 && load > 400000);
   const int64_t tiles = (max_visible + 63) / 64 + 1;                  // of 64 keys, of a group at most
   // Whole groups, a CTA each, take their waves x (a CTA's start and end and its
   // tiles), the line an even share of all places after its start, parts and join.
@@ -1027,7 +1081,8 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
     double chain, hbm, start, line, place;   // a tile, a whole group's start; the line's start, a place
     int group;
   };
-  const Costs u = codes ? (D == 128 ? Costs{0.267, 0.308, 4.75, 8.6, 0.31, 12} : Costs{0.228, 0.24, 4.2, 8.0, 0.238, 14})
+  const Costs u = p.wide ? Costs{0.16, 0.17, 4.4, 8.4, 0.19, 14}
+                  : codes ? (D == 128 ? Costs{0.267, 0.308, 4.75, 8.6, 0.31, 12} : Costs{0.228, 0.24, 4.2, 8.0, 0.238, 14})
                         : (D == 128 ? Costs{0.29, 0.71, 4.0, 8.2, 0.44, group_cost<false>()}
                                     : Costs{0.24, 0.4, 2.8, 7.6, 0.33, group_cost<false>()});
   const double stream = p.groups < nsm ? u.hbm * p.groups / nsm : u.hbm;
@@ -1036,8 +1091,9 @@ PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm
   const double shared = u.line + u.place * (double)(tiles + u.group) * p.groups / nsm;
   if (split && (tiles > 40 || whole > shared) && p.groups <= QWM_PAGED_COUNTER_BYTES / 4) {
     // a CTA per SM, or as many as have min_tiles places each
-    const int tk = D == 128 && !codes ? 64 : 128;
-    const int64_t places = ((max_visible + tk - 1) / tk + 1 + (codes ? group_cost<true>() : group_cost<false>())) * p.groups;
+    const int tk = D == 128 && !codes ? 64 : (p.wide ? 256 : 128);
+    if (p.wide) p.min_tiles = 3;
+    const int64_t places = ((max_visible + tk - 1) / tk + 1 + (!codes ? group_cost<false>() : p.wide ? group_cost<true, 4>() : group_cost<true>())) * p.groups;
     const int64_t want = (places + p.min_tiles - 1) / p.min_tiles;
     p.nsplit = (int)(want < nsm ? want : nsm);
   }

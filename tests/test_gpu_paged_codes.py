@@ -299,6 +299,16 @@ def test_step_over_many_sequences(D, dtype, Hq, Hk, new):
     run_case(300 + D, lens, Hq, Hk, D, dtype, 16, 1, 600, 9)
 
 
+@pytest.mark.parametrize("Hq,Hk,new,lens", [
+    (8, 4, 1, [(1, 501), (1, 900), (0, 700), (1, 255), (1, 257), (1, 1)]),          # 256-key tiles, whole groups
+    (4, 4, 2, [(2, 7000), (1, 6400), (2, 511), (2, 2), (1, 3000)]),                 # shared out
+    (12, 4, 4, [(4, 6100), (3, 6144), (1, 256), (4, 4)] + [(2, 30 + 97 * i) for i in range(16)]),   # 12 rows
+])
+@pytest.mark.parametrize("dtype,page,window,sinks", [(BF, 16, 0, 0), (HF, 128, 0, 0), (BF, 32, 2600, 70)])
+def test_wide_tiles(Hq, Hk, new, lens, dtype, page, window, sinks):
+    run_case(700 + Hq, lens, Hq, Hk, 64, dtype, page, 1, window, sinks)
+
+
 @pytest.mark.parametrize("D,dtype,B,Hk,new", [(128, BF, 10, 8, 40), (64, HF, 20, 8, 33), (128, HF, 4, 20, 300)])
 def test_groups_past_a_full_wave_are_cut(D, dtype, B, Hk, new):
     """A little more work than the GPU has places for: the first groups whole, the rest in parts."""
