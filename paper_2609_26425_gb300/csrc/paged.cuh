@@ -74,7 +74,7 @@ struct PagedArgs {
   // min_tiles tiles; step: nsplit CTAs share the line of all tiles, at least
   // min_tiles places each.  nsplit 1: no split
   int32_t nsplit, min_tiles;
-  int32_t wide;                          // step: tiles of 256 keys
+  int32_t wide, blocks;                  // step: tiles of 256 keys; blocks of 8 rows of a head (1: one, of all)
   int32_t whole, rtiles;                 // chunk: >= 0: groups in one line, of which so many first ones are not cut;
                                          // row tiles of a sequence and head
   float* part_o;                         // chunk [group][nsplit][D / 4][row][4]; step [CTA][2][row][D]
@@ -91,6 +91,7 @@ struct PagedPlan {
   int32_t nsplit, min_tiles;
   int32_t whole;     // chunk: groups not cut (-1: none, or all if nsplit is 1)
   int32_t wide;      // step: tiles of 256 keys (8-bit pages of 64 channels)
+  int32_t blocks;    // step: blocks of 8 rows that a cache head's rows are taken in (1: all together)
 };
 PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split, bool codes);
 PagedPlan plan_chunk(int B, int Hk, int D, int64_t rows, int64_t max_visible, int nsm, bool split, bool codes);
@@ -142,8 +143,10 @@ inline cudaError_t launch_ahead(void (*kernel)(P...), dim3 grid, int threads, si
 // chunk kernel's 77 (one sequence of 131071 tokens, 4 cache heads), 20 against 16
 // (4000 tokens); a step kernel with a second tile of 16 rows lost on nearly every
 // length (24 rows: 88 against 79 us and 27 against 16).  Over codes the step
-// kernel wins at every length: 61 against 103 us, 20 against 23.
+// kernel wins at every length: 50 against 110 us, 18 against 24.
 constexpr int kStepRows = 16;
+// Over codes up to 32 rows go to the step kernel, in blocks of 8.
+constexpr int kStepRowsCodes = 32;
 
 // Pages as rows of D channels, [num_pages * 2 * heads][page_tokens][D]: boxes of
 // 64 channels x min(page_tokens, 64) tokens, 128-byte swizzle.

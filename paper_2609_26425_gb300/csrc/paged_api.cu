@@ -227,7 +227,7 @@ PagedPlan make_plan(const qwm_paged* c, const qwm_paged_batch* b, int32_t q_head
     const int64_t w = (int64_t)m->window + m->sinks + m->block + 256;
     if (w < seen) seen = w;
   }
-  return rows <= qwm::kStepRows ? qwm::plan_step(b->num_seqs, c->cfg.kv_heads, c->cfg.head_dim, (int)rows, seen, c->nsm,
+  return rows <= (c->codes ? qwm::kStepRowsCodes : qwm::kStepRows) ? qwm::plan_step(b->num_seqs, c->cfg.kv_heads, c->cfg.head_dim, (int)rows, seen, c->nsm,
                                                split, c->codes)
                                 : qwm::plan_chunk(b->num_seqs, c->cfg.kv_heads, c->cfg.head_dim, rows, seen, c->nsm, split,
                                                   c->codes);
@@ -445,6 +445,7 @@ qwm_status qwm_paged_attend(qwm_paged* c, const qwm_paged_batch* b, const qwm_ro
   a.min_tiles = p.nsplit > 1 ? p.min_tiles : 1 << 24;
   a.whole = p.step ? -1 : p.whole;
   a.wide = p.wide;
+  a.blocks = p.step ? p.blocks : 1;
   if (p.nsplit > 1) {
     const Carve w = carve(p, D);
     uint8_t* ws = static_cast<uint8_t*>(workspace);

@@ -142,6 +142,9 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     tl = make_tiles<TK>(sq.kv - sq.qn, sq.kv - 1, sq.kv, a.block, a.window, a.sinks);
     return max(tl.n, 1);
   };
+  // a sequence's groups: a cache head's rows, or blocks of 8 of them, side by side
+  auto blocks_of = [&](const Seq& of) -> int { return N8 && a.blocks > 1 ? (of.qn * a.G + 7) / 8 : 1; };
+  auto groups_of = [&](const Seq& of) -> int { return a.Hk * blocks_of(of); };
   auto full = [&](int s) { return smem_u32(&bars[s]); };
   auto empty = [&](int s) { return smem_u32(&bars[NS + s]); };
   if (tid == 0) {
@@ -162,7 +165,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   const bool split = a.nsplit > 1;
   Seq sq;
   Tiles tl;
-  int b, n, hk;
+  int b, n, hk;                                    // hk: group of the sequence
   int64_t x0, x1, g0, share = 0;
   if (split) {
     const bool alone = a.B <= 32;
@@ -171,7 +174,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     int64_t mine = 0;
     for (int i = b0; i < b1; ++i) {
       n = tiles_of(i, sq, tl);
-      mine += n ? n + kGroupCost : 0;
+      mine += n ? (int64_t)(n + kGroupCost) * groups_of(sq) : 0;
     }
     int64_t incl = mine;
 #pragma unroll
@@ -190,9 +193,6 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         total += s_scan[w];
       }
     }
-    before *= a.Hk;
-    mine *= a.Hk;
-    total *= a.Hk;
     share = max(divide(total + gridDim.x - 1, gridDim.x), (int64_t)a.min_tiles);
     x0 = blockIdx.x * share;
     if (x0 >= total) return;
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         int64_t at = before;
         for (int i = b0; i < b1; ++i) {
           n = tiles_of(i, sq, tl);
-          const int64_t len = n ? (int64_t)(n + kGroupCost) * a.Hk : 0;
+          const int64_t len = n ? (int64_t)(n + kGroupCost) * groups_of(sq) : 0;
           if (x0 < at + len) {
             s_seq = i;
             s_first = at;
@@ -241,10 +241,10 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     hk = (int)divide(x0 - g0, n + kGroupCost);
     g0 += (int64_t)hk * (n + kGroupCost);
   } else {
-    b = blockIdx.x / a.Hk;
-    hk = blockIdx.x % a.Hk;
+    b = blockIdx.x / (a.Hk * a.blocks);
+    hk = blockIdx.x % (a.Hk * a.blocks);
     n = tiles_of(b, sq, tl);
-    if (n == 0) return;
+    if (n == 0 || hk >= groups_of(sq)) return;
     x0 = g0 = 0;
     x1 = n + kGroupCost;
     __syncthreads();
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   auto next_group = [&]() -> bool {
     g0 += n + kGroupCost;
     if (g0 >= x1) return false;
-    if (++hk == a.Hk) {
+    if (++hk == groups_of(sq)) {
       hk = 0;
       do n = tiles_of(++b, sq, tl); while (n == 0);
     }
@@ -285,6 +285,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       piece();
       t1 = min(t1, tl.n);
       const int32_t* trow = a.table + (int64_t)b * a.table_stride;
+      const int head = hk / blocks_of(sq);
       // this lane's entry: box lane % boxes of tile t + lane / boxes
       auto ask = [&](int t, bool& want) -> int {
         t += lane / boxes;
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         if (lane == 0) mbar_arrive_expect_tx(full(s), bytes);
         __syncwarp();
         if (want) {
-          const int block = (page * 2 + kv) * a.Hk + hk;
+          const int block = (page * 2 + kv) * a.Hk + head;
           tma_load_3d(dst + s * L::SLOT, &map, half * 64, y, block, full(s));
         }
         if constexpr (C8) {
@@ -326,7 +327,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
           const bool swant = __shfl_sync(0xFFFFFFFFu, (int)wants, (at * boxes + sbox) & 31) && skey < TK;
           if (swant)
             cp_async16(smem_u32(sm) + L::SCALES + s * (TK * 2) + 2 * skey,
-                       a.scales + ((((int64_t)spage * 2 + kv) * a.Hk + hk) << a.page_log2) +
+                       a.scales + ((((int64_t)spage * 2 + kv) * a.Hk + head) << a.page_log2) +
                            ((tile_at(tl, t) * TK + skey) & ((1 << a.page_log2) - 1)));
           cp_async_arrive(full(s));
         }
@@ -349,16 +350,17 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   const int mrow = lane & 7, mi = lane >> 3;
   const int kkey = key0 + (mi >> 1) * 8 + mrow, kch = mi & 1;           // K: (keys 0-7 | 8-15) x (chunk, chunk + 1)
   const int vkey = key0 + (mi & 1) * 8 + mrow, vch = mi >> 1;           // V (and codes): the same, keys innermost
-  const int maxrows = a.max_q * a.G;
+  const int maxrows = a.blocks > 1 ? 8 : a.max_q * a.G;
   float* so = reinterpret_cast<float*>(sm + L::MERGE);                  // [warp][ROWS][D]
   bool ok = true;                                                       // no wait of this warp has run out
   int filled = 0;                                                       // slots of the pieces before
   do {
     piece();
     if (t0 >= t1) continue;
-    const int rows = sq.qn * a.G;                                       // <= 16
+    const int nb = blocks_of(sq), head = hk / nb, r0 = N8 ? 8 * (hk - head * nb) : 0;
+    const int rows = N8 ? min(sq.qn * a.G - r0, 8) : sq.qn * a.G;       // <= ROWS, of the head's from r0 on
     const int t_end = min(t1, tl.n);
-    const int64_t group = (int64_t)b * a.Hk + hk, first = g0 + kGroupCost;
+    const int64_t group = (int64_t)b * (a.Hk * a.blocks) + hk, first = g0 + kGroupCost;
     const bool whole = first >= x0 && first + n <= x1;                  // the group is this CTA's alone
     const int64_t c0 = whole ? 0 : divide(first, share), c1 = whole ? 0 : divide(first + n - 1, share);   // its CTAs
     const int parts = (int)(c1 - c0) + 1;
@@ -376,8 +378,8 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       {
         // Queries as B: this lane row g's channels 4 tq .. of each k16 step
         const bool has = g < rows;
-        const int tok = has ? g / a.G : 0;
-        const T* src = static_cast<const T*>(a.q) + (sq.q0 + tok) * a.q_tok + (int64_t)(hk * a.G + (has ? g % a.G : 0)) * a.q_head;
+        const int tok = has ? (r0 + g) / a.G : 0;
+        const T* src = static_cast<const T*>(a.q) + (sq.q0 + tok) * a.q_tok + (int64_t)(head * a.G + (has ? (r0 + g) % a.G : 0)) * a.q_head;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           const uint2 w = has ? *reinterpret_cast<const uint2*>(src + ks * 16 + tq * 4) : make_uint2(0u, 0u);
@@ -405,7 +407,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
           l_run[x] = 0.0f;
           slr[x] = sl2;
           if constexpr (Elem<T>::bf16) slr[x] = row_scale(sl2, __shfl_sync(0xFFFFFFFFu, up, 4 * r));
-          const Span sp = r < rows ? row_span(p0 + r / a.G, sq.kv, a.block, a.window) : Span{0, 0};
+          const Span sp = r < rows ? row_span(p0 + (r0 + r) / a.G, sq.kv, a.block, a.window) : Span{0, 0};
           hi[x] = sp.hi;
           lo[x] = sp.lo;
         }
@@ -555,7 +557,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
                 wa = keep(sp.lo, sp.hi, ja);
                 wb = keep(sp.lo, sp.hi, ja + 8);
               }
-              const bool own[2] = {!odd || (2 * tq) / a.G == tk, !odd || (2 * tq + 1) / a.G == tk};
+              const bool own[2] = {!odd || (r0 + 2 * tq) / a.G == tk, !odd || (r0 + 2 * tq + 1) / a.G == tk};
 #pragma unroll
               for (int nb = 0; nb < KS; nb += 2) {
                 uint32_t af[2][4];
@@ -621,7 +623,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         const Span sp = has ? row_span(p0 + tok, sq.kv, a.block, a.window) : Span{0, 0};
         hi[rr] = sp.hi;
         lo[rr] = sp.lo;
-        const T* src = static_cast<const T*>(a.q) + (sq.q0 + tok) * a.q_tok + (int64_t)(hk * a.G + (has ? r % a.G : 0)) * a.q_head;
+        const T* src = static_cast<const T*>(a.q) + (sq.q0 + tok) * a.q_tok + (int64_t)(head * a.G + (has ? r % a.G : 0)) * a.q_head;
         if constexpr (C8) {
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
@@ -917,7 +919,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
     }
     named_bar_sync(1, kWarps * 32);
     auto emit = [&](int r, int c, float m, float l, float4 v) {
-      const int tok = r / a.G, h = hk * a.G + r % a.G;
+      const int tok = (r0 + r) / a.G, h = head * a.G + (r0 + r) % a.G;
       const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
       T* dst = static_cast<T*>(a.out) + (sq.q0 + tok) * a.o_tok + (int64_t)h * a.o_head + 4 * c;
       *reinterpret_cast<uint2*>(dst) = make_uint2(Elem<T>::pack(v.x * inv, v.y * inv), Elem<T>::pack(v.z * inv, v.w * inv));
@@ -1032,13 +1034,13 @@ cudaError_t go(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   static bool done[64];
   cudaError_t e = allow_smem(paged_step<T, D, KP, C8, N8>, smem, done);
   if (e != cudaSuccess) return e;
-  return launch_ahead(paged_step<T, D, KP, C8, N8>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk)), NT, smem, s, 1,
+  return launch_ahead(paged_step<T, D, KP, C8, N8>, dim3((unsigned)(a.nsplit > 1 ? a.nsplit : a.B * a.Hk * a.blocks)), NT, smem, s, 1,
                       map, a);
 }
 template <typename T, int D>
 cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
   if (a.scales) {
-    const bool few = (int64_t)a.max_q * a.G <= 8;
+    const bool few = a.blocks > 1 || (int64_t)a.max_q * a.G <= 8;
     if constexpr (D == 64)
       if (a.wide) return few ? go<T, D, 4, true, true>(a, map, s) : go<T, D, 4, true, false>(a, map, s);
     return few ? go<T, D, 2, true, true>(a, map, s) : go<T, D, 2, true, false>(a, map, s);
@@ -1052,8 +1054,9 @@ cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
 PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split, bool codes) {
   PagedPlan p{};
   p.step = 1;
-  p.groups = B * Hk;
-  p.rows = rows;
+  p.blocks = rows > kStepRows ? (rows + 7) / 8 : 1;
+  p.groups = B * Hk * p.blocks;
+  p.rows = rows = p.blocks > 1 ? 8 : rows;
   // the shortest stretch, in places (3 and 6 were no better from 300 to 4000 keys)
   p.min_tiles = 4;
   p.nsplit = 1;

@@ -309,6 +309,19 @@ def test_wide_tiles(Hq, Hk, new, lens, dtype, page, window, sinks):
     run_case(700 + Hq, lens, Hq, Hk, 64, dtype, page, 1, window, sinks)
 
 
+@pytest.mark.parametrize("Hq,Hk,new,lens,window,sinks", [
+    (10, 2, 4, [(4, 900), (1, 300), (3, 3), (0, 5), (2, 777)], 0, 0),               # 20, 5, 15, 0 and 10 rows
+    (3, 3, 32, [(32, 40), (17, 1100), (8, 2600), (9, 9), (1, 4000), (31, 31)], 0, 0),
+    (24, 4, 5, [(5, 1 + 61 * i) if i % 3 else (1 + i % 5, 5 + 150 * i) for i in range(40)], 600, 33),
+    (17, 1, 1, [(1, 5000), (1, 1), (1, 64)], 0, 0),
+])
+@pytest.mark.parametrize("dtype,D,page", [(BF, 128, 64), (HF, 64, 16), (BF, 64, 32), (HF, 128, 128)])
+def test_rows_in_blocks(Hq, Hk, new, lens, window, sinks, dtype, D, page):
+    """More rows of a cache head than one block of the step's, of another number in each sequence."""
+    lens = [(q, max(q, kv)) for q, kv in lens]
+    run_case(800 + Hq, lens, Hq, Hk, D, dtype, page, 1, window, sinks)
+
+
 @pytest.mark.parametrize("D,dtype,B,Hk,new", [(128, BF, 10, 8, 40), (64, HF, 20, 8, 33), (128, HF, 4, 20, 300)])
 def test_groups_past_a_full_wave_are_cut(D, dtype, B, Hk, new):
     """A little more work than the GPU has places for: the first groups whole, the rest in parts."""
