@@ -142,11 +142,10 @@ inline cudaError_t launch_ahead(void (*kernel)(P...), dim3 grid, int threads, si
 // to the step kernel.  With 16 rows of 128 channels it takes 67 us against the
 // chunk kernel's 77 (one sequence of 131071 tokens, 4 cache heads), 20 against 16
 // (4000 tokens); a step kernel with a second tile of 16 rows lost on nearly every
-// length (24 rows: 88 against 79 us and 27 against 16).  Over codes the step
-// kernel wins at every length: 50 against 110 us, 18 against 24.
+// length (24 rows: 88 against 79 us and 27 against 16).
 constexpr int kStepRows = 16;
-// Over codes up to 32 rows go to the step kernel, in blocks of 8.
-constexpr int kStepRowsCodes = 32;
+// (Over codes step_blocks() says how many blocks of rows the step kernel takes, 0: none.)
+int step_blocks(int B, int Hk, int D, int64_t rows, int64_t max_visible, int nsm, bool codes);
 
 // Pages as rows of D channels, [num_pages * 2 * heads][page_tokens][D]: boxes of
 // 64 channels x min(page_tokens, 64) tokens, 128-byte swizzle.

@@ -227,10 +227,10 @@ PagedPlan make_plan(const qwm_paged* c, const qwm_paged_batch* b, int32_t q_head
     const int64_t w = (int64_t)m->window + m->sinks + m->block + 256;
     if (w < seen) seen = w;
   }
-  return rows <= (c->codes ? qwm::kStepRowsCodes : qwm::kStepRows) ? qwm::plan_step(b->num_seqs, c->cfg.kv_heads, c->cfg.head_dim, (int)rows, seen, c->nsm,
-                                               split, c->codes)
-                                : qwm::plan_chunk(b->num_seqs, c->cfg.kv_heads, c->cfg.head_dim, rows, seen, c->nsm, split,
-                                                  c->codes);
+  const int B = b->num_seqs, Hk = c->cfg.kv_heads, D = c->cfg.head_dim;
+  return qwm::step_blocks(B, Hk, D, rows, seen, c->nsm, c->codes)
+             ? qwm::plan_step(B, Hk, D, (int)rows, seen, c->nsm, split, c->codes)
+             : qwm::plan_chunk(B, Hk, D, rows, seen, c->nsm, split, c->codes);
 }
 
 // A workspace: counters, at the same place for every call (they stay zero between

@@ -1,5 +1,6 @@
 // paged_step.cu -- attention of a few rows of a sequence over its pages: single
-// new tokens and short drafts (Query tokens x grouped heads <= 16 rows).
+// new tokens and short drafts (Query tokens x grouped heads <= 16 rows; over 8-bit pages up
+// to 32, in blocks of 8).
 //
 // Mathematics: softmax over the visible keys with a running maximum m and sum l
 // per row (O and l scaled by 2^((m_old - m_new) c) when m grows), so one pass
@@ -1051,10 +1052,28 @@ cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
 
 }  // namespace
 
+// Blocks that a cache head's rows are taken in, each a group of its own that reads the head's
+// keys again (from L2): 1: all at once, 0: not by this kernel.  In us, codes, by the SMs' and
+// the groups' number: of 128 channels 16 rows at once (as M) and in two blocks: 4 heads x 600 keys
+// 10.9 and 8.6, x 40000 33.1 and 23.3, 64 heads x 2000 19.6 and 16.0, 32 x 8000 25.0 and 28.5, 256 x 600 22.1
+// and 33.4.  20 rows by the chunk kernel and in three blocks: 4 x 600 17.9 and 9.0, 4 x 40000 49.9 and
+// 27.6, 256 x 600 71.7 and 46.0; 32 rows in four 18.3 and 9.1, 50.1 and 31.8, 73.7 and 58.7.  Of 64
+// channels 9 to 16 rows lose in blocks; 24 rows by the chunk kernel and in three: 4 x 600 12.5 and
+// 7.9, 32 x 40000 105 and 90, 64 x 600 13.4 and 14.9; 32 rows in four: 4 x 40000 36.3 and 23.3, 32 x
+// 8000 30.9 and 33.1.
+int step_blocks(int B, int Hk, int D, int64_t rows, int64_t max_visible, int nsm, bool codes) {
+  if (!codes || rows <= 8) return rows <= kStepRows ? 1 : 0;
+  const int64_t blocks = (rows + 7) / 8, groups = (int64_t)B * Hk, keys = groups * max_visible;
+  if (blocks > 4) return 0;
+  const bool wave = groups * blocks <= nsm;                           // a CTA for each block at once
+  if (rows <= kStepRows) return D == 128 && wave && keys <= 200000 ? (int)blocks : 1;
+  return D == 128 || (wave && (blocks <= 3 || keys <= 200000)) ? (int)blocks : 0;
+}
+
 PagedPlan plan_step(int B, int Hk, int D, int rows, int64_t max_visible, int nsm, bool split, bool codes) {
   PagedPlan p{};
   p.step = 1;
-  p.blocks = rows > kStepRows ? (rows + 7) / 8 : 1;
+  p.blocks = step_blocks(B, Hk, D, rows, max_visible, nsm, codes);
   p.groups = B * Hk * p.blocks;
   p.rows = rows = p.blocks > 1 ? 8 : rows;
   // the shortest stretch, in places (3 and 6 were no better from 300 to 4000 keys)
