@@ -355,6 +355,17 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
   float* so = reinterpret_cast<float*>(sm + L::MERGE);                  // [warp][ROWS][D]
   bool ok = true;                                                       // no wait of this warp has run out
   int filled = 0;                                                       // slots of the pieces before
+  // A slot of Values goes back when they are in registers.  An arrival waits neither for loads that
+  // are under way nor for the products that use them (the chunk kernel lost a stage of codes to
+  // the next copy that way), so which lane tells depends on a sum that each load of the tile has gone into:
+  // `sum(nb)` of every block that a load covers.  (Of Keys the vote on the maximum does that.)
+  auto give_back = [&](int slot, auto sum) {
+    uint32_t all = 0;
+#pragma unroll
+    for (int nb = 0; nb < KS; nb += C8 ? 2 : 1) all ^= __float_as_uint(sum(nb));
+    const int teller = __any_sync(0xFFFFFFFFu, all == 0x5A3C96E1u) ? 1 : 0;
+    if (lane == teller) mbar_arrive(empty(slot));
+  };
   do {
     piece();
     if (t0 >= t1) continue;
@@ -578,8 +589,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
             }
           }
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(empty(s + 1));
+        give_back(s + 1, [&](int nb) { return o[nb][0]; });
       }
       filled += 2 * max(0, t_end - t0);
       if (!ok && lane == 0) record_status(a.status, QWM_ERR_TIMEOUT);
@@ -886,8 +896,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
             }
           }
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(empty(s + 1));
+        give_back(s + 1, [&](int nb) { return o[2 * nb][0]; });
       }
       filled += 2 * max(0, t_end - t0);
       if (!ok && lane == 0) record_status(a.status, QWM_ERR_TIMEOUT);
