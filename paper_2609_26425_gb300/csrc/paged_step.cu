@@ -41,12 +41,9 @@ constexpr int group_cost() { return !C8 ? 4 : KP == 4 ? 5 : 8; }
 
 // Of 8-bit pages P enters the products as binary16, 2^15 at a row's maximum: from 2^-29 of
 // it on with all its bits, down to 2^-39 at all (with 1 at the maximum from 2^-14 on, which
-// the many keys beside a first token that draws most of the weight can lie below).  A piece's
-// sums are brought back when they are written.
+// the many keys beside a first token that draws most of the weight can lie below).
 template <bool C8>
 constexpr float kTop = C8 ? 15.0f : 0.0f;
-template <bool C8>
-constexpr float kUnit = C8 ? 0x1p-15f : 1.0f;
 
 // KP 16-key groups of a warp.  A tile's chain of products, exponentials and
 // products takes as long for two groups as for one, so two where the chain bounds
@@ -346,6 +343,10 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
 
   // ------------------------------------------------------------ consumers
   const float sl2 = a.scale * 1.4426950408889634f;
+  // The maxima that warps and CTAs hand on are in units of q k^T; with 8-bit pages the powers that P was taken
+  // against, since a row's q k^T may be past fp32 there where its logits are not (bf16 Queries have a scale
+  // for each row).
+  const float unit = C8 ? 1.0f : sl2;
   const int g = lane >> 2, tq = lane & 3;
   const int wg = warp >> 2, key0 = (warp & 3) * 16 * KP;                // tile parity, first key of the tile
   const int mrow = lane & 7, mi = lane >> 3;
@@ -605,13 +606,13 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         l += __shfl_xor_sync(0xFFFFFFFFu, l, 16);
         if (r >= rows) continue;
         if (g == 0) {
-          s_ml[warp][r][0] = m_run[x] * (slr[x] / sl2);   // in the units of q k^T
-          s_ml[warp][r][1] = l * kUnit<C8>;
+          s_ml[warp][r][0] = fmaf(m_run[x], slr[x], -kTop<C8>);   // what P is taken against
+          s_ml[warp][r][1] = l;
         }
 #pragma unroll
         for (int k = 0; k < KS; ++k)
           *reinterpret_cast<float2*>(so + ((warp * ROWS + r) * D + k * 16 + g * 2)) =
-              make_float2(o[k][x] * kUnit<C8>, o[k][2 + x] * kUnit<C8>);
+              make_float2(o[k][x], o[k][2 + x]);
       }
     } else {
       // the fragments of mma.sync: this lane has rows g and g + 8 (index rr)
@@ -911,15 +912,14 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
         l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
         if (r >= rows) continue;
         if (tq == 0) {
-          s_ml[warp][r][0] = C8 ? m_run[rr] * (slr[rr] / sl2) : m_run[rr];   // in the units of q k^T
-          s_ml[warp][r][1] = l * kUnit<C8>;
+          s_ml[warp][r][0] = C8 ? fmaf(m_run[rr], slr[rr], -kTop<C8>) : m_run[rr];
+          s_ml[warp][r][1] = l;
         }
         if constexpr (C8) {
 #pragma unroll
           for (int k = 0; k < 2 * KS; k += 2)
             *reinterpret_cast<float4*>(so + ((warp * ROWS + r) * D + k * 8 + tq * 4)) =
-                make_float4(o[k][2 * rr] * kUnit<C8>, o[k + 1][2 * rr] * kUnit<C8>, o[k][2 * rr + 1] * kUnit<C8>,
-                            o[k + 1][2 * rr + 1] * kUnit<C8>);
+                make_float4(o[k][2 * rr], o[k + 1][2 * rr], o[k][2 * rr + 1], o[k + 1][2 * rr + 1]);
         } else {
 #pragma unroll
           for (int k = 0; k < 2 * KS; ++k)
@@ -933,7 +933,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
       T* dst = static_cast<T*>(a.out) + (sq.q0 + tok) * a.o_tok + (int64_t)h * a.o_head + 4 * c;
       *reinterpret_cast<uint2*>(dst) = make_uint2(Elem<T>::pack(v.x * inv, v.y * inv), Elem<T>::pack(v.z * inv, v.w * inv));
-      if (a.lse && c == 0) a.lse[(int64_t)h * a.N + sq.q0 + tok] = m * a.scale + logf(l);   // -inf + log 0; NaN with a NaN l
+      if (a.lse && c == 0) a.lse[(int64_t)h * a.N + sq.q0 + tok] = m * (C8 ? 0.69314718055994531f : a.scale) + logf(l);   // -inf + log 0; NaN with a NaN l
     };
     // (m, l, O) of row r's channels 4c .. over the first `count` entries of s_ml and so
     auto merge = [&](int count, int r, int c, float& m, float& l, float4& v) {
@@ -944,7 +944,7 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
       v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
       for (int w = 0; w < count; ++w) {
-        const float f = ex2f((s_ml[w][r][0] - ref) * sl2);
+        const float f = ex2f((s_ml[w][r][0] - ref) * unit);
         const float4 x = *reinterpret_cast<const float4*>(so + ((w * ROWS + r) * D + 4 * c));
         l = fmaf(s_ml[w][r][1], f, l);
         v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
@@ -1002,14 +1002,14 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
 #pragma unroll
         for (int u = 0; u < PU; ++u) mn = fmaxf(mn, ml[u].x);
         const float ref = mn == -INFINITY ? 0.0f : mn;
-        const float al = ex2f((m - ref) * sl2);
+        const float al = ex2f((m - ref) * unit);
         m = mn;
         l *= al;
         v.x *= al; v.y *= al; v.z *= al; v.w *= al;
 #pragma unroll
         for (int u = 0; u < PU; ++u) {
           if (p + u >= q1) break;
-          const float f = ex2f((ml[u].x - ref) * sl2);
+          const float f = ex2f((ml[u].x - ref) * unit);
           l = fmaf(ml[u].y, f, l);
           v.x = fmaf(x[u].x, f, v.x); v.y = fmaf(x[u].y, f, v.y); v.z = fmaf(x[u].z, f, v.z); v.w = fmaf(x[u].w, f, v.w);
         }

@@ -1,13 +1,13 @@
 """GPU: paged storage in 8 bits at its edges -- rings that turn many times, ranges, scales of a
 caller's own, and the paths that only large calls take -- against the definitions in 64 bits
 (tests/codes_ref.py)."""
-import math
-
 import pytest
 import torch
 
 import paper_2609_26425_gb300 as qwm
+from codes_ref import attend_codes64, make_code_case, quantise64, stands_for
 from paged_ref import offsets
+from test_gpu_paged import compare
 
 pytestmark = pytest.mark.gpu
 BF, HF, E4 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
@@ -23,6 +23,14 @@ def _cuda():
 def batch_of(lens, table, **more):
     return qwm.PagedBatch(offsets(lens).cuda(), torch.tensor([kv for _, kv in lens], dtype=torch.int32).cuda(),
                           table.cuda(), max(a for a, _ in lens), max(kv for _, kv in lens), **more)
+
+
+def made(Hk, num, page, D, dtype, codes=None, scales=None):
+    cache = qwm.PagedCache(Hk, num, page_tokens=page, head_dim=D, dtype=dtype, storage=E4)
+    if codes is not None:
+        cache.pages.view(torch.uint8).copy_(codes)
+        cache.scales.copy_(scales)
+    return cache
 
 
 def filled(seed, Hk, num, page, D, dtype, codes):
@@ -61,4 +69,45 @@ def test_every_step_gives_the_same_bits(codes, dtype, D, Hq, Hk, new, window):
         qwm.qwm_paged_attend(cache, batch, q, out=out, lse=lse, workspace=ws, **mask)
         differ += (out.view(torch.int16) != first.view(torch.int16)).any() | (lse != first_lse).any()
     assert int(differ) == 0
+    assert cache.status() == 0
+
+
+# ------------------------------------------------------------------ ranges
+def in_pages(page, table, lens, rows, which, codes, scales):
+    """Writes the codes and scales of `rows` (per sequence, [kv][heads][channels], 64 bits) into their pages;
+    returns what they stand for."""
+    held = []
+    for b, ((_, kv), x) in enumerate(zip(lens, rows)):
+        c, s = quantise64(x)
+        held.append(stands_for(c, s))
+        for i in range(-(-kv // page)):
+            n = min(page, kv - i * page)
+            codes[int(table[b, i]), which, :, :n] = c[i * page:i * page + n].permute(1, 0, 2)
+            scales[int(table[b, i]), which, :, :n] = s[i * page:i * page + n].t().half()
+    return held
+
+
+@pytest.mark.parametrize("new,G,kv,B", [(1, 2, 300, 1), (3, 2, 300, 1), (5, 2, 300, 1), (5, 2, 200, 80), (2, 2, 9000, 1),
+                                        (5, 2, 9000, 1), (5, 2, 2600, 80), (150, 2, 300, 1)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("side", [1.0, -1.0])
+def test_products_beyond_fp32_with_a_scale_that_brings_them_back(new, G, kv, B, D, side):
+    """q k^T about 2^131 (fp32 ends at 2^128), logits about 32 side: the maxima that warps, CTAs and parts
+    hand on have to be those of the logits."""
+    lens, page, scale = [(new, kv - i) for i in range(B)], 16, 2.0 ** -126
+    q, _, values, c, s, table = make_code_case(19, lens, G, 1, D, BF, page)
+    g = torch.Generator().manual_seed(kv + D)
+    x = [torch.randn(n, 1, D, generator=g).clamp(-3, 3).double() * 2.0 ** 8 for _, n in lens]
+    for y in x:
+        y[..., 0] = 2.0 ** 11
+    keys = in_pages(page, table, lens, x, 0, c, s)
+    q = torch.randn(new * B, G, D, generator=g).clamp(-3, 3).double() * 2.0 ** 117
+    q[..., 0] = side * 2.0 ** 120
+    q = q.to(BF)
+    cache, batch = made(1, c.shape[0], page, D, BF, c, s), batch_of(lens, table)
+    want = attend_codes64(q, keys, values, lens, 1, 0, 0, scale=scale)
+    assert float((want[1].abs() > 4).float().mean()) > 0.99    # (log-sum-exps: |q k^T| > 2^128 at the maxima)
+    for ws in (None, qwm.paged_attend_workspace(cache, batch, G)):
+        out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), sm_scale=scale, want_lse=True, workspace=ws)
+        compare(out, lse, want)
     assert cache.status() == 0
