@@ -259,10 +259,12 @@ __global__ void __launch_bounds__(NT, 4) read_kernel(const ReadArgs a) {
           from_codes(x[i][z].y, w[2], w[3]);
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
-            w[m] = mul_f16x2(w[m], s2);
+            // (in fp32 for bf16, which has values that binary16 has not where a caller wrote the scale)
             if (Elem<T>::bf16) {
-              const float2 f = Elem<__half>::unpack(w[m]);
-              w[m] = Elem<T>::pack(f.x, f.y);
+              const float2 f = Elem<__half>::unpack(w[m]), g = Elem<__half>::unpack(s2);
+              w[m] = Elem<T>::pack(f.x * g.x, f.y * g.x);
+            } else {
+              w[m] = mul_f16x2(w[m], s2);
             }
           }
           x[i][z] = make_uint4(w[0], w[1], w[2], w[3]);

@@ -1,6 +1,8 @@
 """GPU: paged storage in 8 bits at its edges -- rings that turn many times, ranges, scales of a
 caller's own, and the paths that only large calls take -- against the definitions in 64 bits
 (tests/codes_ref.py)."""
+import math
+
 import pytest
 import torch
 
@@ -111,3 +113,34 @@ def test_products_beyond_fp32_with_a_scale_that_brings_them_back(new, G, kv, B, 
         out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), sm_scale=scale, want_lse=True, workspace=ws)
         compare(out, lse, want)
     assert cache.status() == 0
+
+
+# ------------------------------------------------------------------ scales that a caller wrote
+ODD = [0.1, 1 / 3, 3.0, 0.75, 1000.3, 512.0, 65504.0, 2.0 ** -16, 3 * 2.0 ** -24, 2.0 ** -24, 0.00123, -1.0, -0.3, 0.0, math.inf,
+       -math.inf, math.nan, 1.0, 256.0, 2.0 ** -15]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("D", [64, 128])
+def test_read_back_with_any_scale_rounds_once(dtype, D):
+    """Every code with scales of every kind: the product of the two, rounded to the cache's type."""
+    rows = 256 // D                                            # tokens for all codes, of each scale
+    N, page = rows * len(ODD), 16
+    scales = torch.tensor(ODD).half().repeat_interleave(rows)
+    codes = torch.arange(256, dtype=torch.uint8).view(rows, D).repeat(len(ODD), 1)
+    num = -(-N // page)
+    pc, ps = torch.full((num * page, D), 127, dtype=torch.uint8), torch.zeros(num * page).half()
+    pc[:N], ps[:N] = codes, scales
+    cache = made(1, num, page, D, dtype)
+    for x in (0, 1):
+        cache.pages.view(torch.uint8)[:, x, 0].copy_(pc.view(num, page, D))
+        cache.scales[:, x, 0].copy_(ps.view(num, page))
+    k, v = qwm.qwm_paged_read(cache, batch_of([(N, N)], torch.arange(num, dtype=torch.int32)[None], tokens=N))
+    # 4 x 11 bits: the product is a number of fp32, so this rounds once
+    exact = stands_for(codes, scales)
+    assert torch.equal(exact.float().double().nan_to_num(), exact.nan_to_num())
+    want = exact.float().to(dtype)
+    for got in (k[:, 0].cpu(), v[:, 0].cpu()):
+        nan = want.isnan()
+        assert torch.equal(got.isnan(), nan)
+        assert torch.equal(got.view(torch.int16)[~nan], want.view(torch.int16)[~nan])
