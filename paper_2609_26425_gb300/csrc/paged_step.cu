@@ -23,6 +23,8 @@
 // fp32 form's).
 // A group cut by the ends of stretches is joined by the CTA that finishes last,
 // in the order of the keys, so the result does not depend on which one that is.
+#include <type_traits>
+
 #include "paged.cuh"
 
 namespace qwm {
@@ -106,10 +108,25 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t w) {
   return r;
 }
 
+// Whether scales (binary16, any number in words of one or two) are such that their products with
+// every code are binary16 numbers: 0 or a power of two from 2^-14 to 2^7.
+struct CodeScales {
+  uint32_t all = 0, top = 0;
+  __device__ __forceinline__ void add(uint32_t w) {
+    all |= w;
+    top = vmax_u16x2(top, w);
+  }
+  __device__ __forceinline__ bool exact() const {
+    return (all & 0x83FF83FFu) == 0u && (top & 0xFFFFu) <= 0x5800u && (top >> 16) <= 0x5800u;
+  }
+};
+
 // Codes enter the products as binary16: a lane's word of four of a Key's channels is its
 // fragment of one k16 step (the channels of a step in the order 4 tq .. 4 tq + 3 for Q and
 // K alike), a transposed word of Values two tokens' pairs of channels, which are put in
-// order before the conversion.  The Keys' scales multiply the logits, the Values' the
+// order before the conversion.  The Keys' scales multiply the logits where code x scale is a binary16 number
+// for every code, and the fragments where one may not be (a scale that a caller wrote, or one at
+// the ends of the range): every kernel rounds code x scale to binary16.  The Values' multiply the
 // fragments (P times a scale would leave binary16's range).  Up to 8 rows (N8) are the
 // N = 8 side, keys and channels M = 16 (S^T = K Q^T, O^T += V^T P^T): a conversion then feeds
 // half as many MMAs and no half of a fragment is idle rows (131071 keys, 8 rows: 56 us
@@ -441,26 +458,43 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
           for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
             for (int e = 0; e < 4; ++e) sc[kp][0][e] = sc[kp][1][e] = 0.0f;
+          uint32_t hs[KP][2];                          // scales of keys g and g + 8
+          CodeScales kind;
 #pragma unroll
-          for (int ks = 0; ks < KS; ks += 2)
+          for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
-            for (int kp = 0; kp < KP; ++kp) {
-              uint32_t w[4];                           // (keys 0-7 | 8-15) x (step ks, ks + 1)
-              ldsm4(kb + at_code<D>(vkey + 16 * kp, ks + vch), w);
-#pragma unroll
-              for (int x = 0; x < 2; ++x) {
-                uint32_t af[4];
-                from_codes(w[2 * x], af[0], af[2]);
-                from_codes(w[2 * x + 1], af[1], af[3]);
-                Elem<Op>::mma(sc[kp][x], af, qf[ks + x][0], qf[ks + x][1]);
-              }
+            for (int x = 0; x < 2; ++x) {
+              hs[kp][x] = *reinterpret_cast<const uint16_t*>(sc_k + 2 * (kp * 16 + 8 * x + g));
+              kind.add(hs[kp][x]);
             }
+          const bool exact = __all_sync(0xFFFFFFFFu, kind.exact());
+          auto products = [&](auto scaled) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ks += 2)
+#pragma unroll
+              for (int kp = 0; kp < KP; ++kp) {
+                uint32_t w[4];                         // (keys 0-7 | 8-15) x (step ks, ks + 1)
+                ldsm4(kb + at_code<D>(vkey + 16 * kp, ks + vch), w);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                  uint32_t af[4];
+                  from_codes(w[2 * x], af[0], af[2]);
+                  from_codes(w[2 * x + 1], af[1], af[3]);
+                  if constexpr (scaled) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) af[e] = mul_f16x2(af[e], hs[kp][e & 1] * 0x10001u);
+                  }
+                  Elem<Op>::mma(sc[kp][x], af, qf[ks + x][0], qf[ks + x][1]);
+                }
+              }
+          };
+          if (exact) products(std::false_type{});
+          else products(std::true_type{});
           bool grow = false;
           float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
           for (int kp = 0; kp < KP; ++kp) {
-            const float f0 = __half2float(*reinterpret_cast<const __half*>(sc_k + 2 * (kp * 16 + g)));
-            const float f1 = __half2float(*reinterpret_cast<const __half*>(sc_k + 2 * (kp * 16 + g + 8)));
+            const float f0 = exact ? Elem<__half>::unpack(hs[kp][0]).x : 1.0f, f1 = exact ? Elem<__half>::unpack(hs[kp][1]).x : 1.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               float& v = sc[kp][0][e];
@@ -716,39 +750,58 @@ __global__ void __launch_bounds__(NT, 1) paged_step(const __grid_constant__ CUte
 #pragma unroll
               for (int e = 0; e < 4; ++e) sc[kp][k][e] = 0.0f;
           if constexpr (C8) {
-#pragma unroll
-            for (int ks = 0; ks < KS; ks += 2) {
-              uint32_t qa[2][4];
-#pragma unroll
-              for (int x = 0; x < 2; ++x) {
-                if constexpr (L::QS) {
-                  const uint4 v = qs[32 * (ks + x)];
-                  qa[x][0] = v.x; qa[x][1] = v.y; qa[x][2] = v.z; qa[x][3] = v.w;
-                } else {
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) qa[x][e] = qf[ks + x][e];
-                }
-              }
-#pragma unroll
-              for (int kp = 0; kp < KP; ++kp) {
-                uint32_t w[4];                         // (keys 0-7 | 8-15) x (step ks, ks + 1)
-                ldsm4(kb + at_code<D>(vkey + 16 * kp, ks + vch), w);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                  uint32_t b0, b1;
-                  from_codes(w[x], b0, b1);
-                  Elem<Op>::mma(sc[kp][x & 1], qa[x >> 1], b0, b1);
-                }
-              }
-            }
+            CodeScales kind;
 #pragma unroll
             for (int kp = 0; kp < KP; ++kp)
 #pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const float2 f = Elem<Op>::unpack(scales_at(s, kp * 16 + k * 8));
+              for (int k = 0; k < 2; ++k) kind.add(scales_at(s, kp * 16 + k * 8));
+            const bool exact = __all_sync(0xFFFFFFFFu, kind.exact());
+            auto products = [&](auto scaled) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sc[kp][k][e] *= e & 1 ? f.y : f.x;
+              for (int ks = 0; ks < KS; ks += 2) {
+                uint32_t qa[2][4];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                  if constexpr (L::QS) {
+                    const uint4 v = qs[32 * (ks + x)];
+                    qa[x][0] = v.x; qa[x][1] = v.y; qa[x][2] = v.z; qa[x][3] = v.w;
+                  } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) qa[x][e] = qf[ks + x][e];
+                  }
+                }
+#pragma unroll
+                for (int kp = 0; kp < KP; ++kp) {
+                  uint32_t w[4];                       // (keys 0-7 | 8-15) x (step ks, ks + 1)
+                  ldsm4(kb + at_code<D>(vkey + 16 * kp, ks + vch), w);
+#pragma unroll
+                  for (int x = 0; x < 4; ++x) {
+                    uint32_t b0, b1;
+                    from_codes(w[x], b0, b1);
+                    if constexpr (scaled) {            // (this lane's key is g of eight here)
+                      const uint32_t s2 = *reinterpret_cast<const uint16_t*>(sm + L::SCALES + s * (TK * 2) +
+                                                                             2 * (key0 + kp * 16 + (x & 1) * 8 + g)) * 0x10001u;
+                      b0 = mul_f16x2(b0, s2);
+                      b1 = mul_f16x2(b1, s2);
+                    }
+                    Elem<Op>::mma(sc[kp][x & 1], qa[x >> 1], b0, b1);
+                  }
+                }
               }
+            };
+            if (exact) {
+              products(std::false_type{});
+#pragma unroll
+              for (int kp = 0; kp < KP; ++kp)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  const float2 f = Elem<Op>::unpack(scales_at(s, kp * 16 + k * 8));
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) sc[kp][k][e] *= e & 1 ? f.y : f.x;
+                }
+            } else {
+              products(std::true_type{});
+            }
           } else {
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)

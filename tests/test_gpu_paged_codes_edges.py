@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2609_26425_gb300 as qwm
-from codes_ref import attend_codes64, make_code_case, quantise64, stands_for
+from codes_ref import VALUE, attend_codes64, make_code_case, quantise64, stands_for
 from paged_ref import offsets
 from test_gpu_paged import compare
 
@@ -144,3 +144,59 @@ def test_read_back_with_any_scale_rounds_once(dtype, D):
         nan = want.isnan()
         assert torch.equal(got.isnan(), nan)
         assert torch.equal(got.view(torch.int16)[~nan], want.view(torch.int16)[~nan])
+
+
+@pytest.mark.parametrize("new,G", [(1, 2), (3, 2), (5, 2), (6, 4), (150, 2)])
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (HF, 128), (HF, 64)])
+@pytest.mark.parametrize("kv,B,some", [(300, 1, False), (300, 1, True), (200, 80, False), (6500, 1, True)])
+def test_attention_over_any_scale_is_one_rule(new, G, dtype, D, kv, B, some):
+    """Products of scales that are no power of two, or below 2^-15, are rounded to binary16 before they enter,
+    in steps and chunks alike; `some`: one token in 40 has one, the others as appended."""
+    if new == 150:
+        B = min(B, 2)
+    lens, page = [(new, kv - i) for i in range(B)], 16
+    q, _, _, c, s, table = make_code_case(29, lens, G, 1, D, dtype, page)
+    g = torch.Generator().manual_seed(kv)
+    pool = torch.tensor([0.1, 1 / 3, 0.37, 0.0123, -0.21, 2.0 ** -17, 3 * 2.0 ** -18])
+    held = [[], []]
+    for b, (_, n) in enumerate(lens):
+        for x in (0, 1):
+            codes, sc = quantise64(torch.randn(n, 1, D, generator=g).double())
+            codes = torch.where(VALUE[codes.long()].abs() > 240, codes ^ 8, codes)      # (so that q k^T stays moderate)
+            odd = pool[torch.randint(0, len(pool), (n, 1), generator=g)] / 16
+            use = torch.rand(n, 1, generator=g) < (1 / 40 if some else 1.0)
+            sc = torch.where(use, odd, sc.float()).half()
+            held[x].append(stands_for(codes, sc).half().double())
+            for i in range(-(-n // page)):
+                m = min(page, n - i * page)
+                c[int(table[b, i]), x, :, :m] = codes[i * page:i * page + m].permute(1, 0, 2)
+                s[int(table[b, i]), x, :, :m] = sc[i * page:i * page + m].t()
+    cache, batch = made(1, c.shape[0], page, D, dtype, c, s), batch_of(lens, table)
+    want = attend_codes64(q, held[0], held[1], lens, 1, 0, 0)
+    for ws in (None, qwm.paged_attend_workspace(cache, batch, G)):
+        out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True, workspace=ws)
+        compare(out, lse, want)
+
+
+@pytest.mark.parametrize("new,G", [(1, 2), (4, 2), (5, 2), (150, 2)])
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 64)])
+def test_a_product_beyond_binary16_is_an_infinity_in_steps_and_chunks(new, G, dtype, D):
+    """Code 448 at scale 512 of one Key's channel: +inf times q there, so the rows of head 0 (q > 0) are NaN and
+    those of head 1 (q < 0) do not see the token."""
+    lens, kv, page, at = [(new, 400)], 400, 16, 37
+    q, keys, values, c, s, table = make_code_case(33, lens, G, 1, D, dtype, page)
+    q[:, 0, 3], q[:, 1, 3] = 0.5, -0.5
+    pid, slot = int(table[0, at // page]), at % page
+    c[pid, 0, 0, slot] = 0
+    c[pid, 0, 0, slot, 3] = 126                                # 448
+    s[pid, 0, 0, slot] = 512.0
+    cache, batch = made(1, c.shape[0], page, D, dtype, c, s), batch_of(lens, table)
+    keys[0][at] = 0
+    keys[0][at, 0, 3] = 1e6                                    # (its weight in 64 bits: exp(-1e6 / 2 / sqrt(D)) = 0)
+    want = attend_codes64(q[:, 1:], keys, values, lens, 1, 0, 0)
+    keys[0][at, 0, 3] = 0                                      # (the bounds, without it)
+    bound = attend_codes64(q[:, 1:], keys, values, lens, 1, 0, 0)[2:]
+    for ws in (None, qwm.paged_attend_workspace(cache, batch, G)):
+        out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True, workspace=ws)
+        assert bool(out[:, 0].isnan().all()) and bool(lse[0].isnan().all())
+        compare(out[:, 1:], lse[1:], (*want[:2], *bound))
