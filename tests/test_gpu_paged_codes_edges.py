@@ -7,8 +7,8 @@ import pytest
 import torch
 
 import paper_2609_26425_gb300 as qwm
-from codes_ref import VALUE, attend_codes64, make_code_case, quantise64, stands_for
-from paged_ref import offsets
+from codes_ref import VALUE, attend_codes64, make_code_case, quantise64, scale64, stands_for
+from paged_ref import inv_freq, offsets, rope64, rope_bound
 from test_gpu_paged import compare
 
 pytestmark = pytest.mark.gpu
@@ -200,3 +200,161 @@ def test_a_product_beyond_binary16_is_an_infinity_in_steps_and_chunks(new, G, dt
         out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), want_lse=True, workspace=ws)
         assert bool(out[:, 0].isnan().all()) and bool(lse[0].isnan().all())
         compare(out[:, 1:], lse[1:], (*want[:2], *bound))
+
+
+# ------------------------------------------------------------------ paths that only large calls take
+@pytest.mark.parametrize("dtype,D,il,Hq,Hk,part,lens", [
+    (BF, 128, True, 3, 2, 64, [(4680, 4999), (0, 7), (31, 40)]),               # 7 tokens a CTA
+    (HF, 64, False, 1, 1, 24, [(1, 1), (12007, 12100), (903, 903)]),           # 16, the most
+    (BF, 64, True, 40, 1, 32, [(2500, 2500), (77, 5000)]),                     # 3
+    (HF, 128, False, 0, 5, 64, [(1217, 1300)]),                                # without Queries
+])
+def test_append_of_many_tokens_a_block(dtype, D, il, Hq, Hk, part, lens):
+    """Blocks of threads with several tokens each, their tables of angles and of places among them."""
+    N, page = sum(a for a, _ in lens), 32
+    g = torch.Generator().manual_seed(N)
+    qkv = (torch.randn(N, Hq + 2 * Hk, D, generator=g) * torch.exp2(torch.rand(N, Hq + 2 * Hk, 1, generator=g) * 12 - 8)).to(dtype)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hk], qkv[:, Hq + Hk:]
+    pos = torch.randint(0, 3000, (N, 3), generator=g, dtype=torch.int32)
+    pairs = (part - 2 * (part // 3), part // 3, part // 3)
+    freq = inv_freq(pairs)
+    width = max(-(-kv // page) for _, kv in lens)
+    num = len(lens) * width + 2
+    table = torch.randperm(num, generator=g)[:len(lens) * width].int().view(len(lens), width)
+    marks = torch.randint(0, 256, (num, 2, Hk, page, D), generator=g, dtype=torch.uint8)
+    smarks = torch.randn(num, 2, Hk, page, generator=g).half()
+    cache, batch = made(Hk, num, page, D, dtype, marks, smarks), batch_of(lens, table, tokens=N)
+    dev = qkv.cuda()
+    rot = qwm.qwm_paged_append(cache, batch, dev[:, Hq:Hq + Hk], dev[:, Hq + Hk:], rope=qwm.Rope(freq.cuda(), pairs, interleaved=il),
+                               pos=pos.cuda(), q=dev[:, :Hq] if Hq else None)
+    if Hq:
+        q64 = rope64(q, pos, freq, pairs, il)
+        assert bool(((rot.double().cpu() - q64).abs() <= rope_bound(q, q64, dtype, pairs, il)).all())
+    at = torch.cat([torch.arange(kv - ql, kv) for ql, kv in lens])
+    seq = torch.cat([torch.full((ql,), b) for b, (ql, _) in enumerate(lens)])
+    pid, slot = table[seq, at // page].long(), at % page
+    got_c, got_s = cache.pages.view(torch.uint8).cpu(), cache.scales.cpu()
+    # Values: the same bits
+    vc, vs = quantise64(v)
+    assert torch.equal(got_c[pid, 1, :, slot], vc) and torch.equal(got_s[pid, 1, :, slot].double(), vs)
+    # Keys: the scale of the largest magnitude give or take the rotation's error, codes within half a step and that
+    k64 = rope64(k, pos, freq, pairs, il)
+    eps = rope_bound(k, torch.zeros_like(k64), BF, pairs, il)
+    most, e = k64.abs().amax(-1), eps.amax(-1)
+    s = got_s[pid, 0, :, slot].double()
+    assert bool(((s >= scale64((most - e)[..., None])) & (s <= scale64((most + e)[..., None]))).all())
+    got = stands_for(got_c[pid, 0, :, slot], got_s[pid, 0, :, slot])
+    half = torch.maximum((k64.abs() + eps) * 2.0 ** -4, s[..., None] * 2.0 ** -10)
+    assert bool(((got - k64).abs() <= half + eps).all())
+    # and nothing else
+    mine = torch.zeros(num, page, dtype=torch.bool)
+    mine[pid, slot] = True
+    keep = ~mine[:, None, None, :].expand(num, 2, Hk, page)
+    assert torch.equal(got_c[keep], marks[keep])
+    assert torch.equal(got_s.view(torch.int16)[keep], smarks.view(torch.int16)[keep])
+    assert cache.status() == 0
+
+
+@pytest.mark.parametrize("codes", [True, False])
+@pytest.mark.parametrize("dtype,D,page,Hk,lens", [
+    (BF, 128, 16, 37, [(2111, 2500), (0, 3), (41, 41)]),                       # 1215 turns
+    (HF, 64, 32, 3, [(5, 5), (60011, 60020), (70, 100)]),                      # rows of a token across turns
+    (HF, 128, 128, 1, [(40003, 40003)]),
+    (BF, 64, 64, 80, [(2009, 2010), (60, 70)]),
+])
+def test_read_back_of_more_rows_than_the_grid_takes_at_once(codes, dtype, D, page, Hk, lens):
+    N = sum(a for a, _ in lens)
+    assert 2 * N * Hk > 2 * 608 * 256 * 4 // (D // 16) or Hk == 1
+    width = max(-(-kv // page) for _, kv in lens)
+    cache = filled(5, Hk, len(lens) * width, page, D, dtype, codes)
+    table = torch.randperm(len(lens) * width, generator=torch.Generator().manual_seed(2)).int().view(len(lens), width)
+    at = torch.cat([torch.arange(kv - ql, kv) for ql, kv in lens])
+    seq = torch.cat([torch.full((ql,), b) for b, (ql, _) in enumerate(lens)])
+    pid, slot = table[seq, at // page].long().cuda(), (at % page).cuda()
+    batch = batch_of(lens, table, tokens=N)
+    k, v = qwm.qwm_paged_read(cache, batch)
+    none, v1 = qwm.qwm_paged_read(cache, batch, keys=False)
+    k1, none2 = qwm.qwm_paged_read(cache, batch, values=False)
+    assert none is None and none2 is None
+    for x, gots in enumerate(((k, k1), (v, v1))):
+        if codes:
+            want = stands_for(cache.pages.view(torch.uint8)[pid, x, :, slot].cpu(), cache.scales[pid, x, :, slot].cpu())
+        else:
+            want = cache.pages[pid, x, :, slot].double().cpu()
+        for got in gots:
+            assert torch.equal(got.double().cpu(), want)
+    assert cache.status() == 0
+
+
+def full_case(seed, lens, Hq, Hk, D, dtype, page, block, window, sinks, cut=None):
+    """Attention of every row against 64 bits, with the closer bounds of codes; `cut`: whether some groups are in parts."""
+    q, keys, values, c, s, table = make_code_case(seed, lens, Hq, Hk, D, dtype, page)
+    cache, batch = made(Hk, c.shape[0], page, D, dtype, c, s), batch_of(lens, table)
+    want = attend_codes64(q, keys, values, lens, block, window, sinks)
+    ws = qwm.paged_attend_workspace(cache, batch, Hq, window, sinks, block)
+    for w in (None, ws):
+        out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), window=window, sinks=sinks, block=block, want_lse=True, workspace=w)
+        compare(out, lse, want)
+    assert cache.status() == 0
+    return ws
+
+
+@pytest.mark.parametrize("case", [
+    # lens, Hq, Hk, D, dtype, page, block, window, sinks: several groups of 512 (256) rows of a head
+    ([(700, 900), (1, 5), (513, 513)], 1, 1, 128, BF, 16, 1, 0, 0),
+    ([(301, 640), (40, 700)], 4, 1, 128, HF, 64, 1, 333, 21),                   # 1204 rows of four heads
+    ([(600, 1200)], 2, 2, 128, BF, 128, 600, 900, 100),
+    ([(257, 300), (511, 800)], 3, 1, 64, HF, 32, 1, 200, 5),
+])
+def test_several_groups_of_rows(case):
+    full_case(401, *case)
+
+
+@pytest.mark.parametrize("case", [
+    # a little more groups than the SMs (pairs of them) hold
+    ([(40, 1500 - 7 * i) for i in range(10)], 24, 8, 128, BF, 64, 1, 1100, 33),
+    ([(33, 1500 - 7 * i) for i in range(20)], 16, 8, 64, HF, 16, 1, 1200, 70),
+    ([(30, 1500 - 60 * i) for i in range(20)], 8, 4, 128, HF, 128, 30, 0, 0),
+])
+def test_cut_groups_under_windows_first_tokens_and_grouped_heads(case):
+    lens, Hq, Hk, D = case[:4]
+    ws = full_case(403, *case)
+    rows = 512 if D == 128 else 256
+    # parts are kept for the last groups only: fewer bytes than one part of every group
+    assert ws is not None and ws.numel() < len(lens) * Hk * rows * (4 * D + 8)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 64)])
+def test_append_stores_what_is_in_range_and_nothing_else(new, dtype, D):
+    """One entry of the table out of range: the tokens of its page are left out, all others stored, bit for bit."""
+    Hk, page, kv = 2, 16, 3000
+    lens = [(new, kv), (20 + new, kv), (0, 50), (3, 700)]      # the second has tokens before, in and after the broken page
+    N = sum(a for a, _ in lens)
+    g = torch.Generator().manual_seed(new)
+    width = -(-kv // page)
+    num = len(lens) * width
+    table = torch.randperm(num, generator=g).int().view(len(lens), width)
+    k, v = ((torch.randn(N, Hk, D, generator=g) * torch.exp2(torch.rand(N, Hk, 1, generator=g) * 8 - 4)).to(dtype) for _ in range(2))
+    for bad in (num, -7, 1 << 30):
+        broken = table.clone()
+        broken[1, (kv - 10) // page] = bad
+        marks = torch.randint(0, 256, (num, 2, Hk, page, D), generator=g, dtype=torch.uint8)
+        smarks = torch.randn(num, 2, Hk, page, generator=g).half()
+        cache = made(Hk, num, page, D, dtype, marks, smarks)
+        qwm.qwm_paged_append(cache, batch_of(lens, broken, tokens=N), k.cuda(), v.cuda())
+        assert cache.status() == 1 and cache.status() == 0
+        stored = 0
+        for x, rows in enumerate((k, v)):
+            codes, scales = quantise64(rows)
+            row = 0
+            for b, (ql, n) in enumerate(lens):
+                for p in range(n - ql, n):
+                    if 0 <= broken[b, p // page] < num:
+                        at = int(broken[b, p // page])
+                        marks[at, x, :, p % page], smarks[at, x, :, p % page] = codes[row], scales[row].half()
+                        stored += 1
+                    row += 1
+        assert 0 < stored < 2 * N
+        assert torch.equal(cache.pages.view(torch.uint8).cpu(), marks)
+        assert torch.equal(cache.scales.cpu().view(torch.int16), smarks.view(torch.int16))
