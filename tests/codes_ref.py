@@ -7,7 +7,7 @@ import math
 
 import torch
 
-from paged_ref import attend64, make_case
+from paged_ref import HALF_ULP, TINY, attend64, make_case, visible
 
 MOST = 61440.0
 
@@ -78,3 +78,49 @@ def attend_codes64(q, keys, values, lens, block, window, sinks, scale=None):
                 ob[row:row + ql] += v.abs().sum(0).repeat_interleave(G, 0) * 2.0 ** -25
             row += ql
     return out, lse, ob, lb
+
+
+def attend_codes64_close(q, keys, values, lens, block, window, sinks, scale=None, step=True, round_p=None):
+    """attend_codes64 with what the kernels over codes claim of their products, apart from the output's type:
+    P is rounded to binary16 (2^-11 of itself), keeping 2^-40 of the row's largest in steps (P is 2^15
+    there, binary16 ends at 2^-24: half a step is 2^-25) and 2^-27 in chunks (2^2 at a new maximum); a running sum
+    of n / 16 products in fp32 is cut by 2^-22 of its parts' sizes each time.  `round_p`: takes the probabilities,
+    1 at the maximum, through that rounding first (a plain model of a kernel, to try the bounds on)."""
+    N, Hq, D = q.shape
+    G = Hq // keys[0].shape[1]
+    scale = 1.0 / math.sqrt(D) if scale is None else scale
+    u = HALF_ULP[q.dtype]
+    out, ob = torch.zeros(N, Hq, D, dtype=torch.float64), torch.zeros(N, Hq, D, dtype=torch.float64)
+    lse, lb = torch.full((Hq, N), -math.inf, dtype=torch.float64), torch.zeros(Hq, N, dtype=torch.float64)
+    row = 0
+    for (ql, kv), k, v in zip(lens, keys, values):
+        for p in range(kv - ql, kv):
+            see = visible(p, kv, block, window, sinks)
+            n = int(see.sum())
+            for h in range(Hq if n else 0):
+                kk, vv, x = k[see, h // G].double(), v[see, h // G].double(), q[row, h].double()
+                s = kk @ x * scale
+                w = torch.exp(s - s.max())
+                l = w.sum()
+                o = (w if round_p is None else round_p(w)) @ vv / l
+                mag, ends = w @ vv.abs() / l, vv.abs().sum(0) / l * 2.0 ** (-40 if step else -27)
+                # a logit's error, and its exponential's, as in attend64
+                ds = float((kk.abs() @ x.abs()).max()) * scale * 2.0 ** -20 + 2.0 ** -20 + float(s.abs().max()) * 2.0 ** -22
+                out[row, h], lse[h, row] = o, s.max() + torch.log(l)
+                ob[row, h] = mag * (2.0 ** -11 + 2 * ds + 2.0 ** -20 + 2.0 ** -22 * (n / 16 + 8)) + ends + o.abs() * u * 1.01 + TINY[q.dtype]
+                lb[h, row] = ds + 2.0 ** -20 * (1 + abs(float(lse[h, row])))
+            row += 1
+    return out, lse, ob, lb
+
+
+def alternating_case(lens, G, D, dtype, page, seed=83):
+    """Tokens of Values +c and -c by turns: with a window of two, a row's output is the difference of two
+    probabilities times c, and their rounding stands out."""
+    q, keys, values, codes, scales, table = make_code_case(seed, lens, G, 1, D, dtype, page)
+    c, one = quantise64(torch.randn(1, 1, D, generator=torch.Generator().manual_seed(seed)).double().abs() + 0.25)
+    for b, (_, kv) in enumerate(lens):
+        for j in range(kv):
+            codes[int(table[b, j // page]), 1, :, j % page] = c[0] + 128 * (j & 1)
+            scales[int(table[b, j // page]), 1, :, j % page] = one[0].half()
+        values[b] = stands_for(c, one) * (1 - 2 * (torch.arange(kv) & 1))[:, None, None]
+    return (q.double() / 4).to(dtype), keys, values, codes, scales, table     # (logits close to one another)

@@ -7,7 +7,8 @@ import pytest
 import torch
 
 import paper_2609_26425_gb300 as qwm
-from codes_ref import VALUE, attend_codes64, make_code_case, quantise64, scale64, stands_for
+from codes_ref import (VALUE, alternating_case, attend_codes64, attend_codes64_close, make_code_case, quantise64, scale64,
+                       stands_for)
 from paged_ref import inv_freq, offsets, rope64, rope_bound
 from test_gpu_paged import compare
 
@@ -358,3 +359,38 @@ def test_append_stores_what_is_in_range_and_nothing_else(new, dtype, D):
         assert 0 < stored < 2 * N
         assert torch.equal(cache.pages.view(torch.uint8).cpu(), marks)
         assert torch.equal(cache.scales.cpu().view(torch.int16), smarks.view(torch.int16))
+
+
+# ------------------------------------------------------------------ the products' own rounding
+@pytest.mark.parametrize("new,G,B", [(1, 2, 1), (4, 2, 3), (5, 2, 1), (5, 2, 80), (12, 2, 2), (150, 2, 1)])
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (HF, 128), (HF, 64)])
+def test_probabilities_keep_binary16s_bits(new, G, B, dtype, D):
+    """Differences of two probabilities, whatever the tensors' type is."""
+    lens, page = [(new, new + 40 + i) for i in range(B)], 16
+    q, keys, values, c, s, table = alternating_case(lens, G, D, dtype, page)
+    cache, batch = made(1, c.shape[0], page, D, dtype, c, s), batch_of(lens, table)
+    want = attend_codes64_close(q, keys, values, lens, 1, 2, 0, step=new * G <= 32)
+    for ws in (None, qwm.paged_attend_workspace(cache, batch, G, 2, 0, 1)):
+        out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), window=2, want_lse=True, workspace=ws)
+        compare(out, lse, want)
+
+
+@pytest.mark.parametrize("case", [
+    # lens, Hq, Hk, D, dtype, page, block, window, sinks
+    ([(1, 2900), (1, 17), (0, 5)], 8, 1, 128, BF, 16, 1, 0, 0),
+    ([(1, 7000)], 4, 4, 64, BF, 64, 1, 0, 0),
+    ([(4, 5000), (3, 40)], 3, 1, 128, BF, 32, 1, 2100, 9),
+    ([(5, 4000)], 4, 2, 64, BF, 16, 1, 0, 0),
+    ([(9, 2500)], 2, 1, 128, HF, 128, 1, 0, 0),
+    ([(90, 1300)], 2, 1, 128, BF, 16, 90, 0, 0),
+    ([(70, 900), (40, 20)], 3, 1, 64, BF, 32, 1, 500, 30),
+    ([(150, 1000)], 1, 1, 128, HF, 64, 1, 0, 0),
+])
+def test_attention_within_the_closer_bounds(case):
+    lens, Hq, Hk, D, dtype, page, block, window, sinks = case
+    q, keys, values, c, s, table = make_code_case(87, lens, Hq, Hk, D, dtype, page)
+    cache, batch = made(Hk, c.shape[0], page, D, dtype, c, s), batch_of(lens, table)
+    want = attend_codes64_close(q, keys, values, lens, block, window, sinks, step=max(a for a, _ in lens) * (Hq // Hk) <= 32)
+    for ws in (None, qwm.paged_attend_workspace(cache, batch, Hq, window, sinks, block)):
+        out, lse = qwm.qwm_paged_attend(cache, batch, q.cuda(), window=window, sinks=sinks, block=block, want_lse=True, workspace=ws)
+        compare(out, lse, want)
