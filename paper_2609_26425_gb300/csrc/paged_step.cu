@@ -1108,18 +1108,21 @@ cudaError_t pick(const PagedArgs& a, const CUtensorMap& map, cudaStream_t s) {
       if (a.wide) return few ? go<T, D, 4, true, true>(a, map, s) : go<T, D, 4, true, false>(a, map, s);
     return few ? go<T, D, 2, true, true>(a, map, s) : go<T, D, 2, true, false>(a, map, s);
   }
-  if (D == 64) return go<T, D, 2, false, false>(a, map, s);
-  return a.nsplit > 1 ? go<T, D, 1, false, false>(a, map, s) : go<T, D, 2, false, false>(a, map, s);
+  if constexpr (D == 128)
+    if (a.nsplit > 1) return go<T, D, 1, false, false>(a, map, s);
+  return go<T, D, 2, false, false>(a, map, s);
 }
 
 }  // namespace
 
 // Blocks that a cache head's rows are taken in, each a group of its own that reads the head's
-// keys again (from L2): 1: all at once, 0: not by this kernel.  In us, codes, by the SMs' and
+// keys again (from L2 while it holds them): 1: all at once, 0: not by this kernel.  In us, codes, by the SMs' and
 // the groups' number: of 128 channels 16 rows at once (as M) and in two blocks: 4 heads x 600 keys
 // 10.9 and 8.6, x 40000 33.1 and 23.3, 64 heads x 2000 19.6 and 16.0, 32 x 8000 25.0 and 28.5, 256 x 600 22.1
 // and 33.4.  20 rows by the chunk kernel and in three blocks: 4 x 600 17.9 and 9.0, 4 x 40000 49.9 and
-// 27.6, 256 x 600 71.7 and 46.0; 32 rows in four 18.3 and 9.1, 50.1 and 31.8, 73.7 and 58.7.  Of 64
+// 27.6, 256 x 600 71.7 and 46.0; 32 rows in four 18.3 and 9.1, 50.1 and 31.8, 73.7 and 58.7.  Codes past
+// L2 change nothing in that, since the chunk kernel's chain is as far from HBM: 64 x 40000 437 and 294 (20 rows), 386
+// (32); 256 x 8000 (530 MB) 358 and 243, 322; 128 x 40000 791 and 572, 759; 256 x 40000 (2.6 GB) 1500 and 1505 (32 rows).  Of 64
 // channels 9 to 16 rows lose in blocks; 24 rows by the chunk kernel and in three: 4 x 600 12.5 and
 // 7.9, 32 x 40000 105 and 90, 64 x 600 13.4 and 14.9; 32 rows in four: 4 x 40000 36.3 and 23.3, 32 x
 // 8000 30.9 and 33.1.
